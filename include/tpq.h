@@ -329,6 +329,115 @@ tpq_status tpq_dequant_reduce_arrivals(tpq_ctx *ctx, const void *const *payloads
                                        const float *bias_dev, const uint32_t *arrived_dev, uint32_t epoch,
                                        uint64_t timeout_ns, void *cuda_stream);
 
+/* ------------------------------------------------- the attention block ahead of the layer: keys and values in 4 bits
+ *
+ * What a device of a tensor-parallel group computes ahead of the output projection (tpq_linear_quantize_pack):
+ * attention of its own heads over keys and values that stay in memory in 4 bits.  The three calls below append a
+ * step's keys and values to a paged cache, read them back, and attend to them.
+ *
+ * The cache of one layer is a pool of n_pages pages of tpq_kv_page_bytes bytes each, owned by the caller, which also
+ * decides which page holds which positions of which sequence.  Format of a page: [n_kv_heads][page_size / 16] blocks
+ * of 16 positions; a block of 16 * (head_dim + 8) bytes holds
+ *   16 rows of head_dim/2 bytes, the keys' codes: code d of a row is the low nibble of byte d/2 if d is even, else
+ *      the high nibble (unsigned, 0 .. 15);
+ *   16 such rows of the values' codes;
+ *   16 32-bit words of the keys, one per position, then 16 words of the values: BF16 `step` in the low half, BF16
+ *      `low` in the high half.
+ * Code c of a vector stands for  low + step * c.  A vector x (one position, one head, head_dim values in binary32)
+ * becomes
+ *   low  = bf16(min x),  step = bf16(max((max x - low) / 15, 2^-16 max |x|, 2^-60)),
+ *   code = clamp(round-half-to-even((x - low) / step), 0, 15),
+ * one range per vector as it arrives: unlike the partial sums' ranges (Section 3) the keys' and values' are not
+ * static.  A vector that holds a NaN or an infinity, or whose max - min exceeds binary32, becomes low = NaN,
+ * step = 1, codes 0: every value of it reads as NaN.  4 + 32/head_dim bits per value (4.25 at head_dim = 128).
+ *
+ * Conventions beside those above: a handle holds no data of a caller's and serves any number of layers and caches
+ * of its geometry; its device must be the current one in every call (BAD_STATE).  What a batch says on the DEVICE
+ * is checked by the kernels: a sequence whose description contradicts itself or the batch, a position outside the rotation's table and a
+ * page number outside the pool are skipped (rows of outputs stay as they were; positions of a bad page are invisible) and the
+ * handle's device status becomes TPQ_ERR_INVALID_ARG (tpq_kv_device_status). */
+
+typedef struct tpq_kv tpq_kv; /* opaque */
+
+/* n_heads query heads in n_kv_heads groups of consecutive heads (n_heads a multiple of n_kv_heads, at most 256 per
+ * key head), head_dim 64 or 128, page_size (positions per page) 16, 32, 64, 128 or 256.  Errors: INVALID_ARG, NOMEM, CUDA. */
+tpq_status tpq_kv_create(tpq_kv **kv, int n_heads, int n_kv_heads, int head_dim, int page_size);
+tpq_status tpq_kv_destroy(tpq_kv *kv); /* NULL is accepted */
+size_t tpq_kv_page_bytes(const tpq_kv *kv); /* 0 for NULL */
+
+/* One step of a batch of sequences.  Sequence s brings rows token_start[s] .. token_start[s+1] - 1 of the step's
+ * tensors (none is allowed); they are its LAST positions: with n rows and length lengths[s] >= n, row i of the
+ * sequence is position lengths[s] - n + i.  Position t lies in page page_table[s][t / page_size], entry t % page_size.
+ * Only entries of the page table that a call needs are read (attention: pages with a visible position), so entries
+ * of pages that a window has left behind may hold anything.  Rows from token_start[n_seqs] on belong to nobody: no
+ * call reads or writes them, and a captured call can be replayed with fewer rows, sequences (n = 0) or other lengths. */
+typedef struct tpq_kv_batch {
+    void *cache_dev;               /* n_pages * tpq_kv_page_bytes bytes, 16-byte aligned */
+    int64_t n_pages;
+    const int32_t *page_table_dev; /* [n_seqs][page_table_stride], 4-byte aligned, as the next two */
+    int64_t page_table_stride;     /* = most pages of a sequence */
+    const int32_t *token_start_dev; /* [n_seqs + 1], ascending from 0 */
+    const int32_t *lengths_dev;    /* [n_seqs] positions of a sequence, the new ones included */
+    int32_t n_seqs;
+    int32_t max_new;               /* no sequence brings more rows than this (it chooses kernels) */
+    int64_t n_tokens;              /* rows of the step's tensors, >= token_start[n_seqs] */
+} tpq_kv_batch;
+
+/* Rotation of the first rot_dim values of a head by their position (rot_dim a multiple of 16, at most head_dim):
+ * pair j, 0 <= j < rot_dim/2, becomes (a cos - b sin, b cos + a sin) in binary32, each product and sum rounded, with
+ * cos = table[p][j], sin = table[p][rot_dim/2 + j].  Pair j is values j and rot_dim/2 + j, or, if interleaved is not 0, values
+ * 2j and 2j + 1. */
+typedef struct tpq_kv_rotation {
+    const float *table_dev;       /* [n_positions][rot_dim], 16-byte aligned */
+    int64_t n_positions;
+    int32_t rot_dim;
+    int32_t interleaved;
+    const int32_t *positions_dev; /* [n_tokens] p of every row, or NULL: a row's position in its sequence */
+} tpq_kv_rotation;
+
+/* Append: the step's keys (rotated) and values (as they are) go to their entries of the cache, quantised as above from the rotated binary32
+ * values; the queries, if given, are rotated and rounded to BF16.
+ *   rotation          : NULL for none (then q must be NULL: there would be nothing to do)
+ *   k, v              : [n_tokens][n_kv_heads * head_dim] BF16; q, q_out : [n_tokens][n_heads * head_dim] BF16; q may
+ *                       be NULL, q_out may be q (same stride).  Rows 16-byte aligned: strides (in elements) multiples of 8.
+ * Two sequences must not append to the same entry (which one it holds is then not specified, nor that it is one of
+ * them).  Enqueues on cuda_stream; n_tokens == 0 or n_seqs == 0 is a no-op.  Errors: INVALID_ARG, ALIGN, BAD_STATE, CUDA. */
+tpq_status tpq_kv_append(tpq_kv *kv, const tpq_kv_batch *batch, const tpq_kv_rotation *rotation, const void *k_bf16_dev,
+                         int64_t k_stride, const void *v_bf16_dev, int64_t v_stride, const void *q_bf16_dev,
+                         int64_t q_stride, void *q_out_dev, int64_t q_out_stride, void *cuda_stream);
+
+/* Read back: the values that the cache holds for the batch's rows, bf16(low + step * code), the sum rounded to binary32 first.  A batch whose
+ * sequences bring all their positions reads whole sequences.  Either output may be NULL.
+ *   k_out, v_out : [n_tokens][n_kv_heads * head_dim] BF16, rows 16-byte aligned
+ * Enqueues on cuda_stream.  Errors as tpq_kv_append. */
+tpq_status tpq_kv_read(tpq_kv *kv, const tpq_kv_batch *batch, void *k_out_dev, int64_t k_out_stride, void *v_out_dev,
+                       int64_t v_out_stride, void *cuda_stream);
+
+/* Attention: row i of a sequence, at position p, and query head h:
+ *   out = sum_t w_t v_t / sum_t w_t,  w_t = exp(scale q . k_t),  over the visible t:
+ *   t <= p, and, if window > 0, t > p - window or t < n_first
+ * (the sliding window of the last `window` positions, p's own among them, and the first n_first positions, which stay
+ * visible).  k_t, v_t: the values low + step * code of key head h / (n_heads / n_kv_heads).  Zeros where nothing is
+ * visible (all pages of a row were bad).  Products of queries and codes are exact, sums and softmax statistics are
+ * binary32; the weights times the values' steps are rounded to 11 bits ahead of their products with the codes; one
+ * rounding to BF16 at the end.
+ *   q, out    : [n_tokens][n_heads * head_dim] BF16, rows 16-byte aligned; out must not overlap q
+ *   scale     : finite (1/sqrt(head_dim) as a rule);  window : 0 for none;  n_first : >= 0, without effect if there is no window
+ *   workspace : >= tpq_kv_attention_workspace(kv, n_seqs, max_new, n_tokens) bytes of device memory, 16-byte aligned, whose
+ *               contents need no preparation and mean nothing afterwards.  Calls that may overlap on the GPU (other
+ *               streams, two graphs) need workspaces of their own.
+ * Enqueues on cuda_stream; n_tokens == 0 or n_seqs == 0 is a no-op.  Errors: INVALID_ARG, ALIGN, SIZE, BAD_STATE, CUDA;
+ * TPQ_ERR_TIMEOUT through tpq_kv_device_status. */
+size_t tpq_kv_attention_workspace(const tpq_kv *kv, int32_t n_seqs, int32_t max_new, int64_t n_tokens);
+tpq_status tpq_kv_attention(tpq_kv *kv, const tpq_kv_batch *batch, const void *q_bf16_dev, int64_t q_stride, float scale,
+                            int64_t window, int64_t n_first, void *out_dev, int64_t out_stride, void *workspace_dev,
+                            size_t workspace_bytes, void *cuda_stream);
+
+/* As tpq_device_status, tpq_launch_count and tpq_last_error, for this handle. */
+tpq_status tpq_kv_device_status(tpq_kv *kv);
+int64_t tpq_kv_launch_count(const tpq_kv *kv);
+const char *tpq_kv_last_error(const tpq_kv *kv);
+
 /* ------------------------------------------------- checkpoint and status */
 
 /* Serialise / restore the whole static state (N, E, bits, gamma, counts, m, M,

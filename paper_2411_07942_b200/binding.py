@@ -36,6 +36,17 @@ class CommReport(ctypes.Structure):
                 ("bits_per_value", c_double), ("bits_per_value_formula", c_double)]
 
 
+class KvBatch(ctypes.Structure):
+    """One step of a batch over a paged cache (tpq_kv_batch; device pointers as integers)."""
+    _fields_ = [("cache_ptr", c_void_p), ("n_pages", c_int64), ("page_table_ptr", c_void_p), ("page_table_stride", c_int64),
+                ("token_start_ptr", c_void_p), ("lengths_ptr", c_void_p), ("n_seqs", c_int32), ("max_new", c_int32), ("n_tokens", c_int64)]
+
+
+class KvRotation(ctypes.Structure):
+    """Rotation by position (tpq_kv_rotation; device pointers as integers, positions_ptr may be None)."""
+    _fields_ = [("table_ptr", c_void_p), ("n_positions", c_int64), ("rot_dim", c_int32), ("interleaved", c_int32), ("positions_ptr", c_void_p)]
+
+
 # name -> (restype, argtypes); one entry per declaration in include/tpq.h
 SIGNATURES = {
     "tpq_create": (c_int, [POINTER(c_void_p), c_int, c_int, c_int, c_float]),
@@ -73,6 +84,18 @@ SIGNATURES = {
     "tpq_set_state": (c_int, [c_void_p, c_void_p, c_size_t]),
     "tpq_device_status": (c_int, [c_void_p]),
     "tpq_launch_count": (c_int64, [c_void_p]),
+    "tpq_kv_create": (c_int, [POINTER(c_void_p), c_int, c_int, c_int, c_int]),
+    "tpq_kv_destroy": (c_int, [c_void_p]),
+    "tpq_kv_page_bytes": (c_size_t, [c_void_p]),
+    "tpq_kv_append": (c_int, [c_void_p, POINTER(KvBatch), POINTER(KvRotation), c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int64, c_void_p,
+                              c_int64, c_void_p]),
+    "tpq_kv_read": (c_int, [c_void_p, POINTER(KvBatch), c_void_p, c_int64, c_void_p, c_int64, c_void_p]),
+    "tpq_kv_attention_workspace": (c_size_t, [c_void_p, c_int32, c_int32, c_int64]),
+    "tpq_kv_attention": (c_int, [c_void_p, POINTER(KvBatch), c_void_p, c_int64, c_float, c_int64, c_int64, c_void_p, c_int64, c_void_p, c_size_t,
+                                 c_void_p]),
+    "tpq_kv_device_status": (c_int, [c_void_p]),
+    "tpq_kv_launch_count": (c_int64, [c_void_p]),
+    "tpq_kv_last_error": (c_char_p, [c_void_p]),
     "tpq_status_string": (c_char_p, [c_int]),
     "tpq_last_error": (c_char_p, [c_void_p]),
     "tpq_version": (c_char_p, []),
@@ -348,6 +371,77 @@ class Tpq:
 
     def launch_count(self) -> int:
         return int(lib().tpq_launch_count(self._h))
+
+
+class TpqKv:
+    """Attention over keys and values held in 4 bits, in the pages of a cache that the caller owns (tpq_kv_*).  One handle
+    serves any number of layers and caches of its geometry."""
+
+    def __init__(self, n_heads: int, n_kv_heads: int, head_dim: int, page_size: int):
+        self._h = c_void_p()
+        st = lib().tpq_kv_create(byref(self._h), n_heads, n_kv_heads, head_dim, page_size)
+        if st != TPQ_OK:
+            self._h = c_void_p()
+            raise TpqError(st, "tpq_kv_create failed")
+        self.n_heads, self.n_kv_heads, self.head_dim, self.page_size = n_heads, n_kv_heads, head_dim, page_size
+
+    def close(self):
+        if getattr(self, "_h", None) and self._h.value:
+            lib().tpq_kv_destroy(self._h)
+            self._h = c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _check(self, st: int):
+        if st != TPQ_OK:
+            raise TpqError(st, lib().tpq_kv_last_error(self._h).decode())
+
+    # raw status-returning calls (for error-path tests)
+    def raw(self, name: str, *args) -> int:
+        return getattr(lib(), name)(self._h, *args)
+
+    def page_bytes(self) -> int:
+        return int(lib().tpq_kv_page_bytes(self._h))
+
+    def append(self, batch: KvBatch, k_ptr: int, v_ptr: int, k_stride: int | None = None, v_stride: int | None = None,
+               rotation: KvRotation | None = None, q_ptr: int | None = None, q_stride: int | None = None, q_out_ptr: int | None = None,
+               q_out_stride: int | None = None, stream: int = 0):
+        kv_row, q_row = self.n_kv_heads * self.head_dim, self.n_heads * self.head_dim
+        st = lib().tpq_kv_append(self._h, batch, rotation, k_ptr, kv_row if k_stride is None else k_stride, v_ptr,
+                                 kv_row if v_stride is None else v_stride, q_ptr, q_row if q_stride is None else q_stride, q_out_ptr,
+                                 q_row if q_out_stride is None else q_out_stride, stream)
+        if st:
+            self._check(st)
+
+    def read(self, batch: KvBatch, k_out_ptr: int | None, v_out_ptr: int | None, k_out_stride: int | None = None,
+             v_out_stride: int | None = None, stream: int = 0):
+        row = self.n_kv_heads * self.head_dim
+        st = lib().tpq_kv_read(self._h, batch, k_out_ptr, row if k_out_stride is None else k_out_stride, v_out_ptr,
+                               row if v_out_stride is None else v_out_stride, stream)
+        if st:
+            self._check(st)
+
+    def attention_workspace_bytes(self, batch: KvBatch) -> int:
+        """Workspace of an attention call over this batch, or over one with fewer sequences, rows or new positions."""
+        return int(lib().tpq_kv_attention_workspace(self._h, batch.n_seqs, batch.max_new, batch.n_tokens))
+
+    def attention(self, batch: KvBatch, q_ptr: int, out_ptr: int, workspace_ptr: int, workspace_bytes: int, scale: float, window: int = 0,
+                  first: int = 0, q_stride: int | None = None, out_stride: int | None = None, stream: int = 0):
+        row = self.n_heads * self.head_dim
+        st = lib().tpq_kv_attention(self._h, batch, q_ptr, row if q_stride is None else q_stride, scale, window, first, out_ptr,
+                                    row if out_stride is None else out_stride, workspace_ptr, workspace_bytes, stream)
+        if st:
+            self._check(st)
+
+    def device_status(self) -> int:
+        return int(lib().tpq_kv_device_status(self._h))
+
+    def launch_count(self) -> int:
+        return int(lib().tpq_kv_launch_count(self._h))
 
 
 def payload_bytes_for(T: int, E: int, k: int, bits: int = 4) -> int:
