@@ -1,10 +1,565 @@
-// Attention over the 4-bit cache (tpq_kv_attention): a warp per row and query head walks the visible positions with the
-// running maximum and sum of the softmax.
+// Attention over the 4-bit cache (tpq_kv_attention) for sequences that bring few rows: decoding, drafts to verify.
+//
+// Mathematics.  With keys k_t = a_t + s_t c_t (a: low, s: step, c: codes) and values v_t = b_t + r_t e_t,
+//   x_t = scale log2(e) (s_t q.c_t + a_t sum(q)),  out = sum_t 2^x_t (b_t + r_t e_t) / sum_t 2^x_t.
+// The products with codes run on the tensor cores with the codes themselves as operands: no key or value is ever formed.
+// The values' steps go into the exponent, P_t = 2^(x_t + log2 r_t - m), so that a product P_t e_t needs no scale of its own
+// and P_t <= 1 whatever the steps are; then
+//   out = sum_t P_t (e_t - 8) + sum_t P_t (b_t / r_t + 8)   over   sum_t P_t / r_t,
+// m the running maximum of x_t + log2 r_t.
+//
+// Codes become operands with one logic instruction for two: a code in the low mantissa bits of BF16 128 (0x4300 | c) is
+// 128 + c, in bits 4 .. 7 of FP16 1024 (0x6400 | 16 c) is 16 (64 + c), both exact.  Of the keys' 128 the sum over q is taken
+// off with a_t's (a_t - 128 s_t); the values' 72 x 16 = 1152 by one more product, of P with a constant, which the
+// accumulators of 32 positions start from: they hold sums of P (e - 8) alone, and what is added up in
+// binary32 over a whole sequence has no common offset to lose digits to.  P is rounded to FP16 (11 bits; below 2^-26
+// of the largest one, with fewer), Q and the codes are exact.
+//
+// Operands.  Rows (query heads of one key head x new positions) are the 8 columns of an m16n8k16 product, positions (for the
+// values: a head's values) its 16 rows, so that 8 query heads per key head leave nothing of the instruction unused.  The scores come
+// out with positions along the lanes' groups; movmatrix turns them into the second product's operand.  Which code is which row
+// or column of a fragment is free as long as both sides agree: lanes read 16 (keys) and 8 (values) contiguous bytes of a
+// position, conflict-free and two-way.  mma.sync and not tcgen05: 16 positions x 8 rows are an eighth of the smallest
+// tcgen05 tile, and what bounds this kernel is the memory that the codes come from and the instructions that unpack them
+// (about 190 per warp and 16 positions of 2176 bytes).
+//
+// Work.  The positions of all sequences and key heads are cut into tiles of 128 and dealt out evenly, in order, to as many
+// blocks as the GPU holds at a time, whatever the lengths are (a graph with this call replays for others).  A block whose
+// run begins or ends inside a (sequence, key head) leaves a partial result, at most two in all; attention_join puts them
+// together.  A warp takes 32 of a tile's 128 positions, by itself: its copies (16 positions = one
+// contiguous block of the cache), its barriers, its running maximum; the warps meet at the end of a (sequence, key head).
 #include "kv_internal.h"
 
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 
 namespace {
+
+constexpr int TILE = 128, WARPS = 4, CHUNK = TILE / WARPS;  // positions of a tile, of a warp's share
+constexpr int MAX_ROWS = 32;                                // rows (new positions x query heads of a key head) of this kernel
+
+// NT: groups of 8 rows.  Blocks of an SM: what registers (32 NT sums and as much besides) allow.
+__host__ __device__ constexpr int stages(int D, int NT) { return D == 64 || NT == 4 ? 4 : 3; }
+__host__ __device__ constexpr int blocks_per_sm(int NT) { return NT == 1 ? 4 : NT == 2 ? 3 : 2; }
+__host__ __device__ constexpr int chunk_bytes(int D) { return CHUNK / KV_BLOCK * kv_block_bytes(D); }
+// floats of a partial result: rows x (sums of D values, maximum, normaliser), rows padded to 16 bytes
+__host__ __device__ constexpr int part_row(int D) { return D + 4; }
+
+template <int D, int NT>
+struct Shared {
+    uint8_t ring[WARPS][stages(D, NT)][chunk_bytes(D)];  // (at a segment's end, a warp's sums: [8 NT][D + 4] floats)
+    float4 words[WARPS][CHUNK];                          // per position: key step and offset, log2 of the value step, its reciprocal
+    float lows[WARPS][CHUNK];                            // (value low) / (value step) + 8
+    uint2 q[NT == 1 ? 1 : NT * (D / 16) * 32];           // (NT > 1) the rows as operands
+    float m[WARPS][8 * NT], l[WARPS][8 * NT];
+    uint64_t full[WARPS][stages(D, NT)];
+    uint32_t there[WARPS][stages(D, NT)];                // bit b: block b of the chunk was copied
+    int scan[WARPS];
+    int begin[3];                                        // where the block's run begins: sequence, tile of that sequence; length of a run
+};
+
+struct split_params {
+    kv_batch b;
+    kv_attention_call c;
+    float *parts;   // [blocks][2][8 NT][part_row]
+    int4 *headers;  // [blocks]: of the part that the block's run ends with: parts of its (sequence, key head), first row, rows, key head
+    float scale2;   // scale * log2(e)
+    int group;      // query heads of a key head
+};
+
+__device__ __forceinline__ float ex2(float x)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float lg2(float x)
+{
+    float r;
+    asm("lg2.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t mask, uint32_t bits)
+{
+    uint32_t r;
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(a), "r"(mask), "r"(bits));
+    return r;
+}
+__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t x)
+{
+    uint32_t r;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+    return r;
+}
+
+// Tiles of a sequence that any of its rows sees: [0, first) and [from, end).
+struct tiles_of {
+    int first, from, count;
+};
+__device__ __forceinline__ tiles_of visible_tiles(const kv_seq &s, const kv_attention_call &c, int group)
+{
+    tiles_of t{0, 0, 0};
+    if (s.n <= 0 || s.n * group > MAX_ROWS) return t;
+    if (c.window) {
+        const int64_t from = (int64_t)(s.len - s.n) - c.window + 1;  // of the first row
+        if (from > 0) {
+            t.from = (int)(from / TILE);
+            const int first = (int)(((c.n_first < from ? c.n_first : from) + TILE - 1) / TILE);
+            t.first = first < t.from ? first : t.from;
+        }
+    }
+    t.count = t.first + (s.len + TILE - 1) / TILE - t.from;
+    return t;
+}
+
+template <int D, int NT>
+__global__ void __launch_bounds__(WARPS * 32, blocks_per_sm(NT))
+attention_split(const split_params p)
+{
+    constexpr int NS = stages(D, NT), R = 8 * NT, KW = D / 32;  // KW: words of a key row that a lane reads
+    extern __shared__ __align__(16) uint8_t raw[];
+    Shared<D, NT> &sh = *reinterpret_cast<Shared<D, NT> *>(raw);
+    const kv_batch &b = p.b;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, i4 = lane & 3;
+    if (lane == 0)
+        for (int s = 0; s < NS; ++s) mbar_init(smem_u32(&sh.full[warp][s]), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    tpq_grid_dep_wait();
+    tpq_grid_dep_launch();
+
+    // ---- where this block's run begins
+    const int per = (b.n_seqs + WARPS * 32 - 1) / (WARPS * 32);
+    const int s0 = tid * per, s1 = s0 + per < b.n_seqs ? s0 + per : b.n_seqs;
+    int64_t want = 0;
+    for (int s = s0; s < s1; ++s) want += (int64_t)visible_tiles(kv_load_seq(b, s), p.c, p.group).count * b.n_kv_heads;
+    if (want >= 1 << 23) {  // (2^30 positions of key heads in a 128th of the sequences: the sums below are in 32 bits)
+        kv_report(b);
+        want = 0;
+    }
+    const int mine = (int)want;
+    int sum = mine;
+#pragma unroll
+    for (int m = 1; m < 32; m <<= 1) {
+        const int o = __shfl_up_sync(0xffffffffu, sum, m);
+        if (lane >= m) sum += o;
+    }
+    if (lane == 31) sh.scan[warp] = sum;
+    __syncthreads();
+    int total = 0, before = sum - mine;
+    for (int w = 0; w < WARPS; ++w) {
+        if (w < warp) before += sh.scan[w];
+        total += sh.scan[w];
+    }
+    const int share = (total + gridDim.x - 1) / gridDim.x;
+    int unit = blockIdx.x * share;
+    const int unit_end = unit + share < total ? unit + share : total;
+    if (unit >= unit_end) {
+        if (tid == 0) p.headers[blockIdx.x] = make_int4(0, 0, 0, 0);
+        return;
+    }
+    if (unit >= before && unit < before + mine) {
+        int off = unit - before, s = s0;
+        for (;; ++s) {
+            const int n = visible_tiles(kv_load_seq(b, s), p.c, p.group).count * b.n_kv_heads;
+            if (off < n) break;
+            off -= n;
+        }
+        sh.begin[0] = s;
+        sh.begin[1] = off;
+    }
+    __syncthreads();
+    int s = sh.begin[0], off = sh.begin[1];
+    int phase = 0;  // chunks of the segments before (a warp's own): chunk j is in stage (phase + j) % NS
+    int issued = 0;
+    bool ok = true;
+    int4 header = make_int4(0, 0, 0, 0);
+
+    while (unit < unit_end) {
+        const kv_seq seq = kv_load_seq(b, s);
+        const tiles_of tl = visible_tiles(seq, p.c, p.group);
+        if (tl.count == 0 || off >= tl.count * b.n_kv_heads) {
+            off -= tl.count * b.n_kv_heads;
+            ++s;
+            continue;
+        }
+        const int kh = off / tl.count, t0 = off - kh * tl.count;
+        const int nt = tl.count - t0 < unit_end - unit ? tl.count - t0 : unit_end - unit;
+        const int rows = seq.n * p.group, p0 = seq.len - seq.n;
+
+        // ---- the rows as operands: column n = lane / 4 of a group of 8, values 8 KW i4 .. of the head in the order (0 4)(1 5)(2 6)(3 7)
+        uint2 qf[NT == 1 ? D / 16 : 1];
+        float qsum[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int r = 8 * n + g, tok = r / p.group, h = kh * p.group + (r - tok * p.group);
+            const uint4 *src = reinterpret_cast<const uint4 *>(p.c.q.p + (int64_t)(seq.start + tok) * p.c.q.stride + (int64_t)h * D + 8 * KW * i4);
+            float sum_q = 0.0f;
+#pragma unroll
+            for (int j = 0; j < KW; ++j) {
+                const uint4 x = r < rows ? src[j] : make_uint4(0, 0, 0, 0);
+                const uint32_t u[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) sum_q += __uint_as_float(u[k] << 16) + __uint_as_float(u[k] & 0xffff0000u);
+                const uint2 f0 = make_uint2(__byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632));
+                const uint2 f1 = make_uint2(__byte_perm(x.y, x.w, 0x5410), __byte_perm(x.y, x.w, 0x7632));
+                if (NT == 1) {
+                    qf[2 * j] = f0;
+                    qf[2 * j + 1] = f1;
+                } else if (n % WARPS == warp || NT == 2) {  // (every warp has them all; one stores)
+                    sh.q[(n * (D / 16) + 2 * j) * 32 + lane] = f0;
+                    sh.q[(n * (D / 16) + 2 * j + 1) * 32 + lane] = f1;
+                }
+            }
+            sum_q += __shfl_xor_sync(0xffffffffu, sum_q, 1);
+            sum_q += __shfl_xor_sync(0xffffffffu, sum_q, 2);
+            qsum[n][0] = __shfl_sync(0xffffffffu, sum_q, 8 * i4);      // of columns 2 i4 and 2 i4 + 1
+            qsum[n][1] = __shfl_sync(0xffffffffu, sum_q, 8 * i4 + 4);
+        }
+        if (NT > 1) __syncthreads();
+        float m[NT][2], l[NT][2], w[NT][2], o[NT][D / 16][4];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) m[n][k] = -INFINITY, l[n][k] = 0.0f, w[n][k] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) o[n][k][0] = o[n][k][1] = o[n][k][2] = o[n][k][3] = 0.0f;
+        }
+
+        // ---- copies: chunk j of the segment, block lane (0 or 1) of it
+        auto base_of = [&](int j) {
+            const int t = t0 + j;
+            return (t < tl.first ? t : tl.from + t - tl.first) * TILE + warp * CHUNK;
+        };
+        auto page_of = [&](int j) {  // page of this lane's block of chunk j, -1: none to copy
+            if (j >= nt || lane > 1) return -1;
+            const int pos = base_of(j) + lane * KV_BLOCK;
+            if (pos >= seq.len) return -1;
+            if (p.c.window && pos >= p.c.n_first && (int64_t)pos + KV_BLOCK <= (int64_t)p0 - p.c.window + 1) return -1;  // no row sees it
+            const int page = b.table[s * b.table_stride + (pos >> b.page_shift)];
+            if (page >= 0 && page < b.n_pages) return page;
+            kv_report(b);
+            return -1;
+        };
+        auto issue = [&](int j, int page) {
+            const int st = (phase + j) % NS;
+            const uint32_t bar = smem_u32(&sh.full[warp][st]);
+            const uint32_t there = __ballot_sync(0xffffffffu, page >= 0) & 3u;
+            issued = phase + j + 1;
+            if (lane == 0) {
+                sh.there[warp][st] = there;
+                mbar_expect_tx(bar, __popc(there) * kv_block_bytes(D));
+            }
+            __syncwarp();
+            if (page >= 0) {
+                const int pos = base_of(j) + lane * KV_BLOCK, blocks = b.page_size / KV_BLOCK;
+                const uint8_t *src = b.cache + (((int64_t)page * b.n_kv_heads + kh) * blocks + (pos & (b.page_size - 1)) / KV_BLOCK) * kv_block_bytes(D);
+                bulk_g2s(smem_u32(&sh.ring[warp][st][lane * kv_block_bytes(D)]), src, kv_block_bytes(D), bar);
+            }
+        };
+#pragma unroll
+        for (int j = 0; j < NS - 1; ++j)
+            if (j < nt) issue(j, page_of(j));
+        int next_page = page_of(NS - 1);
+
+        for (int j = 0; j < nt && ok; ++j) {
+            __syncwarp();  // every lane has read the stage that the next copy overwrites
+            if (j + NS - 1 < nt) issue(j + NS - 1, next_page);
+            next_page = page_of(j + NS);
+            const int st = (phase + j) % NS;
+            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.full[warp][st]), ((phase + j) / NS) & 1));
+            if (!ok) break;
+            const uint8_t *chunk = sh.ring[warp][st];
+            const int base = base_of(j);
+            const uint32_t there = sh.there[warp][st];
+            if (there == 0) continue;
+            {   // lane <-> position: what its words say
+                const int pos = base + lane;
+                const uint32_t *ws = reinterpret_cast<const uint32_t *>(chunk + (lane / KV_BLOCK) * kv_block_bytes(D)) + lane % KV_BLOCK;
+                const uint32_t kw = ws[kv_k_words(D) / 4], vw = ws[kv_v_words(D) / 4];
+                const float ks = __uint_as_float(kw << 16), kl = __uint_as_float(kw & 0xffff0000u);
+                const float vs = __uint_as_float(vw << 16), vl = __uint_as_float(vw & 0xffff0000u);
+                const bool on = pos < seq.len && ((there >> (lane / KV_BLOCK)) & 1u);
+                const float inv = __frcp_rn(vs);
+                // (positions of nobody: whatever their bytes are, NaN among them, weight 0 and finite terms)
+                sh.words[warp][lane] = on ? make_float4(ks * p.scale2, fmaf(-128.0f, ks, kl) * p.scale2, lg2(vs), inv) : make_float4(0.0f, 0.0f, -INFINITY, 0.0f);
+                sh.lows[warp][lane] = on ? fmaf(vl, inv, 8.0f) : 0.0f;
+            }
+            __syncwarp();
+
+            // ---- scores of 32 positions: x[n][block][position half][column]
+            float x[NT][2][4];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                // position of row r of the product: (r >> 1) + 4 (r & 1), and 8 more for rows 8 .. 15 (the values' reads below
+                // then hit few banks twice)
+                const uint8_t *rows_k = chunk + k * kv_block_bytes(D) + ((g >> 1) + 4 * (g & 1)) * (D / 2) + 4 * KW * i4;
+                uint32_t ca[KW], cb[KW];
+                if (KW == 4) {
+                    *reinterpret_cast<uint4 *>(ca) = *reinterpret_cast<const uint4 *>(rows_k);
+                    *reinterpret_cast<uint4 *>(cb) = *reinterpret_cast<const uint4 *>(rows_k + 8 * (D / 2));
+                } else {
+                    *reinterpret_cast<uint2 *>(ca) = *reinterpret_cast<const uint2 *>(rows_k);
+                    *reinterpret_cast<uint2 *>(cb) = *reinterpret_cast<const uint2 *>(rows_k + 8 * (D / 2));
+                }
+#pragma unroll
+                for (int n = 0; n < NT; ++n) x[n][k][0] = x[n][k][1] = x[n][k][2] = x[n][k][3] = 0.0f;
+#pragma unroll
+                for (int jw = 0; jw < KW; ++jw)
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        const uint32_t a0 = and_or(ca[jw] >> (8 * half), 0x000f000fu, 0x43004300u), a2 = and_or(ca[jw] >> (8 * half + 4), 0x000f000fu, 0x43004300u);
+                        const uint32_t a1 = and_or(cb[jw] >> (8 * half), 0x000f000fu, 0x43004300u), a3 = and_or(cb[jw] >> (8 * half + 4), 0x000f000fu, 0x43004300u);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            const uint2 f = NT == 1 ? qf[2 * jw + half] : sh.q[(n * (D / 16) + 2 * jw + half) * 32 + lane];
+                            mma_bf16(x[n][k], a0, a1, a2, a3, f.x, f.y);
+                        }
+                    }
+            }
+            float4 wd[2][2];
+            float lw[2][2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int at = k * KV_BLOCK + (g >> 1) + 4 * (g & 1) + 8 * e;
+                    wd[k][e] = sh.words[warp][at];
+                    lw[k][e] = sh.lows[warp][at];
+                }
+            // every row sees every position of the chunk (that there is)?
+            const bool all = base + CHUNK - 1 <= p0 && (p.c.window == 0 || base > (int64_t)seq.len - 1 - p.c.window || base + CHUNK <= p.c.n_first);
+            uint32_t pf[NT][2][2];
+            float alpha[NT][2];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    float top = m[n][c];
+#pragma unroll
+                    for (int k = 0; k < 2; ++k)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            float y = fmaf(x[n][k][2 * e + c], wd[k][e].x, fmaf(qsum[n][c], wd[k][e].y, wd[k][e].z));
+                            if (!all) {
+                                const int pos = base + k * KV_BLOCK + (g >> 1) + 4 * (g & 1) + 8 * e, at = p0 + (8 * n + 2 * i4 + c) / p.group;
+                                const bool see = pos <= at && (p.c.window == 0 || pos > (int64_t)at - p.c.window || pos < p.c.n_first);
+                                if (!see) y = -INFINITY;
+                            }
+                            x[n][k][2 * e + c] = y;
+                            top = fmaxf(top, y);
+                        }
+                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
+                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+                    const float from = top == -INFINITY ? 0.0f : top;
+                    alpha[n][c] = ex2(m[n][c] - from);
+                    m[n][c] = top;
+                    l[n][c] *= alpha[n][c];
+                    w[n][c] *= alpha[n][c];
+#pragma unroll
+                    for (int k = 0; k < 2; ++k)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            // 2^12 P: FP16 then holds P down to 2^-26 with all its bits (all sums carry the factor)
+                            const float pr = ex2(x[n][k][2 * e + c] - from + 12.0f);
+                            x[n][k][2 * e + c] = pr;
+                            l[n][c] = fmaf(pr, wd[k][e].w, l[n][c]);
+                            w[n][c] = fmaf(pr, lw[k][e], w[n][c]);
+                        }
+                }
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const __half2 h = __floats2half2_rn(x[n][k][2 * e], x[n][k][2 * e + 1]);
+                        pf[n][k][e] = transposed(*reinterpret_cast<const uint32_t *>(&h));
+                    }
+            }
+            // ---- values: -1152 sum of P first, then the codes
+            float start[NT][4];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                start[n][0] = start[n][1] = start[n][2] = start[n][3] = 0.0f;
+#pragma unroll
+                for (int k = 0; k < 2; ++k) mma_f16(start[n], 0xe480e480u, 0xe480e480u, 0xe480e480u, 0xe480e480u, pf[n][k][0], pf[n][k][1]);
+            }
+#pragma unroll
+            for (int jw = 0; jw < D / 64; ++jw) {
+                uint32_t lo[2][2], hi[2][2];  // of block k: positions i4, i4 + 4 (e = 0) and i4 + 8, i4 + 12 (e = 1); codes 0-3 and 4-7 of both
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const uint8_t *row = chunk + k * kv_block_bytes(D) + kv_v_codes(D) + (i4 + 8 * e) * (D / 2) + (D / 16) * g + 4 * jw;
+                        const uint32_t u = *reinterpret_cast<const uint32_t *>(row), v = *reinterpret_cast<const uint32_t *>(row + 4 * (D / 2));
+                        lo[k][e] = __byte_perm(u, v, 0x5410);
+                        hi[k][e] = __byte_perm(u, v, 0x7632);
+                    }
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {  // codes 2q, 2q + 1 of the word
+                    float acc[NT][4];
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) acc[n][0] = start[n][0], acc[n][1] = start[n][1], acc[n][2] = start[n][0], acc[n][3] = start[n][1];
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        uint32_t a[2][2];  // [code][e]
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const uint32_t z = q < 2 ? lo[k][e] : hi[k][e];
+                            a[0][e] = and_or(q & 1 ? z >> 4 : z << 4, 0x00f000f0u, 0x64006400u);
+                            a[1][e] = and_or(q & 1 ? z >> 8 : z, 0x00f000f0u, 0x64006400u);
+                        }
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) mma_f16(acc[n], a[0][0], a[1][0], a[0][1], a[1][1], pf[n][k][0], pf[n][k][1]);
+                    }
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[n][4 * jw + q][e] = fmaf(o[n][4 * jw + q][e], alpha[n][e & 1], acc[n][e]);
+                }
+            }
+        }
+        phase += nt;
+
+        // ---- the four warps' results of this (sequence, key head)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int k = 4; k < 32; k <<= 1) {
+                    l[n][c] += __shfl_xor_sync(0xffffffffu, l[n][c], k);
+                    w[n][c] += __shfl_xor_sync(0xffffffffu, w[n][c], k);
+                }
+        if (g == 0)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    sh.m[warp][8 * n + 2 * i4 + c] = m[n][c];
+                    sh.l[warp][8 * n + 2 * i4 + c] = l[n][c];
+                }
+        float *mine_o = reinterpret_cast<float *>(sh.ring[warp][0]);
+        __syncwarp();
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+                for (int c = 0; c < 2; ++c)  // values (D/8) g + 2k, + 1 of row 8n + 2 i4 + c; the factor 16 of the codes goes
+                    *reinterpret_cast<float2 *>(mine_o + (8 * n + 2 * i4 + c) * (D + 4) + (D / 8) * g + 2 * k) =
+                        make_float2(fmaf(o[n][k][c], 0.0625f, w[n][c]), fmaf(o[n][k][2 + c], 0.0625f, w[n][c]));
+        const bool any_bad = __syncthreads_or(!ok);
+        if (any_bad) break;
+        const bool whole = t0 == 0 && nt == tl.count;
+        float *part = p.parts + ((int64_t)blockIdx.x * 2 + (t0 == 0 ? 1 : 0)) * R * part_row(D);
+        for (int at = tid; at < R * (D / 8); at += WARPS * 32) {
+            const int r = at / (D / 8), d = at % (D / 8) * 8;
+            if (r >= rows) break;
+            float top = -INFINITY;
+#pragma unroll
+            for (int v = 0; v < WARPS; ++v) top = fmaxf(top, sh.m[v][r]);
+            const float from = top == -INFINITY ? 0.0f : top;
+            float sum_l = 0.0f, y[8] = {};
+#pragma unroll
+            for (int v = 0; v < WARPS; ++v) {
+                const float f = ex2(sh.m[v][r] - from);
+                sum_l = fmaf(sh.l[v][r], f, sum_l);
+                const float4 *z = reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(sh.ring[v][0]) + r * (D + 4) + d);
+                const float4 z0 = z[0], z1 = z[1];
+                const float zz[8] = {z0.x, z0.y, z0.z, z0.w, z1.x, z1.y, z1.z, z1.w};
+#pragma unroll
+                for (int k = 0; k < 8; ++k) y[k] = fmaf(zz[k], f, y[k]);
+            }
+            if (whole) {
+                const int tok = r / p.group, h = kh * p.group + (r - tok * p.group);
+                const float inv = sum_l == 0.0f ? 0.0f : 1.0f / sum_l;
+                uint32_t u[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const __nv_bfloat162 v2 = __floats2bfloat162_rn(y[2 * k] * inv, y[2 * k + 1] * inv);
+                    u[k] = *reinterpret_cast<const uint32_t *>(&v2);
+                }
+                *reinterpret_cast<uint4 *>(p.c.out + (int64_t)(seq.start + tok) * p.c.out_stride + (int64_t)h * D + d) = make_uint4(u[0], u[1], u[2], u[3]);
+            } else {
+                float4 *dst = reinterpret_cast<float4 *>(part + r * part_row(D) + d);
+                dst[0] = make_float4(y[0], y[1], y[2], y[3]);
+                dst[1] = make_float4(y[4], y[5], y[6], y[7]);
+                if (d == 0) *reinterpret_cast<float2 *>(part + r * part_row(D) + D) = make_float2(top, sum_l);
+            }
+        }
+        if (t0 == 0 && nt < tl.count)  // begun here, ended by a later block (share tiles each)
+            header = make_int4((int)(1 + (tl.count - nt + share - 1) / share), seq.start, rows, kh);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the sums were written where copies go next
+        __syncthreads();
+        unit += nt;
+        off += nt;
+    }
+    if (!ok && lane == 0) {  // giving up: let the copies in flight land before the shared memory is released
+        atomicExch(b.status, (int)TPQ_ERR_TIMEOUT);
+        for (int k = issued > NS ? issued - NS : 0; k < issued; ++k) (void)mbar_wait(smem_u32(&sh.full[warp][k % NS]), (k / NS) & 1);
+    }
+    if (tid == 0) p.headers[blockIdx.x] = header;
+}
+
+// Puts the partial results of a (sequence, key head) together: block (i, row) for the one that run i ends with the first part of.
+template <int D, int NT>
+__global__ void __launch_bounds__(8 * D / 4)
+attention_join(const split_params p)
+{
+    constexpr int GROUPS = 8, LANES = D / 4;  // parts in flight, threads of a row
+    __shared__ float4 sums[GROUPS][LANES];
+    __shared__ float2 ml[GROUPS];
+    tpq_grid_dep_wait();
+    const int4 head = p.headers[blockIdx.x];  // parts, first row of the sequence, rows, key head
+    const int r = blockIdx.y, lane = threadIdx.x % LANES, grp = threadIdx.x / LANES;
+    if (head.x == 0 || r >= head.z) return;
+    float m = -INFINITY, l = 0.0f;
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int i = grp; i < head.x; i += GROUPS) {
+        // the first part is this run's last result, the others are the following runs' first
+        const float *part = p.parts + (((int64_t)blockIdx.x + i) * 2 + (i == 0 ? 1 : 0)) * (8 * NT) * part_row(D) + r * part_row(D);
+        const float2 v = __ldcg(reinterpret_cast<const float2 *>(part + D));
+        const float4 z = __ldcg(reinterpret_cast<const float4 *>(part) + lane);
+        const float top = fmaxf(m, v.x), from = top == -INFINITY ? 0.0f : top, a = ex2(m - from), f = ex2(v.x - from);
+        m = top;
+        l = fmaf(v.y, f, l * a);
+        o = make_float4(fmaf(z.x, f, o.x * a), fmaf(z.y, f, o.y * a), fmaf(z.z, f, o.z * a), fmaf(z.w, f, o.w * a));
+    }
+    sums[grp][lane] = o;
+    if (lane == 0) ml[grp] = make_float2(m, l);
+    __syncthreads();
+    if (grp != 0) return;
+    float top = -INFINITY, sum_l = 0.0f;
+#pragma unroll
+    for (int v = 0; v < GROUPS; ++v) top = fmaxf(top, ml[v].x);
+    const float from = top == -INFINITY ? 0.0f : top;
+    float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+    for (int v = 0; v < GROUPS; ++v) {
+        const float f = ex2(ml[v].x - from);
+        const float4 z = sums[v][lane];
+        sum_l = fmaf(ml[v].y, f, sum_l);
+        y = make_float4(fmaf(z.x, f, y.x), fmaf(z.y, f, y.y), fmaf(z.z, f, y.z), fmaf(z.w, f, y.w));
+    }
+    const float inv = sum_l == 0.0f ? 0.0f : 1.0f / sum_l;
+    const int tok = r / p.group, h = head.w * p.group + (r - tok * p.group);
+    const __nv_bfloat162 a = __floats2bfloat162_rn(y.x * inv, y.y * inv), c = __floats2bfloat162_rn(y.z * inv, y.w * inv);
+    *reinterpret_cast<uint2 *>(p.c.out + (int64_t)(head.y + tok) * p.c.out_stride + (int64_t)h * D + 4 * lane) =
+        make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&c));
+}
 
 template <int D>
 __global__ void __launch_bounds__(128)
@@ -20,7 +575,7 @@ attention_rows(const kv_batch b, const kv_attention_call c)
     const int s = kv_find_seq(b, row, lane);
     if (s < 0) return;
     const kv_seq seq = kv_load_seq(b, s);
-    if (seq.n < 0 || row >= seq.start + seq.n) return;
+    if (seq.n < 0 || row >= seq.start + seq.n || seq.n * (b.n_heads / b.n_kv_heads) <= MAX_ROWS) return;
     const int pos = seq.len - seq.n + (int)(row - seq.start);
     float q[V], o[V], m = -INFINITY, l = 0.0f;
     for (int i = 0; i < V; ++i) {
@@ -60,16 +615,51 @@ attention_rows(const kv_batch b, const kv_attention_call c)
         reinterpret_cast<__nv_bfloat16 *>(c.out)[row * c.out_stride + (int64_t)h * D + lane * V + i] = __float2bfloat16_rn(l > 0.0f || l != l ? o[i] / l : 0.0f);
 }
 
-}  // namespace
+// Groups of 8 rows that the largest sequence of this kernel may need.
+int row_groups(int64_t max_rows) { return max_rows <= 8 ? 1 : max_rows <= 16 ? 2 : 4; }
 
-size_t kv_attention_workspace(int, int, int, int, int64_t, int64_t, int64_t) { return 0; }
-
-cudaError_t kv_launch_attention(const kv_batch &b, int D, const kv_attention_call &c, int, cudaStream_t st, int64_t *launches)
+template <int D, int NT>
+cudaError_t launch_split(const split_params &p, int sm_count, cudaStream_t st, int64_t *launches)
 {
-    const int64_t blocks = (b.n_tokens * b.n_heads + 3) / 4;
-    if (blocks > INT32_MAX) return cudaErrorInvalidConfiguration;
-    auto go = [&](auto kern) { return tpq_launch_pdl(kern, dim3((unsigned)blocks), dim3(128), 0, st, b, c); };
-    const cudaError_t e = D == 128 ? go(attention_rows<128>) : go(attention_rows<64>);
+    constexpr size_t smem = sizeof(Shared<D, NT>);
+    static_assert(8 * NT * (D + 4) * 4 <= stages(D, NT) * chunk_bytes(D), "a warp's sums fit its ring");
+    cudaError_t e = cudaFuncSetAttribute(attention_split<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+    const int blocks = sm_count * blocks_per_sm(NT);
+    e = tpq_launch_pdl(attention_split<D, NT>, dim3(blocks), dim3(WARPS * 32), smem, st, p);
+    if (e != cudaSuccess) return e;
+    ++*launches;
+    e = tpq_launch_pdl(attention_join<D, NT>, dim3(blocks, 8 * NT), dim3(8 * D / 4), 0, st, p);
     if (e == cudaSuccess) ++*launches;
     return e;
+}
+
+}  // namespace
+
+size_t kv_attention_workspace(int D, int n_heads, int n_kv_heads, int sm_count, int64_t, int64_t max_new, int64_t)
+{
+    const int64_t group = n_heads / n_kv_heads;
+    const int nt = row_groups(max_new * group);
+    const size_t blocks = (size_t)sm_count * blocks_per_sm(nt);
+    return blocks * 16 + blocks * 2 * 8 * nt * part_row(D) * 4;
+}
+
+cudaError_t kv_launch_attention(const kv_batch &b, int D, const kv_attention_call &c, int sm_count, cudaStream_t st, int64_t *launches)
+{
+    const int group = b.n_heads / b.n_kv_heads;
+    const int64_t max_rows = (int64_t)b.max_new * group;
+    const int nt = row_groups(max_rows);
+    cudaError_t e = cudaSuccess;
+    if (max_rows > MAX_ROWS) {
+        const int64_t blocks = (b.n_tokens * b.n_heads + 3) / 4;
+        if (blocks > INT32_MAX) return cudaErrorInvalidConfiguration;
+        auto go = [&](auto kern) { return tpq_launch_pdl(kern, dim3((unsigned)blocks), dim3(128), 0, st, b, c); };
+        e = D == 128 ? go(attention_rows<128>) : go(attention_rows<64>);
+        if (e != cudaSuccess) return e;
+        ++*launches;
+    }
+    split_params p{b, c, nullptr, static_cast<int4 *>(c.workspace), c.scale * 1.4426950408889634f, group};
+    p.parts = reinterpret_cast<float *>(p.headers + (size_t)sm_count * blocks_per_sm(nt));
+    if (D == 128) return nt == 1 ? launch_split<128, 1>(p, sm_count, st, launches) : nt == 2 ? launch_split<128, 2>(p, sm_count, st, launches) : launch_split<128, 4>(p, sm_count, st, launches);
+    return nt == 1 ? launch_split<64, 1>(p, sm_count, st, launches) : nt == 2 ? launch_split<64, 2>(p, sm_count, st, launches) : launch_split<64, 4>(p, sm_count, st, launches);
 }
