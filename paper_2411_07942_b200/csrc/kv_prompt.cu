@@ -1,0 +1,899 @@
+// Attention over the 4-bit cache (tpq_kv_attention) for sequences that bring many rows: prompts and chunks of them.
+//
+// The mathematics is that of kv_attention.cu: codes are the operands, the values' steps go into the exponent.  Here the products
+// run on tcgen05: S = Q C^T of 128 rows x 128 positions with the keys' codes as BF16 128 + c, O += P E with P from tensor
+// memory and the values' codes as FP16 e - 8 (both exact).  A row (query head x new position) of S is one thread's, which
+// finds
+//   y_t = S_t (s_t scale log2 e) + (a_t - 128 s_t) scale log2(e) sum(q) + log2 r_t,   P_t = 2^(y_t - m + 7) in FP16,
+//   l = sum P_t / r_t,  w = sum P_t (b_t / r_t + 8),   out = (O + w) / l.
+// m moves only when a row's maximum has grown by more than 8 (P stays below 2^15): O is rescaled in tensor memory then, which
+// after a sequence's first tiles hardly happens.
+//
+// A block has 256 rows (two tiles of 128, A and B) of one key head and walks tiles of 128 positions.  Tensor memory holds S_A, S_B
+// (P in their place) and O_A, O_B, all of it.  While the exponentials of one row tile run, the tensor cores work for the other:
+//   ... P_A E(j), Q_A C(j+1), P_B E(j), Q_B C(j+1), P_A E(j+1), ...
+//   warp 0       copies: blocks of 16 positions as they lie in the pages, 64 positions a stage
+//   warp 1       tensor memory, MMA issue (one elected lane)
+//   warps 4-7    unpack: codes to the two operands' tiles (128-byte swizzle), words to the five terms of a position
+//   warps 8-15   softmax: a thread per row; the rows themselves into shared memory at the start, the output at the end
+// Unpacking a tile costs as much however many rows use it: 256 rows, which the query heads of a key head share.
+//
+// Work.  attention_plan lists the (sequence, 256 rows) pairs and adds up their tiles (causal, window); a run of tiles in that order
+// goes to each block, all of the same length.  A run that begins or ends inside a pair's key head leaves a partial result, at
+// most two a block, which attention_prompt_join puts together.
+// Every wait is bounded: on expiry the block records TPQ_ERR_TIMEOUT, frees its tensor memory and returns.
+#include "kv_internal.h"
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+namespace {
+
+constexpr int BM = 256, TILE = 128, HALF = 64;  // rows of a block, positions of a tile, of a copy stage
+constexpr int RAW = 3;                          // copy stages
+constexpr int THREADS = 512;
+constexpr int PLAN_THREADS = 1024;
+
+struct alignas(16) plan_item {
+    int seq, block, before, tiles;  // `block`: its rows start at BM * block; `before`: tiles x key heads of the items ahead
+};
+struct alignas(16) plan_head {
+    int items, total, pad[2];
+};
+struct prompt_params {
+    kv_batch b;
+    kv_attention_call c;
+    plan_head *head;
+    plan_item *items;
+    int *seq_items;  // [sequences] items ahead of a sequence's
+    int most_items;
+    int4 *headers;  // as in attention_split
+    float *parts;   // [blocks][2][BM][D + 4]
+    float scale2;
+    int group, few;  // sequences of up to `few` rows are attention_split's
+};
+
+// Rows of an item and the tiles they see: [0, first) and [from, end).
+struct item_tiles {
+    int rows, first, from, count;
+};
+__device__ __forceinline__ item_tiles tiles_of_rows(const kv_seq &s, const kv_attention_call &c, int group, int block)
+{
+    item_tiles t;
+    const int left = s.n * group - block * BM;  // (rows of a sequence fit 31 bits: checked by the host)
+    t.rows = left < BM ? left : BM;
+    const int p_lo = s.len - s.n + block * BM / group, p_hi = s.len - s.n + (block * BM + t.rows - 1) / group;
+    t.first = t.from = 0;
+    if (c.window) {
+        const int64_t from = (int64_t)p_lo - c.window + 1;
+        if (from > 0) {
+            t.from = (int)(from / TILE);
+            const int first = (int)(((c.n_first < from ? c.n_first : from) + TILE - 1) / TILE);
+            t.first = first < t.from ? first : t.from;
+        }
+    }
+    t.count = t.first + p_hi / TILE + 1 - t.from;
+    return t;
+}
+
+__device__ __forceinline__ int block_scan(int x, int *warps, int &total)  // inclusive; PLAN_THREADS threads
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+    for (int m = 1; m < 32; m <<= 1) {
+        const int o = __shfl_up_sync(0xffffffffu, x, m);
+        if (lane >= m) x += o;
+    }
+    __syncthreads();
+    if (lane == 31) warps[warp] = x;
+    __syncthreads();
+    if (warp == 0) {
+        int y = warps[lane];
+#pragma unroll
+        for (int m = 1; m < 32; m <<= 1) {
+            const int o = __shfl_up_sync(0xffffffffu, y, m);
+            if (lane >= m) y += o;
+        }
+        warps[lane] = y;
+    }
+    __syncthreads();
+    total = warps[31];
+    return x + (warp ? warps[warp - 1] : 0);
+}
+
+// One block: the list of items, and the tiles ahead of each.
+__global__ void __launch_bounds__(PLAN_THREADS) attention_plan(const prompt_params p)
+{
+    __shared__ int warps[32];
+    tpq_grid_dep_wait();
+    tpq_grid_dep_launch();
+    const kv_batch &b = p.b;
+    int items = 0;
+    for (int s0 = 0; s0 < b.n_seqs; s0 += PLAN_THREADS) {
+        const int s = s0 + threadIdx.x;
+        int n = 0;
+        if (s < b.n_seqs) {
+            const kv_seq q = kv_load_seq(b, s);
+            if (q.n * p.group > p.few) n = (q.n * p.group + BM - 1) / BM;
+        }
+        int total;
+        const int at = items + block_scan(n, warps, total) - n;
+        if (s < b.n_seqs) p.seq_items[s] = at;
+        items += total;
+        if (items > p.most_items) break;  // (uniform)
+    }
+    if (items > p.most_items) {  // starts that overlap: more rows than there are
+        if (threadIdx.x == 0) {
+            kv_report(b);
+            *p.head = plan_head{0, 0, {0, 0}};
+        }
+        return;
+    }
+    __syncthreads();
+    int64_t before = 0;
+    for (int i0 = 0; i0 < items; i0 += PLAN_THREADS) {
+        const int i = i0 + threadIdx.x;
+        int n = 0, s = 0, block = 0;
+        if (i < items) {
+            int lo = 0, hi = b.n_seqs;  // the last sequence whose items begin at or before i
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) / 2;
+                if (p.seq_items[mid] <= i) lo = mid;
+                else hi = mid;
+            }
+            s = lo;
+            block = i - p.seq_items[s];
+            n = tiles_of_rows(kv_load_seq(b, s), p.c, p.group, block).count;
+        }
+        int total;
+        const int64_t at = before + (int64_t)(block_scan(n, warps, total) - n) * b.n_kv_heads;
+        before += (int64_t)total * b.n_kv_heads;
+        if (i < items) p.items[i] = plan_item{s, block, (int)at, n};
+    }
+    if (threadIdx.x == 0) {
+        if (before > INT32_MAX - 1024) {
+            kv_report(b);
+            before = 0;
+        }
+        *p.head = plan_head{items, (int)before, {0, 0}};
+    }
+}
+
+// ---- waits, tensor memory, MMA
+
+constexpr int WAIT_LIMIT = 1 << 24;
+constexpr unsigned long long WAIT_NS = 1000000000ull;
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity)
+{
+    unsigned long long t0 = 0;
+    for (int i = 0; i < WAIT_LIMIT; ++i) {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok)
+            : "r"(bar), "r"(parity)
+            : "memory");
+        if (ok) return true;
+        if ((i & 63) == 63) {
+            unsigned long long t;
+            asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+            if (t0 == 0) t0 = t;
+            else if (t - t0 > WAIT_NS) return false;
+        }
+    }
+    return false;
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void commit(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool elect()
+{
+    uint32_t one;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "elect.sync _|p, 0xFFFFFFFF;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(one));
+    return one != 0;
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+#define R8(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]), "=r"(r[i + 4]), "=r"(r[i + 5]), "=r"(r[i + 6]), "=r"(r[i + 7])
+#define W8(r, i) "r"(r[i]), "r"(r[i + 1]), "r"(r[i + 2]), "r"(r[i + 3]), "r"(r[i + 4]), "r"(r[i + 5]), "r"(r[i + 6]), "r"(r[i + 7])
+// 32 columns of the thread's row (the values are there after ld_wait)
+__device__ __forceinline__ void ld32(uint32_t addr, uint32_t *r)
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : R8(r, 0), R8(r, 8), R8(r, 16), R8(r, 24)
+        : "r"(addr)
+        : "memory");
+}
+__device__ __forceinline__ void ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void st32(uint32_t addr, const uint32_t *r)
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+        ::W8(r, 0), W8(r, 8), W8(r, 16), W8(r, 24), "r"(addr)
+        : "memory");
+}
+__device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Operands of 128-byte rows with the 128-byte swizzle, 8-row groups of 1024 bytes.  Depth along the row (Q, keys): a step of 16 is 32
+// bytes of the row, 64-deep sub-tiles lie behind each other.  Depth along the rows (values: a row is a position, along it the head's
+// values): a step of 16 is 16 rows, the next 64 values are `lead` bytes on.
+__device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t lead)
+{
+    return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(lead >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+}
+// FP32 sums of 128 rows x n columns; `bf16`: both operands BF16 (else FP16); `rows_deep`: B's depth runs along its rows
+__host__ __device__ constexpr uint32_t instr(int n, bool bf16, bool rows_deep)
+{
+    return (1u << 4) | (bf16 ? (1u << 7) | (1u << 10) : 0u) | (rows_deep ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+}
+
+__device__ __forceinline__ float ex2(float x)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float lg2(float x)
+{
+    float r;
+    asm("lg2.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t mask, uint32_t bits)
+{
+    uint32_t r;
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(a), "r"(mask), "r"(bits));
+    return r;
+}
+// two binary32 operations an instruction
+typedef unsigned long long f2;
+__device__ __forceinline__ f2 pack2(float a, float b)
+{
+    f2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpack2(f2 v, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c)
+{
+    f2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ f2 add2(f2 a, f2 b)
+{
+    f2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+// terms of the positions of a tile, by array: score step, score offset, log2 of the value step, its reciprocal, (value low)/(value step) + 8
+enum { T_STEP, T_OFF, T_LOG, T_INV, T_LOW, TERMS };
+
+template <int D>
+struct Smem {
+    static constexpr uint32_t TILE_BYTES = TILE * D * 2;  // an operand tile
+    static constexpr uint32_t Q = 0, K = Q + 2 * TILE_BYTES, V = K + 2 * TILE_BYTES, RAWS = V + 2 * TILE_BYTES;
+    static constexpr uint32_t RAW_BYTES = HALF / KV_BLOCK * kv_block_bytes(D);
+    static constexpr uint32_t TERM = RAWS + RAW * RAW_BYTES, TERM_BYTES = TERMS * TILE * 4;
+    static constexpr uint32_t BARS = TERM + 3 * TERM_BYTES;
+    static constexpr uint32_t BYTES = BARS + 256 + 1024;  // (1024: slack for the alignment)
+};
+// barriers, 8 bytes each from BARS
+enum { B_RAW_FULL = 0, B_RAW_EMPTY = 3, B_KV_FULL = 6, B_K_EMPTY = 8, B_V_EMPTY = 10, B_Q_FULL = 12, B_S_FULL = 14, B_P_FULL = 16, B_O_FULL = 18, B_O_EMPTY = 20, B_COUNT = 22 };
+
+// A block's run of tiles, one (item, key head) after the other.
+struct run {
+    int unit, end, item;
+    __device__ bool more() const { return unit < end; }
+};
+struct segment {
+    kv_seq seq;
+    int s, kh, row0, t0, nt;  // rows row0 .. of the sequence; tiles t0 .. t0 + nt - 1 of the item's
+    item_tiles it;
+    __device__ __forceinline__ int base(int j) const  // first position of tile j of the segment
+    {
+        const int t = t0 + j;
+        return (t < it.first ? t : it.from + t - it.first) * TILE;
+    }
+};
+__device__ __forceinline__ segment next_segment(const prompt_params &p, run &r)
+{
+    segment g;
+    plan_item it = p.items[r.item];
+    while (r.unit >= it.before + it.tiles * p.b.n_kv_heads) it = p.items[++r.item];
+    g.s = it.seq;
+    g.seq = kv_load_seq(p.b, it.seq);
+    g.row0 = it.block * BM;
+    g.it = tiles_of_rows(g.seq, p.c, p.group, it.block);
+    const int off = r.unit - it.before;
+    g.kh = off / it.tiles;
+    g.t0 = off - g.kh * it.tiles;
+    g.nt = it.tiles - g.t0 < r.end - r.unit ? it.tiles - g.t0 : r.end - r.unit;
+    r.unit += g.nt;
+    return g;
+}
+// Whether row tile t (0: A, 1: B) sees any position of a tile that starts at `base`; whether all of its rows see all of it.
+struct reach {
+    int lo, hi;  // positions of the row tile's first and last row (hi < lo: it has no rows)
+};
+__device__ __forceinline__ reach reach_of(const prompt_params &p, const segment &g, int t)
+{
+    const int p0 = g.seq.len - g.seq.n, r0 = g.row0 + t * 128, rows = g.it.rows - t * 128;
+    reach r;
+    r.lo = p0 + r0 / p.group;
+    r.hi = rows > 0 ? p0 + (r0 + (rows < 128 ? rows : 128) - 1) / p.group : r.lo - 1;
+    return r;
+}
+__device__ __forceinline__ bool sees(const prompt_params &p, const reach &r, int base)
+{
+    return r.hi >= r.lo && base <= r.hi && (p.c.window == 0 || (int64_t)base + TILE - 1 > (int64_t)r.lo - p.c.window || base < p.c.n_first);
+}
+__device__ __forceinline__ bool sees_all(const prompt_params &p, const reach &r, int base)
+{
+    return base + TILE - 1 <= r.lo && (p.c.window == 0 || base > (int64_t)r.hi - p.c.window || base + TILE <= p.c.n_first);
+}
+
+template <int D>
+__global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_params p)
+{
+    using L = Smem<D>;
+    extern __shared__ uint8_t raw_smem[];
+    const uint32_t smem = (smem_u32(raw_smem) + 1023u) & ~1023u;
+    uint8_t *const gen = raw_smem + (smem - smem_u32(raw_smem));
+    const uint32_t bars = smem + L::BARS;
+    auto bar = [&](int i) { return bars + 8u * i; };
+    uint32_t *const there = reinterpret_cast<uint32_t *>(gen + L::BARS + 8 * B_COUNT);  // [RAW]: blocks of a copy stage that were copied
+    uint32_t *const tmem_slot = there + RAW;
+    const kv_batch &b = p.b;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+    if (tid == 0) {
+        for (int i = 0; i < RAW; ++i) {
+            mbar_init(bar(B_RAW_FULL + i), 1);
+            mbar_init(bar(B_RAW_EMPTY + i), 4);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar(B_KV_FULL + i), 4);
+            mbar_init(bar(B_K_EMPTY + i), 1);
+            mbar_init(bar(B_V_EMPTY + i), 1);
+            mbar_init(bar(B_Q_FULL + i), 4);
+            mbar_init(bar(B_S_FULL + i), 1);
+            mbar_init(bar(B_P_FULL + i), 4);
+            mbar_init(bar(B_O_FULL + i), 1);
+            mbar_init(bar(B_O_EMPTY + i), 4);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    fence_before();
+    tpq_grid_dep_wait();
+    __syncthreads();
+    tpq_grid_dep_launch();
+    fence_after();
+    const uint32_t tmem = *tmem_slot;
+    bool ok = true;
+
+    // ---- this block's run
+    run r0;
+    {
+        const plan_head h = *p.head;
+        const int share = (int)(((int64_t)h.total + gridDim.x - 1) / gridDim.x);
+        r0.unit = (int)min((int64_t)blockIdx.x * share, (int64_t)h.total);
+        r0.end = min(r0.unit + share, h.total);
+        int lo = 0, n = h.items;  // the last item that begins at or before the unit (every warp for itself): as in kv_find_seq
+        while (n > 0) {
+            const int step = (n + 31) / 32, at = (lane + 1) * step - 1 < n ? (lane + 1) * step - 1 : n - 1;
+            const int c = __popc(__ballot_sync(0xffffffffu, p.items[lo + at].before <= r0.unit));
+            const int skip = c * step < n ? c * step : n;
+            lo += skip;
+            n = c == 32 ? 0 : (n - skip < step - 1 ? n - skip : step - 1);
+        }
+        r0.item = lo > 0 ? lo - 1 : 0;
+    }
+    run r = r0;
+
+    // Registers: 128 a thread at launch; 64 + 80 + 2 x 184 are the four warpgroups' 512.
+    if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    if (warp == 0) {
+        // ---------------- copies
+        int stage = 0;  // copy stages so far
+        while (r.more() && ok) {
+            const segment g = next_segment(p, r);
+            auto page_of = [&](int h) {  // page of this lane's block (of four) of copy stage h of the segment, -1: not copied
+                if (h >= 2 * g.nt || lane >= HALF / KV_BLOCK) return -1;
+                const int pos = g.base(h >> 1) + (h & 1) * HALF + lane * KV_BLOCK;
+                if (pos >= g.seq.len) return -1;
+                const int64_t from = (int64_t)(g.seq.len - g.seq.n + g.row0 / p.group) - p.c.window + 1;
+                if (p.c.window && pos >= p.c.n_first && (int64_t)pos + KV_BLOCK <= from) return -1;  // no row sees it
+                const int hi = g.seq.len - g.seq.n + (g.row0 + g.it.rows - 1) / p.group;
+                if (pos > hi) return -1;
+                const int page = b.table[g.s * b.table_stride + (pos >> b.page_shift)];
+                if (page >= 0 && page < b.n_pages) return page;
+                kv_report(b);
+                return -1;
+            };
+            int page = page_of(0);
+            for (int h = 0; h < 2 * g.nt; ++h, ++stage) {
+                const int st = stage % RAW;
+                const int next = page_of(h + 1);
+                if (stage >= RAW) ok = __all_sync(0xffffffffu, wait(bar(B_RAW_EMPTY + st), (stage / RAW - 1) & 1));
+                if (!ok) break;
+                const uint32_t have = __ballot_sync(0xffffffffu, page >= 0);
+                if (lane == 0) {
+                    there[st] = have;
+                    mbar_expect_tx(bar(B_RAW_FULL + st), __popc(have) * kv_block_bytes(D));
+                }
+                __syncwarp();
+                if (page >= 0) {
+                    const int pos = g.base(h >> 1) + (h & 1) * HALF + lane * KV_BLOCK, blocks = b.page_size / KV_BLOCK;
+                    const uint8_t *src = b.cache + (((int64_t)page * b.n_kv_heads + g.kh) * blocks + (pos & (b.page_size - 1)) / KV_BLOCK) * kv_block_bytes(D);
+                    bulk_g2s(smem + L::RAWS + st * L::RAW_BYTES + lane * kv_block_bytes(D), src, kv_block_bytes(D), bar(B_RAW_FULL + st));
+                }
+                page = next;
+            }
+        }
+        if (!ok)  // let the copies in flight land before the shared memory is released
+            for (int k = stage > RAW ? stage - RAW : 0; k < stage; ++k) (void)wait(bar(B_RAW_FULL + k % RAW), (k / RAW) & 1);
+    } else if (warp == 1) {
+        // ---------------- MMA
+        constexpr uint32_t qk_instr = instr(TILE, true, false), pv_instr = instr(D, false, true);
+        int it = 0;                             // tiles so far: operand buffer it % 2
+        int s_count[2] = {0, 0}, segs[2] = {0, 0};  // scores computed, segments begun, of each row tile
+        while (r.more() && ok) {
+            const segment g = next_segment(p, r);
+            const reach re[2] = {reach_of(p, g, 0), reach_of(p, g, 1)};
+            int last[2] = {-1, -1};
+            bool any[2] = {false, false};
+            for (int t = 0; t < 2; ++t)
+                for (int j = g.nt - 1; j >= 0 && last[t] < 0; --j)
+                    if (sees(p, re[t], g.base(j))) last[t] = j;
+            auto scores = [&](int t, int j) {  // Q_t C(j)
+                if (!ok || !sees(p, re[t], g.base(j))) return;
+                if (elect()) {
+                    const uint64_t a = operand(smem + L::Q + t * L::TILE_BYTES, 16), k = operand(smem + L::K + ((it + j) & 1) * L::TILE_BYTES, 16);
+#pragma unroll
+                    for (int x = 0; x < D / 16; ++x) {
+                        const uint64_t at = (uint64_t)((x / 4) * (128 * 128 >> 4) + 2 * (x % 4));
+                        mma_ss(tmem + t * TILE, a + at, k + at, qk_instr, x != 0);
+                    }
+                    commit(bar(B_S_FULL + t));
+                }
+                __syncwarp();
+            };
+            for (int t = 0; t < 2 && ok; ++t)
+                if (last[t] >= 0) ok = __all_sync(0xffffffffu, wait(bar(B_Q_FULL + t), segs[t] & 1));
+            if (ok) ok = __all_sync(0xffffffffu, wait(bar(B_KV_FULL + (it & 1)), (it >> 1) & 1));
+            if (!ok) break;
+            fence_after();
+            scores(0, 0);
+            scores(1, 0);
+            if (elect()) commit(bar(B_K_EMPTY + (it & 1)));
+            __syncwarp();
+            for (int j = 0; j < g.nt && ok; ++j) {
+                const int i = it + j;
+                for (int t = 0; t < 2 && ok; ++t) {
+                    if (sees(p, re[t], g.base(j))) {
+                        if (!any[t] && segs[t] > 0) ok = __all_sync(0xffffffffu, wait(bar(B_O_EMPTY + t), (segs[t] - 1) & 1));
+                        if (ok) ok = __all_sync(0xffffffffu, wait(bar(B_P_FULL + t), s_count[t] & 1));
+                        if (!ok) break;
+                        fence_after();
+                        if (elect()) {
+                            const uint64_t v = operand(smem + L::V + (i & 1) * L::TILE_BYTES, TILE * 128);
+#pragma unroll
+                            for (int x = 0; x < TILE / 16; ++x)
+                                mma_ts(tmem + 256 + t * 128, tmem + t * TILE + 8 * x, v + (uint64_t)(x * (2048 >> 4)), pv_instr, any[t] || x != 0);
+                            if (j == last[t]) commit(bar(B_O_FULL + t));
+                        }
+                        __syncwarp();
+                        any[t] = true;
+                        ++s_count[t];
+                    }
+                    if (j + 1 < g.nt) {
+                        if (t == 0) {
+                            ok = __all_sync(0xffffffffu, wait(bar(B_KV_FULL + ((i + 1) & 1)), ((i + 1) >> 1) & 1));
+                            fence_after();
+                        }
+                        scores(t, j + 1);
+                    }
+                }
+                if (!ok) break;
+                if (elect()) {
+                    commit(bar(B_V_EMPTY + (i & 1)));
+                    if (j + 1 < g.nt) commit(bar(B_K_EMPTY + ((i + 1) & 1)));
+                }
+                __syncwarp();
+            }
+            it += g.nt;
+            for (int t = 0; t < 2; ++t)
+                if (last[t] >= 0) ++segs[t];
+        }
+    }
+    } else if (warp < 8) {
+        // ---------------- unpack: warp w - 4 takes one block of 16 positions of each copy stage
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+        const int w4 = warp - 4;
+        int stage = 0, it = 0;
+        while (r.more() && ok) {
+            const segment g = next_segment(p, r);
+            for (int j = 0; j < g.nt && ok; ++j, ++it) {
+                if (it >= 2) {
+                    ok = __all_sync(0xffffffffu, wait(bar(B_K_EMPTY + (it & 1)), ((it >> 1) - 1) & 1)) &&
+                         __all_sync(0xffffffffu, wait(bar(B_V_EMPTY + (it & 1)), ((it >> 1) - 1) & 1));
+                    if (!ok) break;
+                }
+                float *const term = reinterpret_cast<float *>(gen + L::TERM + (it % 3) * L::TERM_BYTES);
+                for (int half = 0; half < 2; ++half, ++stage) {
+                    const int st = stage % RAW;
+                    ok = __all_sync(0xffffffffu, wait(bar(B_RAW_FULL + st), (stage / RAW) & 1));
+                    if (!ok) break;
+                    const uint8_t *const blk = gen + L::RAWS + st * L::RAW_BYTES + w4 * kv_block_bytes(D);
+                    const int row0 = half * HALF + w4 * KV_BLOCK;  // of the tile
+                    if (lane < KV_BLOCK) {
+                        const uint32_t kw = reinterpret_cast<const uint32_t *>(blk + kv_k_words(D))[lane], vw = reinterpret_cast<const uint32_t *>(blk + kv_v_words(D))[lane];
+                        const float ks = __uint_as_float(kw << 16), kl = __uint_as_float(kw & 0xffff0000u);
+                        const float vs = __uint_as_float(vw << 16), vl = __uint_as_float(vw & 0xffff0000u), inv = __frcp_rn(vs);
+                        const bool on = g.base(j) + row0 + lane < g.seq.len && ((there[st] >> w4) & 1u);
+                        float *t = term + row0 + lane;
+                        t[T_STEP * TILE] = on ? ks * p.scale2 : 0.0f;
+                        t[T_OFF * TILE] = on ? fmaf(-128.0f, ks, kl) * p.scale2 : 0.0f;
+                        t[T_LOG * TILE] = on ? lg2(vs) : -INFINITY;
+                        t[T_INV * TILE] = on ? inv : 0.0f;
+                        t[T_LOW * TILE] = on ? fmaf(vl, inv, 8.0f) : 0.0f;
+                    }
+#pragma unroll
+                    for (int k = 0; k < D / 64; ++k) {
+                        // 16 bytes (32 codes) of position `row`; eight lanes read and write 128 different bytes of banks
+                        const int row = D == 128 ? (lane & 7) + 8 * k : lane & 15, q = D == 128 ? ((lane >> 3) + (row >> 1)) & 3 : lane >> 4;
+                        const uint4 ck = *reinterpret_cast<const uint4 *>(blk + row * (D / 2) + 16 * q);
+                        const uint4 cv = *reinterpret_cast<const uint4 *>(blk + kv_v_codes(D) + row * (D / 2) + 16 * q);
+                        const uint32_t kk[4] = {ck.x, ck.y, ck.z, ck.w}, vv[4] = {cv.x, cv.y, cv.z, cv.w};
+                        const uint32_t line = (uint32_t)((q >> 1) * (TILE * 128) + (row0 + row) * 128);
+                        uint8_t *const kd = gen + L::K + (it & 1) * L::TILE_BYTES + line, *const vd = gen + L::V + (it & 1) * L::TILE_BYTES + line;
+                        const __half2 sixteenth = __float2half2_rn(0.0625f), off = __float2half2_rn(-72.0f), off0 = __float2half2_rn(-1032.0f);
+#pragma unroll
+                        for (int jw = 0; jw < 4; ++jw) {
+                            const uint32_t at = (uint32_t)((((q & 1) * 4 + jw) ^ (row & 7)) * 16);
+                            const uint32_t u = kk[jw], v = vv[jw];
+                            *reinterpret_cast<uint4 *>(kd + at) =
+                                make_uint4(and_or(u, 0x000f000fu, 0x43004300u), and_or(u >> 4, 0x000f000fu, 0x43004300u),
+                                           and_or(u >> 8, 0x000f000fu, 0x43004300u), and_or(u >> 12, 0x000f000fu, 0x43004300u));
+                            uint32_t e[4] = {and_or(v, 0x000f000fu, 0x64006400u), and_or(v, 0x00f000f0u, 0x64006400u),
+                                             and_or(v >> 8, 0x000f000fu, 0x64006400u), and_or(v >> 8, 0x00f000f0u, 0x64006400u)};
+#pragma unroll
+                            for (int z = 0; z < 4; ++z) {
+                                const __half2 h = *reinterpret_cast<const __half2 *>(&e[z]);
+                                const __half2 y = z & 1 ? __hfma2(h, sixteenth, off) : __hadd2(h, off0);
+                                e[z] = *reinterpret_cast<const uint32_t *>(&y);
+                            }
+                            *reinterpret_cast<uint4 *>(vd + at) = make_uint4(e[0], e[1], e[2], e[3]);
+                        }
+                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(B_RAW_EMPTY + st));
+                }
+                if (!ok) break;
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(B_KV_FULL + (it & 1)));
+            }
+        }
+    } else {
+        // ---------------- softmax: thread <-> row `row` of row tile t
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+        const int t = (warp - 8) >> 2, row = tid & 127;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t s_addr = tmem + t * TILE + lanes, o_addr = tmem + 256 + t * 128 + lanes;
+        int it = 0, s_count = 0, segs = 0;
+        int4 header = make_int4(0, 0, 0, 0);
+        const plan_head ph = *p.head;
+        const int share = (int)(((int64_t)ph.total + gridDim.x - 1) / gridDim.x);
+        while (r.more() && ok) {
+            const segment g = next_segment(p, r);
+            const reach re = reach_of(p, g, t);
+            bool works = false;
+            for (int j = 0; j < g.nt && !works; ++j) works = sees(p, re, g.base(j));
+            const int rr = g.row0 + t * 128 + row, tok = rr / p.group, h = g.kh * p.group + (rr - tok * p.group);  // row of the sequence
+            const bool mine = t * 128 + row < g.it.rows;
+            const int pos = mine ? g.seq.len - g.seq.n + tok : -1;
+            float m = -INFINITY, qsum = 0.0f;
+            f2 l2 = 0, w2 = 0;
+            bool any = false;
+            if (works) {
+                // the row as an operand, 8 values of a chunk in the codes' order 0 4 1 5 2 6 3 7
+                const uint4 *src = reinterpret_cast<const uint4 *>(p.c.q.p + (int64_t)(g.seq.start + tok) * p.c.q.stride + (int64_t)h * D);
+                uint8_t *const dst = gen + L::Q + t * L::TILE_BYTES + row * 128;
+#pragma unroll
+                for (int k = 0; k < D / 8; ++k) {
+                    const uint4 x = mine ? src[k] : make_uint4(0, 0, 0, 0);
+                    const uint32_t u[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) qsum += __uint_as_float(u[z] << 16) + __uint_as_float(u[z] & 0xffff0000u);
+                    *reinterpret_cast<uint4 *>(dst + (k / 8) * (128 * 128) + (((k & 7) ^ (row & 7)) * 16)) =
+                        make_uint4(__byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632), __byte_perm(x.y, x.w, 0x5410), __byte_perm(x.y, x.w, 0x7632));
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(B_Q_FULL + t));
+            }
+            const f2 qsum2 = pack2(qsum, qsum);
+            for (int j = 0; j < g.nt; ++j) {
+                const int base = g.base(j), i = it + j;
+                if (!sees(p, re, base)) continue;
+                // (the terms: written ahead of this barrier's arrivals; the scores)
+                ok = __all_sync(0xffffffffu, wait(bar(B_KV_FULL + (i & 1)), (i >> 1) & 1)) && __all_sync(0xffffffffu, wait(bar(B_S_FULL + t), s_count & 1));
+                if (!ok) break;
+                ++s_count;
+                fence_after();
+                const float *term = reinterpret_cast<const float *>(gen + L::TERM + (i % 3) * L::TERM_BYTES);
+                uint32_t x[TILE];
+#pragma unroll
+                for (int k = 0; k < TILE; k += 32) ld32(s_addr + k, x + k);
+                ld_wait();
+                float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                const bool all = sees_all(p, re, base);
+                // visible of this row, of the tile's positions: below `end`, and from `begin` on or below `head`
+                const int end = pos - base + 1;
+                const int64_t begin64 = p.c.window ? (int64_t)pos - p.c.window + 1 - base : -1, head64 = p.c.n_first - base;
+                const int begin = begin64 > TILE ? TILE : begin64 < 0 ? 0 : (int)begin64, head = head64 > TILE ? TILE : head64 < 0 ? 0 : (int)head64;
+#pragma unroll
+                for (int k = 0; k < TILE; k += 4) {
+                    const ulonglong2 st = *reinterpret_cast<const ulonglong2 *>(term + T_STEP * TILE + k);
+                    const ulonglong2 of = *reinterpret_cast<const ulonglong2 *>(term + T_OFF * TILE + k);
+                    const ulonglong2 lg = *reinterpret_cast<const ulonglong2 *>(term + T_LOG * TILE + k);
+                    const f2 y0 = fma2(pack2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), st.x, fma2(of.x, qsum2, lg.x));
+                    const f2 y1 = fma2(pack2(__uint_as_float(x[k + 2]), __uint_as_float(x[k + 3])), st.y, fma2(of.y, qsum2, lg.y));
+                    float y[4];
+                    unpack2(y0, y[0], y[1]);
+                    unpack2(y1, y[2], y[3]);
+                    if (!all) {
+#pragma unroll
+                        for (int z = 0; z < 4; ++z)
+                            if (k + z >= end || (k + z < begin && k + z >= head)) y[z] = -INFINITY;
+                    }
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) {
+                        x[k + z] = __float_as_uint(y[z]);
+                        top[z] = fmaxf(top[z], y[z]);
+                    }
+                }
+                const float tile_top = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+                if (!any) {
+                    m = tile_top;
+                } else if (__any_sync(0xffffffffu, tile_top > m + 8.0f)) {
+                    const float m2 = fmaxf(m, tile_top), a = ex2(m - (m2 == -INFINITY ? 0.0f : m2));
+                    m = m2;
+                    const f2 a2 = pack2(a, a);
+                    l2 = fma2(l2, a2, 0);
+                    w2 = fma2(w2, a2, 0);
+                    // (the scores of this tile were computed behind the products that O holds)
+#pragma unroll
+                    for (int k = 0; k < D; k += 32) {
+                        uint32_t o[32];
+                        ld32(o_addr + k, o);
+                        ld_wait();
+#pragma unroll
+                        for (int z = 0; z < 32; ++z) o[z] = __float_as_uint(__uint_as_float(o[z]) * a);
+                        st32(o_addr + k, o);
+                    }
+                    st_wait();
+                }
+                any = true;
+                const float from = (m == -INFINITY ? 0.0f : m) - 7.0f;
+                const f2 minus = pack2(-from, -from);
+#pragma unroll
+                for (int k = 0; k < TILE; k += 4) {
+                    const ulonglong2 iv = *reinterpret_cast<const ulonglong2 *>(term + T_INV * TILE + k);
+                    const ulonglong2 lw = *reinterpret_cast<const ulonglong2 *>(term + T_LOW * TILE + k);
+                    float y[4];
+                    unpack2(add2(pack2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), minus), y[0], y[1]);
+                    unpack2(add2(pack2(__uint_as_float(x[k + 2]), __uint_as_float(x[k + 3])), minus), y[2], y[3]);
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) y[z] = ex2(y[z]);
+                    const f2 e0 = pack2(y[0], y[1]), e1 = pack2(y[2], y[3]);
+                    l2 = fma2(e0, iv.x, l2);
+                    w2 = fma2(e0, lw.x, w2);
+                    l2 = fma2(e1, iv.y, l2);
+                    w2 = fma2(e1, lw.y, w2);
+                    const __half2 h0 = __floats2half2_rn(y[0], y[1]), h1 = __floats2half2_rn(y[2], y[3]);
+                    x[k / 2] = *reinterpret_cast<const uint32_t *>(&h0);
+                    x[k / 2 + 1] = *reinterpret_cast<const uint32_t *>(&h1);
+                }
+                st32(s_addr, x);
+                st32(s_addr + 32, x + 32);
+                st_wait();
+                fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(B_P_FULL + t));
+            }
+            it += g.nt;
+            if (!ok) break;
+            float l_a, l_b, w_a, w_b;
+            unpack2(l2, l_a, l_b);
+            unpack2(w2, w_a, w_b);
+            const float l = l_a + l_b, w = w_a + w_b;
+            if (works) {
+                ok = __all_sync(0xffffffffu, wait(bar(B_O_FULL + t), segs & 1));
+                if (!ok) break;
+                ++segs;
+                fence_after();
+            }
+            const bool whole = g.t0 == 0 && g.nt == g.it.count;
+            float *part = p.parts + (((int64_t)blockIdx.x * 2 + (g.t0 == 0 ? 1 : 0)) * BM + t * 128 + row) * (D + 4);
+            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+            for (int k = 0; k < D; k += 32) {
+                uint32_t o[32];
+                if (works) {
+                    ld32(o_addr + k, o);
+                    ld_wait();
+                } else {
+#pragma unroll
+                    for (int z = 0; z < 32; ++z) o[z] = 0;
+                }
+                if (mine)
+#pragma unroll
+                for (int c = 0; c < 32; c += 8) {
+                    const int from[8] = {0, 2, 4, 6, 1, 3, 5, 7};  // value d of a chunk is column from[d]
+                    float y[8];
+#pragma unroll
+                    for (int z = 0; z < 8; ++z) y[z] = __uint_as_float(o[c + from[z]]) + w;
+                    if (whole) {
+                        uint32_t u[4];
+#pragma unroll
+                        for (int z = 0; z < 4; ++z) {
+                            const __nv_bfloat162 v = __floats2bfloat162_rn(y[2 * z] * inv, y[2 * z + 1] * inv);
+                            u[z] = *reinterpret_cast<const uint32_t *>(&v);
+                        }
+                        *reinterpret_cast<uint4 *>(p.c.out + (int64_t)(g.seq.start + tok) * p.c.out_stride + (int64_t)h * D + k + c) = make_uint4(u[0], u[1], u[2], u[3]);
+                    } else {
+                        reinterpret_cast<float4 *>(part + k + c)[0] = make_float4(y[0], y[1], y[2], y[3]);
+                        reinterpret_cast<float4 *>(part + k + c)[1] = make_float4(y[4], y[5], y[6], y[7]);
+                    }
+                }
+                __syncwarp();
+            }
+            if (mine && !whole) *reinterpret_cast<float2 *>(part + D) = make_float2(m, l);
+            if (works) {
+                fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(B_O_EMPTY + t));
+            }
+            if (g.t0 == 0 && !whole)
+                header = make_int4(1 + (g.it.count - g.nt + share - 1) / share, g.seq.start, g.row0, (g.it.rows << 16) | g.kh);
+        }
+        if (tid == 256) p.headers[blockIdx.x] = header;
+    }
+    if (!ok && lane == 0) atomicExch(b.status, (int)TPQ_ERR_TIMEOUT);
+    fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        __syncwarp();
+        fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+    }
+}
+
+// Puts the partial results together that run blockIdx.x ends with the first part of: a warp per row.
+template <int D>
+__global__ void __launch_bounds__(256) attention_prompt_join(const prompt_params p)
+{
+    constexpr int V = D / 32;  // values of a lane
+    tpq_grid_dep_wait();
+    const int4 head = p.headers[blockIdx.x];  // parts, first row of the sequence, first row of the item in it, rows and key head
+    const int lane = threadIdx.x & 31, r = blockIdx.y * 8 + (threadIdx.x >> 5), rows = head.w >> 16, kh = head.w & 0xffff;
+    if (head.x == 0 || r >= rows) return;
+    float m = -INFINITY, l = 0.0f, o[V] = {};
+    for (int i = 0; i < head.x; ++i) {
+        const float *part = p.parts + ((((int64_t)blockIdx.x + i) * 2 + (i == 0 ? 1 : 0)) * BM + r) * (D + 4);
+        const float2 v = __ldcg(reinterpret_cast<const float2 *>(part + D));
+        float z[V];
+        if (V == 4) {
+            const float4 q = __ldcg(reinterpret_cast<const float4 *>(part) + lane);
+            z[0] = q.x, z[1] = q.y, z[V - 2] = q.z, z[V - 1] = q.w;
+        } else {
+            const float2 q = __ldcg(reinterpret_cast<const float2 *>(part) + lane);
+            z[0] = q.x, z[1] = q.y;
+        }
+        const float top = fmaxf(m, v.x), from = top == -INFINITY ? 0.0f : top, a = ex2(m - from), f = ex2(v.x - from);
+        m = top;
+        l = fmaf(v.y, f, l * a);
+#pragma unroll
+        for (int k = 0; k < V; ++k) o[k] = fmaf(z[k], f, o[k] * a);
+    }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    const int rr = head.z + r, tok = rr / p.group, h = kh * p.group + (rr - tok * p.group);
+    uint32_t *dst = reinterpret_cast<uint32_t *>(p.c.out + (int64_t)(head.y + tok) * p.c.out_stride + (int64_t)h * D + V * lane);
+#pragma unroll
+    for (int k = 0; k < V / 2; ++k) {
+        const __nv_bfloat162 v = __floats2bfloat162_rn(o[2 * k] * inv, o[2 * k + 1] * inv);
+        dst[k] = *reinterpret_cast<const uint32_t *>(&v);
+    }
+}
+
+int64_t most_items(int64_t n_seqs, int64_t n_tokens, int64_t group, int few)
+{
+    const int64_t rows = n_tokens * group, seqs = rows / (few + 1);  // sequences with more than `few` rows, full items
+    return rows / BM + (seqs < n_seqs ? seqs : n_seqs) + 1;
+}
+
+size_t up16(size_t n) { return (n + 15) / 16 * 16; }
+
+}  // namespace
+
+size_t kv_prompt_workspace(int D, int group, int sm_count, int64_t n_seqs, int64_t n_tokens, int few)
+{
+    return up16(sizeof(plan_head)) + up16(sizeof(plan_item) * most_items(n_seqs, n_tokens, group, few)) + up16(4 * (size_t)n_seqs) + 16 * (size_t)sm_count +
+           (size_t)sm_count * 2 * BM * (D + 4) * 4;
+}
+
+cudaError_t kv_launch_prompt(const kv_batch &b, int D, const kv_attention_call &c, int few, void *workspace, int sm_count, cudaStream_t st, int64_t *launches)
+{
+    const int group = b.n_heads / b.n_kv_heads;
+    const int64_t items = most_items(b.n_seqs, b.n_tokens, group, few);
+    if (b.n_tokens * group > INT32_MAX / 2 || items > INT32_MAX / 2) return cudaErrorInvalidConfiguration;
+    uint8_t *w = static_cast<uint8_t *>(workspace);
+    prompt_params p{b, c};
+    p.head = reinterpret_cast<plan_head *>(w);
+    w += up16(sizeof(plan_head));
+    p.items = reinterpret_cast<plan_item *>(w);
+    w += up16(sizeof(plan_item) * items);
+    p.seq_items = reinterpret_cast<int *>(w);
+    w += up16(4 * (size_t)b.n_seqs);
+    p.headers = reinterpret_cast<int4 *>(w);
+    w += 16 * (size_t)sm_count;
+    p.parts = reinterpret_cast<float *>(w);
+    p.most_items = (int)items;
+    p.scale2 = c.scale * 1.4426950408889634f;
+    p.group = group;
+    p.few = few;
+    cudaError_t e = tpq_launch_pdl(attention_plan, dim3(1), dim3(PLAN_THREADS), 0, st, p);
+    if (e != cudaSuccess) return e;
+    ++*launches;
+    auto main = [&](auto kern, size_t smem) {
+        cudaError_t f = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        return f != cudaSuccess ? f : tpq_launch_pdl(kern, dim3(sm_count), dim3(THREADS), smem, st, p);
+    };
+    e = D == 128 ? main(attention_prompt<128>, Smem<128>::BYTES) : main(attention_prompt<64>, Smem<64>::BYTES);
+    if (e != cudaSuccess) return e;
+    ++*launches;
+    e = D == 128 ? tpq_launch_pdl(attention_prompt_join<128>, dim3(sm_count, BM / 8), dim3(256), 0, st, p)
+                 : tpq_launch_pdl(attention_prompt_join<64>, dim3(sm_count, BM / 8), dim3(256), 0, st, p);
+    if (e == cudaSuccess) ++*launches;
+    return e;
+}
