@@ -377,7 +377,7 @@ typedef struct tpq_kv_batch {
     const int32_t *page_table_dev; /* [n_seqs][page_table_stride], 4-byte aligned, as the next two */
     int64_t page_table_stride;     /* = most pages of a sequence */
     const int32_t *token_start_dev; /* [n_seqs + 1], ascending from 0 */
-    const int32_t *lengths_dev;    /* [n_seqs] positions of a sequence, the new ones included */
+    const int32_t *lengths_dev;    /* [n_seqs] positions of a sequence, the new ones included; at most 2^30 */
     int32_t n_seqs;
     int32_t max_new;               /* no sequence brings more rows than this (it chooses kernels) */
     int64_t n_tokens;              /* rows of the step's tensors, >= token_start[n_seqs] */

@@ -190,10 +190,9 @@ tpq_status tpq_kv_attention(tpq_kv *kv, const tpq_kv_batch *batch, const void *q
     if (need && !workspace) return fail(kv, TPQ_ERR_INVALID_ARG, "workspace is NULL");
     if (!aligned(workspace, 16)) return fail(kv, TPQ_ERR_ALIGN, "the workspace must be 16-byte aligned");
     if (workspace_bytes < need) return fail(kv, TPQ_ERR_SIZE, "workspace of %zu bytes < %zu", workspace_bytes, need);
-    // (positions are 32-bit numbers: a larger window or prefix than any length is as good as this one)
-    const int64_t most = INT32_MAX;
+    const int64_t most = KV_MOST;  // (a window or prefix beyond any length is as good as this one)
     kv_attention_call c{kv_rows{static_cast<const uint16_t *>(q), q_stride}, static_cast<uint16_t *>(out), out_stride, scale,
-                        window < most ? window : most, n_first < most ? n_first : most, workspace};
+                        (int)(window < most ? window : most), (int)(n_first < most ? n_first : most), workspace};
     cudaError_t e = kv_launch_attention(b, kv->head_dim, c, kv->sm_count, static_cast<cudaStream_t>(stream), &kv->launches);
     if (e != cudaSuccess) return cuda_fail(kv, e, "kv_attention kernel");
     return TPQ_OK;

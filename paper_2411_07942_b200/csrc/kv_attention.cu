@@ -113,10 +113,10 @@ __device__ __forceinline__ tiles_of visible_tiles(const kv_seq &s, const kv_atte
     tiles_of t{0, 0, 0};
     if (s.n <= 0 || s.n * group > MAX_ROWS) return t;
     if (c.window) {
-        const int64_t from = (int64_t)(s.len - s.n) - c.window + 1;  // of the first row
+        const int from = s.len - s.n - c.window + 1;  // of the first row
         if (from > 0) {
-            t.from = (int)(from / TILE);
-            const int first = (int)(((c.n_first < from ? c.n_first : from) + TILE - 1) / TILE);
+            t.from = from / TILE;
+            const int first = ((c.n_first < from ? c.n_first : from) + TILE - 1) / TILE;
             t.first = first < t.from ? first : t.from;
         }
     }
@@ -246,7 +246,7 @@ attention_split(const split_params p)
             if (j >= nt || lane > 1) return -1;
             const int pos = base_of(j) + lane * KV_BLOCK;
             if (pos >= seq.len) return -1;
-            if (p.c.window && pos >= p.c.n_first && (int64_t)pos + KV_BLOCK <= (int64_t)p0 - p.c.window + 1) return -1;  // no row sees it
+            if (p.c.window && pos >= p.c.n_first && pos + KV_BLOCK <= p0 - p.c.window + 1) return -1;  // no row sees it
             const int page = b.table[s * b.table_stride + (pos >> b.page_shift)];
             if (page >= 0 && page < b.n_pages) return page;
             kv_report(b);
@@ -339,7 +339,7 @@ attention_split(const split_params p)
                     lw[k][e] = sh.lows[warp][at];
                 }
             // every row sees every position of the chunk (that there is)?
-            const bool all = base + CHUNK - 1 <= p0 && (p.c.window == 0 || base > (int64_t)seq.len - 1 - p.c.window || base + CHUNK <= p.c.n_first);
+            const bool all = base + CHUNK - 1 <= p0 && (p.c.window == 0 || base > seq.len - 1 - p.c.window || base + CHUNK <= p.c.n_first);
             uint32_t pf[NT][2][2];
             float alpha[NT][2];
 #pragma unroll
@@ -354,7 +354,7 @@ attention_split(const split_params p)
                             float y = fmaf(x[n][k][2 * e + c], wd[k][e].x, fmaf(qsum[n][c], wd[k][e].y, wd[k][e].z));
                             if (!all) {
                                 const int pos = base + k * KV_BLOCK + (g >> 1) + 4 * (g & 1) + 8 * e, at = p0 + (8 * n + 2 * i4 + c) / p.group;
-                                const bool see = pos <= at && (p.c.window == 0 || pos > (int64_t)at - p.c.window || pos < p.c.n_first);
+                                const bool see = pos <= at && (p.c.window == 0 || pos > at - p.c.window || pos < p.c.n_first);
                                 if (!see) y = -INFINITY;
                             }
                             x[n][k][2 * e + c] = y;

@@ -4,6 +4,7 @@
 #include "tpq_internal.h"
 
 #define KV_BLOCK 16  // positions of a block of the cache
+#define KV_MOST (1 << 30)  // positions of a sequence
 
 struct tpq_kv {
     int n_heads, n_kv_heads, head_dim, page_size;
@@ -39,7 +40,7 @@ struct kv_attention_call {
     uint16_t *out;
     int64_t out_stride;
     float scale;
-    int64_t window, n_first;  // window 0: none
+    int window, n_first;  // at most KV_MOST; window 0: none
     void *workspace;
 };
 size_t kv_attention_workspace(int D, int n_heads, int n_kv_heads, int sm_count, int64_t n_seqs, int64_t max_new, int64_t n_tokens);
@@ -69,7 +70,7 @@ __device__ __forceinline__ kv_seq kv_load_seq(const kv_batch &b, int s)
     q.n = b.start[s + 1];
     q.len = b.lengths[s];
     const bool ok = q.start >= 0 && q.start <= q.n && q.n <= b.n_tokens && q.n - q.start <= b.max_new && q.n - q.start <= q.len &&
-                    q.len <= b.table_stride * (int64_t)b.page_size;
+                    q.len <= b.table_stride * (int64_t)b.page_size && q.len <= KV_MOST;
     q.n -= q.start;
     if (!ok) {
         kv_report(b);

@@ -65,10 +65,10 @@ __device__ __forceinline__ item_tiles tiles_of_rows(const kv_seq &s, const kv_at
     const int p_lo = s.len - s.n + block * BM / group, p_hi = s.len - s.n + (block * BM + t.rows - 1) / group;
     t.first = t.from = 0;
     if (c.window) {
-        const int64_t from = (int64_t)p_lo - c.window + 1;
+        const int from = p_lo - c.window + 1;
         if (from > 0) {
-            t.from = (int)(from / TILE);
-            const int first = (int)(((c.n_first < from ? c.n_first : from) + TILE - 1) / TILE);
+            t.from = from / TILE;
+            const int first = ((c.n_first < from ? c.n_first : from) + TILE - 1) / TILE;
             t.first = first < t.from ? first : t.from;
         }
     }
@@ -201,22 +201,26 @@ __device__ __forceinline__ bool elect()
         : "=r"(one));
     return one != 0;
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+// (the descriptors' high halves are constants: only the low ones are held)
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t high, uint32_t idesc, uint32_t accumulate)
 {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        "{\n\t.reg .pred p;\n\t.reg .b64 x, y;\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "mov.b64 x, {%1, %3};\n\t"
+        "mov.b64 y, {%2, %3};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %4, p;\n\t}"
+        ::"r"(d), "r"(a), "r"(b), "r"(high), "r"(idesc), "r"(accumulate)
         : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t high, uint32_t idesc, uint32_t accumulate)
 {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-        ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        "{\n\t.reg .pred p;\n\t.reg .b64 y;\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "mov.b64 y, {%2, %3};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %4, p;\n\t}"
+        ::"r"(d), "r"(a), "r"(b), "r"(high), "r"(idesc), "r"(accumulate)
         : "memory");
 }
 #define R8(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]), "=r"(r[i + 4]), "=r"(r[i + 5]), "=r"(r[i + 6]), "=r"(r[i + 7])
@@ -242,15 +246,21 @@ __device__ __forceinline__ void st32(uint32_t addr, const uint32_t *r)
         ::W8(r, 0), W8(r, 8), W8(r, 16), W8(r, 24), "r"(addr)
         : "memory");
 }
+__device__ __forceinline__ void ld8(uint32_t addr, uint32_t *r)
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];" : R8(r, 0) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void st8(uint32_t addr, const uint32_t *r)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::W8(r, 0), "r"(addr) : "memory");
+}
 __device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // Operands of 128-byte rows with the 128-byte swizzle, 8-row groups of 1024 bytes.  Depth along the row (Q, keys): a step of 16 is 32
 // bytes of the row, 64-deep sub-tiles lie behind each other.  Depth along the rows (values: a row is a position, along it the head's
 // values): a step of 16 is 16 rows, the next 64 values are `lead` bytes on.
-__device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t lead)
-{
-    return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(lead >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
-}
+__device__ __forceinline__ uint32_t operand(uint32_t addr, uint32_t lead) { return ((addr & 0x3FFFFu) >> 4) | ((lead >> 4) << 16); }
+constexpr uint32_t OPERAND_HIGH = (1024 >> 4) | (1u << 14) | (2u << 29);  // 1024 bytes from 8 rows to the next; version; 128-byte swizzle
 // FP32 sums of 128 rows x n columns; `bf16`: both operands BF16 (else FP16); `rows_deep`: B's depth runs along its rows
 __host__ __device__ constexpr uint32_t instr(int n, bool bf16, bool rows_deep)
 {
@@ -294,6 +304,14 @@ __device__ __forceinline__ f2 add2(f2 a, f2 b)
 {
     f2 r;
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+// (volatile: in the order of the program, or the loads of a whole tile's terms would pile up ahead of their use)
+__device__ __forceinline__ ulonglong2 lds2(uint32_t addr)
+{
+    ulonglong2 r;
+    asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(r.x), "=l"(r.y) : "r"(addr));
     return r;
 }
 
@@ -357,11 +375,11 @@ __device__ __forceinline__ reach reach_of(const prompt_params &p, const segment 
 }
 __device__ __forceinline__ bool sees(const prompt_params &p, const reach &r, int base)
 {
-    return r.hi >= r.lo && base <= r.hi && (p.c.window == 0 || (int64_t)base + TILE - 1 > (int64_t)r.lo - p.c.window || base < p.c.n_first);
+    return r.hi >= r.lo && base <= r.hi && (p.c.window == 0 || base + TILE - 1 > r.lo - p.c.window || base < p.c.n_first);
 }
 __device__ __forceinline__ bool sees_all(const prompt_params &p, const reach &r, int base)
 {
-    return base + TILE - 1 <= r.lo && (p.c.window == 0 || base > (int64_t)r.hi - p.c.window || base + TILE <= p.c.n_first);
+    return base + TILE - 1 <= r.lo && (p.c.window == 0 || base > r.hi - p.c.window || base + TILE <= p.c.n_first);
 }
 
 template <int D>
@@ -427,9 +445,9 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
     }
     run r = r0;
 
-    // Registers: 128 a thread at launch; 64 + 80 + 2 x 184 are the four warpgroups' 512.
+    // Registers: 128 a thread at launch; 96 + 64 + 2 x 176 are the four warpgroups' 512.
     if (warp < 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
     if (warp == 0) {
         // ---------------- copies
         int stage = 0;  // copy stages so far
@@ -439,8 +457,8 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                 if (h >= 2 * g.nt || lane >= HALF / KV_BLOCK) return -1;
                 const int pos = g.base(h >> 1) + (h & 1) * HALF + lane * KV_BLOCK;
                 if (pos >= g.seq.len) return -1;
-                const int64_t from = (int64_t)(g.seq.len - g.seq.n + g.row0 / p.group) - p.c.window + 1;
-                if (p.c.window && pos >= p.c.n_first && (int64_t)pos + KV_BLOCK <= from) return -1;  // no row sees it
+                const int from = g.seq.len - g.seq.n + g.row0 / p.group - p.c.window + 1;
+                if (p.c.window && pos >= p.c.n_first && pos + KV_BLOCK <= from) return -1;  // no row sees it
                 const int hi = g.seq.len - g.seq.n + (g.row0 + g.it.rows - 1) / p.group;
                 if (pos > hi) return -1;
                 const int page = b.table[g.s * b.table_stride + (pos >> b.page_shift)];
@@ -486,11 +504,11 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
             auto scores = [&](int t, int j) {  // Q_t C(j)
                 if (!ok || !sees(p, re[t], g.base(j))) return;
                 if (elect()) {
-                    const uint64_t a = operand(smem + L::Q + t * L::TILE_BYTES, 16), k = operand(smem + L::K + ((it + j) & 1) * L::TILE_BYTES, 16);
+                    const uint32_t a = operand(smem + L::Q + t * L::TILE_BYTES, 16), k = operand(smem + L::K + ((it + j) & 1) * L::TILE_BYTES, 16);
 #pragma unroll
                     for (int x = 0; x < D / 16; ++x) {
-                        const uint64_t at = (uint64_t)((x / 4) * (128 * 128 >> 4) + 2 * (x % 4));
-                        mma_ss(tmem + t * TILE, a + at, k + at, qk_instr, x != 0);
+                        const uint32_t at = (x / 4) * (128 * 128 >> 4) + 2 * (x % 4);
+                        mma_ss(tmem + t * TILE, a + at, k + at, OPERAND_HIGH, qk_instr, x != 0);
                     }
                     commit(bar(B_S_FULL + t));
                 }
@@ -514,10 +532,10 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                         if (!ok) break;
                         fence_after();
                         if (elect()) {
-                            const uint64_t v = operand(smem + L::V + (i & 1) * L::TILE_BYTES, TILE * 128);
+                            const uint32_t v = operand(smem + L::V + (i & 1) * L::TILE_BYTES, TILE * 128);
 #pragma unroll
                             for (int x = 0; x < TILE / 16; ++x)
-                                mma_ts(tmem + 256 + t * 128, tmem + t * TILE + 8 * x, v + (uint64_t)(x * (2048 >> 4)), pv_instr, any[t] || x != 0);
+                                mma_ts(tmem + 256 + t * 128, tmem + t * TILE + 8 * x, v + x * (2048 >> 4), OPERAND_HIGH, pv_instr, any[t] || x != 0);
                             if (j == last[t]) commit(bar(B_O_FULL + t));
                         }
                         __syncwarp();
@@ -546,7 +564,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
     }
     } else if (warp < 8) {
         // ---------------- unpack: warp w - 4 takes one block of 16 positions of each copy stage
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         const int w4 = warp - 4;
         int stage = 0, it = 0;
         while (r.more() && ok) {
@@ -615,26 +633,26 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
         }
     } else {
         // ---------------- softmax: thread <-> row `row` of row tile t
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
         const int t = (warp - 8) >> 2, row = tid & 127;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t s_addr = tmem + t * TILE + lanes, o_addr = tmem + 256 + t * 128 + lanes;
         int it = 0, s_count = 0, segs = 0;
-        int4 header = make_int4(0, 0, 0, 0);
-        const plan_head ph = *p.head;
-        const int share = (int)(((int64_t)ph.total + gridDim.x - 1) / gridDim.x);
+        if (tid == 256) p.headers[blockIdx.x] = make_int4(0, 0, 0, 0);
         while (r.more() && ok) {
+            const run begin_run = r;
             const segment g = next_segment(p, r);
             const reach re = reach_of(p, g, t);
             bool works = false;
             for (int j = 0; j < g.nt && !works; ++j) works = sees(p, re, g.base(j));
-            const int rr = g.row0 + t * 128 + row, tok = rr / p.group, h = g.kh * p.group + (rr - tok * p.group);  // row of the sequence
-            const bool mine = t * 128 + row < g.it.rows;
-            const int pos = mine ? g.seq.len - g.seq.n + tok : -1;
+            int pos = -1;  // of this thread's row
             float m = -INFINITY, qsum = 0.0f;
             f2 l2 = 0, w2 = 0;
             bool any = false;
             if (works) {
+                const int rr = g.row0 + t * 128 + row, tok = rr / p.group, h = g.kh * p.group + (rr - tok * p.group);  // row of the sequence
+                const bool mine = t * 128 + row < g.it.rows;
+                if (mine) pos = g.seq.len - g.seq.n + tok;
                 // the row as an operand, 8 values of a chunk in the codes' order 0 4 1 5 2 6 3 7
                 const uint4 *src = reinterpret_cast<const uint4 *>(p.c.q.p + (int64_t)(g.seq.start + tok) * p.c.q.stride + (int64_t)h * D);
                 uint8_t *const dst = gen + L::Q + t * L::TILE_BYTES + row * 128;
@@ -660,39 +678,40 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                 if (!ok) break;
                 ++s_count;
                 fence_after();
-                const float *term = reinterpret_cast<const float *>(gen + L::TERM + (i % 3) * L::TERM_BYTES);
+                const uint32_t term = smem + L::TERM + (i % 3) * L::TERM_BYTES;
                 uint32_t x[TILE];
-#pragma unroll
-                for (int k = 0; k < TILE; k += 32) ld32(s_addr + k, x + k);
-                ld_wait();
-                float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                ld32(s_addr, x);
+                float top[2] = {-INFINITY, -INFINITY};
                 const bool all = sees_all(p, re, base);
-                // visible of this row, of the tile's positions: below `end`, and from `begin` on or below `head`
-                const int end = pos - base + 1;
-                const int64_t begin64 = p.c.window ? (int64_t)pos - p.c.window + 1 - base : -1, head64 = p.c.n_first - base;
-                const int begin = begin64 > TILE ? TILE : begin64 < 0 ? 0 : (int)begin64, head = head64 > TILE ? TILE : head64 < 0 ? 0 : (int)head64;
 #pragma unroll
-                for (int k = 0; k < TILE; k += 4) {
-                    const ulonglong2 st = *reinterpret_cast<const ulonglong2 *>(term + T_STEP * TILE + k);
-                    const ulonglong2 of = *reinterpret_cast<const ulonglong2 *>(term + T_OFF * TILE + k);
-                    const ulonglong2 lg = *reinterpret_cast<const ulonglong2 *>(term + T_LOG * TILE + k);
-                    const f2 y0 = fma2(pack2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), st.x, fma2(of.x, qsum2, lg.x));
-                    const f2 y1 = fma2(pack2(__uint_as_float(x[k + 2]), __uint_as_float(x[k + 3])), st.y, fma2(of.y, qsum2, lg.y));
-                    float y[4];
-                    unpack2(y0, y[0], y[1]);
-                    unpack2(y1, y[2], y[3]);
+                for (int c = 0; c < TILE; c += 32) {
+                    ld_wait();
+                    if (c + 32 < TILE) ld32(s_addr + c + 32, x + c + 32);
+#pragma unroll
+                    for (int k = c; k < c + 32; k += 4) {
+                        const ulonglong2 st = lds2(term + T_STEP * TILE * 4 + k * 4), of = lds2(term + T_OFF * TILE * 4 + k * 4), lg = lds2(term + T_LOG * TILE * 4 + k * 4);
+                        const f2 y0 = fma2(pack2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), st.x, fma2(of.x, qsum2, lg.x));
+                        const f2 y1 = fma2(pack2(__uint_as_float(x[k + 2]), __uint_as_float(x[k + 3])), st.y, fma2(of.y, qsum2, lg.y));
+                        float y[4];
+                        unpack2(y0, y[0], y[1]);
+                        unpack2(y1, y[2], y[3]);
+#pragma unroll
+                        for (int z = 0; z < 4; ++z) x[k + z] = __float_as_uint(y[z]);
+                    }
                     if (!all) {
+                        // visible of this row: below `end`, and from `begin` on or below `head`
+                        const int end = pos - base + 1, begin = p.c.window ? pos - p.c.window + 1 - base : 0, head = p.c.n_first - base;
 #pragma unroll
-                        for (int z = 0; z < 4; ++z)
-                            if (k + z >= end || (k + z < begin && k + z >= head)) y[z] = -INFINITY;
+                        for (int k = c; k < c + 32; ++k)
+                            if (k >= end || (k < begin && k >= head)) x[k] = 0xff800000u;
                     }
 #pragma unroll
-                    for (int z = 0; z < 4; ++z) {
-                        x[k + z] = __float_as_uint(y[z]);
-                        top[z] = fmaxf(top[z], y[z]);
+                    for (int k = c; k < c + 32; k += 2) {
+                        top[0] = fmaxf(top[0], __uint_as_float(x[k]));
+                        top[1] = fmaxf(top[1], __uint_as_float(x[k + 1]));
                     }
                 }
-                const float tile_top = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+                const float tile_top = fmaxf(top[0], top[1]);
                 if (!any) {
                     m = tile_top;
                 } else if (__any_sync(0xffffffffu, tile_top > m + 8.0f)) {
@@ -703,13 +722,13 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                     w2 = fma2(w2, a2, 0);
                     // (the scores of this tile were computed behind the products that O holds)
 #pragma unroll
-                    for (int k = 0; k < D; k += 32) {
-                        uint32_t o[32];
-                        ld32(o_addr + k, o);
+                    for (int k = 0; k < D; k += 8) {
+                        uint32_t o[8];
+                        ld8(o_addr + k, o);
                         ld_wait();
 #pragma unroll
-                        for (int z = 0; z < 32; ++z) o[z] = __float_as_uint(__uint_as_float(o[z]) * a);
-                        st32(o_addr + k, o);
+                        for (int z = 0; z < 8; ++z) o[z] = __float_as_uint(__uint_as_float(o[z]) * a);
+                        st8(o_addr + k, o);
                     }
                     st_wait();
                 }
@@ -718,8 +737,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                 const f2 minus = pack2(-from, -from);
 #pragma unroll
                 for (int k = 0; k < TILE; k += 4) {
-                    const ulonglong2 iv = *reinterpret_cast<const ulonglong2 *>(term + T_INV * TILE + k);
-                    const ulonglong2 lw = *reinterpret_cast<const ulonglong2 *>(term + T_LOW * TILE + k);
+                    const ulonglong2 iv = lds2(term + T_INV * TILE * 4 + k * 4), lw = lds2(term + T_LOW * TILE * 4 + k * 4);
                     float y[4];
                     unpack2(add2(pack2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), minus), y[0], y[1]);
                     unpack2(add2(pack2(__uint_as_float(x[k + 2]), __uint_as_float(x[k + 3])), minus), y[2], y[3]);
@@ -753,8 +771,12 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                 ++segs;
                 fence_after();
             }
-            const bool whole = g.t0 == 0 && g.nt == g.it.count;
-            float *part = p.parts + (((int64_t)blockIdx.x * 2 + (g.t0 == 0 ? 1 : 0)) * BM + t * 128 + row) * (D + 4);
+            // (what the walk over the tiles had no use for is worked out again instead of held in registers)
+            run again = begin_run;
+            const segment f = next_segment(p, again);
+            const int rr = f.row0 + t * 128 + row, tok = rr / p.group, h = f.kh * p.group + (rr - tok * p.group);
+            const bool mine = t * 128 + row < f.it.rows, whole = f.t0 == 0 && f.nt == f.it.count;
+            float *part = p.parts + (((int64_t)blockIdx.x * 2 + (f.t0 == 0 ? 1 : 0)) * BM + t * 128 + row) * (D + 4);
             const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
             for (int k = 0; k < D; k += 32) {
@@ -780,7 +802,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                             const __nv_bfloat162 v = __floats2bfloat162_rn(y[2 * z] * inv, y[2 * z + 1] * inv);
                             u[z] = *reinterpret_cast<const uint32_t *>(&v);
                         }
-                        *reinterpret_cast<uint4 *>(p.c.out + (int64_t)(g.seq.start + tok) * p.c.out_stride + (int64_t)h * D + k + c) = make_uint4(u[0], u[1], u[2], u[3]);
+                        *reinterpret_cast<uint4 *>(p.c.out + (int64_t)(f.seq.start + tok) * p.c.out_stride + (int64_t)h * D + k + c) = make_uint4(u[0], u[1], u[2], u[3]);
                     } else {
                         reinterpret_cast<float4 *>(part + k + c)[0] = make_float4(y[0], y[1], y[2], y[3]);
                         reinterpret_cast<float4 *>(part + k + c)[1] = make_float4(y[4], y[5], y[6], y[7]);
@@ -794,10 +816,11 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(B_O_EMPTY + t));
             }
-            if (g.t0 == 0 && !whole)
-                header = make_int4(1 + (g.it.count - g.nt + share - 1) / share, g.seq.start, g.row0, (g.it.rows << 16) | g.kh);
+            if (tid == 256 && f.t0 == 0 && !whole) {  // the runs behind this one have `share` tiles each of what is left
+                const int share = (int)(((int64_t)p.head->total + gridDim.x - 1) / gridDim.x);
+                p.headers[blockIdx.x] = make_int4(1 + (f.it.count - f.nt + share - 1) / share, f.seq.start, f.row0, (f.it.rows << 16) | f.kh);
+            }
         }
-        if (tid == 256) p.headers[blockIdx.x] = header;
     }
     if (!ok && lane == 0) atomicExch(b.status, (int)TPQ_ERR_TIMEOUT);
     fence_before();
