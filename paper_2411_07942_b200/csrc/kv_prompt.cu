@@ -1,11 +1,12 @@
 // Attention over the 4-bit cache (tpq_kv_attention) for sequences that bring many rows: prompts and chunks of them.
 //
-// The mathematics is that of kv_attention.cu: codes are the operands, the values' steps go into the exponent.  Here the products
-// run on tcgen05: S = Q C^T of 128 rows x 128 positions with the keys' codes as BF16 128 + c, O += P E with P from tensor
-// memory and the values' codes as FP16 e - 8 (both exact).  A row (query head x new position) of S is one thread's, which
-// finds
-//   y_t = S_t (s_t scale log2 e) + (a_t - 128 s_t) scale log2(e) sum(q) + log2 r_t,   P_t = 2^(y_t - m + 7) in FP16,
-//   l = sum P_t / r_t,  w = sum P_t (b_t / r_t + 8),   out = (O + w) / l.
+// The mathematics is that of kv_attention.cu, the products run on tcgen05: S = Q C^T of 128 rows x 128 positions with the keys' codes
+// as BF16 128 + c (exact), O += P V with P from tensor memory.  What a row's thread does per element decides the speed here, so
+// the values are formed, in FP16: with 2^F the scale of a block of 16 positions (its largest magnitude is 2^14 .. 2^15 of it),
+// v_t 2^-F is rounded once to 11 bits of at least 2^-28 of that magnitude, and F goes into the exponent.  A row (query head x new
+// position) of S is one thread's, which finds
+//   y_t = S_t (s_t scale log2 e) + (a_t - 128 s_t) scale log2(e) sum(q) + F,   P_t = 2^(y_t - m + 7) in FP16,
+//   l = sum over blocks of 2^-F sum P_t,   out = O / l.
 // m moves only when a row's maximum has grown by more than 8 (P stays below 2^15): O is rescaled in tensor memory then, which
 // after a sequence's first tiles hardly happens.
 //
@@ -14,7 +15,7 @@
 //   ... P_A E(j), Q_A C(j+1), P_B E(j), Q_B C(j+1), P_A E(j+1), ...
 //   warp 0       copies: blocks of 16 positions as they lie in the pages, 64 positions a stage
 //   warp 1       tensor memory, MMA issue (one elected lane)
-//   warps 4-7    unpack: codes to the two operands' tiles (128-byte swizzle), words to the five terms of a position
+//   warps 4-7    unpack: codes to the two operands' tiles (128-byte swizzle), words to the terms of a position
 //   warps 8-15   softmax: a thread per row; the rows themselves into shared memory at the start, the output at the end
 // Unpacking a tile costs as much however many rows use it: 256 rows, which the query heads of a key head share.
 //
@@ -36,6 +37,8 @@ constexpr int PLAN_THREADS = 1024;
 
 struct alignas(16) plan_item {
     int seq, block, before, tiles;  // `block`: its rows start at BM * block; `before`: tiles x key heads of the items ahead
+    kv_seq rows;
+    int pad;
 };
 struct alignas(16) plan_head {
     int items, total, pad[2];
@@ -134,6 +137,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) attention_plan(const prompt_para
     for (int i0 = 0; i0 < items; i0 += PLAN_THREADS) {
         const int i = i0 + threadIdx.x;
         int n = 0, s = 0, block = 0;
+        kv_seq q{};
         if (i < items) {
             int lo = 0, hi = b.n_seqs;  // the last sequence whose items begin at or before i
             while (hi - lo > 1) {
@@ -143,12 +147,13 @@ __global__ void __launch_bounds__(PLAN_THREADS) attention_plan(const prompt_para
             }
             s = lo;
             block = i - p.seq_items[s];
-            n = tiles_of_rows(kv_load_seq(b, s), p.c, p.group, block).count;
+            q = kv_load_seq(b, s);
+            n = tiles_of_rows(q, p.c, p.group, block).count;
         }
         int total;
         const int64_t at = before + (int64_t)(block_scan(n, warps, total) - n) * b.n_kv_heads;
         before += (int64_t)total * b.n_kv_heads;
-        if (i < items) p.items[i] = plan_item{s, block, (int)at, n};
+        if (i < items) p.items[i] = plan_item{s, block, (int)at, n, q, 0};
     }
     if (threadIdx.x == 0) {
         if (before > INT32_MAX - 1024) {
@@ -273,18 +278,13 @@ __device__ __forceinline__ float ex2(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
-__device__ __forceinline__ float lg2(float x)
-{
-    float r;
-    asm("lg2.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
-}
 __device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t mask, uint32_t bits)
 {
     uint32_t r;
     asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(a), "r"(mask), "r"(bits));
     return r;
 }
+__device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
 // two binary32 operations an instruction
 typedef unsigned long long f2;
 __device__ __forceinline__ f2 pack2(float a, float b)
@@ -315,15 +315,22 @@ __device__ __forceinline__ ulonglong2 lds2(uint32_t addr)
     return r;
 }
 
-// terms of the positions of a tile, by array: score step, score offset, log2 of the value step, its reciprocal, (value low)/(value step) + 8
-enum { T_STEP, T_OFF, T_LOG, T_INV, T_LOW, TERMS };
+__device__ __forceinline__ float lds1(uint32_t addr)
+{
+    float r;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(r) : "r"(addr));
+    return r;
+}
+// Terms of a tile: score step and score offset of every position; of every block of 16 positions the exponent F of its values' scale
+// and 2^-F.
+enum { T_STEP = 0, T_OFF = TILE * 4, T_F = 2 * TILE * 4, T_INV = T_F + TILE / KV_BLOCK * 4, TERM_BYTES = T_INV + TILE / KV_BLOCK * 4 };
 
 template <int D>
 struct Smem {
     static constexpr uint32_t TILE_BYTES = TILE * D * 2;  // an operand tile
     static constexpr uint32_t Q = 0, K = Q + 2 * TILE_BYTES, V = K + 2 * TILE_BYTES, RAWS = V + 2 * TILE_BYTES;
     static constexpr uint32_t RAW_BYTES = HALF / KV_BLOCK * kv_block_bytes(D);
-    static constexpr uint32_t TERM = RAWS + RAW * RAW_BYTES, TERM_BYTES = TERMS * TILE * 4;
+    static constexpr uint32_t TERM = RAWS + RAW * RAW_BYTES;
     static constexpr uint32_t BARS = TERM + 3 * TERM_BYTES;
     static constexpr uint32_t BYTES = BARS + 256 + 1024;  // (1024: slack for the alignment)
 };
@@ -351,7 +358,7 @@ __device__ __forceinline__ segment next_segment(const prompt_params &p, run &r)
     plan_item it = p.items[r.item];
     while (r.unit >= it.before + it.tiles * p.b.n_kv_heads) it = p.items[++r.item];
     g.s = it.seq;
-    g.seq = kv_load_seq(p.b, it.seq);
+    g.seq = it.rows;
     g.row0 = it.block * BM;
     g.it = tiles_of_rows(g.seq, p.c, p.group, it.block);
     const int off = r.unit - it.before;
@@ -575,24 +582,41 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                          __all_sync(0xffffffffu, wait(bar(B_V_EMPTY + (it & 1)), ((it >> 1) - 1) & 1));
                     if (!ok) break;
                 }
-                float *const term = reinterpret_cast<float *>(gen + L::TERM + (it % 3) * L::TERM_BYTES);
+                uint8_t *const term = gen + L::TERM + (it % 3) * TERM_BYTES;
                 for (int half = 0; half < 2; ++half, ++stage) {
                     const int st = stage % RAW;
                     ok = __all_sync(0xffffffffu, wait(bar(B_RAW_FULL + st), (stage / RAW) & 1));
                     if (!ok) break;
                     const uint8_t *const blk = gen + L::RAWS + st * L::RAW_BYTES + w4 * kv_block_bytes(D);
                     const int row0 = half * HALF + w4 * KV_BLOCK;  // of the tile
-                    if (lane < KV_BLOCK) {
-                        const uint32_t kw = reinterpret_cast<const uint32_t *>(blk + kv_k_words(D))[lane], vw = reinterpret_cast<const uint32_t *>(blk + kv_v_words(D))[lane];
+                    uint32_t scaled;  // FP16 step and low of this lane's position (lane % 16) for the values' scale 2^-F
+                    {
+                        const int r = lane & 15;
+                        const uint32_t kw = reinterpret_cast<const uint32_t *>(blk + kv_k_words(D))[r], vw = reinterpret_cast<const uint32_t *>(blk + kv_v_words(D))[r];
                         const float ks = __uint_as_float(kw << 16), kl = __uint_as_float(kw & 0xffff0000u);
-                        const float vs = __uint_as_float(vw << 16), vl = __uint_as_float(vw & 0xffff0000u), inv = __frcp_rn(vs);
-                        const bool on = g.base(j) + row0 + lane < g.seq.len && ((there[st] >> w4) & 1u);
-                        float *t = term + row0 + lane;
-                        t[T_STEP * TILE] = on ? ks * p.scale2 : 0.0f;
-                        t[T_OFF * TILE] = on ? fmaf(-128.0f, ks, kl) * p.scale2 : 0.0f;
-                        t[T_LOG * TILE] = on ? lg2(vs) : -INFINITY;
-                        t[T_INV * TILE] = on ? inv : 0.0f;
-                        t[T_LOW * TILE] = on ? fmaf(vl, inv, 8.0f) : 0.0f;
+                        const float vs = __uint_as_float(vw << 16), vl = __uint_as_float(vw & 0xffff0000u);
+                        const bool have = (there[st] >> w4) & 1u, on = have && g.base(j) + row0 + r < g.seq.len;
+                        float big = on ? fmaxf(fabsf(vl), fabsf(fmaf(15.0f, vs, vl))) : 0.0f;
+                        const bool bad = !(fabsf(vl) + vs < INFINITY) || !(big < INFINITY);
+                        if (bad) big = 0.0f;
+#pragma unroll
+                        for (int m = 8; m > 0; m >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, m));
+                        // 2^14 <= largest magnitude of the block * 2^-F < 2^15 (nothing is below 2^-57 but zeros)
+                        const int e = big < 0x1p-60f ? 67 : (int)(__float_as_uint(big) >> 23);
+                        const float inv = __uint_as_float((uint32_t)(268 - e) << 23);  // 2^(14 - (e - 127)) = 2^-F
+                        const __half2 h = __floats2half2_rn(on && !bad ? vs * inv : 0.0f, on && !bad ? vl * inv : 0.0f);
+                        scaled = *reinterpret_cast<const uint32_t *>(&h);
+                        if (lane < KV_BLOCK) {
+                            float *t = reinterpret_cast<float *>(term) + row0 + r;
+                            t[T_STEP / 4] = on ? ks * p.scale2 : 0.0f;
+                            // (a value vector that is no number makes the rows that see it NaN by way of their scores: a weight
+                            // of 0 times NaN would reach the others)
+                            t[T_OFF / 4] = !on ? 0.0f : bad ? NAN : fmaf(-128.0f, ks, kl) * p.scale2;
+                        }
+                        if (lane == 0) {
+                            reinterpret_cast<float *>(term + T_F)[row0 / KV_BLOCK] = have ? (float)(e - 141) : -INFINITY;
+                            reinterpret_cast<float *>(term + T_INV)[row0 / KV_BLOCK] = have ? inv : 0.0f;
+                        }
                     }
 #pragma unroll
                     for (int k = 0; k < D / 64; ++k) {
@@ -603,7 +627,9 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                         const uint32_t kk[4] = {ck.x, ck.y, ck.z, ck.w}, vv[4] = {cv.x, cv.y, cv.z, cv.w};
                         const uint32_t line = (uint32_t)((q >> 1) * (TILE * 128) + (row0 + row) * 128);
                         uint8_t *const kd = gen + L::K + (it & 1) * L::TILE_BYTES + line, *const vd = gen + L::V + (it & 1) * L::TILE_BYTES + line;
-                        const __half2 sixteenth = __float2half2_rn(0.0625f), off = __float2half2_rn(-72.0f), off0 = __float2half2_rn(-1032.0f);
+                        const uint32_t sl = __shfl_sync(0xffffffffu, scaled, row);
+                        const __half2 step_low = *reinterpret_cast<const __half2 *>(&sl), step = __low2half2(step_low), low = __high2half2(step_low);
+                        const __half2 sixteenth = __float2half2_rn(0.0625f), off = __float2half2_rn(-64.0f), off0 = __float2half2_rn(-1024.0f);
 #pragma unroll
                         for (int jw = 0; jw < 4; ++jw) {
                             const uint32_t at = (uint32_t)((((q & 1) * 4 + jw) ^ (row & 7)) * 16);
@@ -615,8 +641,8 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                                              and_or(v >> 8, 0x000f000fu, 0x64006400u), and_or(v >> 8, 0x00f000f0u, 0x64006400u)};
 #pragma unroll
                             for (int z = 0; z < 4; ++z) {
-                                const __half2 h = *reinterpret_cast<const __half2 *>(&e[z]);
-                                const __half2 y = z & 1 ? __hfma2(h, sixteenth, off) : __hadd2(h, off0);
+                                const __half2 c = *reinterpret_cast<const __half2 *>(&e[z]);
+                                const __half2 y = __hfma2(z & 1 ? __hfma2(c, sixteenth, off) : __hadd2(c, off0), step, low);  // (the codes: exact)
                                 e[z] = *reinterpret_cast<const uint32_t *>(&y);
                             }
                             *reinterpret_cast<uint4 *>(vd + at) = make_uint4(e[0], e[1], e[2], e[3]);
@@ -647,27 +673,32 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
             for (int j = 0; j < g.nt && !works; ++j) works = sees(p, re, g.base(j));
             int pos = -1;  // of this thread's row
             float m = -INFINITY, qsum = 0.0f;
-            f2 l2 = 0, w2 = 0;
+            f2 l2 = 0;
             bool any = false;
+            uint8_t *const q_tile = gen + L::Q + t * L::TILE_BYTES;
             if (works) {
-                const int rr = g.row0 + t * 128 + row, tok = rr / p.group, h = g.kh * p.group + (rr - tok * p.group);  // row of the sequence
-                const bool mine = t * 128 + row < g.it.rows;
-                if (mine) pos = g.seq.len - g.seq.n + tok;
-                // the row as an operand, 8 values of a chunk in the codes' order 0 4 1 5 2 6 3 7
-                const uint4 *src = reinterpret_cast<const uint4 *>(p.c.q.p + (int64_t)(g.seq.start + tok) * p.c.q.stride + (int64_t)h * D);
-                uint8_t *const dst = gen + L::Q + t * L::TILE_BYTES + row * 128;
+                const int rr = g.row0 + t * 128 + row;
+                if (t * 128 + row < g.it.rows) pos = g.seq.len - g.seq.n + rr / p.group;
+                // the warp's 32 rows as an operand, D/8 lanes a row; 8 values of a chunk in the codes' order 0 4 1 5 2 6 3 7
 #pragma unroll
                 for (int k = 0; k < D / 8; ++k) {
-                    const uint4 x = mine ? src[k] : make_uint4(0, 0, 0, 0);
-                    const uint32_t u[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                    for (int z = 0; z < 4; ++z) qsum += __uint_as_float(u[z] << 16) + __uint_as_float(u[z] & 0xffff0000u);
-                    *reinterpret_cast<uint4 *>(dst + (k / 8) * (128 * 128) + (((k & 7) ^ (row & 7)) * 16)) =
+                    const int w_row = (warp & 3) * 32 + k * (256 / D) + lane / (D / 8), c = lane % (D / 8), r1 = g.row0 + t * 128 + w_row, tok = r1 / p.group;
+                    uint4 x = make_uint4(0, 0, 0, 0);
+                    if (t * 128 + w_row < g.it.rows)
+                        x = reinterpret_cast<const uint4 *>(p.c.q.p + (int64_t)(g.seq.start + tok) * p.c.q.stride + (int64_t)(g.kh * p.group + r1 - tok * p.group) * D)[c];
+                    *reinterpret_cast<uint4 *>(q_tile + (c / 8) * (128 * 128) + w_row * 128 + (((c & 7) ^ (w_row & 7)) * 16)) =
                         make_uint4(__byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632), __byte_perm(x.y, x.w, 0x5410), __byte_perm(x.y, x.w, 0x7632));
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(B_Q_FULL + t));
+#pragma unroll
+                for (int c = 0; c < D / 8; ++c) {
+                    const uint4 x = *reinterpret_cast<const uint4 *>(q_tile + (c / 8) * (128 * 128) + row * 128 + (((c & 7) ^ (row & 7)) * 16));
+                    const uint32_t u[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) qsum += __uint_as_float(u[z] << 16) + __uint_as_float(u[z] & 0xffff0000u);
+                }
             }
             const f2 qsum2 = pack2(qsum, qsum);
             for (int j = 0; j < g.nt; ++j) {
@@ -678,7 +709,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                 if (!ok) break;
                 ++s_count;
                 fence_after();
-                const uint32_t term = smem + L::TERM + (i % 3) * L::TERM_BYTES;
+                const uint32_t term = smem + L::TERM + (i % 3) * TERM_BYTES;
                 uint32_t x[TILE];
                 ld32(s_addr, x);
                 float top[2] = {-INFINITY, -INFINITY};
@@ -687,11 +718,14 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                 for (int c = 0; c < TILE; c += 32) {
                     ld_wait();
                     if (c + 32 < TILE) ld32(s_addr + c + 32, x + c + 32);
+                    const float fa = lds1(term + T_F + c / KV_BLOCK * 4), fb = lds1(term + T_F + c / KV_BLOCK * 4 + 4);
+                    const f2 f2a = pack2(fa, fa), f2b = pack2(fb, fb);
 #pragma unroll
                     for (int k = c; k < c + 32; k += 4) {
-                        const ulonglong2 st = lds2(term + T_STEP * TILE * 4 + k * 4), of = lds2(term + T_OFF * TILE * 4 + k * 4), lg = lds2(term + T_LOG * TILE * 4 + k * 4);
-                        const f2 y0 = fma2(pack2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), st.x, fma2(of.x, qsum2, lg.x));
-                        const f2 y1 = fma2(pack2(__uint_as_float(x[k + 2]), __uint_as_float(x[k + 3])), st.y, fma2(of.y, qsum2, lg.y));
+                        const ulonglong2 st = lds2(term + T_STEP + k * 4), of = lds2(term + T_OFF + k * 4);
+                        const f2 f = k - c < KV_BLOCK ? f2a : f2b;
+                        const f2 y0 = fma2(pack2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), st.x, fma2(of.x, qsum2, f));
+                        const f2 y1 = fma2(pack2(__uint_as_float(x[k + 2]), __uint_as_float(x[k + 3])), st.y, fma2(of.y, qsum2, f));
                         float y[4];
                         unpack2(y0, y[0], y[1]);
                         unpack2(y1, y[2], y[3]);
@@ -699,11 +733,10 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                         for (int z = 0; z < 4; ++z) x[k + z] = __float_as_uint(y[z]);
                     }
                     if (!all) {
-                        // visible of this row: below `end`, and from `begin` on or below `head`
-                        const int end = pos - base + 1, begin = p.c.window ? pos - p.c.window + 1 - base : 0, head = p.c.n_first - base;
+                        const int at = base + c;
+                        const uint32_t see = low_bits(pos - at + 1) & (p.c.window ? ~low_bits(pos - p.c.window + 1 - at) | low_bits(p.c.n_first - at) : 0xffffffffu);
 #pragma unroll
-                        for (int k = c; k < c + 32; ++k)
-                            if (k >= end || (k < begin && k >= head)) x[k] = 0xff800000u;
+                        for (int k = 0; k < 32; ++k) x[c + k] = see >> k & 1u ? x[c + k] : 0xff800000u;
                     }
 #pragma unroll
                     for (int k = c; k < c + 32; k += 2) {
@@ -719,7 +752,6 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                     m = m2;
                     const f2 a2 = pack2(a, a);
                     l2 = fma2(l2, a2, 0);
-                    w2 = fma2(w2, a2, 0);
                     // (the scores of this tile were computed behind the products that O holds)
 #pragma unroll
                     for (int k = 0; k < D; k += 8) {
@@ -736,21 +768,23 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                 const float from = (m == -INFINITY ? 0.0f : m) - 7.0f;
                 const f2 minus = pack2(-from, -from);
 #pragma unroll
-                for (int k = 0; k < TILE; k += 4) {
-                    const ulonglong2 iv = lds2(term + T_INV * TILE * 4 + k * 4), lw = lds2(term + T_LOW * TILE * 4 + k * 4);
-                    float y[4];
-                    unpack2(add2(pack2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), minus), y[0], y[1]);
-                    unpack2(add2(pack2(__uint_as_float(x[k + 2]), __uint_as_float(x[k + 3])), minus), y[2], y[3]);
+                for (int c = 0; c < TILE; c += KV_BLOCK) {
+                    const float inv = lds1(term + T_INV + c / KV_BLOCK * 4);
+                    f2 sum[2] = {0, 0};
 #pragma unroll
-                    for (int z = 0; z < 4; ++z) y[z] = ex2(y[z]);
-                    const f2 e0 = pack2(y[0], y[1]), e1 = pack2(y[2], y[3]);
-                    l2 = fma2(e0, iv.x, l2);
-                    w2 = fma2(e0, lw.x, w2);
-                    l2 = fma2(e1, iv.y, l2);
-                    w2 = fma2(e1, lw.y, w2);
-                    const __half2 h0 = __floats2half2_rn(y[0], y[1]), h1 = __floats2half2_rn(y[2], y[3]);
-                    x[k / 2] = *reinterpret_cast<const uint32_t *>(&h0);
-                    x[k / 2 + 1] = *reinterpret_cast<const uint32_t *>(&h1);
+                    for (int k = c; k < c + KV_BLOCK; k += 4) {
+                        float y[4];
+                        unpack2(add2(pack2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), minus), y[0], y[1]);
+                        unpack2(add2(pack2(__uint_as_float(x[k + 2]), __uint_as_float(x[k + 3])), minus), y[2], y[3]);
+#pragma unroll
+                        for (int z = 0; z < 4; ++z) y[z] = ex2(y[z]);
+                        sum[0] = add2(sum[0], pack2(y[0], y[1]));
+                        sum[1] = add2(sum[1], pack2(y[2], y[3]));
+                        const __half2 h0 = __floats2half2_rn(y[0], y[1]), h1 = __floats2half2_rn(y[2], y[3]);
+                        x[k / 2] = *reinterpret_cast<const uint32_t *>(&h0);
+                        x[k / 2 + 1] = *reinterpret_cast<const uint32_t *>(&h1);
+                    }
+                    l2 = fma2(add2(sum[0], sum[1]), pack2(inv, inv), l2);
                 }
                 st32(s_addr, x);
                 st32(s_addr + 32, x + 32);
@@ -761,10 +795,9 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
             }
             it += g.nt;
             if (!ok) break;
-            float l_a, l_b, w_a, w_b;
+            float l_a, l_b;
             unpack2(l2, l_a, l_b);
-            unpack2(w2, w_a, w_b);
-            const float l = l_a + l_b, w = w_a + w_b;
+            const float l = l_a + l_b;
             if (works) {
                 ok = __all_sync(0xffffffffu, wait(bar(B_O_FULL + t), segs & 1));
                 if (!ok) break;
@@ -774,7 +807,6 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
             // (what the walk over the tiles had no use for is worked out again instead of held in registers)
             run again = begin_run;
             const segment f = next_segment(p, again);
-            const int rr = f.row0 + t * 128 + row, tok = rr / p.group, h = f.kh * p.group + (rr - tok * p.group);
             const bool mine = t * 128 + row < f.it.rows, whole = f.t0 == 0 && f.nt == f.it.count;
             float *part = p.parts + (((int64_t)blockIdx.x * 2 + (f.t0 == 0 ? 1 : 0)) * BM + t * 128 + row) * (D + 4);
             const float inv = l == 0.0f ? 0.0f : 1.0f / l;
@@ -788,25 +820,35 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
 #pragma unroll
                     for (int z = 0; z < 32; ++z) o[z] = 0;
                 }
-                if (mine)
 #pragma unroll
                 for (int c = 0; c < 32; c += 8) {
                     const int from[8] = {0, 2, 4, 6, 1, 3, 5, 7};  // value d of a chunk is column from[d]
                     float y[8];
 #pragma unroll
-                    for (int z = 0; z < 8; ++z) y[z] = __uint_as_float(o[c + from[z]]) + w;
-                    if (whole) {
+                    for (int z = 0; z < 8; ++z) y[z] = __uint_as_float(o[c + from[z]]);
+                    if (whole) {  // through shared memory (the rows' own place), so that a warp's stores are of whole rows
                         uint32_t u[4];
 #pragma unroll
                         for (int z = 0; z < 4; ++z) {
                             const __nv_bfloat162 v = __floats2bfloat162_rn(y[2 * z] * inv, y[2 * z + 1] * inv);
                             u[z] = *reinterpret_cast<const uint32_t *>(&v);
                         }
-                        *reinterpret_cast<uint4 *>(p.c.out + (int64_t)(f.seq.start + tok) * p.c.out_stride + (int64_t)h * D + k + c) = make_uint4(u[0], u[1], u[2], u[3]);
-                    } else {
+                        const int ch = (k + c) / 8;
+                        *reinterpret_cast<uint4 *>(q_tile + (ch / 8) * (128 * 128) + row * 128 + (((ch & 7) ^ (row & 7)) * 16)) = make_uint4(u[0], u[1], u[2], u[3]);
+                    } else if (mine) {
                         reinterpret_cast<float4 *>(part + k + c)[0] = make_float4(y[0], y[1], y[2], y[3]);
                         reinterpret_cast<float4 *>(part + k + c)[1] = make_float4(y[4], y[5], y[6], y[7]);
                     }
+                }
+                __syncwarp();
+            }
+            if (whole) {
+#pragma unroll 4
+                for (int k = 0; k < D / 8; ++k) {
+                    const int w_row = (warp & 3) * 32 + k * (256 / D) + lane / (D / 8), c = lane % (D / 8), r1 = f.row0 + t * 128 + w_row, tok = r1 / p.group;
+                    const uint4 x = *reinterpret_cast<const uint4 *>(q_tile + (c / 8) * (128 * 128) + w_row * 128 + (((c & 7) ^ (w_row & 7)) * 16));
+                    if (t * 128 + w_row < f.it.rows)
+                        reinterpret_cast<uint4 *>(p.c.out + (int64_t)(f.seq.start + tok) * p.c.out_stride + (int64_t)(f.kh * p.group + r1 - tok * p.group) * D)[c] = x;
                 }
                 __syncwarp();
             }

@@ -214,6 +214,23 @@ def test_attention_against_64_bits(case):
     assert np.array_equal(got, s.attention(q, scale, window, first, q_stride=heads * dim + 16, out_pad=8))   # and the same twice
 
 
+@pytest.mark.parametrize("new", [3, 40])
+@pytest.mark.parametrize("which", [0, 1])
+def test_a_vector_that_is_no_number_reaches_the_rows_that_see_it_and_no_others(new, which):
+    s = Setup(4, 2, 128, 16, [new, new], [200, 150], seed=21, fill=0xFF).fill_with_data()
+    at = 200 - new + 2                              # position of the first sequence's row 2: rows 0 and 1 do not see it
+    s.cache.put(s.table[0, at // 16], 1, at % 16, which, np.zeros(128, np.uint8), 0x7FC03F80)
+    gone = 30                                       # and one that the window hides from everybody
+    s.cache.put(s.table[0, gone // 16], 0, gone % 16, which, np.zeros(128, np.uint8), 0x7FC03F80)
+    s.d_cache.copy_(torch.from_numpy(s.cache.bytes))
+    q, q32 = rows_of(s.rng, s.T, 512)
+    got = kv_ref.wide(s.attention(q, 0.08, window=100, first=5)).reshape(s.T, 4, 128)
+    nan = np.isnan(got)
+    assert nan[2:new, 2:].all() and not nan[:2].any() and not nan[:, :2].any() and not nan[new:].any()
+    want, bound = kv_ref.attention(s.cache, s.table, s.start, s.lengths, q32.reshape(s.T, 4, 128), 0.08, 100, 5)
+    assert (np.abs(got - want)[~nan] <= np.broadcast_to(tolerance(want, bound), got.shape)[~nan]).all()
+
+
 def test_attention_reads_no_page_that_a_window_left_behind():
     s = Setup(4, 2, 128, 16, [1, 90], [500, 700], seed=12, fill=0xFF).fill_with_data()
     q, q32 = rows_of(s.rng, s.T, 512)
