@@ -294,7 +294,7 @@ attention_split(const split_params p)
                 const float inv = __frcp_rn(vs);
                 // (positions of nobody: whatever their bytes are, NaN among them, weight 0 and finite terms.  A value vector that is
                 // no number makes the rows that see it NaN by way of their scores: a weight of 0 times NaN would reach the others)
-                const bool bad = !(fabsf(vl) + vs < INFINITY);
+                const bool bad = !(fabsf(vl) < INFINITY) || !(vs < INFINITY);
                 sh.words[warp][lane] = on ? make_float4(ks * p.scale2, bad ? NAN : fmaf(-128.0f, ks, kl) * p.scale2, lg2(vs), inv) : make_float4(0.0f, 0.0f, -INFINITY, 0.0f);
                 sh.lows[warp][lane] = on && !bad ? fmaf(vl, inv, 8.0f) : 0.0f;
             }

@@ -1,11 +1,11 @@
 // Attention over the 4-bit cache (tpq_kv_attention) for sequences that bring many rows: prompts and chunks of them.
 //
-// The mathematics is that of kv_attention.cu, the products run on tcgen05: S = Q C^T of 128 rows x 128 positions with the keys' codes
-// as BF16 128 + c (exact), O += P V with P from tensor memory.  What a row's thread does per element decides the speed here, so
-// the values are formed, in FP16: with 2^F the scale of a block of 16 positions (its largest magnitude is 2^14 .. 2^15 of it),
-// v_t 2^-F is rounded once to 11 bits of at least 2^-28 of that magnitude, and F goes into the exponent.  A row (query head x new
-// position) of S is one thread's, which finds
-//   y_t = S_t (s_t scale log2 e) + (a_t - 128 s_t) scale log2(e) sum(q) + F,   P_t = 2^(y_t - m + 7) in FP16,
+// Scores S = Q K^T of 128 rows x 128 positions and sums O += P V run on tcgen05, P from tensor memory.  What a row's thread does per
+// element decides the speed, so that here, unlike in kv_attention.cu, keys and values are formed, in FP16: with 2^F the scale of a
+// block of 16 positions' values (their largest magnitude is 2^14 .. 2^15 of it), v_t 2^-F is rounded once, to 11 bits where it is at
+// least 2^-28 of that magnitude; keys likewise with 2^Fk, and a row of Q with its own power of two, which is exact.  A row (query head
+// x new position) of S is one thread's, which finds
+//   y_t = S_t (2^Fk 2^Fq scale log2 e) + F,   P_t = 2^(y_t - m + 7) in FP16,
 //   l = sum over blocks of 2^-F sum P_t,   out = O / l.
 // m moves only when a row's maximum has grown by more than 8 (P stays below 2^15): O is rescaled in tensor memory then, which
 // after a sequence's first tiles hardly happens.
@@ -266,10 +266,10 @@ __device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.
 // values): a step of 16 is 16 rows, the next 64 values are `lead` bytes on.
 __device__ __forceinline__ uint32_t operand(uint32_t addr, uint32_t lead) { return ((addr & 0x3FFFFu) >> 4) | ((lead >> 4) << 16); }
 constexpr uint32_t OPERAND_HIGH = (1024 >> 4) | (1u << 14) | (2u << 29);  // 1024 bytes from 8 rows to the next; version; 128-byte swizzle
-// FP32 sums of 128 rows x n columns; `bf16`: both operands BF16 (else FP16); `rows_deep`: B's depth runs along its rows
-__host__ __device__ constexpr uint32_t instr(int n, bool bf16, bool rows_deep)
+// FP32 sums of 128 rows x n columns of FP16 products; `rows_deep`: B's depth runs along its rows
+__host__ __device__ constexpr uint32_t instr(int n, bool rows_deep)
 {
-    return (1u << 4) | (bf16 ? (1u << 7) | (1u << 10) : 0u) | (rows_deep ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+    return (1u << 4) | (rows_deep ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
 }
 
 __device__ __forceinline__ float ex2(float x)
@@ -307,23 +307,40 @@ __device__ __forceinline__ f2 add2(f2 a, f2 b)
     return r;
 }
 
-// (volatile: in the order of the program, or the loads of a whole tile's terms would pile up ahead of their use)
-__device__ __forceinline__ ulonglong2 lds2(uint32_t addr)
+__device__ __forceinline__ float4 lds4(uint32_t addr)
 {
-    ulonglong2 r;
-    asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(r.x), "=l"(r.y) : "r"(addr));
+    float4 r;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(r.x), "=f"(r.y), "=f"(r.z), "=f"(r.w) : "r"(addr));
     return r;
 }
-
-__device__ __forceinline__ float lds1(uint32_t addr)
+// Terms of a block of 16 positions: 2^Fk, F, 2^-F (Fk, F: exponents of its keys' and values' scales).
+constexpr uint32_t TERM_BYTES = TILE / KV_BLOCK * 16;
+// FP16 step and low of a position for a scale that puts the block's largest magnitude in [2^14, 2^15); e: that one's exponent field.
+// Called by a warp, lane <-> position lane % 16; a vector of nobody counts as zeros.
+__device__ __forceinline__ uint32_t to_scale(float step, float low, bool on, int &e)
 {
-    float r;
-    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(r) : "r"(addr));
-    return r;
+    float big = on ? fminf(fmaxf(fabsf(low), fabsf(fmaf(15.0f, step, low))), 3.4e38f) : 0.0f;
+#pragma unroll
+    for (int m = 8; m > 0; m >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, m));
+    e = big < 0x1p-60f ? 67 : (int)(__float_as_uint(big) >> 23);  // (nothing is below 2^-57 but zeros)
+    const float inv = __uint_as_float((uint32_t)(268 - e) << 23);  // 2^(141 - e)
+    const __half2 h = __floats2half2_rn(on ? step * inv : 0.0f, on ? low * inv : 0.0f);
+    return *reinterpret_cast<const uint32_t *>(&h);
 }
-// Terms of a tile: score step and score offset of every position; of every block of 16 positions the exponent F of its values' scale
-// and 2^-F.
-enum { T_STEP = 0, T_OFF = TILE * 4, T_F = 2 * TILE * 4, T_INV = T_F + TILE / KV_BLOCK * 4, TERM_BYTES = T_INV + TILE / KV_BLOCK * 4 };
+// 8 codes -> low + step * code in the order 0 4 1 5 2 6 3 7, one rounding
+__device__ __forceinline__ uint4 values(uint32_t w, uint32_t step_low)
+{
+    const __half2 sl = *reinterpret_cast<const __half2 *>(&step_low), step = __low2half2(sl), low = __high2half2(sl);
+    const uint32_t hi = w >> 8;
+    uint32_t u[4] = {and_or(w, 0x000f000fu, 0x64006400u), and_or(w, 0x00f000f0u, 0x64006400u), and_or(hi, 0x000f000fu, 0x64006400u), and_or(hi, 0x00f000f0u, 0x64006400u)};
+#pragma unroll
+    for (int z = 0; z < 4; ++z) {  // 1024 + c, 1024 + 16 c -> c, exactly
+        const __half2 c = *reinterpret_cast<const __half2 *>(&u[z]);
+        const __half2 y = __hfma2(z & 1 ? __hfma2(c, __float2half2_rn(0.0625f), __float2half2_rn(-64.0f)) : __hadd2(c, __float2half2_rn(-1024.0f)), step, low);
+        u[z] = *reinterpret_cast<const uint32_t *>(&y);
+    }
+    return make_uint4(u[0], u[1], u[2], u[3]);
+}
 
 template <int D>
 struct Smem {
@@ -497,7 +514,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
             for (int k = stage > RAW ? stage - RAW : 0; k < stage; ++k) (void)wait(bar(B_RAW_FULL + k % RAW), (k / RAW) & 1);
     } else if (warp == 1) {
         // ---------------- MMA
-        constexpr uint32_t qk_instr = instr(TILE, true, false), pv_instr = instr(D, false, true);
+        constexpr uint32_t qk_instr = instr(TILE, false), pv_instr = instr(D, true);
         int it = 0;                             // tiles so far: operand buffer it % 2
         int s_count[2] = {0, 0}, segs[2] = {0, 0};  // scores computed, segments begun, of each row tile
         while (r.more() && ok) {
@@ -589,34 +606,24 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                     if (!ok) break;
                     const uint8_t *const blk = gen + L::RAWS + st * L::RAW_BYTES + w4 * kv_block_bytes(D);
                     const int row0 = half * HALF + w4 * KV_BLOCK;  // of the tile
-                    uint32_t scaled;  // FP16 step and low of this lane's position (lane % 16) for the values' scale 2^-F
+                    uint32_t k_scaled, v_scaled;  // step and low of position lane % 16
                     {
                         const int r = lane & 15;
                         const uint32_t kw = reinterpret_cast<const uint32_t *>(blk + kv_k_words(D))[r], vw = reinterpret_cast<const uint32_t *>(blk + kv_v_words(D))[r];
                         const float ks = __uint_as_float(kw << 16), kl = __uint_as_float(kw & 0xffff0000u);
                         const float vs = __uint_as_float(vw << 16), vl = __uint_as_float(vw & 0xffff0000u);
                         const bool have = (there[st] >> w4) & 1u, on = have && g.base(j) + row0 + r < g.seq.len;
-                        float big = on ? fmaxf(fabsf(vl), fabsf(fmaf(15.0f, vs, vl))) : 0.0f;
-                        const bool bad = !(fabsf(vl) + vs < INFINITY) || !(big < INFINITY);
-                        if (bad) big = 0.0f;
-#pragma unroll
-                        for (int m = 8; m > 0; m >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, m));
-                        // 2^14 <= largest magnitude of the block * 2^-F < 2^15 (nothing is below 2^-57 but zeros)
-                        const int e = big < 0x1p-60f ? 67 : (int)(__float_as_uint(big) >> 23);
-                        const float inv = __uint_as_float((uint32_t)(268 - e) << 23);  // 2^(14 - (e - 127)) = 2^-F
-                        const __half2 h = __floats2half2_rn(on && !bad ? vs * inv : 0.0f, on && !bad ? vl * inv : 0.0f);
-                        scaled = *reinterpret_cast<const uint32_t *>(&h);
-                        if (lane < KV_BLOCK) {
-                            float *t = reinterpret_cast<float *>(term) + row0 + r;
-                            t[T_STEP / 4] = on ? ks * p.scale2 : 0.0f;
-                            // (a value vector that is no number makes the rows that see it NaN by way of their scores: a weight
-                            // of 0 times NaN would reach the others)
-                            t[T_OFF / 4] = !on ? 0.0f : bad ? NAN : fmaf(-128.0f, ks, kl) * p.scale2;
-                        }
-                        if (lane == 0) {
-                            reinterpret_cast<float *>(term + T_F)[row0 / KV_BLOCK] = have ? (float)(e - 141) : -INFINITY;
-                            reinterpret_cast<float *>(term + T_INV)[row0 / KV_BLOCK] = have ? inv : 0.0f;
-                        }
+                        // (a key or value vector that is no number makes the rows that see it NaN by way of their scores: a weight
+                        // of 0 times NaN would reach the others)
+                        const bool bad = !(fabsf(vl) < INFINITY) || !(vs < INFINITY) || !(fabsf(kl) < INFINITY) || !(ks < INFINITY);
+                        int ek, ev;
+                        k_scaled = to_scale(ks, kl, on && !bad, ek);
+                        v_scaled = to_scale(vs, vl, on && !bad, ev);
+                        if (on && bad) k_scaled = 0x7fff0000u;
+                        if (lane == 0)
+                            *reinterpret_cast<float4 *>(term + row0 / KV_BLOCK * 16) =
+                                have ? make_float4(__uint_as_float((uint32_t)(ek - 14) << 23), (float)(ev - 141), __uint_as_float((uint32_t)(268 - ev) << 23), 0.0f)
+                                     : make_float4(1.0f, -INFINITY, 0.0f, 0.0f);
                     }
 #pragma unroll
                     for (int k = 0; k < D / 64; ++k) {
@@ -627,25 +634,12 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                         const uint32_t kk[4] = {ck.x, ck.y, ck.z, ck.w}, vv[4] = {cv.x, cv.y, cv.z, cv.w};
                         const uint32_t line = (uint32_t)((q >> 1) * (TILE * 128) + (row0 + row) * 128);
                         uint8_t *const kd = gen + L::K + (it & 1) * L::TILE_BYTES + line, *const vd = gen + L::V + (it & 1) * L::TILE_BYTES + line;
-                        const uint32_t sl = __shfl_sync(0xffffffffu, scaled, row);
-                        const __half2 step_low = *reinterpret_cast<const __half2 *>(&sl), step = __low2half2(step_low), low = __high2half2(step_low);
-                        const __half2 sixteenth = __float2half2_rn(0.0625f), off = __float2half2_rn(-64.0f), off0 = __float2half2_rn(-1024.0f);
+                        const uint32_t k_sl = __shfl_sync(0xffffffffu, k_scaled, row), v_sl = __shfl_sync(0xffffffffu, v_scaled, row);
 #pragma unroll
                         for (int jw = 0; jw < 4; ++jw) {
                             const uint32_t at = (uint32_t)((((q & 1) * 4 + jw) ^ (row & 7)) * 16);
-                            const uint32_t u = kk[jw], v = vv[jw];
-                            *reinterpret_cast<uint4 *>(kd + at) =
-                                make_uint4(and_or(u, 0x000f000fu, 0x43004300u), and_or(u >> 4, 0x000f000fu, 0x43004300u),
-                                           and_or(u >> 8, 0x000f000fu, 0x43004300u), and_or(u >> 12, 0x000f000fu, 0x43004300u));
-                            uint32_t e[4] = {and_or(v, 0x000f000fu, 0x64006400u), and_or(v, 0x00f000f0u, 0x64006400u),
-                                             and_or(v >> 8, 0x000f000fu, 0x64006400u), and_or(v >> 8, 0x00f000f0u, 0x64006400u)};
-#pragma unroll
-                            for (int z = 0; z < 4; ++z) {
-                                const __half2 c = *reinterpret_cast<const __half2 *>(&e[z]);
-                                const __half2 y = __hfma2(z & 1 ? __hfma2(c, sixteenth, off) : __hadd2(c, off0), step, low);  // (the codes: exact)
-                                e[z] = *reinterpret_cast<const uint32_t *>(&y);
-                            }
-                            *reinterpret_cast<uint4 *>(vd + at) = make_uint4(e[0], e[1], e[2], e[3]);
+                            *reinterpret_cast<uint4 *>(kd + at) = values(kk[jw], k_sl);
+                            *reinterpret_cast<uint4 *>(vd + at) = values(vv[jw], v_sl);
                         }
                     }
                     __syncwarp();
@@ -666,41 +660,60 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
         int it = 0, s_count = 0, segs = 0;
         if (tid == 256) p.headers[blockIdx.x] = make_int4(0, 0, 0, 0);
         while (r.more() && ok) {
-            const run begin_run = r;
             const segment g = next_segment(p, r);
             const reach re = reach_of(p, g, t);
             bool works = false;
             for (int j = 0; j < g.nt && !works; ++j) works = sees(p, re, g.base(j));
             int pos = -1;  // of this thread's row
-            float m = -INFINITY, qsum = 0.0f;
+            float m = -INFINITY, row_scale = 0.0f;
             f2 l2 = 0;
             bool any = false;
             uint8_t *const q_tile = gen + L::Q + t * L::TILE_BYTES;
             if (works) {
                 const int rr = g.row0 + t * 128 + row;
                 if (t * 128 + row < g.it.rows) pos = g.seq.len - g.seq.n + rr / p.group;
-                // the warp's 32 rows as an operand, D/8 lanes a row; 8 values of a chunk in the codes' order 0 4 1 5 2 6 3 7
+                // the warp's 32 rows as they are, D/8 lanes a row
 #pragma unroll
                 for (int k = 0; k < D / 8; ++k) {
                     const int w_row = (warp & 3) * 32 + k * (256 / D) + lane / (D / 8), c = lane % (D / 8), r1 = g.row0 + t * 128 + w_row, tok = r1 / p.group;
                     uint4 x = make_uint4(0, 0, 0, 0);
                     if (t * 128 + w_row < g.it.rows)
                         x = reinterpret_cast<const uint4 *>(p.c.q.p + (int64_t)(g.seq.start + tok) * p.c.q.stride + (int64_t)(g.kh * p.group + r1 - tok * p.group) * D)[c];
-                    *reinterpret_cast<uint4 *>(q_tile + (c / 8) * (128 * 128) + w_row * 128 + (((c & 7) ^ (w_row & 7)) * 16)) =
-                        make_uint4(__byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632), __byte_perm(x.y, x.w, 0x5410), __byte_perm(x.y, x.w, 0x7632));
+                    *reinterpret_cast<uint4 *>(q_tile + (c / 8) * (128 * 128) + w_row * 128 + (((c & 7) ^ (w_row & 7)) * 16)) = x;
+                }
+                __syncwarp();
+                // a thread's own row in FP16, scaled so that its largest magnitude is in [2^14, 2^15) (BF16's 8 bits stay exact down to
+                // 2^-31 of that), in the codes' order; a negative scale goes into the sign
+                auto chunk = [&](int c) { return reinterpret_cast<uint4 *>(q_tile + (c / 8) * (128 * 128) + row * 128 + (((c & 7) ^ (row & 7)) * 16)); };
+                uint32_t big = 0;  // magnitudes as integers, in both halves
+#pragma unroll
+                for (int c = 0; c < D / 8; ++c) {
+                    const uint4 x = *chunk(c);
+                    big = __vmaxu2(__vmaxu2(__vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu)), big);
+                }
+                big = max(big & 0xffffu, big >> 16);
+                int e = (int)(big >> 7);
+                const bool bad = e == 255;  // infinite or NaN: so is the row's answer
+                if (e < 16 || bad) e = 16;
+                const float up = __uint_as_float((uint32_t)(268 - e) << 23);
+                row_scale = bad ? NAN : fabsf(p.scale2) * __uint_as_float((uint32_t)(e - 14) << 23);
+                const uint32_t sign = p.scale2 < 0.0f ? 0x80008000u : 0u;
+#pragma unroll
+                for (int c = 0; c < D / 8; ++c) {
+                    const uint4 x = *chunk(c);
+                    const uint32_t pairs[4] = {__byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632), __byte_perm(x.y, x.w, 0x5410), __byte_perm(x.y, x.w, 0x7632)};
+                    uint32_t u[4];
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) {
+                        const __half2 h = __floats2half2_rn(__uint_as_float(pairs[z] << 16) * up, __uint_as_float(pairs[z] & 0xffff0000u) * up);
+                        u[z] = (bad ? 0u : *reinterpret_cast<const uint32_t *>(&h)) ^ sign;
+                    }
+                    *chunk(c) = make_uint4(u[0], u[1], u[2], u[3]);
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(B_Q_FULL + t));
-#pragma unroll
-                for (int c = 0; c < D / 8; ++c) {
-                    const uint4 x = *reinterpret_cast<const uint4 *>(q_tile + (c / 8) * (128 * 128) + row * 128 + (((c & 7) ^ (row & 7)) * 16));
-                    const uint32_t u[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                    for (int z = 0; z < 4; ++z) qsum += __uint_as_float(u[z] << 16) + __uint_as_float(u[z] & 0xffff0000u);
-                }
             }
-            const f2 qsum2 = pack2(qsum, qsum);
             for (int j = 0; j < g.nt; ++j) {
                 const int base = g.base(j), i = it + j;
                 if (!sees(p, re, base)) continue;
@@ -711,38 +724,31 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                 fence_after();
                 const uint32_t term = smem + L::TERM + (i % 3) * TERM_BYTES;
                 uint32_t x[TILE];
-                ld32(s_addr, x);
+#pragma unroll
+                for (int c = 0; c < TILE; c += 32) ld32(s_addr + c, x + c);
                 float top[2] = {-INFINITY, -INFINITY};
                 const bool all = sees_all(p, re, base);
+                ld_wait();
+                if (!all) {  // scores of positions that this row does not see; the others' scales here instead of below
 #pragma unroll
-                for (int c = 0; c < TILE; c += 32) {
-                    ld_wait();
-                    if (c + 32 < TILE) ld32(s_addr + c + 32, x + c + 32);
-                    const float fa = lds1(term + T_F + c / KV_BLOCK * 4), fb = lds1(term + T_F + c / KV_BLOCK * 4 + 4);
-                    const f2 f2a = pack2(fa, fa), f2b = pack2(fb, fb);
-#pragma unroll
-                    for (int k = c; k < c + 32; k += 4) {
-                        const ulonglong2 st = lds2(term + T_STEP + k * 4), of = lds2(term + T_OFF + k * 4);
-                        const f2 f = k - c < KV_BLOCK ? f2a : f2b;
-                        const f2 y0 = fma2(pack2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), st.x, fma2(of.x, qsum2, f));
-                        const f2 y1 = fma2(pack2(__uint_as_float(x[k + 2]), __uint_as_float(x[k + 3])), st.y, fma2(of.y, qsum2, f));
-                        float y[4];
-                        unpack2(y0, y[0], y[1]);
-                        unpack2(y1, y[2], y[3]);
-#pragma unroll
-                        for (int z = 0; z < 4; ++z) x[k + z] = __float_as_uint(y[z]);
-                    }
-                    if (!all) {
+                    for (int c = 0; c < TILE; c += KV_BLOCK) {
                         const int at = base + c;
                         const uint32_t see = low_bits(pos - at + 1) & (p.c.window ? ~low_bits(pos - p.c.window + 1 - at) | low_bits(p.c.n_first - at) : 0xffffffffu);
+                        const float4 tm = lds4(term + c / KV_BLOCK * 16);
+                        const float sc = tm.x * row_scale;
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) x[c + k] = see >> k & 1u ? x[c + k] : 0xff800000u;
+                        for (int k = 0; k < KV_BLOCK; ++k) x[c + k] = see >> k & 1u ? __float_as_uint(fmaf(__uint_as_float(x[c + k]), sc, tm.y)) : 0xff800000u;
                     }
+                }
 #pragma unroll
-                    for (int k = c; k < c + 32; k += 2) {
-                        top[0] = fmaxf(top[0], __uint_as_float(x[k]));
-                        top[1] = fmaxf(top[1], __uint_as_float(x[k + 1]));
-                    }
+                for (int c = 0; c < TILE; c += KV_BLOCK) {
+                    const float4 tm = lds4(term + c / KV_BLOCK * 16);
+                    float y[4];
+#pragma unroll
+                    for (int z = 0; z < 4; ++z)
+                        y[z] = fmaxf(fmaxf(__uint_as_float(x[c + z]), __uint_as_float(x[c + 4 + z])), fmaxf(__uint_as_float(x[c + 8 + z]), __uint_as_float(x[c + 12 + z])));
+                    const float big = fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]));
+                    top[c / KV_BLOCK & 1] = fmaxf(top[c / KV_BLOCK & 1], all ? fmaf(big, tm.x * row_scale, tm.y) : big);
                 }
                 const float tile_top = fmaxf(top[0], top[1]);
                 if (!any) {
@@ -766,16 +772,17 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                 }
                 any = true;
                 const float from = (m == -INFINITY ? 0.0f : m) - 7.0f;
-                const f2 minus = pack2(-from, -from);
 #pragma unroll
                 for (int c = 0; c < TILE; c += KV_BLOCK) {
-                    const float inv = lds1(term + T_INV + c / KV_BLOCK * 4);
+                    const float4 tm = lds4(term + c / KV_BLOCK * 16);
+                    const float sc = all ? tm.x * row_scale : 1.0f, of = (all ? tm.y : 0.0f) - from;
+                    const f2 sc2 = pack2(sc, sc), of2 = pack2(of, of);
                     f2 sum[2] = {0, 0};
 #pragma unroll
                     for (int k = c; k < c + KV_BLOCK; k += 4) {
                         float y[4];
-                        unpack2(add2(pack2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), minus), y[0], y[1]);
-                        unpack2(add2(pack2(__uint_as_float(x[k + 2]), __uint_as_float(x[k + 3])), minus), y[2], y[3]);
+                        unpack2(fma2(pack2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), sc2, of2), y[0], y[1]);
+                        unpack2(fma2(pack2(__uint_as_float(x[k + 2]), __uint_as_float(x[k + 3])), sc2, of2), y[2], y[3]);
 #pragma unroll
                         for (int z = 0; z < 4; ++z) y[z] = ex2(y[z]);
                         sum[0] = add2(sum[0], pack2(y[0], y[1]));
@@ -784,7 +791,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                         x[k / 2] = *reinterpret_cast<const uint32_t *>(&h0);
                         x[k / 2 + 1] = *reinterpret_cast<const uint32_t *>(&h1);
                     }
-                    l2 = fma2(add2(sum[0], sum[1]), pack2(inv, inv), l2);
+                    l2 = fma2(add2(sum[0], sum[1]), pack2(tm.z, tm.z), l2);
                 }
                 st32(s_addr, x);
                 st32(s_addr + 32, x + 32);
@@ -805,7 +812,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                 fence_after();
             }
             // (what the walk over the tiles had no use for is worked out again instead of held in registers)
-            run again = begin_run;
+            run again{r.unit - g.nt, r.end, r.item};
             const segment f = next_segment(p, again);
             const bool mine = t * 128 + row < f.it.rows, whole = f.t0 == 0 && f.nt == f.it.count;
             float *part = p.parts + (((int64_t)blockIdx.x * 2 + (f.t0 == 0 ? 1 : 0)) * BM + t * 128 + row) * (D + 4);
