@@ -15,7 +15,7 @@
 //   ... P_A E(j), Q_A C(j+1), P_B E(j), Q_B C(j+1), P_A E(j+1), ...
 //   warp 0       copies: blocks of 16 positions as they lie in the pages, 64 positions a stage
 //   warp 1       tensor memory, MMA issue (one elected lane)
-//   warps 4-7    unpack: codes to the two operands' tiles (128-byte swizzle), words to the terms of a position
+//   warps 2-7    unpack: codes to the two operands' tiles (128-byte swizzle), words to the terms of a block
 //   warps 8-15   softmax: a thread per row; the rows themselves into shared memory at the start, the output at the end
 // Unpacking a tile costs as much however many rows use it: 256 rows, which the query heads of a key head share.
 //
@@ -31,7 +31,8 @@
 namespace {
 
 constexpr int BM = 256, TILE = 128, HALF = 64;  // rows of a block, positions of a tile, of a copy stage
-constexpr int RAW = 3;                          // copy stages
+constexpr int RAW = 4;                          // copy stages
+constexpr int UNPACKERS = 6;                    // warps
 constexpr int THREADS = 512;
 constexpr int PLAN_THREADS = 1024;
 
@@ -53,7 +54,7 @@ struct prompt_params {
     int4 *headers;  // as in attention_split
     float *parts;   // [blocks][2][BM][D + 4]
     float scale2;
-    int group, few;  // sequences of up to `few` rows are attention_split's
+    int group, group_inv, few;  // group_inv: 2^20 / group rounded up; sequences of up to `few` rows are attention_split's
 };
 
 // Rows of an item and the tiles they see: [0, first) and [from, end).
@@ -251,14 +252,6 @@ __device__ __forceinline__ void st32(uint32_t addr, const uint32_t *r)
         ::W8(r, 0), W8(r, 8), W8(r, 16), W8(r, 24), "r"(addr)
         : "memory");
 }
-__device__ __forceinline__ void ld8(uint32_t addr, uint32_t *r)
-{
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];" : R8(r, 0) : "r"(addr) : "memory");
-}
-__device__ __forceinline__ void st8(uint32_t addr, const uint32_t *r)
-{
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::W8(r, 0), "r"(addr) : "memory");
-}
 __device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // Operands of 128-byte rows with the 128-byte swizzle, 8-row groups of 1024 bytes.  Depth along the row (Q, keys): a step of 16 is 32
@@ -349,10 +342,12 @@ struct Smem {
     static constexpr uint32_t RAW_BYTES = HALF / KV_BLOCK * kv_block_bytes(D);
     static constexpr uint32_t TERM = RAWS + RAW * RAW_BYTES;
     static constexpr uint32_t BARS = TERM + 3 * TERM_BYTES;
-    static constexpr uint32_t BYTES = BARS + 256 + 1024;  // (1024: slack for the alignment)
+    static constexpr uint32_t BYTES = BARS + 256;
+    static_assert(BYTES <= 227 * 1024, "shared memory of a block");
 };
 // barriers, 8 bytes each from BARS
-enum { B_RAW_FULL = 0, B_RAW_EMPTY = 3, B_KV_FULL = 6, B_K_EMPTY = 8, B_V_EMPTY = 10, B_Q_FULL = 12, B_S_FULL = 14, B_P_FULL = 16, B_O_FULL = 18, B_O_EMPTY = 20, B_COUNT = 22 };
+enum { B_RAW_FULL = 0, B_RAW_EMPTY = B_RAW_FULL + RAW, B_K_FULL = B_RAW_EMPTY + RAW, B_V_FULL = B_K_FULL + 2, B_K_EMPTY = B_V_FULL + 2, B_V_EMPTY = B_K_EMPTY + 2,
+       B_Q_FULL = B_V_EMPTY + 2, B_S_FULL = B_Q_FULL + 2, B_P_FULL = B_S_FULL + 2, B_O_FULL = B_P_FULL + 2, B_O_EMPTY = B_O_FULL + 2, B_COUNT = B_O_EMPTY + 2 };
 
 // A block's run of tiles, one (item, key head) after the other.
 struct run {
@@ -406,13 +401,98 @@ __device__ __forceinline__ bool sees_all(const prompt_params &p, const reach &r,
     return base + TILE - 1 <= r.lo && (p.c.window == 0 || base > r.hi - p.c.window || base + TILE <= p.c.n_first);
 }
 
+// A warp that unpacks (`which` of UNPACKERS).  A tile is sixteen jobs, the keys of its eight blocks and then their values; job x of
+// tile i is warp (16 i + x) % 6's, which gives every warp a part of every copy stage and of every operand tile: none misses a barrier's phase.
+template <int D>
+__device__ __forceinline__ bool unpack(const prompt_params &p, run r, uint8_t *gen, uint32_t bars, const uint32_t *there, int which, int lane)
+{
+    using L = Smem<D>;
+    constexpr int BLOCKS = TILE / KV_BLOCK, PER_STAGE = HALF / KV_BLOCK;
+    static_assert(2 * BLOCKS == 16 && UNPACKERS == 6 && PER_STAGE == 4, "see above");
+    int it = 0, next = which;  // next: index of this warp's next job among the tile's
+    while (r.more()) {
+        const segment g = next_segment(p, r);
+        for (int j = 0; j < g.nt; ++j, ++it) {
+            for (; next < 2 * BLOCKS; next += UNPACKERS) {
+                const bool values_job = next >= BLOCKS;
+                const int block = next & (BLOCKS - 1), stage = 2 * it + block / PER_STAGE, st = stage % RAW, at = block % PER_STAGE, row0 = block * KV_BLOCK;
+                if (!__all_sync(0xffffffffu, wait(bars + 8 * (B_RAW_FULL + st), (stage / RAW) & 1))) return false;
+                if (it >= 2 && !__all_sync(0xffffffffu, wait(bars + 8 * ((values_job ? B_V_EMPTY : B_K_EMPTY) + (it & 1)), ((it >> 1) - 1) & 1))) return false;
+                const uint8_t *const blk = gen + L::RAWS + st * L::RAW_BYTES + at * kv_block_bytes(D);
+                const bool have = (there[st] >> at) & 1u;
+                uint32_t scaled;  // step and low of position lane % 16
+                {
+                    const int n = lane & 15;
+                    const bool on = have && g.base(j) + row0 + n < g.seq.len;
+                    const uint32_t vw = reinterpret_cast<const uint32_t *>(blk + kv_v_words(D))[n];
+                    const float vs = __uint_as_float(vw << 16), vl = __uint_as_float(vw & 0xffff0000u);
+                    bool bad = !(fabsf(vl) < INFINITY) || !(vs < INFINITY);
+                    int ev;
+                    scaled = to_scale(vs, vl, on && !bad, ev);
+                    if (!values_job) {
+                        const uint32_t kw = reinterpret_cast<const uint32_t *>(blk + kv_k_words(D))[n];
+                        const float ks = __uint_as_float(kw << 16), kl = __uint_as_float(kw & 0xffff0000u);
+                        bad = bad || !(fabsf(kl) < INFINITY) || !(ks < INFINITY);
+                        int ek;
+                        scaled = to_scale(ks, kl, on && !bad, ek);
+                        // (a key or value vector that is no number makes the rows that see it NaN by way of their scores: a weight of
+                        // 0 times NaN would reach the others)
+                        if (on && bad) scaled = 0x7fff0000u;
+                        if (lane == 0)
+                            *reinterpret_cast<float4 *>(gen + L::TERM + (it % 3) * TERM_BYTES + block * 16) =
+                                have ? make_float4(__uint_as_float((uint32_t)(ek - 14) << 23), (float)(ev - 141), __uint_as_float((uint32_t)(268 - ev) << 23), 0.0f)
+                                     : make_float4(1.0f, -INFINITY, 0.0f, 0.0f);
+                    }
+                }
+                const uint8_t *const codes = blk + (values_job ? kv_v_codes(D) : 0);
+                uint8_t *const tile = gen + (values_job ? L::V : L::K) + (it & 1) * L::TILE_BYTES;
+                uint4 c[D / 64];
+                uint32_t sl[D / 64];
+#pragma unroll
+                for (int k = 0; k < D / 64; ++k) {
+                    // 16 bytes (32 codes) of position `row`; eight lanes read and write 128 different bytes of banks
+                    const int row = D == 128 ? (lane & 7) + 8 * k : lane & 15, q = D == 128 ? ((lane >> 3) + (row >> 1)) & 3 : lane >> 4;
+                    c[k] = *reinterpret_cast<const uint4 *>(codes + row * (D / 2) + 16 * q);
+                    sl[k] = __shfl_sync(0xffffffffu, scaled, row);
+                }
+#pragma unroll
+                for (int k = 0; k < D / 64; ++k) {
+                    const int row = D == 128 ? (lane & 7) + 8 * k : lane & 15, q = D == 128 ? ((lane >> 3) + (row >> 1)) & 3 : lane >> 4;
+                    uint8_t *const line = tile + (q >> 1) * (TILE * 128) + (row0 + row) * 128;
+                    const uint32_t w[4] = {c[k].x, c[k].y, c[k].z, c[k].w};
+#pragma unroll
+                    for (int jw = 0; jw < 4; ++jw) *reinterpret_cast<uint4 *>(line + ((((q & 1) * 4 + jw) ^ (row & 7)) * 16)) = values(w[jw], sl[k]);
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(bars + 8 * ((values_job ? B_V_FULL : B_K_FULL) + (it & 1)));
+                    mbar_arrive(bars + 8 * (B_RAW_EMPTY + st));
+                }
+            }
+            next -= 2 * BLOCKS;  // (16 = 2 x 6 + 4)
+        }
+    }
+    return true;
+}
+
+// Which of the 32 positions from `at` on a row at `pos` sees.
+__device__ __forceinline__ uint32_t visible(const prompt_params &p, int pos, int at)
+{
+    return low_bits(pos - at + 1) & (p.c.window ? ~low_bits(pos - p.c.window + 1 - at) | low_bits(p.c.n_first - at) : 0xffffffffu);
+}
+
 template <int D>
 __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_params p)
 {
     using L = Smem<D>;
-    extern __shared__ uint8_t raw_smem[];
-    const uint32_t smem = (smem_u32(raw_smem) + 1023u) & ~1023u;
-    uint8_t *const gen = raw_smem + (smem - smem_u32(raw_smem));
+    extern __shared__ __align__(1024) uint8_t raw_smem[];
+    const uint32_t smem = smem_u32(raw_smem);
+    uint8_t *const gen = raw_smem;
+    if (smem & 1023u) {  // (dynamic shared memory begins on such a boundary where there is no other; the swizzle needs it)
+        if (threadIdx.x == 0) atomicExch(p.b.status, (int)TPQ_ERR_ALIGN);
+        return;
+    }
     const uint32_t bars = smem + L::BARS;
     auto bar = [&](int i) { return bars + 8u * i; };
     uint32_t *const there = reinterpret_cast<uint32_t *>(gen + L::BARS + 8 * B_COUNT);  // [RAW]: blocks of a copy stage that were copied
@@ -423,10 +503,11 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
     if (tid == 0) {
         for (int i = 0; i < RAW; ++i) {
             mbar_init(bar(B_RAW_FULL + i), 1);
-            mbar_init(bar(B_RAW_EMPTY + i), 4);
+            mbar_init(bar(B_RAW_EMPTY + i), 8);  // the keys and the values of four blocks
         }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(bar(B_KV_FULL + i), 4);
+            mbar_init(bar(B_K_FULL + i), TILE / KV_BLOCK);
+            mbar_init(bar(B_V_FULL + i), TILE / KV_BLOCK);
             mbar_init(bar(B_K_EMPTY + i), 1);
             mbar_init(bar(B_V_EMPTY + i), 1);
             mbar_init(bar(B_Q_FULL + i), 4);
@@ -469,9 +550,6 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
     }
     run r = r0;
 
-    // Registers: 128 a thread at launch; 96 + 64 + 2 x 176 are the four warpgroups' 512.
-    if (warp < 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
     if (warp == 0) {
         // ---------------- copies
         int stage = 0;  // copy stages so far
@@ -516,149 +594,85 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
         // ---------------- MMA
         constexpr uint32_t qk_instr = instr(TILE, false), pv_instr = instr(D, true);
         int it = 0;                             // tiles so far: operand buffer it % 2
-        int s_count[2] = {0, 0}, segs[2] = {0, 0};  // scores computed, segments begun, of each row tile
+        // a bit for each row tile: phase of its scores' barrier, of its rows' and sums' barriers, whether it has had sums before
+        uint32_t p_phase = 0, q_phase = 0, begun = 0;
         while (r.more() && ok) {
             const segment g = next_segment(p, r);
-            const reach re[2] = {reach_of(p, g, 0), reach_of(p, g, 1)};
-            int last[2] = {-1, -1};
-            bool any[2] = {false, false};
-            for (int t = 0; t < 2; ++t)
-                for (int j = g.nt - 1; j >= 0 && last[t] < 0; --j)
-                    if (sees(p, re[t], g.base(j))) last[t] = j;
-            auto scores = [&](int t, int j) {  // Q_t C(j)
-                if (!ok || !sees(p, re[t], g.base(j))) return;
-                if (elect()) {
-                    const uint32_t a = operand(smem + L::Q + t * L::TILE_BYTES, 16), k = operand(smem + L::K + ((it + j) & 1) * L::TILE_BYTES, 16);
-#pragma unroll
-                    for (int x = 0; x < D / 16; ++x) {
-                        const uint32_t at = (x / 4) * (128 * 128 >> 4) + 2 * (x % 4);
-                        mma_ss(tmem + t * TILE, a + at, k + at, OPERAND_HIGH, qk_instr, x != 0);
-                    }
-                    commit(bar(B_S_FULL + t));
-                }
-                __syncwarp();
-            };
-            for (int t = 0; t < 2 && ok; ++t)
-                if (last[t] >= 0) ok = __all_sync(0xffffffffu, wait(bar(B_Q_FULL + t), segs[t] & 1));
-            if (ok) ok = __all_sync(0xffffffffu, wait(bar(B_KV_FULL + (it & 1)), (it >> 1) & 1));
-            if (!ok) break;
-            fence_after();
-            scores(0, 0);
-            scores(1, 0);
-            if (elect()) commit(bar(B_K_EMPTY + (it & 1)));
-            __syncwarp();
-            for (int j = 0; j < g.nt && ok; ++j) {
+            const reach re_a = reach_of(p, g, 0), re_b = reach_of(p, g, 1);
+            int last_a = -1, last_b = -1;
+            for (int j = g.nt - 1; j >= 0 && last_a < 0; --j)
+                if (sees(p, re_a, g.base(j))) last_a = j;
+            for (int j = g.nt - 1; j >= 0 && last_b < 0; --j)
+                if (sees(p, re_b, g.base(j))) last_b = j;
+            uint32_t any = 0;  // row tiles with sums of this segment
+            // step j: P_t V(j) for both row tiles, each followed by Q_t K(j + 1); step -1 has the first scores only
+            for (int j = -1; j < g.nt && ok; ++j) {
                 const int i = it + j;
+                const bool more = j + 1 < g.nt;
+                if (j >= 0) ok = __all_sync(0xffffffffu, wait(bar(B_V_FULL + (i & 1)), (i >> 1) & 1));
+#pragma unroll 1
                 for (int t = 0; t < 2 && ok; ++t) {
-                    if (sees(p, re[t], g.base(j))) {
-                        if (!any[t] && segs[t] > 0) ok = __all_sync(0xffffffffu, wait(bar(B_O_EMPTY + t), (segs[t] - 1) & 1));
-                        if (ok) ok = __all_sync(0xffffffffu, wait(bar(B_P_FULL + t), s_count[t] & 1));
+                    if (j >= 0 && sees(p, t ? re_b : re_a, g.base(j))) {
+                        if (!(any >> t & 1) && (begun >> t & 1)) ok = __all_sync(0xffffffffu, wait(bar(B_O_EMPTY + t), (q_phase >> t & 1) ^ 1));
+                        if (ok) ok = __all_sync(0xffffffffu, wait(bar(B_P_FULL + t), p_phase >> t & 1));
                         if (!ok) break;
                         fence_after();
                         if (elect()) {
                             const uint32_t v = operand(smem + L::V + (i & 1) * L::TILE_BYTES, TILE * 128);
 #pragma unroll
                             for (int x = 0; x < TILE / 16; ++x)
-                                mma_ts(tmem + 256 + t * 128, tmem + t * TILE + 8 * x, v + x * (2048 >> 4), OPERAND_HIGH, pv_instr, any[t] || x != 0);
-                            if (j == last[t]) commit(bar(B_O_FULL + t));
+                                mma_ts(tmem + 256 + t * 128, tmem + t * TILE + 8 * x, v + x * (2048 >> 4), OPERAND_HIGH, pv_instr, (any >> t & 1) | (x != 0));
+                            if (j == (t ? last_b : last_a)) commit(bar(B_O_FULL + t));
                         }
                         __syncwarp();
-                        any[t] = true;
-                        ++s_count[t];
+                        any |= 1u << t;
+                        p_phase ^= 1u << t;
                     }
-                    if (j + 1 < g.nt) {
-                        if (t == 0) {
-                            ok = __all_sync(0xffffffffu, wait(bar(B_KV_FULL + ((i + 1) & 1)), ((i + 1) >> 1) & 1));
-                            fence_after();
+                    if (more) {
+                        if (j < 0 && (t ? last_b : last_a) >= 0) ok = __all_sync(0xffffffffu, wait(bar(B_Q_FULL + t), q_phase >> t & 1));
+                        if (t == 0 && ok) ok = __all_sync(0xffffffffu, wait(bar(B_K_FULL + ((i + 1) & 1)), ((i + 1) >> 1) & 1));
+                        if (!ok) break;
+                        fence_after();
+                        if (sees(p, t ? re_b : re_a, g.base(j + 1))) {
+                            if (elect()) {
+                                const uint32_t a = operand(smem + L::Q + t * L::TILE_BYTES, 16), k = operand(smem + L::K + ((i + 1) & 1) * L::TILE_BYTES, 16);
+#pragma unroll
+                                for (int x = 0; x < D / 16; ++x) {
+                                    const uint32_t at = (x / 4) * (128 * 128 >> 4) + 2 * (x % 4);
+                                    mma_ss(tmem + t * TILE, a + at, k + at, OPERAND_HIGH, qk_instr, x != 0);
+                                }
+                                commit(bar(B_S_FULL + t));
+                            }
+                            __syncwarp();
                         }
-                        scores(t, j + 1);
                     }
                 }
                 if (!ok) break;
                 if (elect()) {
-                    commit(bar(B_V_EMPTY + (i & 1)));
-                    if (j + 1 < g.nt) commit(bar(B_K_EMPTY + ((i + 1) & 1)));
+                    if (j >= 0) commit(bar(B_V_EMPTY + (i & 1)));
+                    if (more) commit(bar(B_K_EMPTY + ((i + 1) & 1)));
                 }
                 __syncwarp();
             }
             it += g.nt;
-            for (int t = 0; t < 2; ++t)
-                if (last[t] >= 0) ++segs[t];
+            begun |= any;
+            q_phase ^= any;
         }
-    }
     } else if (warp < 8) {
-        // ---------------- unpack: warp w - 4 takes one block of 16 positions of each copy stage
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-        const int w4 = warp - 4;
-        int stage = 0, it = 0;
-        while (r.more() && ok) {
-            const segment g = next_segment(p, r);
-            for (int j = 0; j < g.nt && ok; ++j, ++it) {
-                if (it >= 2) {
-                    ok = __all_sync(0xffffffffu, wait(bar(B_K_EMPTY + (it & 1)), ((it >> 1) - 1) & 1)) &&
-                         __all_sync(0xffffffffu, wait(bar(B_V_EMPTY + (it & 1)), ((it >> 1) - 1) & 1));
-                    if (!ok) break;
-                }
-                uint8_t *const term = gen + L::TERM + (it % 3) * TERM_BYTES;
-                for (int half = 0; half < 2; ++half, ++stage) {
-                    const int st = stage % RAW;
-                    ok = __all_sync(0xffffffffu, wait(bar(B_RAW_FULL + st), (stage / RAW) & 1));
-                    if (!ok) break;
-                    const uint8_t *const blk = gen + L::RAWS + st * L::RAW_BYTES + w4 * kv_block_bytes(D);
-                    const int row0 = half * HALF + w4 * KV_BLOCK;  // of the tile
-                    uint32_t k_scaled, v_scaled;  // step and low of position lane % 16
-                    {
-                        const int r = lane & 15;
-                        const uint32_t kw = reinterpret_cast<const uint32_t *>(blk + kv_k_words(D))[r], vw = reinterpret_cast<const uint32_t *>(blk + kv_v_words(D))[r];
-                        const float ks = __uint_as_float(kw << 16), kl = __uint_as_float(kw & 0xffff0000u);
-                        const float vs = __uint_as_float(vw << 16), vl = __uint_as_float(vw & 0xffff0000u);
-                        const bool have = (there[st] >> w4) & 1u, on = have && g.base(j) + row0 + r < g.seq.len;
-                        // (a key or value vector that is no number makes the rows that see it NaN by way of their scores: a weight
-                        // of 0 times NaN would reach the others)
-                        const bool bad = !(fabsf(vl) < INFINITY) || !(vs < INFINITY) || !(fabsf(kl) < INFINITY) || !(ks < INFINITY);
-                        int ek, ev;
-                        k_scaled = to_scale(ks, kl, on && !bad, ek);
-                        v_scaled = to_scale(vs, vl, on && !bad, ev);
-                        if (on && bad) k_scaled = 0x7fff0000u;
-                        if (lane == 0)
-                            *reinterpret_cast<float4 *>(term + row0 / KV_BLOCK * 16) =
-                                have ? make_float4(__uint_as_float((uint32_t)(ek - 14) << 23), (float)(ev - 141), __uint_as_float((uint32_t)(268 - ev) << 23), 0.0f)
-                                     : make_float4(1.0f, -INFINITY, 0.0f, 0.0f);
-                    }
-#pragma unroll
-                    for (int k = 0; k < D / 64; ++k) {
-                        // 16 bytes (32 codes) of position `row`; eight lanes read and write 128 different bytes of banks
-                        const int row = D == 128 ? (lane & 7) + 8 * k : lane & 15, q = D == 128 ? ((lane >> 3) + (row >> 1)) & 3 : lane >> 4;
-                        const uint4 ck = *reinterpret_cast<const uint4 *>(blk + row * (D / 2) + 16 * q);
-                        const uint4 cv = *reinterpret_cast<const uint4 *>(blk + kv_v_codes(D) + row * (D / 2) + 16 * q);
-                        const uint32_t kk[4] = {ck.x, ck.y, ck.z, ck.w}, vv[4] = {cv.x, cv.y, cv.z, cv.w};
-                        const uint32_t line = (uint32_t)((q >> 1) * (TILE * 128) + (row0 + row) * 128);
-                        uint8_t *const kd = gen + L::K + (it & 1) * L::TILE_BYTES + line, *const vd = gen + L::V + (it & 1) * L::TILE_BYTES + line;
-                        const uint32_t k_sl = __shfl_sync(0xffffffffu, k_scaled, row), v_sl = __shfl_sync(0xffffffffu, v_scaled, row);
-#pragma unroll
-                        for (int jw = 0; jw < 4; ++jw) {
-                            const uint32_t at = (uint32_t)((((q & 1) * 4 + jw) ^ (row & 7)) * 16);
-                            *reinterpret_cast<uint4 *>(kd + at) = values(kk[jw], k_sl);
-                            *reinterpret_cast<uint4 *>(vd + at) = values(vv[jw], v_sl);
-                        }
-                    }
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(bar(B_RAW_EMPTY + st));
-                }
-                if (!ok) break;
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(B_KV_FULL + (it & 1)));
-            }
-        }
+        ok = unpack<D>(p, r, gen, bars, there, warp - 2, lane);
     } else {
         // ---------------- softmax: thread <-> row `row` of row tile t
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
         const int t = (warp - 8) >> 2, row = tid & 127;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t s_addr = tmem + t * TILE + lanes, o_addr = tmem + 256 + t * 128 + lanes;
         int it = 0, s_count = 0, segs = 0;
         if (tid == 256) p.headers[blockIdx.x] = make_int4(0, 0, 0, 0);
+        // Of a warp's 32 rows, the 16 bytes that lane l has of step k (D/8 lanes a row).  Rows behind the item's last: that one.
+        auto row_chunk = [&](const segment &g, int k, const uint16_t *x, int64_t stride) {
+            const int w_row = t * 128 + (warp & 3) * 32 + k * (256 / D) + lane / (D / 8), in = w_row < g.it.rows ? w_row : g.it.rows - 1;
+            const int tok0 = g.row0 / p.group, local = g.row0 - tok0 * p.group + in, dt = (local * p.group_inv) >> 20;  // local / group: exact below 2^12
+            return reinterpret_cast<const uint4 *>(x + (int64_t)(g.seq.start + tok0 + dt) * stride + (int64_t)(g.kh * p.group + local - dt * p.group) * D) + lane % (D / 8);
+        };
         while (r.more() && ok) {
             const segment g = next_segment(p, r);
             const reach re = reach_of(p, g, t);
@@ -672,21 +686,24 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
             if (works) {
                 const int rr = g.row0 + t * 128 + row;
                 if (t * 128 + row < g.it.rows) pos = g.seq.len - g.seq.n + rr / p.group;
-                // the warp's 32 rows as they are, D/8 lanes a row
+                // the warp's 32 rows as they are, D/8 lanes a row, eight loads at a time
+#pragma unroll 1
+                for (int k0 = 0; k0 < D / 8; k0 += 8) {
+                    uint4 x[8];
 #pragma unroll
-                for (int k = 0; k < D / 8; ++k) {
-                    const int w_row = (warp & 3) * 32 + k * (256 / D) + lane / (D / 8), c = lane % (D / 8), r1 = g.row0 + t * 128 + w_row, tok = r1 / p.group;
-                    uint4 x = make_uint4(0, 0, 0, 0);
-                    if (t * 128 + w_row < g.it.rows)
-                        x = reinterpret_cast<const uint4 *>(p.c.q.p + (int64_t)(g.seq.start + tok) * p.c.q.stride + (int64_t)(g.kh * p.group + r1 - tok * p.group) * D)[c];
-                    *reinterpret_cast<uint4 *>(q_tile + (c / 8) * (128 * 128) + w_row * 128 + (((c & 7) ^ (w_row & 7)) * 16)) = x;
+                    for (int k = 0; k < 8; ++k) x[k] = *row_chunk(g, k0 + k, p.c.q.p, p.c.q.stride);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const int w_row = (warp & 3) * 32 + (k0 + k) * (256 / D) + lane / (D / 8), c = lane % (D / 8);
+                        *reinterpret_cast<uint4 *>(q_tile + (c / 8) * (128 * 128) + w_row * 128 + (((c & 7) ^ (w_row & 7)) * 16)) = x[k];
+                    }
                 }
                 __syncwarp();
                 // a thread's own row in FP16, scaled so that its largest magnitude is in [2^14, 2^15) (BF16's 8 bits stay exact down to
                 // 2^-31 of that), in the codes' order; a negative scale goes into the sign
                 auto chunk = [&](int c) { return reinterpret_cast<uint4 *>(q_tile + (c / 8) * (128 * 128) + row * 128 + (((c & 7) ^ (row & 7)) * 16)); };
                 uint32_t big = 0;  // magnitudes as integers, in both halves
-#pragma unroll
+#pragma unroll 2
                 for (int c = 0; c < D / 8; ++c) {
                     const uint4 x = *chunk(c);
                     big = __vmaxu2(__vmaxu2(__vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu)), big);
@@ -698,7 +715,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                 const float up = __uint_as_float((uint32_t)(268 - e) << 23);
                 row_scale = bad ? NAN : fabsf(p.scale2) * __uint_as_float((uint32_t)(e - 14) << 23);
                 const uint32_t sign = p.scale2 < 0.0f ? 0x80008000u : 0u;
-#pragma unroll
+#pragma unroll 2
                 for (int c = 0; c < D / 8; ++c) {
                     const uint4 x = *chunk(c);
                     const uint32_t pairs[4] = {__byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632), __byte_perm(x.y, x.w, 0x5410), __byte_perm(x.y, x.w, 0x7632)};
@@ -718,37 +735,40 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                 const int base = g.base(j), i = it + j;
                 if (!sees(p, re, base)) continue;
                 // (the terms: written ahead of this barrier's arrivals; the scores)
-                ok = __all_sync(0xffffffffu, wait(bar(B_KV_FULL + (i & 1)), (i >> 1) & 1)) && __all_sync(0xffffffffu, wait(bar(B_S_FULL + t), s_count & 1));
+                ok = __all_sync(0xffffffffu, wait(bar(B_K_FULL + (i & 1)), (i >> 1) & 1)) && __all_sync(0xffffffffu, wait(bar(B_S_FULL + t), s_count & 1));
                 if (!ok) break;
                 ++s_count;
                 fence_after();
                 const uint32_t term = smem + L::TERM + (i % 3) * TERM_BYTES;
-                uint32_t x[TILE];
-#pragma unroll
-                for (int c = 0; c < TILE; c += 32) ld32(s_addr + c, x + c);
+                // Twice over the scores, 64 columns at a time (they stay in tensor memory, and the code in the instruction cache: with all
+                // 128 in registers and no loop, half of the warps' time went into fetching instructions)
                 float top[2] = {-INFINITY, -INFINITY};
                 const bool all = sees_all(p, re, base);
-                ld_wait();
-                if (!all) {  // scores of positions that this row does not see; the others' scales here instead of below
+#pragma unroll 1
+                for (int c = 0; c < TILE; c += 64) {
+                    uint32_t x[64];
+                    ld32(s_addr + c, x);
+                    ld32(s_addr + c + 32, x + 32);
+                    ld_wait();
+                    if (!all) {
 #pragma unroll
-                    for (int c = 0; c < TILE; c += KV_BLOCK) {
-                        const int at = base + c;
-                        const uint32_t see = low_bits(pos - at + 1) & (p.c.window ? ~low_bits(pos - p.c.window + 1 - at) | low_bits(p.c.n_first - at) : 0xffffffffu);
-                        const float4 tm = lds4(term + c / KV_BLOCK * 16);
-                        const float sc = tm.x * row_scale;
+                        for (int k0 = 0; k0 < 64; k0 += 32) {
+                            const uint32_t see = visible(p, pos, base + c + k0);
 #pragma unroll
-                        for (int k = 0; k < KV_BLOCK; ++k) x[c + k] = see >> k & 1u ? __float_as_uint(fmaf(__uint_as_float(x[c + k]), sc, tm.y)) : 0xff800000u;
+                            for (int k = 0; k < 32; ++k) x[k0 + k] = see >> k & 1u ? x[k0 + k] : 0xff7fffffu;
+                        }
                     }
-                }
 #pragma unroll
-                for (int c = 0; c < TILE; c += KV_BLOCK) {
-                    const float4 tm = lds4(term + c / KV_BLOCK * 16);
-                    float y[4];
+                    for (int k = 0; k < 64; k += KV_BLOCK) {
+                        const float4 tm = lds4(term + (c + k) / KV_BLOCK * 16);
+                        float y[4];
 #pragma unroll
-                    for (int z = 0; z < 4; ++z)
-                        y[z] = fmaxf(fmaxf(__uint_as_float(x[c + z]), __uint_as_float(x[c + 4 + z])), fmaxf(__uint_as_float(x[c + 8 + z]), __uint_as_float(x[c + 12 + z])));
-                    const float big = fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]));
-                    top[c / KV_BLOCK & 1] = fmaxf(top[c / KV_BLOCK & 1], all ? fmaf(big, tm.x * row_scale, tm.y) : big);
+                        for (int z = 0; z < 4; ++z)
+                            y[z] = fmaxf(fmaxf(__uint_as_float(x[k + z]), __uint_as_float(x[k + 4 + z])), fmaxf(__uint_as_float(x[k + 8 + z]), __uint_as_float(x[k + 12 + z])));
+                        const float big = fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]));
+                        // (-FLT_MAX: nothing of the block is visible)
+                        top[k / KV_BLOCK & 1] = fmaxf(top[k / KV_BLOCK & 1], big == -3.402823466e38f ? -INFINITY : fmaf(big, tm.x * row_scale, tm.y));
+                    }
                 }
                 const float tile_top = fmaxf(top[0], top[1]);
                 if (!any) {
@@ -759,42 +779,53 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                     const f2 a2 = pack2(a, a);
                     l2 = fma2(l2, a2, 0);
                     // (the scores of this tile were computed behind the products that O holds)
-#pragma unroll
-                    for (int k = 0; k < D; k += 8) {
-                        uint32_t o[8];
-                        ld8(o_addr + k, o);
+#pragma unroll 1
+                    for (int k = 0; k < D; k += 32) {
+                        uint32_t o[32];
+                        ld32(o_addr + k, o);
                         ld_wait();
 #pragma unroll
-                        for (int z = 0; z < 8; ++z) o[z] = __float_as_uint(__uint_as_float(o[z]) * a);
-                        st8(o_addr + k, o);
+                        for (int z = 0; z < 32; ++z) o[z] = __float_as_uint(__uint_as_float(o[z]) * a);
+                        st32(o_addr + k, o);
                     }
                     st_wait();
                 }
                 any = true;
                 const float from = (m == -INFINITY ? 0.0f : m) - 7.0f;
+#pragma unroll 1
+                for (int c = 0; c < TILE; c += 64) {
+                    uint32_t x[64], h[32];
+                    ld32(s_addr + c, x);
+                    ld32(s_addr + c + 32, x + 32);
+                    ld_wait();
 #pragma unroll
-                for (int c = 0; c < TILE; c += KV_BLOCK) {
-                    const float4 tm = lds4(term + c / KV_BLOCK * 16);
-                    const float sc = all ? tm.x * row_scale : 1.0f, of = (all ? tm.y : 0.0f) - from;
-                    const f2 sc2 = pack2(sc, sc), of2 = pack2(of, of);
-                    f2 sum[2] = {0, 0};
+                    for (int b0 = 0; b0 < 64; b0 += KV_BLOCK) {
+                        const float4 tm = lds4(term + (c + b0) / KV_BLOCK * 16);
+                        const float sc = tm.x * row_scale, of = tm.y - from;
+                        const f2 sc2 = pack2(sc, sc), of2 = pack2(of, of);
+                        f2 sum[2] = {0, 0};
 #pragma unroll
-                    for (int k = c; k < c + KV_BLOCK; k += 4) {
-                        float y[4];
-                        unpack2(fma2(pack2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), sc2, of2), y[0], y[1]);
-                        unpack2(fma2(pack2(__uint_as_float(x[k + 2]), __uint_as_float(x[k + 3])), sc2, of2), y[2], y[3]);
+                        for (int k = b0; k < b0 + KV_BLOCK; k += 4) {
+                            float y[4];
+                            unpack2(fma2(pack2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), sc2, of2), y[0], y[1]);
+                            unpack2(fma2(pack2(__uint_as_float(x[k + 2]), __uint_as_float(x[k + 3])), sc2, of2), y[2], y[3]);
 #pragma unroll
-                        for (int z = 0; z < 4; ++z) y[z] = ex2(y[z]);
-                        sum[0] = add2(sum[0], pack2(y[0], y[1]));
-                        sum[1] = add2(sum[1], pack2(y[2], y[3]));
-                        const __half2 h0 = __floats2half2_rn(y[0], y[1]), h1 = __floats2half2_rn(y[2], y[3]);
-                        x[k / 2] = *reinterpret_cast<const uint32_t *>(&h0);
-                        x[k / 2 + 1] = *reinterpret_cast<const uint32_t *>(&h1);
+                            for (int z = 0; z < 4; ++z) y[z] = ex2(y[z]);
+                            if (!all) {
+                                const uint32_t see = visible(p, pos, base + c + b0);
+#pragma unroll
+                                for (int z = 0; z < 4; ++z) y[z] = see >> (k - b0 + z) & 1u ? y[z] : 0.0f;
+                            }
+                            sum[0] = add2(sum[0], pack2(y[0], y[1]));
+                            sum[1] = add2(sum[1], pack2(y[2], y[3]));
+                            const __half2 h0 = __floats2half2_rn(y[0], y[1]), h1 = __floats2half2_rn(y[2], y[3]);
+                            h[k / 2] = *reinterpret_cast<const uint32_t *>(&h0);
+                            h[k / 2 + 1] = *reinterpret_cast<const uint32_t *>(&h1);
+                        }
+                        l2 = fma2(add2(sum[0], sum[1]), pack2(tm.z, tm.z), l2);
                     }
-                    l2 = fma2(add2(sum[0], sum[1]), pack2(tm.z, tm.z), l2);
+                    st32(s_addr + c / 2, h);  // (columns c/2 .. c/2 + 31: scores that have been read)
                 }
-                st32(s_addr, x);
-                st32(s_addr + 32, x + 32);
                 st_wait();
                 fence_before();
                 __syncwarp();
@@ -817,7 +848,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
             const bool mine = t * 128 + row < f.it.rows, whole = f.t0 == 0 && f.nt == f.it.count;
             float *part = p.parts + (((int64_t)blockIdx.x * 2 + (f.t0 == 0 ? 1 : 0)) * BM + t * 128 + row) * (D + 4);
             const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-#pragma unroll
+#pragma unroll 1
             for (int k = 0; k < D; k += 32) {
                 uint32_t o[32];
                 if (works) {
@@ -850,12 +881,11 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                 __syncwarp();
             }
             if (whole) {
-#pragma unroll 4
+#pragma unroll 2
                 for (int k = 0; k < D / 8; ++k) {
-                    const int w_row = (warp & 3) * 32 + k * (256 / D) + lane / (D / 8), c = lane % (D / 8), r1 = f.row0 + t * 128 + w_row, tok = r1 / p.group;
+                    const int w_row = (warp & 3) * 32 + k * (256 / D) + lane / (D / 8), c = lane % (D / 8);
                     const uint4 x = *reinterpret_cast<const uint4 *>(q_tile + (c / 8) * (128 * 128) + w_row * 128 + (((c & 7) ^ (w_row & 7)) * 16));
-                    if (t * 128 + w_row < f.it.rows)
-                        reinterpret_cast<uint4 *>(p.c.out + (int64_t)(f.seq.start + tok) * p.c.out_stride + (int64_t)(f.kh * p.group + r1 - tok * p.group) * D)[c] = x;
+                    if (t * 128 + w_row < f.it.rows) *const_cast<uint4 *>(row_chunk(f, k, p.c.out, p.c.out_stride)) = x;
                 }
                 __syncwarp();
             }
@@ -953,6 +983,7 @@ cudaError_t kv_launch_prompt(const kv_batch &b, int D, const kv_attention_call &
     p.most_items = (int)items;
     p.scale2 = c.scale * 1.4426950408889634f;
     p.group = group;
+    p.group_inv = (1 << 20) / group + 1;
     p.few = few;
     cudaError_t e = tpq_launch_pdl(attention_plan, dim3(1), dim3(PLAN_THREADS), 0, st, p);
     if (e != cudaSuccess) return e;
