@@ -35,12 +35,18 @@ constexpr int RAW = 4;                          // copy stages
 constexpr int UNPACKERS = 6;                    // warps
 constexpr int THREADS = 512;
 constexpr int PLAN_THREADS = 1024;
+// Runs are dealt out in units: a (256 rows, key head) pair is its tiles and EXTRA more, which stand for its beginning and end.
+constexpr int EXTRA = 2;
 
+// A sequence's rows row0 .. row0 + rows - 1 (row: new position x query head of a key head).
 struct alignas(16) plan_item {
-    int seq, block, before, tiles;  // `block`: its rows start at BM * block; `before`: tiles x key heads of the items ahead
-    kv_seq rows;
-    int pad;
+    int seq, before, tiles, rows;   // before: units (below) of the items ahead
+    int first, from;                // tiles that any row sees: [0, first) and [from, ...), `tiles` in all
+    int lo[2], hi[2];               // positions of the first and last row of row tiles A and B (hi < lo: it has none)
+    int tok, head, row0, len;       // of the first row: row of the step's tensors and query head in its group; the sequence's length
+    int pad[2];
 };
+static_assert(sizeof(plan_item) == 64, "four vector loads");
 struct alignas(16) plan_head {
     int items, total, pad[2];
 };
@@ -57,26 +63,30 @@ struct prompt_params {
     int group, group_inv, few;  // group_inv: 2^20 / group rounded up; sequences of up to `few` rows are attention_split's
 };
 
-// Rows of an item and the tiles they see: [0, first) and [from, end).
-struct item_tiles {
-    int rows, first, from, count;
-};
-__device__ __forceinline__ item_tiles tiles_of_rows(const kv_seq &s, const kv_attention_call &c, int group, int block)
+__device__ __forceinline__ plan_item item_of(const kv_seq &s, const kv_attention_call &c, int group, int block)
 {
-    item_tiles t;
-    const int left = s.n * group - block * BM;  // (rows of a sequence fit 31 bits: checked by the host)
+    plan_item t{};
+    t.row0 = block * BM;
+    const int left = s.n * group - t.row0;  // (rows of a sequence fit 31 bits: checked by the host)
     t.rows = left < BM ? left : BM;
-    const int p_lo = s.len - s.n + block * BM / group, p_hi = s.len - s.n + (block * BM + t.rows - 1) / group;
-    t.first = t.from = 0;
+    const int p0 = s.len - s.n, tok = t.row0 / group;
+    t.tok = s.start + tok;
+    t.head = t.row0 - tok * group;
+    t.len = s.len;
+    for (int k = 0; k < 2; ++k) {
+        const int rows = t.rows - 128 * k;
+        t.lo[k] = p0 + (t.row0 + 128 * k) / group;
+        t.hi[k] = rows > 0 ? p0 + (t.row0 + 128 * k + (rows < 128 ? rows : 128) - 1) / group : t.lo[k] - 1;
+    }
     if (c.window) {
-        const int from = p_lo - c.window + 1;
+        const int from = t.lo[0] - c.window + 1;
         if (from > 0) {
             t.from = from / TILE;
             const int first = ((c.n_first < from ? c.n_first : from) + TILE - 1) / TILE;
             t.first = first < t.from ? first : t.from;
         }
     }
-    t.count = t.first + p_hi / TILE + 1 - t.from;
+    t.tiles = t.first + (t.rows > 128 ? t.hi[1] : t.hi[0]) / TILE + 1 - t.from;
     return t;
 }
 
@@ -137,8 +147,8 @@ __global__ void __launch_bounds__(PLAN_THREADS) attention_plan(const prompt_para
     int64_t before = 0;
     for (int i0 = 0; i0 < items; i0 += PLAN_THREADS) {
         const int i = i0 + threadIdx.x;
-        int n = 0, s = 0, block = 0;
-        kv_seq q{};
+        int n = 0;
+        plan_item it{};
         if (i < items) {
             int lo = 0, hi = b.n_seqs;  // the last sequence whose items begin at or before i
             while (hi - lo > 1) {
@@ -146,15 +156,17 @@ __global__ void __launch_bounds__(PLAN_THREADS) attention_plan(const prompt_para
                 if (p.seq_items[mid] <= i) lo = mid;
                 else hi = mid;
             }
-            s = lo;
-            block = i - p.seq_items[s];
-            q = kv_load_seq(b, s);
-            n = tiles_of_rows(q, p.c, p.group, block).count;
+            it = item_of(kv_load_seq(b, lo), p.c, p.group, i - p.seq_items[lo]);
+            it.seq = lo;
+            n = it.tiles + EXTRA;
         }
         int total;
         const int64_t at = before + (int64_t)(block_scan(n, warps, total) - n) * b.n_kv_heads;
         before += (int64_t)total * b.n_kv_heads;
-        if (i < items) p.items[i] = plan_item{s, block, (int)at, n, q, 0};
+        if (i < items) {
+            it.before = (int)at;
+            p.items[i] = it;
+        }
     }
     if (threadIdx.x == 0) {
         if (before > INT32_MAX - 1024) {
@@ -172,6 +184,7 @@ constexpr unsigned long long WAIT_NS = 1000000000ull;
 __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity)
 {
     unsigned long long t0 = 0;
+#pragma unroll 1
     for (int i = 0; i < WAIT_LIMIT; ++i) {
         uint32_t ok;
         asm volatile(
@@ -349,49 +362,48 @@ struct Smem {
 enum { B_RAW_FULL = 0, B_RAW_EMPTY = B_RAW_FULL + RAW, B_K_FULL = B_RAW_EMPTY + RAW, B_V_FULL = B_K_FULL + 2, B_K_EMPTY = B_V_FULL + 2, B_V_EMPTY = B_K_EMPTY + 2,
        B_Q_FULL = B_V_EMPTY + 2, B_S_FULL = B_Q_FULL + 2, B_P_FULL = B_S_FULL + 2, B_O_FULL = B_P_FULL + 2, B_O_EMPTY = B_O_FULL + 2, B_COUNT = B_O_EMPTY + 2 };
 
-// A block's run of tiles, one (item, key head) after the other.
+// A block's run of units, one (item, key head) after the other.
 struct run {
     int unit, end, item;
-    __device__ bool more() const { return unit < end; }
 };
 struct segment {
-    kv_seq seq;
-    int s, kh, row0, t0, nt;  // rows row0 .. of the sequence; tiles t0 .. t0 + nt - 1 of the item's
-    item_tiles it;
+    const plan_item *item;
+    int kh, t0, nt;  // tiles t0 .. t0 + nt - 1 of the item's
+    int first, skip; // (for base)
     __device__ __forceinline__ int base(int j) const  // first position of tile j of the segment
     {
         const int t = t0 + j;
-        return (t < it.first ? t : it.from + t - it.first) * TILE;
+        return (t < first ? t : t + skip) * TILE;
     }
 };
-__device__ __forceinline__ segment next_segment(const prompt_params &p, run &r)
+// The next segment with a tile in it; false at the run's end.
+__device__ __forceinline__ bool next_segment(const prompt_params &p, run &r, segment &g)
 {
-    segment g;
-    plan_item it = p.items[r.item];
-    while (r.unit >= it.before + it.tiles * p.b.n_kv_heads) it = p.items[++r.item];
-    g.s = it.seq;
-    g.seq = it.rows;
-    g.row0 = it.block * BM;
-    g.it = tiles_of_rows(g.seq, p.c, p.group, it.block);
-    const int off = r.unit - it.before;
-    g.kh = off / it.tiles;
-    g.t0 = off - g.kh * it.tiles;
-    g.nt = it.tiles - g.t0 < r.end - r.unit ? it.tiles - g.t0 : r.end - r.unit;
-    r.unit += g.nt;
-    return g;
+#pragma unroll 1
+    while (r.unit < r.end) {
+        const plan_item *it = p.items + r.item;
+        const int4 q = *reinterpret_cast<const int4 *>(it);  // seq, before, tiles, rows
+        const int weight = q.z + EXTRA, off = r.unit - q.y;
+        if (off >= weight * p.b.n_kv_heads) {
+            ++r.item;
+            continue;
+        }
+        const int kh = off / weight, o = off - kh * weight, n = weight - o < r.end - r.unit ? weight - o : r.end - r.unit;
+        r.unit += n;
+        const int t0 = o > EXTRA ? o - EXTRA : 0, t1 = o + n - EXTRA;
+        if (t1 <= t0) continue;
+        const int2 f = *reinterpret_cast<const int2 *>(&it->first);
+        g = segment{it, kh, t0, t1 - t0, f.x, f.y - f.x};
+        return true;
+    }
+    return false;
 }
-// Whether row tile t (0: A, 1: B) sees any position of a tile that starts at `base`; whether all of its rows see all of it.
+// Positions of a row tile's first and last row (hi < lo: it has none).
 struct reach {
-    int lo, hi;  // positions of the row tile's first and last row (hi < lo: it has no rows)
+    int lo, hi;
 };
-__device__ __forceinline__ reach reach_of(const prompt_params &p, const segment &g, int t)
-{
-    const int p0 = g.seq.len - g.seq.n, r0 = g.row0 + t * 128, rows = g.it.rows - t * 128;
-    reach r;
-    r.lo = p0 + r0 / p.group;
-    r.hi = rows > 0 ? p0 + (r0 + (rows < 128 ? rows : 128) - 1) / p.group : r.lo - 1;
-    return r;
-}
+__device__ __forceinline__ reach reach_of(const segment &g, int t) { return reach{g.item->lo[t], g.item->hi[t]}; }
+// Whether a row tile sees any position of a tile that starts at `base`; whether all of its rows see all of it.
 __device__ __forceinline__ bool sees(const prompt_params &p, const reach &r, int base)
 {
     return r.hi >= r.lo && base <= r.hi && (p.c.window == 0 || base + TILE - 1 > r.lo - p.c.window || base < p.c.n_first);
@@ -410,9 +422,12 @@ __device__ __forceinline__ bool unpack(const prompt_params &p, run r, uint8_t *g
     constexpr int BLOCKS = TILE / KV_BLOCK, PER_STAGE = HALF / KV_BLOCK;
     static_assert(2 * BLOCKS == 16 && UNPACKERS == 6 && PER_STAGE == 4, "see above");
     int it = 0, next = which;  // next: index of this warp's next job among the tile's
-    while (r.more()) {
-        const segment g = next_segment(p, r);
+    segment g;
+    while (next_segment(p, r, g)) {
+        const int len = g.item->len;
+#pragma unroll 1
         for (int j = 0; j < g.nt; ++j, ++it) {
+#pragma unroll 1
             for (; next < 2 * BLOCKS; next += UNPACKERS) {
                 const bool values_job = next >= BLOCKS;
                 const int block = next & (BLOCKS - 1), stage = 2 * it + block / PER_STAGE, st = stage % RAW, at = block % PER_STAGE, row0 = block * KV_BLOCK;
@@ -423,7 +438,7 @@ __device__ __forceinline__ bool unpack(const prompt_params &p, run r, uint8_t *g
                 uint32_t scaled;  // step and low of position lane % 16
                 {
                     const int n = lane & 15;
-                    const bool on = have && g.base(j) + row0 + n < g.seq.len;
+                    const bool on = have && g.base(j) + row0 + n < len;
                     const uint32_t vw = reinterpret_cast<const uint32_t *>(blk + kv_v_words(D))[n];
                     const float vs = __uint_as_float(vw << 16), vl = __uint_as_float(vw & 0xffff0000u);
                     bool bad = !(fabsf(vl) < INFINITY) || !(vs < INFINITY);
@@ -553,25 +568,25 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
     if (warp == 0) {
         // ---------------- copies
         int stage = 0;  // copy stages so far
-        while (r.more() && ok) {
-            const segment g = next_segment(p, r);
+        segment g;
+        while (ok && next_segment(p, r, g)) {
+            const int seq = g.item->seq, len = g.item->len, from = g.item->lo[0] - p.c.window + 1, hi = g.item->rows > 128 ? g.item->hi[1] : g.item->hi[0];
             auto page_of = [&](int h) {  // page of this lane's block (of four) of copy stage h of the segment, -1: not copied
                 if (h >= 2 * g.nt || lane >= HALF / KV_BLOCK) return -1;
                 const int pos = g.base(h >> 1) + (h & 1) * HALF + lane * KV_BLOCK;
-                if (pos >= g.seq.len) return -1;
-                const int from = g.seq.len - g.seq.n + g.row0 / p.group - p.c.window + 1;
+                if (pos >= len || pos > hi) return -1;
                 if (p.c.window && pos >= p.c.n_first && pos + KV_BLOCK <= from) return -1;  // no row sees it
-                const int hi = g.seq.len - g.seq.n + (g.row0 + g.it.rows - 1) / p.group;
-                if (pos > hi) return -1;
-                const int page = b.table[g.s * b.table_stride + (pos >> b.page_shift)];
+                const int page = b.table[seq * b.table_stride + (pos >> b.page_shift)];
                 if (page >= 0 && page < b.n_pages) return page;
                 kv_report(b);
                 return -1;
             };
-            int page = page_of(0);
-            for (int h = 0; h < 2 * g.nt; ++h, ++stage) {
-                const int st = stage % RAW;
-                const int next = page_of(h + 1);
+            int next = -1;
+#pragma unroll 1
+            for (int h = -1; h < 2 * g.nt; ++h) {
+                const int page = next, st = stage % RAW;
+                next = page_of(h + 1);  // a step ahead of its use
+                if (h < 0) continue;
                 if (stage >= RAW) ok = __all_sync(0xffffffffu, wait(bar(B_RAW_EMPTY + st), (stage / RAW - 1) & 1));
                 if (!ok) break;
                 const uint32_t have = __ballot_sync(0xffffffffu, page >= 0);
@@ -585,7 +600,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                     const uint8_t *src = b.cache + (((int64_t)page * b.n_kv_heads + g.kh) * blocks + (pos & (b.page_size - 1)) / KV_BLOCK) * kv_block_bytes(D);
                     bulk_g2s(smem + L::RAWS + st * L::RAW_BYTES + lane * kv_block_bytes(D), src, kv_block_bytes(D), bar(B_RAW_FULL + st));
                 }
-                page = next;
+                ++stage;
             }
         }
         if (!ok)  // let the copies in flight land before the shared memory is released
@@ -596,16 +611,19 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
         int it = 0;                             // tiles so far: operand buffer it % 2
         // a bit for each row tile: phase of its scores' barrier, of its rows' and sums' barriers, whether it has had sums before
         uint32_t p_phase = 0, q_phase = 0, begun = 0;
-        while (r.more() && ok) {
-            const segment g = next_segment(p, r);
-            const reach re_a = reach_of(p, g, 0), re_b = reach_of(p, g, 1);
+        segment g;
+        while (ok && next_segment(p, r, g)) {
+            const reach re_a = reach_of(g, 0), re_b = reach_of(g, 1);
             int last_a = -1, last_b = -1;
+#pragma unroll 1
             for (int j = g.nt - 1; j >= 0 && last_a < 0; --j)
                 if (sees(p, re_a, g.base(j))) last_a = j;
+#pragma unroll 1
             for (int j = g.nt - 1; j >= 0 && last_b < 0; --j)
                 if (sees(p, re_b, g.base(j))) last_b = j;
             uint32_t any = 0;  // row tiles with sums of this segment
             // step j: P_t V(j) for both row tiles, each followed by Q_t K(j + 1); step -1 has the first scores only
+#pragma unroll 1
             for (int j = -1; j < g.nt && ok; ++j) {
                 const int i = it + j;
                 const bool more = j + 1 < g.nt;
@@ -668,15 +686,16 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
         int it = 0, s_count = 0, segs = 0;
         if (tid == 256) p.headers[blockIdx.x] = make_int4(0, 0, 0, 0);
         // Of a warp's 32 rows, the 16 bytes that lane l has of step k (D/8 lanes a row).  Rows behind the item's last: that one.
-        auto row_chunk = [&](const segment &g, int k, const uint16_t *x, int64_t stride) {
-            const int w_row = t * 128 + (warp & 3) * 32 + k * (256 / D) + lane / (D / 8), in = w_row < g.it.rows ? w_row : g.it.rows - 1;
-            const int tok0 = g.row0 / p.group, local = g.row0 - tok0 * p.group + in, dt = (local * p.group_inv) >> 20;  // local / group: exact below 2^12
-            return reinterpret_cast<const uint4 *>(x + (int64_t)(g.seq.start + tok0 + dt) * stride + (int64_t)(g.kh * p.group + local - dt * p.group) * D) + lane % (D / 8);
+        auto row_chunk = [&](const segment &g, int rows, int k, const uint16_t *x, int64_t stride) {
+            const int w_row = t * 128 + (warp & 3) * 32 + k * (256 / D) + lane / (D / 8), in = w_row < rows ? w_row : rows - 1;
+            const int local = g.item->head + in, dt = (local * p.group_inv) >> 20;  // local / group: exact below 2^12
+            return reinterpret_cast<const uint4 *>(x + (int64_t)(g.item->tok + dt) * stride + (int64_t)(g.kh * p.group + local - dt * p.group) * D) + lane % (D / 8);
         };
-        while (r.more() && ok) {
-            const segment g = next_segment(p, r);
-            const reach re = reach_of(p, g, t);
+        segment g;
+        while (ok && next_segment(p, r, g)) {
+            const reach re = reach_of(g, t);
             bool works = false;
+#pragma unroll 1
             for (int j = 0; j < g.nt && !works; ++j) works = sees(p, re, g.base(j));
             int pos = -1;  // of this thread's row
             float m = -INFINITY, row_scale = 0.0f;
@@ -684,14 +703,15 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
             bool any = false;
             uint8_t *const q_tile = gen + L::Q + t * L::TILE_BYTES;
             if (works) {
-                const int rr = g.row0 + t * 128 + row;
-                if (t * 128 + row < g.it.rows) pos = g.seq.len - g.seq.n + rr / p.group;
+                // (position of the first row) + (rows behind it) / group
+                if (t * 128 + row < g.item->rows) pos = g.item->lo[0] + (((g.item->head + t * 128 + row) * p.group_inv) >> 20);
                 // the warp's 32 rows as they are, D/8 lanes a row, eight loads at a time
+                const int rows = g.item->rows;
 #pragma unroll 1
                 for (int k0 = 0; k0 < D / 8; k0 += 8) {
                     uint4 x[8];
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) x[k] = *row_chunk(g, k0 + k, p.c.q.p, p.c.q.stride);
+                    for (int k = 0; k < 8; ++k) x[k] = *row_chunk(g, rows, k0 + k, p.c.q.p, p.c.q.stride);
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
                         const int w_row = (warp & 3) * 32 + (k0 + k) * (256 / D) + lane / (D / 8), c = lane % (D / 8);
@@ -842,11 +862,9 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                 ++segs;
                 fence_after();
             }
-            // (what the walk over the tiles had no use for is worked out again instead of held in registers)
-            run again{r.unit - g.nt, r.end, r.item};
-            const segment f = next_segment(p, again);
-            const bool mine = t * 128 + row < f.it.rows, whole = f.t0 == 0 && f.nt == f.it.count;
-            float *part = p.parts + (((int64_t)blockIdx.x * 2 + (f.t0 == 0 ? 1 : 0)) * BM + t * 128 + row) * (D + 4);
+            const int rows = g.item->rows;
+            const bool mine = t * 128 + row < rows, whole = g.t0 == 0 && g.nt == g.item->tiles;
+            float *part = p.parts + (((int64_t)blockIdx.x * 2 + (g.t0 == 0 ? 1 : 0)) * BM + t * 128 + row) * (D + 4);
             const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll 1
             for (int k = 0; k < D; k += 32) {
@@ -885,7 +903,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                 for (int k = 0; k < D / 8; ++k) {
                     const int w_row = (warp & 3) * 32 + k * (256 / D) + lane / (D / 8), c = lane % (D / 8);
                     const uint4 x = *reinterpret_cast<const uint4 *>(q_tile + (c / 8) * (128 * 128) + w_row * 128 + (((c & 7) ^ (w_row & 7)) * 16));
-                    if (t * 128 + w_row < f.it.rows) *const_cast<uint4 *>(row_chunk(f, k, p.c.out, p.c.out_stride)) = x;
+                    if (t * 128 + w_row < rows) *const_cast<uint4 *>(row_chunk(g, rows, k, p.c.out, p.c.out_stride)) = x;
                 }
                 __syncwarp();
             }
@@ -895,9 +913,9 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(B_O_EMPTY + t));
             }
-            if (tid == 256 && f.t0 == 0 && !whole) {  // the runs behind this one have `share` tiles each of what is left
+            if (tid == 256 && g.t0 == 0 && !whole) {  // the runs behind this one have `share` units each of what is left
                 const int share = (int)(((int64_t)p.head->total + gridDim.x - 1) / gridDim.x);
-                p.headers[blockIdx.x] = make_int4(1 + (f.it.count - f.nt + share - 1) / share, f.seq.start, f.row0, (f.it.rows << 16) | f.kh);
+                p.headers[blockIdx.x] = make_int4(1 + (g.item->tiles - g.nt + share - 1) / share, (int)(g.item - p.items), g.kh, 0);
             }
         }
     }
@@ -917,9 +935,11 @@ __global__ void __launch_bounds__(256) attention_prompt_join(const prompt_params
 {
     constexpr int V = D / 32;  // values of a lane
     tpq_grid_dep_wait();
-    const int4 head = p.headers[blockIdx.x];  // parts, first row of the sequence, first row of the item in it, rows and key head
-    const int lane = threadIdx.x & 31, r = blockIdx.y * 8 + (threadIdx.x >> 5), rows = head.w >> 16, kh = head.w & 0xffff;
-    if (head.x == 0 || r >= rows) return;
+    const int4 head = p.headers[blockIdx.x];  // parts, item, key head
+    const int lane = threadIdx.x & 31, r = blockIdx.y * 8 + (threadIdx.x >> 5);
+    if (head.x == 0) return;
+    const plan_item &it = p.items[head.y];
+    if (r >= it.rows) return;
     float m = -INFINITY, l = 0.0f, o[V] = {};
     for (int i = 0; i < head.x; ++i) {
         const float *part = p.parts + ((((int64_t)blockIdx.x + i) * 2 + (i == 0 ? 1 : 0)) * BM + r) * (D + 4);
@@ -939,8 +959,8 @@ __global__ void __launch_bounds__(256) attention_prompt_join(const prompt_params
         for (int k = 0; k < V; ++k) o[k] = fmaf(z[k], f, o[k] * a);
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    const int rr = head.z + r, tok = rr / p.group, h = kh * p.group + (rr - tok * p.group);
-    uint32_t *dst = reinterpret_cast<uint32_t *>(p.c.out + (int64_t)(head.y + tok) * p.c.out_stride + (int64_t)h * D + V * lane);
+    const int local = it.head + r, dt = local / p.group, h = head.z * p.group + (local - dt * p.group);
+    uint32_t *dst = reinterpret_cast<uint32_t *>(p.c.out + (int64_t)(it.tok + dt) * p.c.out_stride + (int64_t)h * D + V * lane);
 #pragma unroll
     for (int k = 0; k < V / 2; ++k) {
         const __nv_bfloat162 v = __floats2bfloat162_rn(o[2 * k] * inv, o[2 * k + 1] * inv);
