@@ -36,7 +36,7 @@ constexpr int UNPACKERS = 6;                    // warps
 constexpr int THREADS = 512;
 constexpr int PLAN_THREADS = 1024;
 // Runs are dealt out in units: a (256 rows, key head) pair is its tiles and EXTRA more, which stand for its beginning and end.
-constexpr int EXTRA = 2;
+constexpr int EXTRA = 4;
 
 // A sequence's rows row0 .. row0 + rows - 1 (row: new position x query head of a key head).
 struct alignas(16) plan_item {
@@ -265,6 +265,11 @@ __device__ __forceinline__ void st32(uint32_t addr, const uint32_t *r)
         ::W8(r, 0), W8(r, 8), W8(r, 16), W8(r, 24), "r"(addr)
         : "memory");
 }
+__device__ __forceinline__ void st16(uint32_t addr, const uint32_t *r)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::W8(r, 0), W8(r, 8), "r"(addr)
+                 : "memory");
+}
 __device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // Operands of 128-byte rows with the 128-byte swizzle, 8-row groups of 1024 bytes.  Depth along the row (Q, keys): a step of 16 is 32
@@ -489,12 +494,6 @@ __device__ __forceinline__ bool unpack(const prompt_params &p, run r, uint8_t *g
         }
     }
     return true;
-}
-
-// Which of the 32 positions from `at` on a row at `pos` sees.
-__device__ __forceinline__ uint32_t visible(const prompt_params &p, int pos, int at)
-{
-    return low_bits(pos - at + 1) & (p.c.window ? ~low_bits(pos - p.c.window + 1 - at) | low_bits(p.c.n_first - at) : 0xffffffffu);
 }
 
 template <int D>
@@ -733,7 +732,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                 const bool bad = e == 255;  // infinite or NaN: so is the row's answer
                 if (e < 16 || bad) e = 16;
                 const float up = __uint_as_float((uint32_t)(268 - e) << 23);
-                row_scale = bad ? NAN : fabsf(p.scale2) * __uint_as_float((uint32_t)(e - 14) << 23);
+                row_scale = fabsf(p.scale2) * __uint_as_float((uint32_t)(e - 14) << 23);
                 const uint32_t sign = p.scale2 < 0.0f ? 0x80008000u : 0u;
 #pragma unroll 2
                 for (int c = 0; c < D / 8; ++c) {
@@ -743,7 +742,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
 #pragma unroll
                     for (int z = 0; z < 4; ++z) {
                         const __half2 h = __floats2half2_rn(__uint_as_float(pairs[z] << 16) * up, __uint_as_float(pairs[z] & 0xffff0000u) * up);
-                        u[z] = (bad ? 0u : *reinterpret_cast<const uint32_t *>(&h)) ^ sign;
+                        u[z] = (bad ? 0x7fff7fffu : *reinterpret_cast<const uint32_t *>(&h)) ^ sign;
                     }
                     *chunk(c) = make_uint4(u[0], u[1], u[2], u[3]);
                 }
@@ -760,24 +759,29 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                 ++s_count;
                 fence_after();
                 const uint32_t term = smem + L::TERM + (i % 3) * TERM_BYTES;
-                // Twice over the scores, 64 columns at a time (they stay in tensor memory, and the code in the instruction cache: with all
+                if (!sees_all(p, re, base)) {  // scores of positions that this row does not see
+#pragma unroll 1
+                    for (int c = 0; c < TILE; c += 32) {
+                        uint32_t x[32];
+                        ld32(s_addr + c, x);
+                        ld_wait();
+                        const int at = base + c;
+                        const uint32_t see = low_bits(pos - at + 1) & (p.c.window ? ~low_bits(pos - p.c.window + 1 - at) | low_bits(p.c.n_first - at) : 0xffffffffu);
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) x[k] = see >> k & 1u ? x[k] : 0xff800000u;
+                        st32(s_addr + c, x);
+                    }
+                    st_wait();
+                }
+                // Twice over the scores, 64 and 32 columns at a time (they stay in tensor memory, and the code in the instruction cache: with all
                 // 128 in registers and no loop, half of the warps' time went into fetching instructions)
                 float top[2] = {-INFINITY, -INFINITY};
-                const bool all = sees_all(p, re, base);
 #pragma unroll 1
                 for (int c = 0; c < TILE; c += 64) {
                     uint32_t x[64];
                     ld32(s_addr + c, x);
                     ld32(s_addr + c + 32, x + 32);
                     ld_wait();
-                    if (!all) {
-#pragma unroll
-                        for (int k0 = 0; k0 < 64; k0 += 32) {
-                            const uint32_t see = visible(p, pos, base + c + k0);
-#pragma unroll
-                            for (int k = 0; k < 32; ++k) x[k0 + k] = see >> k & 1u ? x[k0 + k] : 0xff7fffffu;
-                        }
-                    }
 #pragma unroll
                     for (int k = 0; k < 64; k += KV_BLOCK) {
                         const float4 tm = lds4(term + (c + k) / KV_BLOCK * 16);
@@ -785,9 +789,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
 #pragma unroll
                         for (int z = 0; z < 4; ++z)
                             y[z] = fmaxf(fmaxf(__uint_as_float(x[k + z]), __uint_as_float(x[k + 4 + z])), fmaxf(__uint_as_float(x[k + 8 + z]), __uint_as_float(x[k + 12 + z])));
-                        const float big = fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]));
-                        // (-FLT_MAX: nothing of the block is visible)
-                        top[k / KV_BLOCK & 1] = fmaxf(top[k / KV_BLOCK & 1], big == -3.402823466e38f ? -INFINITY : fmaf(big, tm.x * row_scale, tm.y));
+                        top[k / KV_BLOCK & 1] = fmaxf(top[k / KV_BLOCK & 1], fmaf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), fmaxf(tm.x * row_scale, 0x1p-120f), tm.y));
                     }
                 }
                 const float tile_top = fmaxf(top[0], top[1]);
@@ -813,15 +815,14 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                 any = true;
                 const float from = (m == -INFINITY ? 0.0f : m) - 7.0f;
 #pragma unroll 1
-                for (int c = 0; c < TILE; c += 64) {
-                    uint32_t x[64], h[32];
+                for (int c = 0; c < TILE; c += 32) {
+                    uint32_t x[32], h[16];
                     ld32(s_addr + c, x);
-                    ld32(s_addr + c + 32, x + 32);
                     ld_wait();
 #pragma unroll
-                    for (int b0 = 0; b0 < 64; b0 += KV_BLOCK) {
+                    for (int b0 = 0; b0 < 32; b0 += KV_BLOCK) {
                         const float4 tm = lds4(term + (c + b0) / KV_BLOCK * 16);
-                        const float sc = tm.x * row_scale, of = tm.y - from;
+                        const float sc = fmaxf(tm.x * row_scale, 0x1p-120f), of = tm.y - from;  // (not 0: -inf * 0)
                         const f2 sc2 = pack2(sc, sc), of2 = pack2(of, of);
                         f2 sum[2] = {0, 0};
 #pragma unroll
@@ -831,11 +832,6 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                             unpack2(fma2(pack2(__uint_as_float(x[k + 2]), __uint_as_float(x[k + 3])), sc2, of2), y[2], y[3]);
 #pragma unroll
                             for (int z = 0; z < 4; ++z) y[z] = ex2(y[z]);
-                            if (!all) {
-                                const uint32_t see = visible(p, pos, base + c + b0);
-#pragma unroll
-                                for (int z = 0; z < 4; ++z) y[z] = see >> (k - b0 + z) & 1u ? y[z] : 0.0f;
-                            }
                             sum[0] = add2(sum[0], pack2(y[0], y[1]));
                             sum[1] = add2(sum[1], pack2(y[2], y[3]));
                             const __half2 h0 = __floats2half2_rn(y[0], y[1]), h1 = __floats2half2_rn(y[2], y[3]);
@@ -844,7 +840,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                         }
                         l2 = fma2(add2(sum[0], sum[1]), pack2(tm.z, tm.z), l2);
                     }
-                    st32(s_addr + c / 2, h);  // (columns c/2 .. c/2 + 31: scores that have been read)
+                    st16(s_addr + c / 2, h);  // (columns c/2 .. c/2 + 15: scores that have been read)
                 }
                 st_wait();
                 fence_before();
