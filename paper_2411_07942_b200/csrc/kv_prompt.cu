@@ -181,20 +181,25 @@ __global__ void __launch_bounds__(PLAN_THREADS) attention_plan(const prompt_para
 
 constexpr int WAIT_LIMIT = 1 << 24;
 constexpr unsigned long long WAIT_NS = 1000000000ull;
-__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity)
+__device__ __forceinline__ bool arrived(uint32_t bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok;
+}
+// (out of line: two dozen waits' loops would not leave the instruction cache room for the arithmetic)
+__device__ __noinline__ bool wait_more(uint32_t bar, uint32_t parity)
 {
     unsigned long long t0 = 0;
 #pragma unroll 1
     for (int i = 0; i < WAIT_LIMIT; ++i) {
-        uint32_t ok;
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t"
-            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-            "selp.u32 %0, 1, 0, p;\n\t}"
-            : "=r"(ok)
-            : "r"(bar), "r"(parity)
-            : "memory");
-        if (ok) return true;
+        if (arrived(bar, parity)) return true;
         if ((i & 63) == 63) {
             unsigned long long t;
             asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
@@ -204,6 +209,7 @@ __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity)
     }
     return false;
 }
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity) { return arrived(bar, parity) || wait_more(bar, parity); }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void commit(uint32_t bar)
@@ -331,9 +337,8 @@ constexpr uint32_t TERM_BYTES = TILE / KV_BLOCK * 16;
 __device__ __forceinline__ uint32_t to_scale(float step, float low, bool on, int &e)
 {
     float big = on ? fminf(fmaxf(fabsf(low), fabsf(fmaf(15.0f, step, low))), 3.4e38f) : 0.0f;
-#pragma unroll
-    for (int m = 8; m > 0; m >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, m));
-    e = big < 0x1p-60f ? 67 : (int)(__float_as_uint(big) >> 23);  // (nothing is below 2^-57 but zeros)
+    const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(big));  // (not negative: in the order of its bits)
+    e = top < 0x21800000u ? 67 : (int)(top >> 23);  // (nothing is below 2^-57 but zeros)
     const float inv = __uint_as_float((uint32_t)(268 - e) << 23);  // 2^(141 - e)
     const __half2 h = __floats2half2_rn(on ? step * inv : 0.0f, on ? low * inv : 0.0f);
     return *reinterpret_cast<const uint32_t *>(&h);
@@ -360,12 +365,14 @@ struct Smem {
     static constexpr uint32_t RAW_BYTES = HALF / KV_BLOCK * kv_block_bytes(D);
     static constexpr uint32_t TERM = RAWS + RAW * RAW_BYTES;
     static constexpr uint32_t BARS = TERM + 3 * TERM_BYTES;
-    static constexpr uint32_t BYTES = BARS + 256;
+    static constexpr uint32_t BYTES = BARS + 304;
     static_assert(BYTES <= 227 * 1024, "shared memory of a block");
 };
 // barriers, 8 bytes each from BARS
 enum { B_RAW_FULL = 0, B_RAW_EMPTY = B_RAW_FULL + RAW, B_K_FULL = B_RAW_EMPTY + RAW, B_V_FULL = B_K_FULL + 2, B_K_EMPTY = B_V_FULL + 2, B_V_EMPTY = B_K_EMPTY + 2,
-       B_Q_FULL = B_V_EMPTY + 2, B_S_FULL = B_Q_FULL + 2, B_P_FULL = B_S_FULL + 2, B_O_FULL = B_P_FULL + 2, B_O_EMPTY = B_O_FULL + 2, B_COUNT = B_O_EMPTY + 2 };
+       B_Q_FULL = B_V_EMPTY + 2, B_S_FULL = B_Q_FULL + 2, B_P_FULL = B_S_FULL + 2 /* 2 x half + row tile */, B_O_FULL = B_P_FULL + 4, B_O_EMPTY = B_O_FULL + 2, B_T_FULL = B_O_EMPTY + 2,
+       B_COUNT = B_T_FULL + 3 };
+static_assert(8 * B_COUNT + 4 * RAW + 4 <= 304, "barriers");
 
 // A block's run of units, one (item, key head) after the other.
 struct run {
@@ -486,6 +493,7 @@ __device__ __forceinline__ bool unpack(const prompt_params &p, run r, uint8_t *g
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) {
+                    if (!values_job) mbar_arrive(bars + 8 * (B_T_FULL + it % 3));
                     mbar_arrive(bars + 8 * ((values_job ? B_V_FULL : B_K_FULL) + (it & 1)));
                     mbar_arrive(bars + 8 * (B_RAW_EMPTY + st));
                 }
@@ -515,6 +523,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
     if (tid == 0) {
+        for (int i = 0; i < 3; ++i) mbar_init(bar(B_T_FULL + i), TILE / KV_BLOCK);
         for (int i = 0; i < RAW; ++i) {
             mbar_init(bar(B_RAW_FULL + i), 1);
             mbar_init(bar(B_RAW_EMPTY + i), 8);  // the keys and the values of four blocks
@@ -527,6 +536,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
             mbar_init(bar(B_Q_FULL + i), 4);
             mbar_init(bar(B_S_FULL + i), 1);
             mbar_init(bar(B_P_FULL + i), 4);
+            mbar_init(bar(B_P_FULL + 2 + i), 4);
             mbar_init(bar(B_O_FULL + i), 1);
             mbar_init(bar(B_O_EMPTY + i), 4);
         }
@@ -605,7 +615,8 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
         if (!ok)  // let the copies in flight land before the shared memory is released
             for (int k = stage > RAW ? stage - RAW : 0; k < stage; ++k) (void)wait(bar(B_RAW_FULL + k % RAW), (k / RAW) & 1);
     } else if (warp == 1) {
-        // ---------------- MMA
+        // ---------------- MMA: one thread, known to the compiler as such
+        if (elect()) {
         constexpr uint32_t qk_instr = instr(TILE, false), pv_instr = instr(D, true);
         int it = 0;                             // tiles so far: operand buffer it % 2
         // a bit for each row tile: phase of its scores' barrier, of its rows' and sums' barriers, whether it has had sums before
@@ -626,32 +637,35 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
             for (int j = -1; j < g.nt && ok; ++j) {
                 const int i = it + j;
                 const bool more = j + 1 < g.nt;
-                if (j >= 0) ok = __all_sync(0xffffffffu, wait(bar(B_V_FULL + (i & 1)), (i >> 1) & 1));
+                if (j >= 0) ok = wait(bar(B_V_FULL + (i & 1)), (i >> 1) & 1);
 #pragma unroll 1
                 for (int t = 0; t < 2 && ok; ++t) {
                     if (j >= 0 && sees(p, t ? re_b : re_a, g.base(j))) {
-                        if (!(any >> t & 1) && (begun >> t & 1)) ok = __all_sync(0xffffffffu, wait(bar(B_O_EMPTY + t), (q_phase >> t & 1) ^ 1));
-                        if (ok) ok = __all_sync(0xffffffffu, wait(bar(B_P_FULL + t), p_phase >> t & 1));
-                        if (!ok) break;
-                        fence_after();
-                        if (elect()) {
-                            const uint32_t v = operand(smem + L::V + (i & 1) * L::TILE_BYTES, TILE * 128);
+                        if (!(any >> t & 1) && (begun >> t & 1)) ok = wait(bar(B_O_EMPTY + t), (q_phase >> t & 1) ^ 1);
+#pragma unroll 1
+                        for (int half = 0; half < 2 && ok; ++half) {
+                            ok = wait(bar(B_P_FULL + 2 * half + t), p_phase >> t & 1);
+                            if (!ok) break;
+                            fence_after();
+                            {
+                                const uint32_t v = operand(smem + L::V + (i & 1) * L::TILE_BYTES + half * (HALF * 128), TILE * 128);
 #pragma unroll
-                            for (int x = 0; x < TILE / 16; ++x)
-                                mma_ts(tmem + 256 + t * 128, tmem + t * TILE + 8 * x, v + x * (2048 >> 4), OPERAND_HIGH, pv_instr, (any >> t & 1) | (x != 0));
-                            if (j == (t ? last_b : last_a)) commit(bar(B_O_FULL + t));
+                                for (int x = 0; x < HALF / 16; ++x)
+                                    mma_ts(tmem + 256 + t * 128, tmem + t * TILE + half * (HALF / 2) + 8 * x, v + x * (2048 >> 4), OPERAND_HIGH, pv_instr, (any >> t & 1) | half | (x != 0));
+                                if (half == 1 && j == (t ? last_b : last_a)) commit(bar(B_O_FULL + t));
+                            }
                         }
-                        __syncwarp();
+                        if (!ok) break;
                         any |= 1u << t;
                         p_phase ^= 1u << t;
                     }
                     if (more) {
-                        if (j < 0 && (t ? last_b : last_a) >= 0) ok = __all_sync(0xffffffffu, wait(bar(B_Q_FULL + t), q_phase >> t & 1));
-                        if (t == 0 && ok) ok = __all_sync(0xffffffffu, wait(bar(B_K_FULL + ((i + 1) & 1)), ((i + 1) >> 1) & 1));
+                        if (j < 0 && (t ? last_b : last_a) >= 0) ok = wait(bar(B_Q_FULL + t), q_phase >> t & 1);
+                        if (t == 0 && ok) ok = wait(bar(B_K_FULL + ((i + 1) & 1)), ((i + 1) >> 1) & 1);
                         if (!ok) break;
                         fence_after();
                         if (sees(p, t ? re_b : re_a, g.base(j + 1))) {
-                            if (elect()) {
+                            {
                                 const uint32_t a = operand(smem + L::Q + t * L::TILE_BYTES, 16), k = operand(smem + L::K + ((i + 1) & 1) * L::TILE_BYTES, 16);
 #pragma unroll
                                 for (int x = 0; x < D / 16; ++x) {
@@ -660,21 +674,21 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                                 }
                                 commit(bar(B_S_FULL + t));
                             }
-                            __syncwarp();
                         }
                     }
                 }
                 if (!ok) break;
-                if (elect()) {
+                {
                     if (j >= 0) commit(bar(B_V_EMPTY + (i & 1)));
                     if (more) commit(bar(B_K_EMPTY + ((i + 1) & 1)));
                 }
-                __syncwarp();
             }
             it += g.nt;
             begun |= any;
             q_phase ^= any;
         }
+        }
+        __syncwarp();
     } else if (warp < 8) {
         ok = unpack<D>(p, r, gen, bars, there, warp - 2, lane);
     } else {
@@ -753,8 +767,8 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
             for (int j = 0; j < g.nt; ++j) {
                 const int base = g.base(j), i = it + j;
                 if (!sees(p, re, base)) continue;
-                // (the terms: written ahead of this barrier's arrivals; the scores)
-                ok = __all_sync(0xffffffffu, wait(bar(B_K_FULL + (i & 1)), (i >> 1) & 1)) && __all_sync(0xffffffffu, wait(bar(B_S_FULL + t), s_count & 1));
+                // (the terms: there ahead of the scores, and not written again before this row tile is done with them)
+                ok = __all_sync(0xffffffffu, wait(bar(B_S_FULL + t), s_count & 1)) && __all_sync(0xffffffffu, wait(bar(B_T_FULL + i % 3), (i / 3) & 1));
                 if (!ok) break;
                 ++s_count;
                 fence_after();
@@ -841,11 +855,13 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                         l2 = fma2(add2(sum[0], sum[1]), pack2(tm.z, tm.z), l2);
                     }
                     st16(s_addr + c / 2, h);  // (columns c/2 .. c/2 + 15: scores that have been read)
+                    if (c & 32) {  // half of the weights: their products may begin
+                        st_wait();
+                        fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(bar(B_P_FULL + 2 * (c >> 6) + t));
+                    }
                 }
-                st_wait();
-                fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(B_P_FULL + t));
             }
             it += g.nt;
             if (!ok) break;
@@ -915,7 +931,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
             }
         }
     }
-    if (!ok && lane == 0) atomicExch(b.status, (int)TPQ_ERR_TIMEOUT);
+    if (!ok) atomicExch(b.status, (int)TPQ_ERR_TIMEOUT);
     fence_before();
     __syncthreads();
     if (warp == 1) {
