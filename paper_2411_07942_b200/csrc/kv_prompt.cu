@@ -15,8 +15,8 @@
 //   ... P_A E(j), Q_A C(j+1), P_B E(j), Q_B C(j+1), P_A E(j+1), ...
 //   warp 0       copies: blocks of 16 positions as they lie in the pages, 64 positions a stage
 //   warp 1       tensor memory, MMA issue (one elected lane)
-//   warps 2-7    unpack: codes to the two operands' tiles (128-byte swizzle), words to the terms of a block
-//   warps 8-15   softmax: a thread per row; the rows themselves into shared memory at the start, the output at the end
+//   warps 2-9    unpack: codes to the two operands' tiles (128-byte swizzle), words to the terms of a block
+//   warps 10-17  softmax: a thread per row; the rows themselves into shared memory at the start, the output at the end
 // Unpacking a tile costs as much however many rows use it: 256 rows, which the query heads of a key head share.
 //
 // Work.  attention_plan lists the (sequence, 256 rows) pairs and adds up their tiles (causal, window); a run of tiles in that order
@@ -32,8 +32,8 @@ namespace {
 
 constexpr int BM = 256, TILE = 128, HALF = 64;  // rows of a block, positions of a tile, of a copy stage
 constexpr int RAW = 4;                          // copy stages
-constexpr int UNPACKERS = 6;                    // warps
-constexpr int THREADS = 512;
+constexpr int THREADS = 18 * 32;
+constexpr int UNPACK = 2, SOFTMAX = 10;         // first warps of those roles (eight each: two on every scheduler)
 constexpr int PLAN_THREADS = 1024;
 // Runs are dealt out in units: a (256 rows, key head) pair is its tiles and EXTRA more, which stand for its beginning and end.
 constexpr int EXTRA = 4;
@@ -425,83 +425,29 @@ __device__ __forceinline__ bool sees_all(const prompt_params &p, const reach &r,
     return base + TILE - 1 <= r.lo && (p.c.window == 0 || base > r.hi - p.c.window || base + TILE <= p.c.n_first);
 }
 
-// A warp that unpacks (`which` of UNPACKERS).  A tile is sixteen jobs, the keys of its eight blocks and then their values; job x of
-// tile i is warp (16 i + x) % 6's, which gives every warp a part of every copy stage and of every operand tile: none misses a barrier's phase.
+// 16 positions' codes to rows row0 .. of an operand tile; scaled: step and low of position lane % 16
 template <int D>
-__device__ __forceinline__ bool unpack(const prompt_params &p, run r, uint8_t *gen, uint32_t bars, const uint32_t *there, int which, int lane)
+__device__ __forceinline__ void unpack(const uint8_t *codes, uint8_t *tile, int row0, uint32_t scaled, int lane)
 {
-    using L = Smem<D>;
-    constexpr int BLOCKS = TILE / KV_BLOCK, PER_STAGE = HALF / KV_BLOCK;
-    static_assert(2 * BLOCKS == 16 && UNPACKERS == 6 && PER_STAGE == 4, "see above");
-    int it = 0, next = which;  // next: index of this warp's next job among the tile's
-    segment g;
-    while (next_segment(p, r, g)) {
-        const int len = g.item->len;
-#pragma unroll 1
-        for (int j = 0; j < g.nt; ++j, ++it) {
-#pragma unroll 1
-            for (; next < 2 * BLOCKS; next += UNPACKERS) {
-                const bool values_job = next >= BLOCKS;
-                const int block = next & (BLOCKS - 1), stage = 2 * it + block / PER_STAGE, st = stage % RAW, at = block % PER_STAGE, row0 = block * KV_BLOCK;
-                if (!__all_sync(0xffffffffu, wait(bars + 8 * (B_RAW_FULL + st), (stage / RAW) & 1))) return false;
-                if (it >= 2 && !__all_sync(0xffffffffu, wait(bars + 8 * ((values_job ? B_V_EMPTY : B_K_EMPTY) + (it & 1)), ((it >> 1) - 1) & 1))) return false;
-                const uint8_t *const blk = gen + L::RAWS + st * L::RAW_BYTES + at * kv_block_bytes(D);
-                const bool have = (there[st] >> at) & 1u;
-                uint32_t scaled;  // step and low of position lane % 16
-                {
-                    const int n = lane & 15;
-                    const bool on = have && g.base(j) + row0 + n < len;
-                    const uint32_t vw = reinterpret_cast<const uint32_t *>(blk + kv_v_words(D))[n];
-                    const float vs = __uint_as_float(vw << 16), vl = __uint_as_float(vw & 0xffff0000u);
-                    bool bad = !(fabsf(vl) < INFINITY) || !(vs < INFINITY);
-                    int ev;
-                    scaled = to_scale(vs, vl, on && !bad, ev);
-                    if (!values_job) {
-                        const uint32_t kw = reinterpret_cast<const uint32_t *>(blk + kv_k_words(D))[n];
-                        const float ks = __uint_as_float(kw << 16), kl = __uint_as_float(kw & 0xffff0000u);
-                        bad = bad || !(fabsf(kl) < INFINITY) || !(ks < INFINITY);
-                        int ek;
-                        scaled = to_scale(ks, kl, on && !bad, ek);
-                        // (a key or value vector that is no number makes the rows that see it NaN by way of their scores: a weight of
-                        // 0 times NaN would reach the others)
-                        if (on && bad) scaled = 0x7fff0000u;
-                        if (lane == 0)
-                            *reinterpret_cast<float4 *>(gen + L::TERM + (it % 3) * TERM_BYTES + block * 16) =
-                                have ? make_float4(__uint_as_float((uint32_t)(ek - 14) << 23), (float)(ev - 141), __uint_as_float((uint32_t)(268 - ev) << 23), 0.0f)
-                                     : make_float4(1.0f, -INFINITY, 0.0f, 0.0f);
-                    }
-                }
-                const uint8_t *const codes = blk + (values_job ? kv_v_codes(D) : 0);
-                uint8_t *const tile = gen + (values_job ? L::V : L::K) + (it & 1) * L::TILE_BYTES;
-                uint4 c[D / 64];
-                uint32_t sl[D / 64];
+    uint4 c[D / 64];
+    uint32_t sl[D / 64];
 #pragma unroll
-                for (int k = 0; k < D / 64; ++k) {
-                    // 16 bytes (32 codes) of position `row`; eight lanes read and write 128 different bytes of banks
-                    const int row = D == 128 ? (lane & 7) + 8 * k : lane & 15, q = D == 128 ? ((lane >> 3) + (row >> 1)) & 3 : lane >> 4;
-                    c[k] = *reinterpret_cast<const uint4 *>(codes + row * (D / 2) + 16 * q);
-                    sl[k] = __shfl_sync(0xffffffffu, scaled, row);
-                }
-#pragma unroll
-                for (int k = 0; k < D / 64; ++k) {
-                    const int row = D == 128 ? (lane & 7) + 8 * k : lane & 15, q = D == 128 ? ((lane >> 3) + (row >> 1)) & 3 : lane >> 4;
-                    uint8_t *const line = tile + (q >> 1) * (TILE * 128) + (row0 + row) * 128;
-                    const uint32_t w[4] = {c[k].x, c[k].y, c[k].z, c[k].w};
-#pragma unroll
-                    for (int jw = 0; jw < 4; ++jw) *reinterpret_cast<uint4 *>(line + ((((q & 1) * 4 + jw) ^ (row & 7)) * 16)) = values(w[jw], sl[k]);
-                }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) {
-                    if (!values_job) mbar_arrive(bars + 8 * (B_T_FULL + it % 3));
-                    mbar_arrive(bars + 8 * ((values_job ? B_V_FULL : B_K_FULL) + (it & 1)));
-                    mbar_arrive(bars + 8 * (B_RAW_EMPTY + st));
-                }
-            }
-            next -= 2 * BLOCKS;  // (16 = 2 x 6 + 4)
-        }
+    for (int k = 0; k < D / 64; ++k) {
+        // 16 bytes (32 codes) of position `row`; eight lanes read and write 128 different bytes of banks
+        const int row = D == 128 ? (lane & 7) + 8 * k : lane & 15, q = D == 128 ? ((lane >> 3) + (row >> 1)) & 3 : lane >> 4;
+        c[k] = *reinterpret_cast<const uint4 *>(codes + row * (D / 2) + 16 * q);
+        sl[k] = __shfl_sync(0xffffffffu, scaled, row);
     }
-    return true;
+#pragma unroll
+    for (int k = 0; k < D / 64; ++k) {
+        const int row = D == 128 ? (lane & 7) + 8 * k : lane & 15, q = D == 128 ? ((lane >> 3) + (row >> 1)) & 3 : lane >> 4;
+        uint8_t *const line = tile + (q >> 1) * (TILE * 128) + (row0 + row) * 128;
+        const uint32_t w[4] = {c[k].x, c[k].y, c[k].z, c[k].w};
+#pragma unroll
+        for (int jw = 0; jw < 4; ++jw) *reinterpret_cast<uint4 *>(line + ((((q & 1) * 4 + jw) ^ (row & 7)) * 16)) = values(w[jw], sl[k]);
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
 }
 
 template <int D>
@@ -526,7 +472,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
         for (int i = 0; i < 3; ++i) mbar_init(bar(B_T_FULL + i), TILE / KV_BLOCK);
         for (int i = 0; i < RAW; ++i) {
             mbar_init(bar(B_RAW_FULL + i), 1);
-            mbar_init(bar(B_RAW_EMPTY + i), 8);  // the keys and the values of four blocks
+            mbar_init(bar(B_RAW_EMPTY + i), HALF / KV_BLOCK);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(bar(B_K_FULL + i), TILE / KV_BLOCK);
@@ -689,15 +635,57 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
         }
         }
         __syncwarp();
-    } else if (warp < 8) {
-        ok = unpack<D>(p, r, gen, bars, there, warp - 2, lane);
+    } else if (warp < SOFTMAX) {
+        // ---------------- unpack: block warp - UNPACK of every tile
+        const int block = warp - UNPACK, at = block & 3, n = lane & 15;
+        int it = 0;
+        segment g;
+        while (ok && next_segment(p, r, g)) {
+            const int len = g.item->len;
+#pragma unroll 1
+            for (int j = 0; j < g.nt; ++j, ++it) {
+                const int stage = 2 * it + block / 4, st = stage % RAW;
+                ok = __all_sync(0xffffffffu, wait(bar(B_RAW_FULL + st), (stage / RAW) & 1));
+                if (!ok) break;
+                const uint8_t *const blk = gen + L::RAWS + st * L::RAW_BYTES + at * kv_block_bytes(D);
+                const bool have = (there[st] >> at) & 1u, on = have && g.base(j) + block * KV_BLOCK + n < len;
+                const uint32_t kw = reinterpret_cast<const uint32_t *>(blk + kv_k_words(D))[n], vw = reinterpret_cast<const uint32_t *>(blk + kv_v_words(D))[n];
+                const float ks = __uint_as_float(kw << 16), kl = __uint_as_float(kw & 0xffff0000u);
+                const float vs = __uint_as_float(vw << 16), vl = __uint_as_float(vw & 0xffff0000u);
+                // (a key or value vector that is no number makes the rows that see it NaN by way of their scores: a weight of
+                // 0 times NaN would reach the others)
+                const bool bad = !(fabsf(vl) < INFINITY) || !(vs < INFINITY) || !(fabsf(kl) < INFINITY) || !(ks < INFINITY);
+                int ek, ev;
+                uint32_t k_scaled = to_scale(ks, kl, on && !bad, ek);
+                const uint32_t v_scaled = to_scale(vs, vl, on && !bad, ev);
+                if (on && bad) k_scaled = 0x7fff0000u;
+                if (it >= 2) ok = __all_sync(0xffffffffu, wait(bar(B_K_EMPTY + (it & 1)), ((it >> 1) - 1) & 1));
+                if (!ok) break;
+                if (lane == 0)
+                    *reinterpret_cast<float4 *>(gen + L::TERM + (it % 3) * TERM_BYTES + block * 16) =
+                        have ? make_float4(__uint_as_float((uint32_t)(ek - 14) << 23), (float)(ev - 141), __uint_as_float((uint32_t)(268 - ev) << 23), 0.0f)
+                             : make_float4(1.0f, -INFINITY, 0.0f, 0.0f);
+                unpack<D>(blk, gen + L::K + (it & 1) * L::TILE_BYTES, block * KV_BLOCK, k_scaled, lane);
+                if (lane == 0) {
+                    mbar_arrive(bar(B_T_FULL + it % 3));
+                    mbar_arrive(bar(B_K_FULL + (it & 1)));
+                }
+                if (it >= 2) ok = __all_sync(0xffffffffu, wait(bar(B_V_EMPTY + (it & 1)), ((it >> 1) - 1) & 1));
+                if (!ok) break;
+                unpack<D>(blk + kv_v_codes(D), gen + L::V + (it & 1) * L::TILE_BYTES, block * KV_BLOCK, v_scaled, lane);
+                if (lane == 0) {
+                    mbar_arrive(bar(B_V_FULL + (it & 1)));
+                    mbar_arrive(bar(B_RAW_EMPTY + st));
+                }
+            }
+        }
     } else {
         // ---------------- softmax: thread <-> row `row` of row tile t
-        const int t = (warp - 8) >> 2, row = tid & 127;
+        const int t = (warp - SOFTMAX) >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t s_addr = tmem + t * TILE + lanes, o_addr = tmem + 256 + t * 128 + lanes;
         int it = 0, s_count = 0, segs = 0;
-        if (tid == 256) p.headers[blockIdx.x] = make_int4(0, 0, 0, 0);
+        if (tid == SOFTMAX * 32) p.headers[blockIdx.x] = make_int4(0, 0, 0, 0);
         // Of a warp's 32 rows, the 16 bytes that lane l has of step k (D/8 lanes a row).  Rows behind the item's last: that one.
         auto row_chunk = [&](const segment &g, int rows, int k, const uint16_t *x, int64_t stride) {
             const int w_row = t * 128 + (warp & 3) * 32 + k * (256 / D) + lane / (D / 8), in = w_row < rows ? w_row : rows - 1;
@@ -925,7 +913,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(B_O_EMPTY + t));
             }
-            if (tid == 256 && g.t0 == 0 && !whole) {  // the runs behind this one have `share` units each of what is left
+            if (tid == SOFTMAX * 32 && g.t0 == 0 && !whole) {  // the runs behind this one have `share` units each of what is left
                 const int share = (int)(((int64_t)p.head->total + gridDim.x - 1) / gridDim.x);
                 p.headers[blockIdx.x] = make_int4(1 + (g.item->tiles - g.nt + share - 1) / share, (int)(g.item - p.items), g.kh, 0);
             }
