@@ -8,12 +8,13 @@
 //   out = sum_t P_t (e_t - 8) + sum_t P_t (b_t / r_t + 8)   over   sum_t P_t / r_t,
 // m the running maximum of x_t + log2 r_t.
 //
-// Codes become operands with one logic instruction for two: a code in the low mantissa bits of BF16 128 (0x4300 | c) is
-// 128 + c, in bits 4 .. 7 of FP16 1024 (0x6400 | 16 c) is 16 (64 + c), both exact.  Of the keys' 128 the sum over q is taken
-// off with a_t's (a_t - 128 s_t); the values' 72 x 16 = 1152 by one more product, of P with a constant, which the
-// accumulators of 32 positions start from: they hold sums of P (e - 8) alone, and what is added up in
-// binary32 over a whole sequence has no common offset to lose digits to.  P is rounded to FP16 (11 bits; below 2^-26
-// of the largest one, with fewer), Q and the codes are exact.
+// Codes become operands with little more than one logic instruction for two: a code in the low mantissa bits of FP16 1024
+// (0x6400 | c) is 1024 + c, in bits 4 .. 7 (0x6400 | 16 c) it is 16 (64 + c), both exact; the sums of offsets are what the
+// accumulators start from.  The keys use both forms, with a 16th of the row's value for the second one (a row has a power of two
+// of its own that makes its BF16 values FP16 ones).  The values use the second form alone, whose offset is small beside the
+// codes: their 72 x 16 = 1152 is taken off by one more product, of P with a constant, from which the sums of 32 positions start:
+// they are sums of P (e - 8), and what is added up in binary32 over a whole sequence has no common offset to lose digits to.  P is
+// rounded to FP16 (11 bits; below 2^-26 of the largest one, with fewer), Q and the codes are exact.
 //
 // Operands.  Rows (query heads of one key head x new positions) are the 8 columns of an m16n8k16 product, positions (for the
 // values: a head's values) its 16 rows, so that 8 query heads per key head leave nothing of the instruction unused.  The scores come
@@ -85,17 +86,12 @@ __device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t mask, uint32_t b
     asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(a), "r"(mask), "r"(bits));
     return r;
 }
-__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+// d = a b + c, FP16 products, FP32 sums
+__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, float c0, float c1, float c2, float c3)
 {
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
-{
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
 }
 __device__ __forceinline__ uint32_t transposed(uint32_t x)
 {
@@ -198,22 +194,43 @@ attention_split(const split_params p)
         const int nt = tl.count - t0 < unit_end - unit ? tl.count - t0 : unit_end - unit;
         const int rows = seq.n * p.group, p0 = seq.len - seq.n;
 
-        // ---- the rows as operands: column n = lane / 4 of a group of 8, values 8 KW i4 .. of the head in the order (0 4)(1 5)(2 6)(3 7)
+        // ---- the rows as operands: column n = lane / 4 of a group of 8, values 8 KW i4 .. of the head in the order (0 4)(1 5)(2 6)(3 7),
+        // in FP16, scaled so that the row's largest magnitude is in [2^14, 2^15) (BF16's 8 bits stay exact down to 2^-27 of that),
+        // a 16th of it where the codes come 16-fold
         uint2 qf[NT == 1 ? D / 16 : 1];
-        float qsum[NT][2];
+        float qsum[NT][2], qoff[NT][2], qscale[NT][2];  // of columns 2 i4 and 2 i4 + 1: sum of the row; what the codes' offsets add; its scale
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const int r = 8 * n + g, tok = r / p.group, h = kh * p.group + (r - tok * p.group);
             const uint4 *src = reinterpret_cast<const uint4 *>(p.c.q.p + (int64_t)(seq.start + tok) * p.c.q.stride + (int64_t)h * D + 8 * KW * i4);
-            float sum_q = 0.0f;
+            uint4 x[KW];
+            uint32_t big = 0;
 #pragma unroll
             for (int j = 0; j < KW; ++j) {
-                const uint4 x = r < rows ? src[j] : make_uint4(0, 0, 0, 0);
-                const uint32_t u[4] = {x.x, x.y, x.z, x.w};
+                x[j] = r < rows ? src[j] : make_uint4(0, 0, 0, 0);
+                big = __vmaxu2(__vmaxu2(__vmaxu2(x[j].x & 0x7fff7fffu, x[j].y & 0x7fff7fffu), __vmaxu2(x[j].z & 0x7fff7fffu, x[j].w & 0x7fff7fffu)), big);
+            }
+            big = max(big & 0xffffu, big >> 16);
+            big = max(big, __shfl_xor_sync(0xffffffffu, big, 1));
+            big = max(big, __shfl_xor_sync(0xffffffffu, big, 2));
+            int e = (int)(big >> 7);
+            const bool bad = e == 255;  // infinite or NaN: so is the row's answer
+            if (e < 16 || bad) e = 16;
+            const float up = __uint_as_float((uint32_t)(268 - e) << 23);
+            float sum_q = 0.0f, off_q = 0.0f;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) sum_q += __uint_as_float(u[k] << 16) + __uint_as_float(u[k] & 0xffff0000u);
-                const uint2 f0 = make_uint2(__byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632));
-                const uint2 f1 = make_uint2(__byte_perm(x.y, x.w, 0x5410), __byte_perm(x.y, x.w, 0x7632));
+            for (int j = 0; j < KW; ++j) {
+                const uint32_t pair[4] = {__byte_perm(x[j].x, x[j].z, 0x5410), __byte_perm(x[j].x, x[j].z, 0x7632), __byte_perm(x[j].y, x[j].w, 0x5410), __byte_perm(x[j].y, x[j].w, 0x7632)};
+                uint32_t u[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float f0 = __uint_as_float(pair[k] << 16) * up, f1 = __uint_as_float(pair[k] & 0xffff0000u) * up;
+                    const __half2 h2 = __floats2half2_rn(k & 1 ? f0 * 0.0625f : f0, k & 1 ? f1 * 0.0625f : f1);
+                    u[k] = *reinterpret_cast<const uint32_t *>(&h2);
+                    sum_q += f0 + f1;
+                    off_q += (__low2float(h2) + __high2float(h2)) * -1024.0f;
+                }
+                const uint2 f0 = make_uint2(u[0], u[1]), f1 = make_uint2(u[2], u[3]);
                 if (NT == 1) {
                     qf[2 * j] = f0;
                     qf[2 * j + 1] = f1;
@@ -222,10 +239,18 @@ attention_split(const split_params p)
                     sh.q[(n * (D / 16) + 2 * j + 1) * 32 + lane] = f1;
                 }
             }
+            float sc = p.scale2 * __uint_as_float((uint32_t)(e - 14) << 23);
+            if (bad) sc = NAN;
             sum_q += __shfl_xor_sync(0xffffffffu, sum_q, 1);
             sum_q += __shfl_xor_sync(0xffffffffu, sum_q, 2);
-            qsum[n][0] = __shfl_sync(0xffffffffu, sum_q, 8 * i4);      // of columns 2 i4 and 2 i4 + 1
-            qsum[n][1] = __shfl_sync(0xffffffffu, sum_q, 8 * i4 + 4);
+            off_q += __shfl_xor_sync(0xffffffffu, off_q, 1);
+            off_q += __shfl_xor_sync(0xffffffffu, off_q, 2);
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                qsum[n][c] = __shfl_sync(0xffffffffu, sum_q, 8 * i4 + 4 * c) * __shfl_sync(0xffffffffu, sc, 8 * i4 + 4 * c);
+                qoff[n][c] = __shfl_sync(0xffffffffu, off_q, 8 * i4 + 4 * c);
+                qscale[n][c] = __shfl_sync(0xffffffffu, sc, 8 * i4 + 4 * c);
+            }
         }
         if (NT > 1) __syncthreads();
         float m[NT][2], l[NT][2], w[NT][2], o[NT][D / 16][4];
@@ -291,11 +316,12 @@ attention_split(const split_params p)
                 const float ks = __uint_as_float(kw << 16), kl = __uint_as_float(kw & 0xffff0000u);
                 const float vs = __uint_as_float(vw << 16), vl = __uint_as_float(vw & 0xffff0000u);
                 const bool on = pos < seq.len && ((there >> (lane / KV_BLOCK)) & 1u);
-                const float inv = __frcp_rn(vs);
+                float inv;
+                asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(vs));
                 // (positions of nobody: whatever their bytes are, NaN among them, weight 0 and finite terms.  A value vector that is
                 // no number makes the rows that see it NaN by way of their scores: a weight of 0 times NaN would reach the others)
                 const bool bad = !(fabsf(vl) < INFINITY) || !(vs < INFINITY);
-                sh.words[warp][lane] = on ? make_float4(ks * p.scale2, bad ? NAN : fmaf(-128.0f, ks, kl) * p.scale2, lg2(vs), inv) : make_float4(0.0f, 0.0f, -INFINITY, 0.0f);
+                sh.words[warp][lane] = on ? make_float4(ks, bad ? NAN : kl, lg2(vs), inv) : make_float4(0.0f, 0.0f, -INFINITY, 0.0f);
                 sh.lows[warp][lane] = on && !bad ? fmaf(vl, inv, 8.0f) : 0.0f;
             }
             __syncwarp();
@@ -316,19 +342,21 @@ attention_split(const split_params p)
                     *reinterpret_cast<uint2 *>(cb) = *reinterpret_cast<const uint2 *>(rows_k + 8 * (D / 2));
                 }
 #pragma unroll
-                for (int n = 0; n < NT; ++n) x[n][k][0] = x[n][k][1] = x[n][k][2] = x[n][k][3] = 0.0f;
-#pragma unroll
-                for (int jw = 0; jw < KW; ++jw)
+                for (int jw = 0; jw < KW; ++jw) {
+                    const uint32_t ha = ca[jw] >> 8, hb = cb[jw] >> 8;
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
-                        const uint32_t a0 = and_or(ca[jw] >> (8 * half), 0x000f000fu, 0x43004300u), a2 = and_or(ca[jw] >> (8 * half + 4), 0x000f000fu, 0x43004300u);
-                        const uint32_t a1 = and_or(cb[jw] >> (8 * half), 0x000f000fu, 0x43004300u), a3 = and_or(cb[jw] >> (8 * half + 4), 0x000f000fu, 0x43004300u);
+                        const uint32_t za = half ? ha : ca[jw], zb = half ? hb : cb[jw];
+                        const uint32_t a0 = and_or(za, 0x000f000fu, 0x64006400u), a2 = and_or(za, 0x00f000f0u, 0x64006400u);
+                        const uint32_t a1 = and_or(zb, 0x000f000fu, 0x64006400u), a3 = and_or(zb, 0x00f000f0u, 0x64006400u);
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
                             const uint2 f = NT == 1 ? qf[2 * jw + half] : sh.q[(n * (D / 16) + 2 * jw + half) * 32 + lane];
-                            mma_bf16(x[n][k], a0, a1, a2, a3, f.x, f.y);
+                            if (jw == 0 && half == 0) mma(x[n][k], a0, a1, a2, a3, f.x, f.y, qoff[n][0], qoff[n][1], qoff[n][0], qoff[n][1]);
+                            else mma(x[n][k], a0, a1, a2, a3, f.x, f.y, x[n][k][0], x[n][k][1], x[n][k][2], x[n][k][3]);
                         }
                     }
+                }
             }
             float4 wd[2][2];
             float lw[2][2];
@@ -353,7 +381,7 @@ attention_split(const split_params p)
                     for (int k = 0; k < 2; ++k)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            float y = fmaf(x[n][k][2 * e + c], wd[k][e].x, fmaf(qsum[n][c], wd[k][e].y, wd[k][e].z));
+                            float y = fmaf(x[n][k][2 * e + c], wd[k][e].x * qscale[n][c], fmaf(qsum[n][c], wd[k][e].y, wd[k][e].z));
                             if (!all) {
                                 const int pos = base + k * KV_BLOCK + (g >> 1) + 4 * (g & 1) + 8 * e, at = p0 + (8 * n + 2 * i4 + c) / p.group;
                                 const bool see = pos <= at && (p.c.window == 0 || pos > at - p.c.window || pos < p.c.n_first);
@@ -365,8 +393,8 @@ attention_split(const split_params p)
                     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
                     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
                     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-                    const float from = top == -INFINITY ? 0.0f : top;
-                    alpha[n][c] = ex2(m[n][c] - from);
+                    const float from = (top == -INFINITY ? 0.0f : top) - 12.0f;
+                    alpha[n][c] = ex2(m[n][c] - from - 12.0f);
                     m[n][c] = top;
                     l[n][c] *= alpha[n][c];
                     w[n][c] *= alpha[n][c];
@@ -375,7 +403,7 @@ attention_split(const split_params p)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
                             // 2^12 P: FP16 then holds P down to 2^-26 with all its bits (all sums carry the factor)
-                            const float pr = ex2(x[n][k][2 * e + c] - from + 12.0f);
+                            const float pr = ex2(x[n][k][2 * e + c] - from);
                             x[n][k][2 * e + c] = pr;
                             l[n][c] = fmaf(pr, wd[k][e].w, l[n][c]);
                             w[n][c] = fmaf(pr, lw[k][e], w[n][c]);
@@ -393,9 +421,8 @@ attention_split(const split_params p)
             float start[NT][4];
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                start[n][0] = start[n][1] = start[n][2] = start[n][3] = 0.0f;
-#pragma unroll
-                for (int k = 0; k < 2; ++k) mma_f16(start[n], 0xe480e480u, 0xe480e480u, 0xe480e480u, 0xe480e480u, pf[n][k][0], pf[n][k][1]);
+                mma(start[n], 0xe480e480u, 0xe480e480u, 0xe480e480u, 0xe480e480u, pf[n][0][0], pf[n][0][1], 0.0f, 0.0f, 0.0f, 0.0f);
+                mma(start[n], 0xe480e480u, 0xe480e480u, 0xe480e480u, 0xe480e480u, pf[n][1][0], pf[n][1][1], start[n][0], start[n][1], start[n][2], start[n][3]);
             }
 #pragma unroll
             for (int jw = 0; jw < D / 64; ++jw) {
@@ -413,8 +440,6 @@ attention_split(const split_params p)
                 for (int q = 0; q < 4; ++q) {  // codes 2q, 2q + 1 of the word
                     float acc[NT][4];
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) acc[n][0] = start[n][0], acc[n][1] = start[n][1], acc[n][2] = start[n][0], acc[n][3] = start[n][1];
-#pragma unroll
                     for (int k = 0; k < 2; ++k) {
                         uint32_t a[2][2];  // [code][e]
 #pragma unroll
@@ -424,7 +449,10 @@ attention_split(const split_params p)
                             a[1][e] = and_or(q & 1 ? z >> 8 : z, 0x00f000f0u, 0x64006400u);
                         }
 #pragma unroll
-                        for (int n = 0; n < NT; ++n) mma_f16(acc[n], a[0][0], a[1][0], a[0][1], a[1][1], pf[n][k][0], pf[n][k][1]);
+                        for (int n = 0; n < NT; ++n) {
+                            if (k == 0) mma(acc[n], a[0][0], a[1][0], a[0][1], a[1][1], pf[n][0][0], pf[n][0][1], start[n][0], start[n][1], start[n][0], start[n][1]);
+                            else mma(acc[n], a[0][0], a[1][0], a[0][1], a[1][1], pf[n][1][0], pf[n][1][1], acc[n][0], acc[n][1], acc[n][2], acc[n][3]);
+                        }
                     }
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
