@@ -12,9 +12,9 @@
 // (0x6400 | c) is 1024 + c, in bits 4 .. 7 (0x6400 | 16 c) it is 16 (64 + c), both exact; the sums of offsets are what the
 // accumulators start from.  The keys use both forms, with a 16th of the row's value for the second one (a row has a power of two
 // of its own that makes its BF16 values FP16 ones).  The values use the second form alone, whose offset is small beside the
-// codes: their 72 x 16 = 1152 is taken off by one more product, of P with a constant, from which the sums of 32 positions start:
+// codes: their 72 x 16 = 1152 is taken off by one more product, of P with a constant, from which the sums of a chunk start:
 // they are sums of P (e - 8), and what is added up in binary32 over a whole sequence has no common offset to lose digits to.  P is
-// rounded to FP16 (11 bits; below 2^-26 of the largest one, with fewer), Q and the codes are exact.
+// rounded to FP16 (11 bits; below 2^-21 of the largest one, with fewer), Q and the codes are exact.
 //
 // Operands.  Rows (query heads of one key head x new positions) are the 8 columns of an m16n8k16 product, positions (for the
 // values: a head's values) its 16 rows, so that 8 query heads per key head leave nothing of the instruction unused.  The scores come
@@ -24,10 +24,10 @@
 // tcgen05 tile, and what bounds this kernel is the memory that the codes come from and the instructions that unpack them
 // (about 190 per warp and 16 positions of 2176 bytes).
 //
-// Work.  The positions of all sequences and key heads are cut into tiles of 128 and dealt out evenly, in order, to as many
+// Work.  The positions of all sequences and key heads are cut into tiles of 256 (128 for more than 8 rows) and dealt out evenly, in order, to as many
 // blocks as the GPU holds at a time, whatever the lengths are (a graph with this call replays for others).  A block whose
 // run begins or ends inside a (sequence, key head) leaves a partial result, at most two in all; attention_join puts them
-// together.  A warp takes 32 of a tile's 128 positions, by itself: its copies (16 positions = one
+// together.  A warp takes a quarter of a tile, by itself: its copies (16 positions = one
 // contiguous block of the cache), its barriers, its running maximum; the warps meet at the end of a (sequence, key head).
 #include "kv_internal.h"
 
@@ -36,27 +36,32 @@
 
 namespace {
 
-constexpr int TILE = 128, WARPS = 4, CHUNK = TILE / WARPS;  // positions of a tile, of a warp's share
-constexpr int MAX_ROWS = 32;                                // rows (new positions x query heads of a key head) of this kernel
+constexpr int WARPS = 4;
+constexpr int MAX_ROWS = 32;  // rows (new positions x query heads of a key head) of this kernel
 
-// NT: groups of 8 rows.  Blocks of an SM: what registers (32 NT sums and as much besides) allow.
-__host__ __device__ constexpr int stages(int D, int NT) { return D == 64 || NT == 4 ? 4 : 3; }
-__host__ __device__ constexpr int blocks_per_sm(int NT) { return NT == 1 ? 4 : NT == 2 ? 3 : 2; }
-__host__ __device__ constexpr int chunk_bytes(int D) { return CHUNK / KV_BLOCK * kv_block_bytes(D); }
-// floats of a partial result: rows x (sums of D values, maximum, normaliser), rows padded to 16 bytes
+// NT: groups of 8 rows.  Blocks of 16 positions that a warp takes at a time: what is done once for them (the copies' bookkeeping, the
+// maxima, adding the sums up) costs less the more they are; four where registers allow.  Stages of a warp's ring and blocks of an SM: what
+// shared memory and registers (32 NT sums and as much besides) allow.
+__host__ __device__ constexpr int chunk_blocks(int NT) { return NT == 1 ? 4 : 2; }
+__host__ __device__ constexpr int chunk(int NT) { return KV_BLOCK * chunk_blocks(NT); }
+__host__ __device__ constexpr int tile(int NT) { return WARPS * chunk(NT); }  // positions of a tile: a chunk of each warp
+__host__ __device__ constexpr int stages(int D, int NT) { return NT == 1 ? (D == 64 ? 3 : 2) : D == 64 || NT == 4 ? 4 : 3; }
+__host__ __device__ constexpr int blocks_per_sm(int NT) { return NT == 1 ? 3 : NT == 2 ? 3 : 2; }
+__host__ __device__ constexpr int chunk_bytes(int D, int NT) { return chunk_blocks(NT) * kv_block_bytes(D); }
+// floats of a partial result's row: sums of D values, maximum, normaliser, padded to 16 bytes
 __host__ __device__ constexpr int part_row(int D) { return D + 4; }
 
 template <int D, int NT>
 struct Shared {
-    uint8_t ring[WARPS][stages(D, NT)][chunk_bytes(D)];  // (at a segment's end, a warp's sums: [8 NT][D + 4] floats)
-    float4 words[WARPS][CHUNK];                          // per position: key step and offset, log2 of the value step, its reciprocal
-    float lows[WARPS][CHUNK];                            // (value low) / (value step) + 8
-    uint2 q[NT == 1 ? 1 : NT * (D / 16) * 32];           // (NT > 1) the rows as operands
+    uint8_t ring[WARPS][stages(D, NT)][chunk_bytes(D, NT)];  // (at a segment's end, a warp's sums: [8 NT][D + 4] floats)
+    float4 words[WARPS][chunk(NT)];                          // per position: key step and low, log2 of the value step, its reciprocal
+    float lows[WARPS][chunk(NT)];                            // (value low) / (value step) + 8
+    uint2 q[NT == 1 ? 1 : NT * (D / 16) * 32];               // (NT > 1) the rows as operands
     float m[WARPS][8 * NT], l[WARPS][8 * NT];
     uint64_t full[WARPS][stages(D, NT)];
-    uint32_t there[WARPS][stages(D, NT)];                // bit b: block b of the chunk was copied
+    uint32_t there[WARPS][stages(D, NT)];                    // bit b: block b of the chunk was copied
     int scan[WARPS];
-    int begin[3];                                        // where the block's run begins: sequence, tile of that sequence; length of a run
+    int begin[2];                                            // where the block's run begins: sequence, tile of that sequence
 };
 
 struct split_params {
@@ -67,6 +72,8 @@ struct split_params {
     float scale2;   // scale * log2(e)
     int group;      // query heads of a key head
 };
+
+constexpr float NONE = -1e30f;  // m of rows that have seen nothing: below every score, and finite, so that differences are numbers
 
 __device__ __forceinline__ float ex2(float x)
 {
@@ -104,19 +111,19 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x)
 struct tiles_of {
     int first, from, count;
 };
-__device__ __forceinline__ tiles_of visible_tiles(const kv_seq &s, const kv_attention_call &c, int group)
+__device__ __forceinline__ tiles_of visible_tiles(const kv_seq &s, const kv_attention_call &c, int group, int tile)
 {
     tiles_of t{0, 0, 0};
     if (s.n <= 0 || s.n * group > MAX_ROWS) return t;
     if (c.window) {
         const int from = s.len - s.n - c.window + 1;  // of the first row
         if (from > 0) {
-            t.from = from / TILE;
-            const int first = ((c.n_first < from ? c.n_first : from) + TILE - 1) / TILE;
+            t.from = from / tile;
+            const int first = ((c.n_first < from ? c.n_first : from) + tile - 1) / tile;
             t.first = first < t.from ? first : t.from;
         }
     }
-    t.count = t.first + (s.len + TILE - 1) / TILE - t.from;
+    t.count = t.first + (s.len + tile - 1) / tile - t.from;
     return t;
 }
 
@@ -124,7 +131,8 @@ template <int D, int NT>
 __global__ void __launch_bounds__(WARPS * 32, blocks_per_sm(NT))
 attention_split(const split_params p)
 {
-    constexpr int NS = stages(D, NT), R = 8 * NT, KW = D / 32;  // KW: words of a key row that a lane reads
+    constexpr int NS = stages(D, NT), R = 8 * NT, C = chunk_blocks(NT), CHUNK = chunk(NT), TILE = tile(NT);
+    constexpr int KW = D / 32;  // words of a key row that a lane reads
     extern __shared__ __align__(16) uint8_t raw[];
     Shared<D, NT> &sh = *reinterpret_cast<Shared<D, NT> *>(raw);
     const kv_batch &b = p.b;
@@ -139,7 +147,7 @@ attention_split(const split_params p)
     const int per = (b.n_seqs + WARPS * 32 - 1) / (WARPS * 32);
     const int s0 = tid * per, s1 = s0 + per < b.n_seqs ? s0 + per : b.n_seqs;
     int64_t want = 0;
-    for (int s = s0; s < s1; ++s) want += (int64_t)visible_tiles(kv_load_seq(b, s), p.c, p.group).count * b.n_kv_heads;
+    for (int s = s0; s < s1; ++s) want += (int64_t)visible_tiles(kv_load_seq(b, s), p.c, p.group, tile(NT)).count * b.n_kv_heads;
     if (want >= 1 << 23) {  // (2^30 positions of key heads in a 128th of the sequences: the sums below are in 32 bits)
         kv_report(b);
         want = 0;
@@ -168,7 +176,7 @@ attention_split(const split_params p)
     if (unit >= before && unit < before + mine) {
         int off = unit - before, s = s0;
         for (;; ++s) {
-            const int n = visible_tiles(kv_load_seq(b, s), p.c, p.group).count * b.n_kv_heads;
+            const int n = visible_tiles(kv_load_seq(b, s), p.c, p.group, tile(NT)).count * b.n_kv_heads;
             if (off < n) break;
             off -= n;
         }
@@ -184,7 +192,7 @@ attention_split(const split_params p)
 
     while (unit < unit_end) {
         const kv_seq seq = kv_load_seq(b, s);
-        const tiles_of tl = visible_tiles(seq, p.c, p.group);
+        const tiles_of tl = visible_tiles(seq, p.c, p.group, tile(NT));
         if (tl.count == 0 || off >= tl.count * b.n_kv_heads) {
             off -= tl.count * b.n_kv_heads;
             ++s;
@@ -253,22 +261,23 @@ attention_split(const split_params p)
             }
         }
         if (NT > 1) __syncthreads();
+        // m: 2^-7 of the running maximum's power, as an exponent (P = 2^(y - m) <= 2^15: below)
         float m[NT][2], l[NT][2], w[NT][2], o[NT][D / 16][4];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
 #pragma unroll
-            for (int k = 0; k < 2; ++k) m[n][k] = -INFINITY, l[n][k] = 0.0f, w[n][k] = 0.0f;
+            for (int k = 0; k < 2; ++k) m[n][k] = NONE, l[n][k] = 0.0f, w[n][k] = 0.0f;
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) o[n][k][0] = o[n][k][1] = o[n][k][2] = o[n][k][3] = 0.0f;
         }
 
-        // ---- copies: chunk j of the segment, block lane (0 or 1) of it
+        // ---- copies: chunk j of the segment, block `lane` (below C) of it
         auto base_of = [&](int j) {
             const int t = t0 + j;
             return (t < tl.first ? t : tl.from + t - tl.first) * TILE + warp * CHUNK;
         };
         auto page_of = [&](int j) {  // page of this lane's block of chunk j, -1: none to copy
-            if (j >= nt || lane > 1) return -1;
+            if (j >= nt || lane >= C) return -1;
             const int pos = base_of(j) + lane * KV_BLOCK;
             if (pos >= seq.len) return -1;
             if (p.c.window && pos >= p.c.n_first && pos + KV_BLOCK <= p0 - p.c.window + 1) return -1;  // no row sees it
@@ -280,7 +289,7 @@ attention_split(const split_params p)
         auto issue = [&](int j, int page) {
             const int st = (phase + j) % NS;
             const uint32_t bar = smem_u32(&sh.full[warp][st]);
-            const uint32_t there = __ballot_sync(0xffffffffu, page >= 0) & 3u;
+            const uint32_t there = __ballot_sync(0xffffffffu, page >= 0);
             issued = phase + j + 1;
             if (lane == 0) {
                 sh.there[warp][st] = there;
@@ -309,27 +318,28 @@ attention_split(const split_params p)
             const int base = base_of(j);
             const uint32_t there = sh.there[warp][st];
             if (there == 0) continue;
-            {   // lane <-> position: what its words say
-                const int pos = base + lane;
-                const uint32_t *ws = reinterpret_cast<const uint32_t *>(chunk + (lane / KV_BLOCK) * kv_block_bytes(D)) + lane % KV_BLOCK;
+#pragma unroll
+            for (int at = lane; at < CHUNK; at += 32) {  // a position: what its words say
+                const int pos = base + at;
+                const uint32_t *ws = reinterpret_cast<const uint32_t *>(chunk + (at / KV_BLOCK) * kv_block_bytes(D)) + at % KV_BLOCK;
                 const uint32_t kw = ws[kv_k_words(D) / 4], vw = ws[kv_v_words(D) / 4];
                 const float ks = __uint_as_float(kw << 16), kl = __uint_as_float(kw & 0xffff0000u);
                 const float vs = __uint_as_float(vw << 16), vl = __uint_as_float(vw & 0xffff0000u);
-                const bool on = pos < seq.len && ((there >> (lane / KV_BLOCK)) & 1u);
+                const bool on = pos < seq.len && ((there >> (at / KV_BLOCK)) & 1u);
                 float inv;
                 asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(vs));
                 // (positions of nobody: whatever their bytes are, NaN among them, weight 0 and finite terms.  A value vector that is
                 // no number makes the rows that see it NaN by way of their scores: a weight of 0 times NaN would reach the others)
                 const bool bad = !(fabsf(vl) < INFINITY) || !(vs < INFINITY);
-                sh.words[warp][lane] = on ? make_float4(ks, bad ? NAN : kl, lg2(vs), inv) : make_float4(0.0f, 0.0f, -INFINITY, 0.0f);
-                sh.lows[warp][lane] = on && !bad ? fmaf(vl, inv, 8.0f) : 0.0f;
+                sh.words[warp][at] = on ? make_float4(ks, bad ? NAN : kl, lg2(vs), inv) : make_float4(0.0f, 0.0f, -INFINITY, 0.0f);
+                sh.lows[warp][at] = on && !bad ? fmaf(vl, inv, 8.0f) : 0.0f;
             }
             __syncwarp();
 
-            // ---- scores of 32 positions: x[n][block][position half][column]
-            float x[NT][2][4];
+            // ---- scores: x[n][block][2 x position half + column]
+            float x[NT][C][4];
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
+            for (int k = 0; k < C; ++k) {
                 // position of row r of the product: (r >> 1) + 4 (r & 1), and 8 more for rows 8 .. 15 (the values' reads below
                 // then hit few banks twice)
                 const uint8_t *rows_k = chunk + k * kv_block_bytes(D) + ((g >> 1) + 4 * (g & 1)) * (D / 2) + 4 * KW * i4;
@@ -358,77 +368,90 @@ attention_split(const split_params p)
                     }
                 }
             }
-            float4 wd[2][2];
-            float lw[2][2];
-#pragma unroll
-            for (int k = 0; k < 2; ++k)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int at = k * KV_BLOCK + (g >> 1) + 4 * (g & 1) + 8 * e;
-                    wd[k][e] = sh.words[warp][at];
-                    lw[k][e] = sh.lows[warp][at];
-                }
             // every row sees every position of the chunk (that there is)?
             const bool all = base + CHUNK - 1 <= p0 && (p.c.window == 0 || base > seq.len - 1 - p.c.window || base + CHUNK <= p.c.n_first);
-            uint32_t pf[NT][2][2];
-            float alpha[NT][2];
+            auto at_of = [&](int k, int e) { return k * KV_BLOCK + (g >> 1) + 4 * (g & 1) + 8 * e; };
+            float top[NT][2];
+            bool more = false;
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
+            for (int n = 0; n < NT; ++n) top[n][0] = top[n][1] = -INFINITY;
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    float top = m[n][c];
+            for (int k = 0; k < C; ++k)
 #pragma unroll
-                    for (int k = 0; k < 2; ++k)
+                for (int e = 0; e < 2; ++e) {
+                    const float4 wd = sh.words[warp][at_of(k, e)];
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            float y = fmaf(x[n][k][2 * e + c], wd[k][e].x * qscale[n][c], fmaf(qsum[n][c], wd[k][e].y, wd[k][e].z));
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+                            float y = fmaf(x[n][k][2 * e + c], wd.x * qscale[n][c], fmaf(qsum[n][c], wd.y, wd.z));
                             if (!all) {
-                                const int pos = base + k * KV_BLOCK + (g >> 1) + 4 * (g & 1) + 8 * e, at = p0 + (8 * n + 2 * i4 + c) / p.group;
+                                const int pos = base + at_of(k, e), at = p0 + (8 * n + 2 * i4 + c) / p.group;
                                 const bool see = pos <= at && (p.c.window == 0 || pos > at - p.c.window || pos < p.c.n_first);
                                 if (!see) y = -INFINITY;
                             }
                             x[n][k][2 * e + c] = y;
-                            top = fmaxf(top, y);
-                        }
-                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
-                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
-                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-                    const float from = (top == -INFINITY ? 0.0f : top) - 12.0f;
-                    alpha[n][c] = ex2(m[n][c] - from - 12.0f);
-                    m[n][c] = top;
-                    l[n][c] *= alpha[n][c];
-                    w[n][c] *= alpha[n][c];
-#pragma unroll
-                    for (int k = 0; k < 2; ++k)
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            // 2^12 P: FP16 then holds P down to 2^-26 with all its bits (all sums carry the factor)
-                            const float pr = ex2(x[n][k][2 * e + c] - from);
-                            x[n][k][2 * e + c] = pr;
-                            l[n][c] = fmaf(pr, wd[k][e].w, l[n][c]);
-                            w[n][c] = fmaf(pr, lw[k][e], w[n][c]);
+                            top[n][c] = fmaxf(top[n][c], y);
                         }
                 }
+            // m moves only where a column's maximum has grown by more than 2^8
 #pragma unroll
-                for (int k = 0; k < 2; ++k)
+            for (int n = 0; n < NT; ++n) more = more || top[n][0] > m[n][0] + 15.0f || top[n][1] > m[n][1] + 15.0f;
+            if (__any_sync(0xffffffffu, more)) {
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const __half2 h = __floats2half2_rn(x[n][k][2 * e], x[n][k][2 * e + 1]);
+                for (int n = 0; n < NT; ++n) {
+                    float alpha[2];
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        float t = top[n][c];
+                        t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 4));
+                        t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 8));
+                        t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 16));
+                        t = fmaxf(t - 7.0f, m[n][c]);
+                        alpha[c] = ex2(m[n][c] - t);
+                        m[n][c] = t;
+                        l[n][c] *= alpha[c];
+                        w[n][c] *= alpha[c];
+                    }
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[n][k][e] *= alpha[e & 1];
+                }
+            }
+            uint32_t pf[NT][C][2];
+#pragma unroll
+            for (int k = 0; k < C; ++k)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float inv = sh.words[warp][at_of(k, e)].w, low = sh.lows[warp][at_of(k, e)];
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        float pr[2];
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+                            pr[c] = ex2(x[n][k][2 * e + c] - m[n][c]);
+                            l[n][c] = fmaf(pr[c], inv, l[n][c]);
+                            w[n][c] = fmaf(pr[c], low, w[n][c]);
+                        }
+                        const __half2 h = __floats2half2_rn(pr[0], pr[1]);
                         pf[n][k][e] = transposed(*reinterpret_cast<const uint32_t *>(&h));
                     }
-            }
+                }
             // ---- values: -1152 sum of P first, then the codes
             float start[NT][4];
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 mma(start[n], 0xe480e480u, 0xe480e480u, 0xe480e480u, 0xe480e480u, pf[n][0][0], pf[n][0][1], 0.0f, 0.0f, 0.0f, 0.0f);
-                mma(start[n], 0xe480e480u, 0xe480e480u, 0xe480e480u, 0xe480e480u, pf[n][1][0], pf[n][1][1], start[n][0], start[n][1], start[n][2], start[n][3]);
+#pragma unroll
+                for (int k = 1; k < C; ++k)
+                    mma(start[n], 0xe480e480u, 0xe480e480u, 0xe480e480u, 0xe480e480u, pf[n][k][0], pf[n][k][1], start[n][0], start[n][1], start[n][2], start[n][3]);
             }
 #pragma unroll
             for (int jw = 0; jw < D / 64; ++jw) {
-                uint32_t lo[2][2], hi[2][2];  // of block k: positions i4, i4 + 4 (e = 0) and i4 + 8, i4 + 12 (e = 1); codes 0-3 and 4-7 of both
+                uint32_t lo[C][2], hi[C][2];  // of block k: positions i4, i4 + 4 (e = 0) and i4 + 8, i4 + 12 (e = 1); codes 0-3 and 4-7 of both
 #pragma unroll
-                for (int k = 0; k < 2; ++k)
+                for (int k = 0; k < C; ++k)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const uint8_t *row = chunk + k * kv_block_bytes(D) + kv_v_codes(D) + (i4 + 8 * e) * (D / 2) + (D / 16) * g + 4 * jw;
@@ -440,7 +463,7 @@ attention_split(const split_params p)
                 for (int q = 0; q < 4; ++q) {  // codes 2q, 2q + 1 of the word
                     float acc[NT][4];
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) {
+                    for (int k = 0; k < C; ++k) {
                         uint32_t a[2][2];  // [code][e]
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
@@ -451,13 +474,13 @@ attention_split(const split_params p)
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
                             if (k == 0) mma(acc[n], a[0][0], a[1][0], a[0][1], a[1][1], pf[n][0][0], pf[n][0][1], start[n][0], start[n][1], start[n][0], start[n][1]);
-                            else mma(acc[n], a[0][0], a[1][0], a[0][1], a[1][1], pf[n][1][0], pf[n][1][1], acc[n][0], acc[n][1], acc[n][2], acc[n][3]);
+                            else mma(acc[n], a[0][0], a[1][0], a[0][1], a[1][1], pf[n][k][0], pf[n][k][1], acc[n][0], acc[n][1], acc[n][2], acc[n][3]);
                         }
                     }
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) o[n][4 * jw + q][e] = fmaf(o[n][4 * jw + q][e], alpha[n][e & 1], acc[n][e]);
+                        for (int e = 0; e < 4; ++e) o[n][4 * jw + q][e] += acc[n][e];
                 }
             }
         }
@@ -498,14 +521,13 @@ attention_split(const split_params p)
         for (int at = tid; at < R * (D / 8); at += WARPS * 32) {
             const int r = at / (D / 8), d = at % (D / 8) * 8;
             if (r >= rows) break;
-            float top = -INFINITY;
+            float top = NONE;
 #pragma unroll
             for (int v = 0; v < WARPS; ++v) top = fmaxf(top, sh.m[v][r]);
-            const float from = top == -INFINITY ? 0.0f : top;
             float sum_l = 0.0f, y[8] = {};
 #pragma unroll
             for (int v = 0; v < WARPS; ++v) {
-                const float f = ex2(sh.m[v][r] - from);
+                const float f = ex2(sh.m[v][r] - top);
                 sum_l = fmaf(sh.l[v][r], f, sum_l);
                 const float4 *z = reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(sh.ring[v][0]) + r * (D + 4) + d);
                 const float4 z0 = z[0], z1 = z[1];
@@ -556,14 +578,14 @@ attention_join(const split_params p)
     const int4 head = p.headers[blockIdx.x];  // parts, first row of the sequence, rows, key head
     const int r = blockIdx.y, lane = threadIdx.x % LANES, grp = threadIdx.x / LANES;
     if (head.x == 0 || r >= head.z) return;
-    float m = -INFINITY, l = 0.0f;
+    float m = NONE, l = 0.0f;
     float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     for (int i = grp; i < head.x; i += GROUPS) {
         // the first part is this run's last result, the others are the following runs' first
         const float *part = p.parts + (((int64_t)blockIdx.x + i) * 2 + (i == 0 ? 1 : 0)) * (8 * NT) * part_row(D) + r * part_row(D);
         const float2 v = __ldcg(reinterpret_cast<const float2 *>(part + D));
         const float4 z = __ldcg(reinterpret_cast<const float4 *>(part) + lane);
-        const float top = fmaxf(m, v.x), from = top == -INFINITY ? 0.0f : top, a = ex2(m - from), f = ex2(v.x - from);
+        const float top = fmaxf(m, v.x), a = ex2(m - top), f = ex2(v.x - top);
         m = top;
         l = fmaf(v.y, f, l * a);
         o = make_float4(fmaf(z.x, f, o.x * a), fmaf(z.y, f, o.y * a), fmaf(z.z, f, o.z * a), fmaf(z.w, f, o.w * a));
@@ -572,14 +594,13 @@ attention_join(const split_params p)
     if (lane == 0) ml[grp] = make_float2(m, l);
     __syncthreads();
     if (grp != 0) return;
-    float top = -INFINITY, sum_l = 0.0f;
+    float top = NONE, sum_l = 0.0f;
 #pragma unroll
     for (int v = 0; v < GROUPS; ++v) top = fmaxf(top, ml[v].x);
-    const float from = top == -INFINITY ? 0.0f : top;
     float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
     for (int v = 0; v < GROUPS; ++v) {
-        const float f = ex2(ml[v].x - from);
+        const float f = ex2(ml[v].x - top);
         const float4 z = sums[v][lane];
         sum_l = fmaf(ml[v].y, f, sum_l);
         y = make_float4(fmaf(z.x, f, y.x), fmaf(z.y, f, y.y), fmaf(z.z, f, y.z), fmaf(z.w, f, y.w));
@@ -598,7 +619,7 @@ template <int D, int NT>
 cudaError_t launch_split(const split_params &p, int sm_count, cudaStream_t st, int64_t *launches)
 {
     constexpr size_t smem = sizeof(Shared<D, NT>);
-    static_assert(8 * NT * (D + 4) * 4 <= stages(D, NT) * chunk_bytes(D), "a warp's sums fit its ring");
+    static_assert(8 * NT * (D + 4) * 4 <= stages(D, NT) * chunk_bytes(D, NT), "a warp's sums fit its ring");
     cudaError_t e = cudaFuncSetAttribute(attention_split<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
     const int blocks = sm_count * blocks_per_sm(NT);
