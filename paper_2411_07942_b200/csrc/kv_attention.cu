@@ -37,7 +37,7 @@
 namespace {
 
 constexpr int WARPS = 4;
-constexpr int MAX_ROWS = 32;  // rows (new positions x query heads of a key head) of this kernel
+constexpr int MAX_ROWS = 32;  // rows (new positions x query heads of a key head) of a sequence here: in groups of 8 NT, one after the other
 
 // NT: groups of 8 rows.  Blocks of 16 positions that a warp takes at a time: what is done once for them (the copies' bookkeeping, the
 // maxima, adding the sums up) costs less the more they are; four where registers allow.  Stages of a warp's ring and blocks of an SM: what
@@ -45,8 +45,8 @@ constexpr int MAX_ROWS = 32;  // rows (new positions x query heads of a key head
 __host__ __device__ constexpr int chunk_blocks(int NT) { return NT == 1 ? 4 : 2; }
 __host__ __device__ constexpr int chunk(int NT) { return KV_BLOCK * chunk_blocks(NT); }
 __host__ __device__ constexpr int tile(int NT) { return WARPS * chunk(NT); }  // positions of a tile: a chunk of each warp
-__host__ __device__ constexpr int stages(int D, int NT) { return NT == 1 ? (D == 64 ? 3 : 2) : D == 64 || NT == 4 ? 4 : 3; }
-__host__ __device__ constexpr int blocks_per_sm(int NT) { return NT == 1 ? 3 : NT == 2 ? 3 : 2; }
+__host__ __device__ constexpr int stages(int D, int NT) { return NT == 1 ? (D == 64 ? 3 : 2) : D == 64 ? 4 : 3; }
+constexpr int BLOCKS_PER_SM = 3;
 __host__ __device__ constexpr int chunk_bytes(int D, int NT) { return chunk_blocks(NT) * kv_block_bytes(D); }
 // floats of a partial result's row: sums of D values, maximum, normaliser, padded to 16 bytes
 __host__ __device__ constexpr int part_row(int D) { return D + 4; }
@@ -68,7 +68,7 @@ struct split_params {
     kv_batch b;
     kv_attention_call c;
     float *parts;   // [blocks][2][8 NT][part_row]
-    int4 *headers;  // [blocks]: of the part that the block's run ends with: parts of its (sequence, key head), first row, rows, key head
+    int4 *headers;  // [blocks]: of the part that the block's run ends with: parts in all, the sequence's first row, first row and rows, key head
     float scale2;   // scale * log2(e)
     int group;      // query heads of a key head
 };
@@ -107,13 +107,13 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x)
     return r;
 }
 
-// Tiles of a sequence that any of its rows sees: [0, first) and [from, end).
+// Tiles of a sequence that any of its rows sees: [0, first) and [from, end); its groups of rows.
 struct tiles_of {
-    int first, from, count;
+    int first, from, count, groups;
 };
-__device__ __forceinline__ tiles_of visible_tiles(const kv_seq &s, const kv_attention_call &c, int group, int tile)
+__device__ __forceinline__ tiles_of visible_tiles(const kv_seq &s, const kv_attention_call &c, int group, int tile, int rows)
 {
-    tiles_of t{0, 0, 0};
+    tiles_of t{0, 0, 0, 0};
     if (s.n <= 0 || s.n * group > MAX_ROWS) return t;
     if (c.window) {
         const int from = s.len - s.n - c.window + 1;  // of the first row
@@ -124,11 +124,12 @@ __device__ __forceinline__ tiles_of visible_tiles(const kv_seq &s, const kv_atte
         }
     }
     t.count = t.first + (s.len + tile - 1) / tile - t.from;
+    t.groups = rows == 8 ? 1 : (s.n * group + rows - 1) / rows;  // (groups of 8 are for sequences that have no more)
     return t;
 }
 
 template <int D, int NT>
-__global__ void __launch_bounds__(WARPS * 32, blocks_per_sm(NT))
+__global__ void __launch_bounds__(WARPS * 32, BLOCKS_PER_SM)
 attention_split(const split_params p)
 {
     constexpr int NS = stages(D, NT), R = 8 * NT, C = chunk_blocks(NT), CHUNK = chunk(NT), TILE = tile(NT);
@@ -147,7 +148,10 @@ attention_split(const split_params p)
     const int per = (b.n_seqs + WARPS * 32 - 1) / (WARPS * 32);
     const int s0 = tid * per, s1 = s0 + per < b.n_seqs ? s0 + per : b.n_seqs;
     int64_t want = 0;
-    for (int s = s0; s < s1; ++s) want += (int64_t)visible_tiles(kv_load_seq(b, s), p.c, p.group, tile(NT)).count * b.n_kv_heads;
+    for (int s = s0; s < s1; ++s) {
+        const tiles_of t = visible_tiles(kv_load_seq(b, s), p.c, p.group, tile(NT), 8 * NT);
+        want += (int64_t)t.count * t.groups * b.n_kv_heads;
+    }
     if (want >= 1 << 23) {  // (2^30 positions of key heads in a 128th of the sequences: the sums below are in 32 bits)
         kv_report(b);
         want = 0;
@@ -176,7 +180,8 @@ attention_split(const split_params p)
     if (unit >= before && unit < before + mine) {
         int off = unit - before, s = s0;
         for (;; ++s) {
-            const int n = visible_tiles(kv_load_seq(b, s), p.c, p.group, tile(NT)).count * b.n_kv_heads;
+            const tiles_of t = visible_tiles(kv_load_seq(b, s), p.c, p.group, tile(NT), 8 * NT);
+            const int n = t.count * t.groups * b.n_kv_heads;
             if (off < n) break;
             off -= n;
         }
@@ -192,15 +197,16 @@ attention_split(const split_params p)
 
     while (unit < unit_end) {
         const kv_seq seq = kv_load_seq(b, s);
-        const tiles_of tl = visible_tiles(seq, p.c, p.group, tile(NT));
-        if (tl.count == 0 || off >= tl.count * b.n_kv_heads) {
-            off -= tl.count * b.n_kv_heads;
+        const tiles_of tl = visible_tiles(seq, p.c, p.group, tile(NT), 8 * NT);
+        const int all_tiles = tl.count * tl.groups * b.n_kv_heads;
+        if (off >= all_tiles) {
+            off -= all_tiles;
             ++s;
             continue;
         }
-        const int kh = off / tl.count, t0 = off - kh * tl.count;
+        const int pair = off / tl.count, kh = NT == 1 ? pair : pair / tl.groups, row0 = NT == 1 ? 0 : (pair - kh * tl.groups) * R, t0 = off - pair * tl.count;
         const int nt = tl.count - t0 < unit_end - unit ? tl.count - t0 : unit_end - unit;
-        const int rows = seq.n * p.group, p0 = seq.len - seq.n;
+        const int rows = seq.n * p.group - row0 < R ? seq.n * p.group - row0 : R, p0 = seq.len - seq.n;
 
         // ---- the rows as operands: column n = lane / 4 of a group of 8, values 8 KW i4 .. of the head in the order (0 4)(1 5)(2 6)(3 7),
         // in FP16, scaled so that the row's largest magnitude is in [2^14, 2^15) (BF16's 8 bits stay exact down to 2^-27 of that),
@@ -209,7 +215,7 @@ attention_split(const split_params p)
         float qsum[NT][2], qoff[NT][2], qscale[NT][2];  // of columns 2 i4 and 2 i4 + 1: sum of the row; what the codes' offsets add; its scale
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const int r = 8 * n + g, tok = r / p.group, h = kh * p.group + (r - tok * p.group);
+            const int r = 8 * n + g, tok = (row0 + r) / p.group, h = kh * p.group + (row0 + r - tok * p.group);
             const uint4 *src = reinterpret_cast<const uint4 *>(p.c.q.p + (int64_t)(seq.start + tok) * p.c.q.stride + (int64_t)h * D + 8 * KW * i4);
             uint4 x[KW];
             uint32_t big = 0;
@@ -242,7 +248,7 @@ attention_split(const split_params p)
                 if (NT == 1) {
                     qf[2 * j] = f0;
                     qf[2 * j + 1] = f1;
-                } else if (n % WARPS == warp || NT == 2) {  // (every warp has them all; one stores)
+                } else if (n == warp) {  // (every warp has them all; one stores)
                     sh.q[(n * (D / 16) + 2 * j) * 32 + lane] = f0;
                     sh.q[(n * (D / 16) + 2 * j + 1) * 32 + lane] = f1;
                 }
@@ -386,7 +392,7 @@ attention_split(const split_params p)
                         for (int c = 0; c < 2; ++c) {
                             float y = fmaf(x[n][k][2 * e + c], wd.x * qscale[n][c], fmaf(qsum[n][c], wd.y, wd.z));
                             if (!all) {
-                                const int pos = base + at_of(k, e), at = p0 + (8 * n + 2 * i4 + c) / p.group;
+                                const int pos = base + at_of(k, e), at = p0 + (row0 + 8 * n + 2 * i4 + c) / p.group;
                                 const bool see = pos <= at && (p.c.window == 0 || pos > at - p.c.window || pos < p.c.n_first);
                                 if (!see) y = -INFINITY;
                             }
@@ -536,7 +542,7 @@ attention_split(const split_params p)
                 for (int k = 0; k < 8; ++k) y[k] = fmaf(zz[k], f, y[k]);
             }
             if (whole) {
-                const int tok = r / p.group, h = kh * p.group + (r - tok * p.group);
+                const int tok = (row0 + r) / p.group, h = kh * p.group + (row0 + r - tok * p.group);
                 const float inv = sum_l == 0.0f ? 0.0f : 1.0f / sum_l;
                 uint32_t u[4];
 #pragma unroll
@@ -553,7 +559,7 @@ attention_split(const split_params p)
             }
         }
         if (t0 == 0 && nt < tl.count)  // begun here, ended by a later block (share tiles each)
-            header = make_int4((int)(1 + (tl.count - nt + share - 1) / share), seq.start, rows, kh);
+            header = make_int4(1 + (tl.count - nt + share - 1) / share, seq.start, row0 << 16 | rows, kh);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the sums were written where copies go next
         __syncthreads();
         unit += nt;
@@ -566,54 +572,69 @@ attention_split(const split_params p)
     if (tid == 0) p.headers[blockIdx.x] = header;
 }
 
-// Puts the partial results of a (sequence, key head) together: block (i, row) for the one that run i ends with the first part of.
+// Puts partial results together, for the ones that run i ends with the first part of: a block takes the (run, row) pairs in turn, of
+// which most have nothing to do.
+constexpr int JOIN_PAIRS = 8;  // (their headers are loaded at once)
 template <int D, int NT>
 __global__ void __launch_bounds__(8 * D / 4)
-attention_join(const split_params p)
+attention_join(const split_params p, int runs)
 {
     constexpr int GROUPS = 8, LANES = D / 4;  // parts in flight, threads of a row
     __shared__ float4 sums[GROUPS][LANES];
     __shared__ float2 ml[GROUPS];
+    __shared__ int4 heads[JOIN_PAIRS];
     tpq_grid_dep_wait();
-    const int4 head = p.headers[blockIdx.x];  // parts, first row of the sequence, rows, key head
-    const int r = blockIdx.y, lane = threadIdx.x % LANES, grp = threadIdx.x / LANES;
-    if (head.x == 0 || r >= head.z) return;
-    float m = NONE, l = 0.0f;
-    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (int i = grp; i < head.x; i += GROUPS) {
-        // the first part is this run's last result, the others are the following runs' first
-        const float *part = p.parts + (((int64_t)blockIdx.x + i) * 2 + (i == 0 ? 1 : 0)) * (8 * NT) * part_row(D) + r * part_row(D);
-        const float2 v = __ldcg(reinterpret_cast<const float2 *>(part + D));
-        const float4 z = __ldcg(reinterpret_cast<const float4 *>(part) + lane);
-        const float top = fmaxf(m, v.x), a = ex2(m - top), f = ex2(v.x - top);
-        m = top;
-        l = fmaf(v.y, f, l * a);
-        o = make_float4(fmaf(z.x, f, o.x * a), fmaf(z.y, f, o.y * a), fmaf(z.z, f, o.z * a), fmaf(z.w, f, o.w * a));
+    const int lane = threadIdx.x % LANES, grp = threadIdx.x / LANES;
+    if (threadIdx.x < JOIN_PAIRS) {
+        const int pair = blockIdx.x + threadIdx.x * gridDim.x;
+        heads[threadIdx.x] = pair < runs * 8 * NT ? __ldcg(p.headers + pair / (8 * NT)) : make_int4(0, 0, 0, 0);
     }
-    sums[grp][lane] = o;
-    if (lane == 0) ml[grp] = make_float2(m, l);
     __syncthreads();
-    if (grp != 0) return;
-    float top = NONE, sum_l = 0.0f;
+    for (int k = 0; k < JOIN_PAIRS; ++k) {
+        const int4 head = heads[k];  // parts, first row of the sequence, first row and rows, key head
+        const int pair = blockIdx.x + k * gridDim.x, first = pair / (8 * NT), r = pair - first * (8 * NT);
+        if (head.x == 0 || r >= (head.z & 0xffff)) continue;
+        float m = NONE, l = 0.0f;
+        float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 2
+        for (int i = grp; i < head.x; i += GROUPS) {
+            // the first part is this run's last result, the others are the following runs' first
+            const float *part = p.parts + (((int64_t)first + i) * 2 + (i == 0 ? 1 : 0)) * (8 * NT) * part_row(D) + r * part_row(D);
+            const float2 v = __ldcg(reinterpret_cast<const float2 *>(part + D));
+            const float4 z = __ldcg(reinterpret_cast<const float4 *>(part) + lane);
+            const float top = fmaxf(m, v.x), a = ex2(m - top), f = ex2(v.x - top);
+            m = top;
+            l = fmaf(v.y, f, l * a);
+            o = make_float4(fmaf(z.x, f, o.x * a), fmaf(z.y, f, o.y * a), fmaf(z.z, f, o.z * a), fmaf(z.w, f, o.w * a));
+        }
+        sums[grp][lane] = o;
+        if (lane == 0) ml[grp] = make_float2(m, l);
+        __syncthreads();
+        if (grp == 0) {
+            float top = NONE, sum_l = 0.0f;
 #pragma unroll
-    for (int v = 0; v < GROUPS; ++v) top = fmaxf(top, ml[v].x);
-    float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            for (int v = 0; v < GROUPS; ++v) top = fmaxf(top, ml[v].x);
+            float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-    for (int v = 0; v < GROUPS; ++v) {
-        const float f = ex2(ml[v].x - top);
-        const float4 z = sums[v][lane];
-        sum_l = fmaf(ml[v].y, f, sum_l);
-        y = make_float4(fmaf(z.x, f, y.x), fmaf(z.y, f, y.y), fmaf(z.z, f, y.z), fmaf(z.w, f, y.w));
+            for (int v = 0; v < GROUPS; ++v) {
+                const float f = ex2(ml[v].x - top);
+                const float4 z = sums[v][lane];
+                sum_l = fmaf(ml[v].y, f, sum_l);
+                y = make_float4(fmaf(z.x, f, y.x), fmaf(z.y, f, y.y), fmaf(z.z, f, y.z), fmaf(z.w, f, y.w));
+            }
+            const float inv = sum_l == 0.0f ? 0.0f : 1.0f / sum_l;
+            const int row = (head.z >> 16) + r, tok = row / p.group, h = head.w * p.group + (row - tok * p.group);
+            const __nv_bfloat162 a = __floats2bfloat162_rn(y.x * inv, y.y * inv), c = __floats2bfloat162_rn(y.z * inv, y.w * inv);
+            *reinterpret_cast<uint2 *>(p.c.out + (int64_t)(head.y + tok) * p.c.out_stride + (int64_t)h * D + 4 * lane) =
+                make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&c));
+        }
+        __syncthreads();
     }
-    const float inv = sum_l == 0.0f ? 0.0f : 1.0f / sum_l;
-    const int tok = r / p.group, h = head.w * p.group + (r - tok * p.group);
-    const __nv_bfloat162 a = __floats2bfloat162_rn(y.x * inv, y.y * inv), c = __floats2bfloat162_rn(y.z * inv, y.w * inv);
-    *reinterpret_cast<uint2 *>(p.c.out + (int64_t)(head.y + tok) * p.c.out_stride + (int64_t)h * D + 4 * lane) =
-        make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&c));
 }
 
-// Groups of 8 rows that the largest sequence of this kernel may need.
-int row_groups(int64_t max_rows) { return max_rows <= 8 ? 1 : max_rows <= 16 ? 2 : 4; }
+// Groups of 8 rows that a warp takes at a time: one where no sequence has more rows, else two (24 sequences of 16 to 32 rows, heads of 64:
+// 55 us; four groups at once, with spilled registers and two blocks an SM, 81; one after the other 63).
+int row_groups(int64_t max_rows) { return max_rows <= 8 ? 1 : 2; }
 
 template <int D, int NT>
 cudaError_t launch_split(const split_params &p, int sm_count, cudaStream_t st, int64_t *launches)
@@ -622,11 +643,11 @@ cudaError_t launch_split(const split_params &p, int sm_count, cudaStream_t st, i
     static_assert(8 * NT * (D + 4) * 4 <= stages(D, NT) * chunk_bytes(D, NT), "a warp's sums fit its ring");
     cudaError_t e = cudaFuncSetAttribute(attention_split<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    const int blocks = sm_count * blocks_per_sm(NT);
+    const int blocks = sm_count * BLOCKS_PER_SM;
     e = tpq_launch_pdl(attention_split<D, NT>, dim3(blocks), dim3(WARPS * 32), smem, st, p);
     if (e != cudaSuccess) return e;
     ++*launches;
-    e = tpq_launch_pdl(attention_join<D, NT>, dim3(blocks, 8 * NT), dim3(8 * D / 4), 0, st, p);
+    e = tpq_launch_pdl(attention_join<D, NT>, dim3((blocks * 8 * NT + JOIN_PAIRS - 1) / JOIN_PAIRS), dim3(8 * D / 4), 0, st, p, blocks);
     if (e == cudaSuccess) ++*launches;
     return e;
 }
@@ -637,7 +658,7 @@ size_t kv_attention_workspace(int D, int n_heads, int n_kv_heads, int sm_count, 
 {
     const int64_t group = n_heads / n_kv_heads;
     const int nt = row_groups(max_new * group);
-    const size_t blocks = (size_t)sm_count * blocks_per_sm(nt);
+    const size_t blocks = (size_t)sm_count * BLOCKS_PER_SM;
     return blocks * 16 + blocks * 2 * 8 * nt * part_row(D) * 4 +
            (max_new * group > MAX_ROWS ? kv_prompt_workspace(D, (int)group, sm_count, n_seqs, n_tokens, MAX_ROWS) : 0);
 }
@@ -648,12 +669,12 @@ cudaError_t kv_launch_attention(const kv_batch &b, int D, const kv_attention_cal
     const int64_t max_rows = (int64_t)b.max_new * group;
     const int nt = row_groups(max_rows);
     split_params p{b, c, nullptr, static_cast<int4 *>(c.workspace), c.scale * 1.4426950408889634f, group};
-    const size_t blocks = (size_t)sm_count * blocks_per_sm(nt);
+    const size_t blocks = (size_t)sm_count * BLOCKS_PER_SM;
     p.parts = reinterpret_cast<float *>(p.headers + blocks);
     if (max_rows > MAX_ROWS) {
         const cudaError_t e = kv_launch_prompt(b, D, c, MAX_ROWS, p.parts + blocks * 2 * 8 * nt * part_row(D), sm_count, st, launches);
         if (e != cudaSuccess) return e;
     }
-    if (D == 128) return nt == 1 ? launch_split<128, 1>(p, sm_count, st, launches) : nt == 2 ? launch_split<128, 2>(p, sm_count, st, launches) : launch_split<128, 4>(p, sm_count, st, launches);
-    return nt == 1 ? launch_split<64, 1>(p, sm_count, st, launches) : nt == 2 ? launch_split<64, 2>(p, sm_count, st, launches) : launch_split<64, 4>(p, sm_count, st, launches);
+    if (D == 128) return nt == 1 ? launch_split<128, 1>(p, sm_count, st, launches) : launch_split<128, 2>(p, sm_count, st, launches);
+    return nt == 1 ? launch_split<64, 1>(p, sm_count, st, launches) : launch_split<64, 2>(p, sm_count, st, launches);
 }
