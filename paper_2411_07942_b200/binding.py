@@ -104,11 +104,12 @@ SIGNATURES = {
 _lib = None
 _calls = None   # the extension module (csrc/calls.c): the calls of a step with plain arguments; it returns None for others
 _CALLS = ("tpq_calibrate_ranges", "tpq_quantize_pack", "tpq_quantize_pack_batch", "tpq_dequant_reduce", "tpq_dequant_reduce_bias",
-          "tpq_dequant_reduce_arrivals", "tpq_quantize_pack_push", "tpq_linear_quantize_pack")   # in the order of its table
+          "tpq_dequant_reduce_arrivals", "tpq_quantize_pack_push", "tpq_linear_quantize_pack", "tpq_kv_append",
+          "tpq_kv_attention")   # in the order of its table
 # where that module cannot be loaded: every call of its functions is left to ctypes
 _ctypes_only = types.SimpleNamespace(**{f: lambda *args: None for f in (
     "calibrate_ranges", "quantize_pack", "quantize_pack_batch", "dequant_reduce", "dequant_reduce_arrivals", "quantize_pack_push",
-    "linear_quantize_pack")})
+    "linear_quantize_pack", "kv_append", "kv_attention")})
 _fast = types.SimpleNamespace()   # the calls below that take pointer arrays, as functions that take what _ptrs returns
 _FAST = ("tpq_quantize_pack_batch", "tpq_dequant_reduce", "tpq_dequant_reduce_bias", "tpq_quantize_pack_push",
          "tpq_dequant_reduce_arrivals")
@@ -134,7 +135,8 @@ def lib() -> ctypes.CDLL:
         try:
             from . import _calls as calls
             calls.bind([ctypes.cast(getattr(L, name), c_void_p).value for name in _CALLS])
-        except (ImportError, ValueError) as e:   # not built, or built for another interpreter or table
+            calls.bind_types(KvBatch, KvRotation)
+        except (ImportError, ValueError, AttributeError) as e:   # not built, or built for another interpreter or table
             warnings.warn(f"the extension module _calls cannot be used ({e}): every call goes through ctypes, 1 to 2 us slower "
                           "each; `python -m paper_2411_07942_b200.build` builds it", RuntimeWarning)
             calls = _ctypes_only
@@ -383,12 +385,14 @@ class TpqKv:
         if st != TPQ_OK:
             self._h = c_void_p()
             raise TpqError(st, "tpq_kv_create failed")
+        self._p = self._h.value   # (as a plain integer, for _calls)
         self.n_heads, self.n_kv_heads, self.head_dim, self.page_size = n_heads, n_kv_heads, head_dim, page_size
 
     def close(self):
         if getattr(self, "_h", None) and self._h.value:
             lib().tpq_kv_destroy(self._h)
             self._h = c_void_p()
+            self._p = None
 
     def __del__(self):
         try:
@@ -411,9 +415,11 @@ class TpqKv:
                rotation: KvRotation | None = None, q_ptr: int | None = None, q_stride: int | None = None, q_out_ptr: int | None = None,
                q_out_stride: int | None = None, stream: int = 0):
         kv_row, q_row = self.n_kv_heads * self.head_dim, self.n_heads * self.head_dim
-        st = lib().tpq_kv_append(self._h, batch, rotation, k_ptr, kv_row if k_stride is None else k_stride, v_ptr,
-                                 kv_row if v_stride is None else v_stride, q_ptr, q_row if q_stride is None else q_stride, q_out_ptr,
-                                 q_row if q_out_stride is None else q_out_stride, stream)
+        ks, vs = kv_row if k_stride is None else k_stride, kv_row if v_stride is None else v_stride
+        qs, os = q_row if q_stride is None else q_stride, q_row if q_out_stride is None else q_out_stride
+        st = _calls.kv_append(self._p, batch, rotation, k_ptr, ks, v_ptr, vs, q_ptr, qs, q_out_ptr, os, stream)
+        if st is None:
+            st = _lib.tpq_kv_append(self._h, batch, rotation, k_ptr, ks, v_ptr, vs, q_ptr, qs, q_out_ptr, os, stream)
         if st:
             self._check(st)
 
@@ -432,8 +438,10 @@ class TpqKv:
     def attention(self, batch: KvBatch, q_ptr: int, out_ptr: int, workspace_ptr: int, workspace_bytes: int, scale: float, window: int = 0,
                   first: int = 0, q_stride: int | None = None, out_stride: int | None = None, stream: int = 0):
         row = self.n_heads * self.head_dim
-        st = lib().tpq_kv_attention(self._h, batch, q_ptr, row if q_stride is None else q_stride, scale, window, first, out_ptr,
-                                    row if out_stride is None else out_stride, workspace_ptr, workspace_bytes, stream)
+        qs, os = row if q_stride is None else q_stride, row if out_stride is None else out_stride
+        st = _calls.kv_attention(self._p, batch, q_ptr, qs, scale, window, first, out_ptr, os, workspace_ptr, workspace_bytes, stream)
+        if st is None:
+            st = _lib.tpq_kv_attention(self._h, batch, q_ptr, qs, scale, window, first, out_ptr, os, workspace_ptr, workspace_bytes, stream)
         if st:
             self._check(st)
 

@@ -26,7 +26,14 @@ static struct {
                                   const uint32_t *, uint32_t, uint64_t, void *);
     tpq_status (*push)(tpq_ctx *, int, const void *, int64_t, int64_t, void *const *, uint32_t *const *, int, size_t, uint32_t, void *);
     tpq_status (*linear)(tpq_ctx *, int, const void *, const void *, int64_t, int64_t, void *, size_t, void *, void *);
+    tpq_status (*kv_append)(tpq_kv *, const tpq_kv_batch *, const tpq_kv_rotation *, const void *, int64_t, const void *, int64_t, const void *,
+                            int64_t, void *, int64_t, void *);
+    tpq_status (*kv_attention)(tpq_kv *, const tpq_kv_batch *, const void *, int64_t, float, int64_t, int64_t, void *, int64_t, void *, size_t,
+                               void *);
 } lib;
+
+/* the types of binding.py that hold a tpq_kv_batch and a tpq_kv_rotation */
+static PyTypeObject *batch_type, *rotation_type;
 
 /* conversions: 1, or 0 where the argument is not of the plain form (no exception is left set) */
 static int as_i64(PyObject *o, int64_t *v)
@@ -73,6 +80,26 @@ static int as_ptrs(PyObject *o, void **v, int *n)
     for (Py_ssize_t i = 0; i < len; ++i)
         if (!as_ptr(PySequence_Fast_GET_ITEM(o, i), &v[i])) return 0;
     *n = (int)len;
+    return 1;
+}
+/* the structure in an object of exactly this type (which the caller holds on to during the call) */
+static int as_struct(PyObject *o, PyTypeObject *type, size_t size, void *v)
+{
+    Py_buffer b;
+    if (type == NULL || Py_TYPE(o) != type) return 0;
+    if (PyObject_GetBuffer(o, &b, PyBUF_SIMPLE) != 0) {
+        PyErr_Clear();
+        return 0;
+    }
+    const int ok = (size_t)b.len == size;
+    if (ok) memcpy(v, b.buf, size);
+    PyBuffer_Release(&b);
+    return ok;
+}
+static int as_float(PyObject *o, float *v)
+{
+    if (!PyFloat_CheckExact(o)) return 0;
+    *v = (float)PyFloat_AS_DOUBLE(o);
     return 1;
 }
 static PyObject *status(tpq_status st) { return PyLong_FromLong((long)st); }
@@ -161,6 +188,44 @@ static PyObject *linear_quantize_pack(PyObject *self, PyObject *const *a, Py_ssi
          lib.linear(ctx, shard, x, w, T, K, payload, cap, y_slots, stream));
 }
 
+static PyObject *kv_append(PyObject *self, PyObject *const *a, Py_ssize_t n_args)
+{
+    tpq_kv_batch batch;
+    tpq_kv_rotation rot;
+    int64_t ks, vs, qs, os;
+    void *k, *v, *q, *q_out, *stream;
+    CALL(12, as_struct(a[1], batch_type, sizeof batch, &batch) && (a[2] == Py_None || as_struct(a[2], rotation_type, sizeof rot, &rot)) && as_ptr(a[3], &k) &&
+             as_i64(a[4], &ks) && as_ptr(a[5], &v) && as_i64(a[6], &vs) && as_ptr_or_none(a[7], &q) && as_i64(a[8], &qs) && as_ptr_or_none(a[9], &q_out) &&
+             as_i64(a[10], &os) && as_ptr(a[11], &stream),
+         lib.kv_append(ctx, &batch, a[2] == Py_None ? NULL : &rot, k, ks, v, vs, q, qs, q_out, os, stream));
+}
+
+static PyObject *kv_attention(PyObject *self, PyObject *const *a, Py_ssize_t n_args)
+{
+    tpq_kv_batch batch;
+    float scale;
+    int64_t qs, window, first, os;
+    uint64_t bytes;
+    void *q, *out, *ws, *stream;
+    CALL(12, as_struct(a[1], batch_type, sizeof batch, &batch) && as_ptr(a[2], &q) && as_i64(a[3], &qs) && as_float(a[4], &scale) && as_i64(a[5], &window) &&
+             as_i64(a[6], &first) && as_ptr(a[7], &out) && as_i64(a[8], &os) && as_ptr(a[9], &ws) && as_u64(a[10], &bytes) && as_ptr(a[11], &stream),
+         lib.kv_attention(ctx, &batch, q, qs, scale, window, first, out, os, ws, bytes, stream));
+}
+
+/* bind_types(batch, rotation): the types that kv_append and kv_attention take */
+static PyObject *bind_types(PyObject *self, PyObject *const *a, Py_ssize_t n_args)
+{
+    if (n_args != 2 || !PyType_Check(a[0]) || !PyType_Check(a[1])) {
+        PyErr_SetString(PyExc_ValueError, "bind_types() takes two types");
+        return NULL;
+    }
+    Py_INCREF(a[0]);
+    Py_INCREF(a[1]);
+    Py_XSETREF(batch_type, (PyTypeObject *)a[0]);
+    Py_XSETREF(rotation_type, (PyTypeObject *)a[1]);
+    Py_RETURN_NONE;
+}
+
 /* bind(addresses): the entry points of the loaded library, in the order of `lib` */
 static PyObject *bind(PyObject *self, PyObject *addresses)
 {
@@ -178,7 +243,7 @@ static PyMethodDef methods[] = {
     {"bind", bind, METH_O, NULL},
 #define METHOD(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, NULL}
     METHOD(calibrate_ranges), METHOD(quantize_pack), METHOD(quantize_pack_batch), METHOD(dequant_reduce),
-    METHOD(dequant_reduce_arrivals), METHOD(quantize_pack_push), METHOD(linear_quantize_pack),
+    METHOD(dequant_reduce_arrivals), METHOD(quantize_pack_push), METHOD(linear_quantize_pack), METHOD(kv_append), METHOD(kv_attention), METHOD(bind_types),
     {NULL, NULL, 0, NULL}};
 
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", NULL, -1, methods, NULL, NULL, NULL, NULL};
