@@ -353,9 +353,10 @@ tpq_status tpq_dequant_reduce_arrivals(tpq_ctx *ctx, const void *const *payloads
  *
  * Conventions beside those above: a handle holds no data of a caller's and serves any number of layers and caches
  * of its geometry; its device must be the current one in every call (BAD_STATE).  What a batch says on the DEVICE
- * is checked by the kernels: a sequence whose description contradicts itself or the batch, a position outside the rotation's table and a
- * page number outside the pool are skipped (rows of outputs stay as they were; positions of a bad page are invisible) and the
- * handle's device status becomes TPQ_ERR_INVALID_ARG (tpq_kv_device_status). */
+ * is checked by the kernels.  A sequence whose description contradicts itself or the batch is left out, and so is a row whose
+ * position is outside the rotation's table (outputs stay as they were, nothing is appended); keys and values of a
+ * position whose page number is outside the pool are not appended, read or seen.  The handle's device status becomes TPQ_ERR_INVALID_ARG in
+ * each case (tpq_kv_device_status). */
 
 typedef struct tpq_kv tpq_kv; /* opaque */
 

@@ -11,7 +11,7 @@
 
 namespace {
 
-constexpr int KV_WARPS = 8;
+constexpr int KV_WARPS = 4;
 
 struct rotation {
     const float *table;
@@ -139,12 +139,12 @@ append_kernel(const kv_batch b, const rotation rot, const kv_rows k, const kv_ro
     float cs[8], sn[8];  // of this lane's values; (half pairs) the partner's value times the signed sine is added
     int partner = lane;
     const bool turn = kind != 2 && rot.table != nullptr;
+    const int p = rot.table && rot.positions ? rot.positions[row] : pos;
+    if (rot.table && (p < 0 || p >= rot.n_positions)) {  // (the whole row is left out: queries, keys and values)
+        if (lane == 0) kv_report(b);
+        return;
+    }
     if (turn) {
-        const int p = rot.positions ? rot.positions[row] : pos;
-        if (p < 0 || p >= rot.n_positions) {
-            if (lane == 0) kv_report(b);
-            return;
-        }
         const int half = rot.dim / 2, d = li * 8;
         const float *t = rot.table + (int64_t)p * rot.dim;
 #pragma unroll

@@ -100,7 +100,7 @@ def check(setup, q32, got_bits, scale, window=0, first=0):
     got = kv_ref.wide(got_bits).reshape(rows, setup.heads, setup.dim).astype(np.float64)
     assert (got_bits[used:] == 0xA5A5).all()                       # rows behind the last sequence, as they were
     err = np.abs(got - want)[:used]
-    ok = err <= tolerance(want, bound)[:used]
+    ok = (err <= tolerance(want, bound)[:used]) | (np.isnan(want) & np.isnan(got))[:used]   # (what was never appended may be NaN: then so is the answer)
     assert ok.all(), f"{int((~ok).sum())} of {ok.size} off; worst {float(np.nanmax(err / tolerance(want, bound)[:used])):.3g} times the tolerance"
 
 
@@ -245,3 +245,327 @@ def test_attention_reads_no_page_that_a_window_left_behind():
     got = s.attention(q, 0.1, window, first)
     assert s.kv.device_status() == binding.TPQ_OK
     check(s, q32, got, 0.1, window, first)
+
+
+MORE = [  # many sequences, several items and runs, odd scales: heads, kv_heads, dim, page, new, lengths, window, first, pad, scale
+    (2, 1, 64, 16, [1] * 300, [1 + (7 * i) % 90 for i in range(300)], 0, 0, 1, 0.2),
+    (3, 3, 128, 16, [i % 3 for i in range(1100)], [i % 3 + (5 * i) % 23 for i in range(1100)], 0, 0, 0, 0.1),
+    (2, 1, 128, 64, [700], [1500], 0, 0, 0, 0.1),
+    (1, 1, 128, 32, [1100], [1100], 300, 5, 0, 0.1),
+    (5, 1, 64, 128, [200, 300, 1, 7, 90], [900, 300, 2000, 7, 450], 0, 0, 4, 0.15),
+    (16, 2, 128, 32, [33, 64, 1], [640, 64, 3000], 128, 128, 0, 0.09),
+    (4, 4, 128, 16, [1, 40], [300, 300], 0, 0, 0, -0.1),
+    (4, 4, 128, 16, [1, 40], [300, 300], 0, 0, 0, 0.0),
+    (4, 2, 128, 16, [2, 40], [500, 300], 0, 0, 0, 1.0),
+    (4, 2, 64, 256, [1, 257], [4096, 257], 1, 0, 0, 0.1),
+    (256, 1, 64, 16, [1], [70], 0, 0, 0, 0.1),
+]
+
+
+@pytest.mark.parametrize("case", MORE, ids=lambda c: f"{c[0]}x{c[1]}x{c[2]}s{len(c[4])}n{max(c[4])}l{max(c[5])}w{c[6]}x{c[9]}")
+def test_attention_over_many_sequences_items_and_scales(case):
+    heads, kvh, dim, page, new, lengths, window, first, pad, scale = case
+    s = Setup(heads, kvh, dim, page, new, lengths, pad=pad, seed=31, fill=0xFF).fill_with_data()
+    q, q32 = rows_of(s.rng, s.T, heads * dim)
+    got = s.attention(q, scale, window, first)
+    assert s.kv.device_status() == binding.TPQ_OK
+    check(s, q32, got, scale, window, first)
+
+
+@pytest.mark.parametrize("new", [1, 50])
+def test_attention_over_vectors_of_very_different_sizes(new):
+    """Keys' and values' magnitudes over 2^14, zero vectors and constant ones among them; queries over 2^20."""
+    s = Setup(4, 2, 128, 16, [new], [260], seed=33, fill=0xFF)
+    for t in range(260):
+        for h in range(2):
+            for which in (0, 1):
+                x = s.rng.standard_normal(128) * 2.0 ** s.rng.integers(-10, 4)
+                if t % 37 == 5:
+                    x[:] = 0 if t % 2 else 0.75
+                codes, words = kv_ref.quantise((x * (0.05 if which == 0 else 1)).astype(np.float32)[None])
+                s.cache.put(s.table[0, t // 16], h, t % 16, which, codes[0], words[0])
+    s.d_cache.copy_(torch.from_numpy(s.cache.bytes))
+    q, q32 = rows_of(s.rng, s.T, 512)
+    q[:, :128] *= 2.0 ** -20
+    q32 = q.float().cpu().numpy()
+    check(s, q32, s.attention(q, 0.1), 0.1)
+
+
+def test_windows_beyond_every_length_are_none():
+    s = Setup(8, 2, 128, 32, [1, 60], [700, 300], seed=35).fill_with_data()
+    q, _ = rows_of(s.rng, s.T, 1024)
+    plain = s.attention(q, 0.1)
+    for window, first in ((700, 0), (2 ** 40, 3), (2 ** 62, 2 ** 62), (0, 5)):
+        assert np.array_equal(plain, s.attention(q, 0.1, window, first))
+
+
+def test_appending_in_pieces_gives_the_same_bytes():
+    whole, parts = (Setup(4, 2, 64, 16, [90], [90], seed=41, fill=0) for _ in range(2))
+    k, _ = rows_of(whole.rng, 90, 128)
+    v, _ = rows_of(whole.rng, 90, 128)
+    a = whole.rng.uniform(0, 7, (90, 32))
+    d = dev(np.concatenate([np.cos(a), np.sin(a)], 1).astype(np.float32))
+    rot = binding.KvRotation(d.data_ptr(), 90, 64, 0, None)
+    whole.kv.append(whole.batch, k.data_ptr(), v.data_ptr(), rotation=rot)
+    at = 0
+    for n in (1, 15, 17, 40, 1, 16):
+        start, lengths = dev(np.array([0, n], np.int32)), dev(np.array([at + n], np.int32))
+        b = binding.KvBatch(parts.d_cache.data_ptr(), parts.n_pages, parts.d_table.data_ptr(), parts.table.shape[1], start.data_ptr(), lengths.data_ptr(), 1, n, n)
+        parts.kv.append(b, k[at:].data_ptr(), v[at:].data_ptr(), rotation=rot)
+        torch.cuda.synchronize()
+        at += n
+    assert at == 90 and torch.equal(whole.d_cache, parts.d_cache)
+
+
+def test_captured_steps_replay_with_other_lengths_and_rows():
+    """A step (append, attention) captured once for a padded batch, replayed with other rows, lengths, pages and fewer sequences; two graphs
+    with workspaces of their own, replayed on two streams at a time."""
+    new, lengths = [1, 40, 1, 1], [200, 90, 64, 33]
+    s = Setup(8, 2, 128, 16, new, lengths, pad=5, seed=51, fill=0xFF).fill_with_data()
+    width = 1024
+    k, v, q = (torch.zeros(s.T, w, dtype=torch.bfloat16, device="cuda") for w in (256, 256, width))
+    graphs, outs, caches = [], [], []
+    for _ in range(2):
+        cache = s.d_cache.clone()
+        batch = binding.KvBatch(cache.data_ptr(), *[getattr(s.batch, f) for f, _ in s.batch._fields_[1:]])
+        ws = torch.empty(s.kv.attention_workspace_bytes(batch), dtype=torch.uint8, device="cuda")
+        out = torch.zeros(s.T, width, dtype=torch.bfloat16, device="cuda")
+        side = torch.cuda.Stream()
+        with torch.cuda.stream(side):
+            run = lambda: (s.kv.append(batch, k.data_ptr(), v.data_ptr(), stream=side.cuda_stream),  # noqa: E731
+                           s.kv.attention(batch, q.data_ptr(), out.data_ptr(), ws.data_ptr(), ws.numel(), 0.1, stream=side.cuda_stream))
+            run()
+            side.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=side):
+                run()
+        graphs.append((graph, side, ws, batch))
+        outs.append(out)
+        caches.append(cache)
+    for step, (new, lengths) in enumerate([([1, 40, 1, 1], [200, 90, 64, 33]), ([1, 3, 0, 1], [17, 90, 64, 40]), ([0, 0, 0, 0], [5, 90, 64, 40]), ([2, 40, 1, 0], [150, 95, 1, 0])]):
+        start = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+        s.start, s.lengths = start, np.array(lengths, np.int32)
+        s.d_start.copy_(torch.from_numpy(start))
+        s.d_lengths.copy_(torch.from_numpy(s.lengths))
+        for t in (k, v, q):
+            t.copy_(torch.from_numpy(s.rng.standard_normal(tuple(t.shape)).astype(np.float32)).to(torch.bfloat16))
+        for out in outs:
+            out.view(torch.int16).fill_(np.int16(np.uint16(0xA5A5).view(np.int16)).item())
+        torch.cuda.synchronize()
+        for graph, side, _, _ in graphs:
+            with torch.cuda.stream(side):
+                graph.replay()
+        torch.cuda.synchronize()
+        assert s.kv.device_status() == binding.TPQ_OK
+        kv_ref.append(s.cache, s.table, start, s.lengths, k.float().cpu().numpy().reshape(s.T, 2, 128), v.float().cpu().numpy().reshape(s.T, 2, 128))
+        for out, cache in zip(outs, caches):
+            assert np.array_equal(cache.cpu().numpy(), s.cache.bytes)
+            check(s, q.float().cpu().numpy(), bits(out), 0.1)
+
+
+def test_offsets_beyond_32_bits():
+    """The last pages of a pool of more than 4 GiB, by append, read and both attention paths."""
+    page, heads = 256, 16
+    s = Setup(16, heads, 128, page, [40, 1], [300, 260], seed=61, fill=0)
+    per_page = s.kv.page_bytes()
+    n_pages = 2 ** 32 // per_page + 12
+    pool = torch.empty(n_pages * per_page, dtype=torch.uint8, device="cuda")
+    last = np.where(s.table >= 0, n_pages - 1 - s.table, s.table).astype(np.int32)
+    d_last = dev(last)
+    s.fill_with_data()
+    for p in range(s.n_pages):
+        pool[(n_pages - 1 - p) * per_page:][:per_page] = torch.from_numpy(s.cache.bytes[p].reshape(-1)).cuda()
+    b = binding.KvBatch(pool.data_ptr(), n_pages, d_last.data_ptr(), last.shape[1], s.d_start.data_ptr(), s.d_lengths.data_ptr(), 2, 40, s.T)
+    s.batch = b
+    k, k32 = rows_of(s.rng, s.T, 16 * 128)
+    s.kv.append(b, k.data_ptr(), k.data_ptr())
+    kv_ref.append(s.cache, s.table, s.start, s.lengths, k32.reshape(s.T, 16, 128), k32.reshape(s.T, 16, 128))
+    out = torch.zeros(s.T, 16 * 128, dtype=torch.bfloat16, device="cuda")
+    s.kv.read(b, out.data_ptr(), None)
+    torch.cuda.synchronize()
+    for p in range(s.n_pages):
+        assert np.array_equal(pool[(n_pages - 1 - p) * per_page:][:per_page].cpu().numpy(), s.cache.bytes[p].reshape(-1))
+    assert (out.float().cpu().numpy() != 0).mean() > 0.9
+    q, q32 = rows_of(s.rng, s.T, 2048)
+    check(s, q32, s.attention(q, 0.1), 0.1)
+
+
+def test_what_contradicts_itself_on_the_device_is_left_out_and_reported():
+    """Bad sequences, pages and positions: nothing of theirs is written, the others are right, the status word says so once."""
+    new, lengths = [1, 2, 1, 40, 1], [100, 64, 30, 80, 50]
+    s = Setup(4, 2, 128, 16, new, lengths, seed=71, fill=0xFF).fill_with_data()
+    q, q32 = rows_of(s.rng, s.T, 512)
+    k, k32 = rows_of(s.rng, s.T, 256)
+    good = s.attention(q, 0.1)
+    for name, change in (("longer than the table", lambda ln, tb, st: ln.__setitem__(1, 7 * 16 + 1)), ("negative length", lambda ln, tb, st: ln.__setitem__(1, -5)),
+                         ("more rows than positions", lambda ln, tb, st: ln.__setitem__(1, 1)), ("more rows than said", None)):
+        ln, tb, st = s.lengths.copy(), s.table.copy(), s.start.copy()
+        b = binding.KvBatch.from_buffer_copy(s.batch)
+        skipped = 1
+        if change is None:
+            b.max_new, skipped = 39, 3
+        else:
+            change(ln, tb, st)
+        d_ln = dev(ln)
+        b.lengths_ptr = d_ln.data_ptr()
+        keep, s.batch = s.batch, b
+        got = s.attention(q, 0.1)
+        assert s.kv.device_status() == binding.TPQ_ERR_INVALID_ARG, name
+        assert s.kv.device_status() == binding.TPQ_OK
+        lo, hi = s.start[skipped], s.start[skipped + 1]
+        assert (got[lo:hi] == 0xA5A5).all() and np.array_equal(np.delete(got, np.s_[lo:hi], 0), np.delete(good, np.s_[lo:hi], 0)), name
+        before = s.d_cache.clone()
+        s.kv.append(b, k.data_ptr(), k.data_ptr())
+        assert s.kv.device_status() == binding.TPQ_ERR_INVALID_ARG
+        want = kv_ref.Cache(s.n_pages, 2, 128, 16, fill=0)
+        want.bytes = before.cpu().numpy().copy()
+        starts = s.start.copy()
+        mask = [i for i in range(5) if i != skipped]
+        for i in mask:
+            r = slice(starts[i], starts[i + 1])
+            kv_ref.append(want, s.table[i:i + 1], np.array([0, starts[i + 1] - starts[i]]), ln[i:i + 1], k32[r].reshape(-1, 2, 128), k32[r].reshape(-1, 2, 128))
+        assert np.array_equal(s.d_cache.cpu().numpy(), want.bytes), name
+        s.d_cache.copy_(before)
+        s.batch = keep
+    # starts that go down, or beyond the rows
+    for bad in ([0, 3, 1, 44, 45], [-1, 1, 3, 4, 44], [0, 1, 3, 4, 1000]):
+        d_st = dev(np.array(bad + [45], np.int32))
+        b = binding.KvBatch.from_buffer_copy(s.batch)
+        b.token_start_ptr = d_st.data_ptr()
+        keep, s.batch = s.batch, b
+        s.attention(q, 0.1)                                        # (guards intact)
+        s.kv.append(b, k.data_ptr(), k.data_ptr())
+        assert s.kv.device_status() == binding.TPQ_ERR_INVALID_ARG
+        s.batch = keep
+    s.d_cache.copy_(torch.from_numpy(s.cache.bytes))
+    # pages outside the pool: their positions are invisible, and a row that sees nothing else is zero
+    for page_id in (-1, s.n_pages, 2 ** 31 - 1, -2 ** 31):
+        table = s.table.copy()
+        table[0, 2], table[3, 0], table[4, :] = page_id, page_id, page_id
+        s.d_table.copy_(torch.from_numpy(table))
+        got = s.attention(q, 0.1)
+        assert s.kv.device_status() == binding.TPQ_ERR_INVALID_ARG
+        keep, s.table = s.table, table
+        check(s, q32, got, 0.1)
+        assert (got[s.start[4]:] == 0).all()
+        before = s.d_cache.clone()
+        s.kv.append(s.batch, k.data_ptr(), k.data_ptr())
+        assert s.kv.device_status() == binding.TPQ_ERR_INVALID_ARG
+        s.d_cache.copy_(before)
+        s.table = keep
+        s.d_table.copy_(torch.from_numpy(s.table))
+    # positions outside the rotation's table
+    d_rot = torch.ones(90, 128, device="cuda")
+    before, out = s.d_cache.clone(), torch.full((s.T, 512), 3, dtype=torch.int16, device="cuda")
+    s.kv.append(s.batch, k.data_ptr(), k.data_ptr(), rotation=binding.KvRotation(d_rot.data_ptr(), 90, 128, 0, None), q_ptr=q.data_ptr(), q_out_ptr=out.data_ptr())
+    assert s.kv.device_status() == binding.TPQ_ERR_INVALID_ARG
+    assert (out[0] == 3).all() and not (out[1:] == 3).all(1).any()           # (position 99 of the first sequence alone)
+    s.d_cache.copy_(before)
+
+
+def test_refusals_launch_nothing():
+    s = Setup(8, 2, 128, 16, [1, 2], [40, 50], seed=81).fill_with_data()
+    q, _ = rows_of(s.rng, s.T, 1024)
+    k, _ = rows_of(s.rng, s.T, 256)
+    out = torch.zeros(s.T, 1024, dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(s.kv.attention_workspace_bytes(s.batch), dtype=torch.uint8, device="cuda")
+    rot_table = torch.ones(64, 128, device="cuda")
+    launches = s.kv.launch_count()
+
+    def with_batch(**kw):
+        b = binding.KvBatch.from_buffer_copy(s.batch)
+        for name, value in kw.items():
+            setattr(b, name, value)
+        return b
+
+    def attention(b=s.batch, q_ptr=q.data_ptr(), qs=1024, scale=0.1, window=0, first=0, o=out.data_ptr(), os=1024, w=ws.data_ptr(), n=ws.numel()):
+        return s.kv.raw("tpq_kv_attention", b, q_ptr, qs, scale, window, first, o, os, w, n, None)
+
+    def append(b=s.batch, rot=None, k_ptr=k.data_ptr(), ks=256, v_ptr=k.data_ptr(), vs=256, q_ptr=None, qs=1024, o=None, os=1024):
+        return s.kv.raw("tpq_kv_append", b, rot, k_ptr, ks, v_ptr, vs, q_ptr, qs, o, os, None)
+
+    def rot(**kw):
+        r = binding.KvRotation(rot_table.data_ptr(), 64, 128, 0, None)
+        for name, value in kw.items():
+            setattr(r, name, value)
+        return r
+
+    A, I, S = binding.TPQ_ERR_ALIGN, binding.TPQ_ERR_INVALID_ARG, binding.TPQ_ERR_SIZE
+    batches = [(I, None), (I, with_batch(n_seqs=-1)), (I, with_batch(max_new=-1)), (I, with_batch(n_tokens=-1)), (I, with_batch(n_tokens=2 ** 31)), (I, with_batch(n_pages=-1)),
+               (I, with_batch(n_pages=2 ** 31)), (I, with_batch(page_table_stride=-1)), (I, with_batch(page_table_stride=2 ** 31)), (I, with_batch(cache_ptr=None)),
+               (I, with_batch(page_table_ptr=None)), (I, with_batch(token_start_ptr=None)), (I, with_batch(lengths_ptr=None)), (A, with_batch(cache_ptr=s.batch.cache_ptr + 8)),
+               (A, with_batch(page_table_ptr=s.batch.page_table_ptr + 2)), (A, with_batch(token_start_ptr=s.batch.token_start_ptr + 1)),
+               (A, with_batch(lengths_ptr=s.batch.lengths_ptr + 2))]
+    for want, b in batches:
+        assert attention(b) == want and append(b) == want and s.kv.raw("tpq_kv_read", b, k.data_ptr(), 256, None, 256, None) == want
+    for want, kw in [(I, dict(q_ptr=None)), (A, dict(q_ptr=q.data_ptr() + 2)), (I, dict(qs=1016)), (A, dict(qs=1028)), (I, dict(o=None)), (A, dict(o=out.data_ptr() + 8)), (I, dict(os=1000)),
+                     (A, dict(os=1025)), (I, dict(o=q.data_ptr())), (I, dict(scale=float("inf"))), (I, dict(scale=float("nan"))), (I, dict(window=-1)), (I, dict(first=-1)),
+                     (I, dict(w=None)), (A, dict(w=ws.data_ptr() + 4)), (S, dict(n=ws.numel() - 1)), (S, dict(n=0))]:
+        assert attention(**kw) == want, kw
+        assert binding.lib().tpq_kv_last_error(s.kv._h) != b""
+    for want, kw in [(I, dict(k_ptr=None)), (I, dict(v_ptr=None)), (A, dict(k_ptr=k.data_ptr() + 8)), (I, dict(ks=248)), (A, dict(vs=260)), (I, dict(q_ptr=q.data_ptr(), o=out.data_ptr())),
+                     (I, dict(o=out.data_ptr())), (I, dict(rot=rot(), q_ptr=q.data_ptr())), (I, dict(rot=rot(), q_ptr=q.data_ptr(), o=q.data_ptr(), os=1032)),
+                     (I, dict(rot=rot(table_ptr=None))), (A, dict(rot=rot(table_ptr=rot_table.data_ptr() + 4))), (I, dict(rot=rot(n_positions=0))), (I, dict(rot=rot(rot_dim=0))),
+                     (I, dict(rot=rot(rot_dim=24))), (I, dict(rot=rot(rot_dim=144))), (A, dict(rot=rot(positions_ptr=rot_table.data_ptr() + 2)))]:
+        assert append(**kw) == want, kw
+    assert s.kv.raw("tpq_kv_read", s.batch, None, 256, None, 256, None) == I and s.kv.raw("tpq_kv_read", s.batch, k.data_ptr(), 256, k.data_ptr(), 256, None) == I
+    for b in (with_batch(n_seqs=0), with_batch(n_tokens=0), with_batch(max_new=0)):   # nothing to do, whatever else is given
+        assert attention(b) == 0 and append(b) == 0 and s.kv.raw("tpq_kv_read", b, None, 0, None, 0, None) == 0
+    assert s.kv.attention_workspace_bytes(with_batch(n_seqs=0)) == 0
+    assert s.kv.launch_count() == launches and s.kv.device_status() == binding.TPQ_OK
+    assert attention() == 0 and append(rot=rot(), q_ptr=q.data_ptr(), o=out.data_ptr()) == 0
+    assert s.kv.launch_count() > launches
+
+
+def test_an_attention_block_up_to_the_synchronised_sum():
+    """Two devices of a tensor-parallel group: each appends its heads' keys and values, attends, multiplies by its part of the output
+    projection and compresses the partial sums (tpq_linear_quantize_pack); the payloads are summed.  Against the same in 64 bits from the cache's
+    values: off by half a step of each device's codes (the ranges cover the partial sums), and by what the partial sums themselves
+    may be off: their rounding to BF16 and the attention's tolerance through the weights' magnitudes."""
+    N, E, heads, kvh, dim, n = 2, 512, 4, 2, 128, 70
+    rng = np.random.default_rng(91)
+    K = heads * dim
+    a = rng.uniform(0, 7, (120, dim // 2))
+    table = np.concatenate([np.cos(a), np.sin(a)], 1).astype(np.float32)
+    d_rot = dev(table)
+    total, allowed, payloads, ys, ws_slots, xs = 0, 0, [], [], [], []
+    t = binding.Tpq(N, E)
+    for i in range(N):
+        s = Setup(heads, kvh, dim, 16, [n, 1], [n + 13, 50], seed=100 + i, fill=0xFF).fill_with_data()
+        k, k32 = rows_of(rng, s.T, kvh * dim)
+        v, v32 = rows_of(rng, s.T, kvh * dim)
+        q, q32 = rows_of(rng, s.T, K)
+        s.kv.append(s.batch, k.data_ptr(), v.data_ptr(), rotation=binding.KvRotation(d_rot.data_ptr(), 120, dim, 0, None), q_ptr=q.data_ptr(), q_out_ptr=q.data_ptr())
+        x = torch.empty(s.T, K, dtype=torch.bfloat16, device="cuda")
+        ws = torch.empty(s.kv.attention_workspace_bytes(s.batch), dtype=torch.uint8, device="cuda")
+        s.kv.attention(s.batch, q.data_ptr(), x.data_ptr(), ws.data_ptr(), ws.numel(), 1 / math.sqrt(dim))
+        qr = kv_ref.wide(kv_ref.append(s.cache, s.table, s.start, s.lengths, k32.reshape(s.T, kvh, dim), v32.reshape(s.T, kvh, dim), q32.reshape(s.T, heads, dim), table, dim))
+        torch.cuda.synchronize()
+        assert np.array_equal(s.d_cache.cpu().numpy(), s.cache.bytes) and s.kv.device_status() == binding.TPQ_OK
+        o, bound = kv_ref.attention(s.cache, s.table, s.start, s.lengths, qr, 1 / math.sqrt(dim))
+        w = (rng.standard_normal((E, K)) / math.sqrt(K)).astype(np.float32)
+        w_bf = torch.from_numpy(w).to(torch.bfloat16)
+        w64 = w_bf.double().numpy()
+        y = o.reshape(s.T, K) @ w64.T
+        total = total + y
+        allowed = allowed + np.broadcast_to(tolerance(o, bound), o.shape).reshape(s.T, K) @ np.abs(w64).T * (1 + 2.0 ** -7) + 2.0 ** -7 * np.abs(y)
+        ys.append(y)
+        xs.append((x, w_bf.cuda()))
+    lim = np.stack([1.1 * np.abs(y).max(0) + 1e-3 for y in ys]).astype(np.float32)
+    t.set_ranges(-lim, lim, [1] * N)
+    t.select_features()
+    for i, (x, w_bf) in enumerate(xs):
+        slots = torch.empty_like(w_bf)
+        t.permute_weight(w_bf.data_ptr(), K, slots.data_ptr())
+        payload = torch.empty(t.payload_bytes(x.shape[0]), dtype=torch.uint8, device="cuda")
+        t.linear_quantize_pack(i, x.data_ptr(), slots.data_ptr(), x.shape[0], K, payload.data_ptr(), payload.numel())
+        payloads.append(payload)
+        ws_slots.append(slots)
+    out = torch.empty(xs[0][0].shape[0], E, dtype=torch.float32, device="cuda")
+    t.dequant_reduce([p.data_ptr() for p in payloads], out.shape[0], out.data_ptr(), binding.TPQ_OUT_FP32)
+    assert t.device_status() == binding.TPQ_OK
+    step, _ = t.get_scales()
+    # (codes reach from -8 to 7 steps of R/15: the upper end is half a step more than half a step away)
+    allowed = allowed + step.astype(np.float64).sum(0)[None] + 1e-5
+    err = np.abs(out.cpu().numpy() - total)
+    assert (err <= allowed).all(), float((err / allowed).max())

@@ -99,3 +99,48 @@ def test_null_handles_are_rejected_not_crashed(binding):
     assert L.tpq_kv_read(None, None, None, 0, None, 0, None) == 1
     assert L.tpq_kv_attention(None, None, None, 0, 1.0, 0, 0, None, 0, None, 0, None) == 1
     assert L.tpq_kv_attention_workspace(None, 1, 1, 1) == 0 and L.tpq_kv_device_status(None) == 1
+
+
+def test_extension_calls_pass_on_what_ctypes_would(binding):
+    """kv_append and kv_attention of the extension module, bound to recorders: structures arrive by value's address, plain arguments as the C
+    signature types them; any other form is left to ctypes without a call."""
+    seen, keep, addresses = [], [], []
+    for name in binding._CALLS:
+        res, types = binding.SIGNATURES[name]
+        plain = [ctypes.c_void_p if isinstance(a, type) and issubclass(a, ctypes._Pointer) else a for a in types]
+
+        def record(*args, _name=name):
+            kinds = {1: binding.KvBatch, 2: binding.KvRotation} if _name == "tpq_kv_append" else {1: binding.KvBatch}
+            seen.append((_name, [bytes(kinds[i].from_address(x)) if i in kinds and x else x for i, x in enumerate(args)]))
+            return 5
+
+        fn = ctypes.CFUNCTYPE(res, *plain)(record)
+        keep.append(fn)
+        addresses.append(ctypes.cast(fn, ctypes.c_void_p).value)
+    c, ctx, big = binding._calls, 2 ** 47 + 8, 2 ** 64 - 16
+    batch = binding.KvBatch(2 ** 47, 2 ** 33, 16, 7, 32, 48, 3, 4, 2 ** 20)
+    rot = binding.KvRotation(64, 2 ** 21, 128, 1, None)
+    try:
+        c.bind(addresses)
+        args = (ctx, batch, rot, 16, 24, 32, 40, 48, 56, 64, 72, big)
+        assert c.kv_append(*args) == 5
+        assert seen.pop() == ("tpq_kv_append", [ctx, bytes(batch), bytes(rot), 16, 24, 32, 40, 48, 56, 64, 72, big])
+        assert c.kv_append(ctx, batch, None, 16, 24, 32, 40, None, 56, None, 72, 0) == 5
+        assert seen.pop() == ("tpq_kv_append", [ctx, bytes(batch), None, 16, 24, 32, 40, None, 56, None, 72, None])
+        for i, bad in ((1, rot), (1, bytes(batch)), (1, None), (2, batch), (3, 1.0), (4, None), (11, "0")):
+            assert c.kv_append(*args[:i], bad, *args[i + 1:]) is None
+        args = (ctx, batch, 16, 24, 0.125, 2 ** 40, -1, 32, 40, 48, 2 ** 63, big)
+        assert c.kv_attention(*args) == 5
+        assert seen.pop() == ("tpq_kv_attention", [ctx, bytes(batch), 16, 24, 0.125, 2 ** 40, -1, 32, 40, 48, 2 ** 63, big])
+        for i, bad in ((1, rot), (1, ctypes.pointer(batch)), (4, 1), (4, np.float64(1)), (5, 1.5), (9, None), (10, -1)):
+            assert c.kv_attention(*args[:i], bad, *args[i + 1:]) is None
+        assert not seen
+    finally:
+        c.bind([ctypes.cast(getattr(binding.lib(), n), ctypes.c_void_p).value for n in binding._CALLS])
+    kv = binding.TpqKv.__new__(binding.TpqKv)   # a closed handle: refused by the library either way
+    kv._h, kv._p, kv.n_heads, kv.n_kv_heads, kv.head_dim, kv.page_size = ctypes.c_void_p(), None, 2, 2, 64, 16
+    for call in (lambda: kv.append(batch, 16, 16), lambda: kv.attention(batch, 16, 32, 48, 64, scale=0.5), lambda: kv.attention(batch, 16, 32, 48, 64, scale=1),
+                 lambda: kv.read(batch, 16, 32)):
+        with pytest.raises(binding.TpqError) as e:
+            call()
+        assert e.value.status == binding.TPQ_ERR_INVALID_ARG
