@@ -419,10 +419,13 @@ tpq_status tpq_kv_read(tpq_kv *kv, const tpq_kv_batch *batch, void *k_out_dev, i
  *   t <= p, and, if window > 0, t > p - window or t < n_first
  * (the sliding window of the last `window` positions, p's own among them, and the first n_first positions, which stay
  * visible).  k_t, v_t: the values low + step * code of key head h / (n_heads / n_kv_heads).  Zeros where nothing is
- * visible (all pages of a row were bad).  Products of queries and codes are exact, sums and softmax statistics are
- * binary32; the weights times the values' steps are rounded to 11 bits ahead of their products with the codes; one
- * rounding to BF16 at the end.
- *   q, out    : [n_tokens][n_heads * head_dim] BF16, rows 16-byte aligned; out must not overlap q
+ * visible (all pages of a row were bad).  Sums and softmax statistics are binary32.  Roundings on the way, each to 11 bits: the weights (times
+ * the values' steps, or a power of two that 16 positions share); where a sequence brings more than 32 rows (new positions times query heads
+ * per key head; any number in a batch of one sequence whose max_new allows more), the keys' and values' values too (bits below
+ * 2^-28 of the largest value of 16 positions are lost).  One rounding to BF16 at the end.  A position whose key or value is NaN makes the rows that
+ * see it NaN, and no others.
+ *   q, out    : [n_tokens][n_heads * head_dim] BF16, rows 16-byte aligned; out must not overlap q; at most 2^30 rows times query
+ *               heads per key head
  *   scale     : finite (1/sqrt(head_dim) as a rule);  window : 0 for none;  n_first : >= 0, without effect if there is no window
  *   workspace : >= tpq_kv_attention_workspace(kv, n_seqs, max_new, n_tokens) bytes of device memory, 16-byte aligned, whose
  *               contents need no preparation and mean nothing afterwards.  Calls that may overlap on the GPU (other

@@ -29,6 +29,15 @@ tpq_status cuda_fail(tpq_kv *kv, cudaError_t e, const char *what)
 
 inline bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
+tpq_status check_device(tpq_kv *kv)
+{
+    int dev = -1;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return cuda_fail(kv, e, "cudaGetDevice");
+    if (dev != kv->device) return fail(kv, TPQ_ERR_BAD_STATE, "the handle's device (%d) must be the current CUDA device (%d)", kv->device, dev);
+    return TPQ_OK;
+}
+
 // Checks of a batch that need no device; nothing is left to do where *empty comes back true.
 tpq_status check_batch(tpq_kv *kv, const tpq_kv_batch *a, kv_batch *b, bool *empty)
 {
@@ -49,10 +58,8 @@ tpq_status check_batch(tpq_kv *kv, const tpq_kv_batch *a, kv_batch *b, bool *emp
         return fail(kv, TPQ_ERR_ALIGN, "page table, token starts and lengths must be 4-byte aligned");
     if (a->n_pages > INT32_MAX || a->page_table_stride > INT32_MAX)
         return fail(kv, TPQ_ERR_INVALID_ARG, "n_pages or page_table_stride above 2^31 - 1");
-    int dev = -1;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return cuda_fail(kv, e, "cudaGetDevice");
-    if (dev != kv->device) return fail(kv, TPQ_ERR_BAD_STATE, "the handle's device (%d) must be the current CUDA device (%d)", kv->device, dev);
+    const tpq_status st = check_device(kv);
+    if (st != TPQ_OK) return st;
     int shift = 0;
     while ((1 << shift) < kv->page_size) ++shift;
     *b = kv_batch{static_cast<uint8_t *>(a->cache_dev), a->page_table_dev, a->token_start_dev, a->lengths_dev, a->n_pages,
@@ -186,6 +193,8 @@ tpq_status tpq_kv_attention(tpq_kv *kv, const tpq_kv_batch *batch, const void *q
     if ((st = check_rows(kv, "q", q, q_stride, kv->n_heads)) != TPQ_OK) return st;
     if ((st = check_rows(kv, "out", out, out_stride, kv->n_heads)) != TPQ_OK) return st;
     if (q == out) return fail(kv, TPQ_ERR_INVALID_ARG, "out is q");
+    if (batch->n_tokens * (kv->n_heads / kv->n_kv_heads) > KV_MOST)
+        return fail(kv, TPQ_ERR_INVALID_ARG, "%lld rows of %d query heads per key head are more than 2^30", (long long)batch->n_tokens, kv->n_heads / kv->n_kv_heads);
     const size_t need = tpq_kv_attention_workspace(kv, batch->n_seqs, batch->max_new, batch->n_tokens);
     if (need && !workspace) return fail(kv, TPQ_ERR_INVALID_ARG, "workspace is NULL");
     if (!aligned(workspace, 16)) return fail(kv, TPQ_ERR_ALIGN, "the workspace must be 16-byte aligned");
@@ -202,6 +211,8 @@ tpq_status tpq_kv_device_status(tpq_kv *kv)
 {
     if (!kv) return TPQ_ERR_INVALID_ARG;
     kv->err[0] = 0;
+    const tpq_status st = check_device(kv);
+    if (st != TPQ_OK) return st;
     int word = 0;
     cudaError_t e = cudaDeviceSynchronize();
     if (e == cudaSuccess) e = cudaMemcpy(&word, kv->status, sizeof word, cudaMemcpyDeviceToHost);

@@ -4,7 +4,9 @@
 // A vector is one head of one row.  D/8 lanes hold it, 8 adjacent values each: one 16-byte load, and the lane's 8 codes
 // are one 32-bit word of the cache.  A warp takes one row and up to KV_ITER * 256/D heads of one kind (queries, keys or values:
 // no lane of a warp does another's work), all loads ahead of the arithmetic.  Nothing is read twice; what bounds a long prompt is
-// memory, what bounds one token is the chain token start -> length -> page number -> store.
+// memory (7652 rows of 64 query and 2 x 8 key and value heads of 128, and reading them back: 70 us, 4.7 TB/s; the division per value
+// that was there first 80 us), what bounds one token is the chain token start -> length -> page number -> store (12 us with the read, all
+// of it launches).  Four heads a lane at a time: two 91 us, eight 110; several jobs a warp one after the other: 76.
 #include "kv_internal.h"
 
 #include <cuda_bf16.h>

@@ -22,13 +22,17 @@
 // or column of a fragment is free as long as both sides agree: lanes read 16 (keys) and 8 (values) contiguous bytes of a
 // position, conflict-free and two-way.  mma.sync and not tcgen05: 16 positions x 8 rows are an eighth of the smallest
 // tcgen05 tile, and what bounds this kernel is the memory that the codes come from and the instructions that unpack them
-// (about 190 per warp and 16 positions of 2176 bytes).
+// (about 300 per warp and 16 positions of 2176 bytes).
 //
 // Work.  The positions of all sequences and key heads are cut into tiles of 256 (128 for more than 8 rows) and dealt out evenly, in order, to as many
 // blocks as the GPU holds at a time, whatever the lengths are (a graph with this call replays for others).  A block whose
 // run begins or ends inside a (sequence, key head) leaves a partial result, at most two in all; attention_join puts them
 // together.  A warp takes a quarter of a tile, by itself: its copies (16 positions = one
 // contiguous block of the cache), its barriers, its running maximum; the warps meet at the end of a (sequence, key head).
+//
+// What bounds it: instructions, 57 % of the issue slots (three warps a scheduler; the rest is their latency).  32 sequences of 16 to 32
+// thousand positions, 64 heads of 128 on 8: 209 us, 4.2 TB/s (two blocks of positions at a time 245 us: copies' bookkeeping and maxima cost as much
+// again); 64 of up to 8000, 4 heads on 2: 34 us, half of it beginnings and ends of runs; one sequence of 777: 11 us, the host's two launches.
 #include "kv_internal.h"
 
 #include <cuda_bf16.h>
@@ -208,6 +212,43 @@ attention_split(const split_params p)
         const int nt = tl.count - t0 < unit_end - unit ? tl.count - t0 : unit_end - unit;
         const int rows = seq.n * p.group - row0 < R ? seq.n * p.group - row0 : R, p0 = seq.len - seq.n;
 
+        // ---- copies: chunk j of the segment, block `lane` (below C) of it; the first ones are under way while the rows are fetched
+        auto base_of = [&](int j) {
+            const int t = t0 + j;
+            return (t < tl.first ? t : tl.from + t - tl.first) * TILE + warp * CHUNK;
+        };
+        auto page_of = [&](int j) {  // page of this lane's block of chunk j, -1: none to copy
+            if (j >= nt || lane >= C) return -1;
+            const int pos = base_of(j) + lane * KV_BLOCK;
+            if (pos >= seq.len) return -1;
+            if (p.c.window && pos >= p.c.n_first && pos + KV_BLOCK <= p0 - p.c.window + 1) return -1;  // no row sees it
+            const int page = b.table[s * b.table_stride + (pos >> b.page_shift)];
+            if (page >= 0 && page < b.n_pages) return page;
+            kv_report(b);
+            return -1;
+        };
+        auto issue = [&](int j, int page) {
+            const int st = (phase + j) % NS;
+            const uint32_t bar = smem_u32(&sh.full[warp][st]);
+            const uint32_t there = __ballot_sync(0xffffffffu, page >= 0);
+            issued = phase + j + 1;
+            if (lane == 0) {
+                sh.there[warp][st] = there;
+                mbar_expect_tx(bar, __popc(there) * kv_block_bytes(D));
+            }
+            __syncwarp();
+            if (page >= 0) {
+                const int pos = base_of(j) + lane * KV_BLOCK, blocks = b.page_size / KV_BLOCK;
+                const uint8_t *src = b.cache + (((int64_t)page * b.n_kv_heads + kh) * blocks + (pos & (b.page_size - 1)) / KV_BLOCK) * kv_block_bytes(D);
+                bulk_g2s(smem_u32(&sh.ring[warp][st][lane * kv_block_bytes(D)]), src, kv_block_bytes(D), bar);
+            }
+        };
+#pragma unroll
+        for (int j = 0; j < NS - 1; ++j)
+            if (j < nt) issue(j, page_of(j));
+        int next_page = page_of(NS - 1);
+
+
         // ---- the rows as operands: column n = lane / 4 of a group of 8, values 8 KW i4 .. of the head in the order (0 4)(1 5)(2 6)(3 7),
         // in FP16, scaled so that the row's largest magnitude is in [2^14, 2^15) (BF16's 8 bits stay exact down to 2^-27 of that),
         // a 16th of it where the codes come 16-fold
@@ -276,42 +317,6 @@ attention_split(const split_params p)
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) o[n][k][0] = o[n][k][1] = o[n][k][2] = o[n][k][3] = 0.0f;
         }
-
-        // ---- copies: chunk j of the segment, block `lane` (below C) of it
-        auto base_of = [&](int j) {
-            const int t = t0 + j;
-            return (t < tl.first ? t : tl.from + t - tl.first) * TILE + warp * CHUNK;
-        };
-        auto page_of = [&](int j) {  // page of this lane's block of chunk j, -1: none to copy
-            if (j >= nt || lane >= C) return -1;
-            const int pos = base_of(j) + lane * KV_BLOCK;
-            if (pos >= seq.len) return -1;
-            if (p.c.window && pos >= p.c.n_first && pos + KV_BLOCK <= p0 - p.c.window + 1) return -1;  // no row sees it
-            const int page = b.table[s * b.table_stride + (pos >> b.page_shift)];
-            if (page >= 0 && page < b.n_pages) return page;
-            kv_report(b);
-            return -1;
-        };
-        auto issue = [&](int j, int page) {
-            const int st = (phase + j) % NS;
-            const uint32_t bar = smem_u32(&sh.full[warp][st]);
-            const uint32_t there = __ballot_sync(0xffffffffu, page >= 0);
-            issued = phase + j + 1;
-            if (lane == 0) {
-                sh.there[warp][st] = there;
-                mbar_expect_tx(bar, __popc(there) * kv_block_bytes(D));
-            }
-            __syncwarp();
-            if (page >= 0) {
-                const int pos = base_of(j) + lane * KV_BLOCK, blocks = b.page_size / KV_BLOCK;
-                const uint8_t *src = b.cache + (((int64_t)page * b.n_kv_heads + kh) * blocks + (pos & (b.page_size - 1)) / KV_BLOCK) * kv_block_bytes(D);
-                bulk_g2s(smem_u32(&sh.ring[warp][st][lane * kv_block_bytes(D)]), src, kv_block_bytes(D), bar);
-            }
-        };
-#pragma unroll
-        for (int j = 0; j < NS - 1; ++j)
-            if (j < nt) issue(j, page_of(j));
-        int next_page = page_of(NS - 1);
 
         for (int j = 0; j < nt && ok; ++j) {
             __syncwarp();  // every lane has read the stage that the next copy overwrites
@@ -660,7 +665,7 @@ size_t kv_attention_workspace(int D, int n_heads, int n_kv_heads, int sm_count, 
     const int nt = row_groups(max_new * group);
     const size_t blocks = (size_t)sm_count * BLOCKS_PER_SM;
     return blocks * 16 + blocks * 2 * 8 * nt * part_row(D) * 4 +
-           (max_new * group > MAX_ROWS ? kv_prompt_workspace(D, (int)group, sm_count, n_seqs, n_tokens, MAX_ROWS) : 0);
+           (max_new * group > MAX_ROWS ? kv_prompt_workspace(D, (int)group, sm_count, n_seqs, n_tokens) : 0);
 }
 
 cudaError_t kv_launch_attention(const kv_batch &b, int D, const kv_attention_call &c, int sm_count, cudaStream_t st, int64_t *launches)
@@ -672,8 +677,9 @@ cudaError_t kv_launch_attention(const kv_batch &b, int D, const kv_attention_cal
     const size_t blocks = (size_t)sm_count * BLOCKS_PER_SM;
     p.parts = reinterpret_cast<float *>(p.headers + blocks);
     if (max_rows > MAX_ROWS) {
-        const cudaError_t e = kv_launch_prompt(b, D, c, MAX_ROWS, p.parts + blocks * 2 * 8 * nt * part_row(D), sm_count, st, launches);
-        if (e != cudaSuccess) return e;
+        // (of one sequence the kernels for many rows take whatever it brings: two launches less)
+        const cudaError_t e = kv_launch_prompt(b, D, c, b.n_seqs == 1 ? 0 : MAX_ROWS, p.parts + blocks * 2 * 8 * nt * part_row(D), sm_count, st, launches);
+        if (e != cudaSuccess || b.n_seqs == 1) return e;
     }
     if (D == 128) return nt == 1 ? launch_split<128, 1>(p, sm_count, st, launches) : launch_split<128, 2>(p, sm_count, st, launches);
     return nt == 1 ? launch_split<64, 1>(p, sm_count, st, launches) : launch_split<64, 2>(p, sm_count, st, launches);

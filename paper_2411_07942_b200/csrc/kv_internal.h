@@ -46,7 +46,7 @@ struct kv_attention_call {
 size_t kv_attention_workspace(int D, int n_heads, int n_kv_heads, int sm_count, int64_t n_seqs, int64_t max_new, int64_t n_tokens);
 cudaError_t kv_launch_attention(const kv_batch &b, int D, const kv_attention_call &c, int sm_count, cudaStream_t st, int64_t *launches);
 // Sequences with more than `few` rows (new positions x query heads of a key head); kv_launch_attention calls it.
-size_t kv_prompt_workspace(int D, int group, int sm_count, int64_t n_seqs, int64_t n_tokens, int few);
+size_t kv_prompt_workspace(int D, int group, int sm_count, int64_t n_seqs, int64_t n_tokens);
 cudaError_t kv_launch_prompt(const kv_batch &b, int D, const kv_attention_call &c, int few, void *workspace, int sm_count, cudaStream_t st,
                              int64_t *launches);
 

@@ -22,6 +22,15 @@
 // Work.  attention_plan lists the (sequence, 256 rows) pairs and adds up their tiles (causal, window); a run of tiles in that order
 // goes to each block, all of the same length.  A run that begins or ends inside a pair's key head leaves a partial result, at
 // most two a block, which attention_prompt_join puts together.
+//
+// What bounds it.  4800 clocks for 256 rows x 128 positions, 2080 of them on the tensor pipe (without contention for shared memory): of each
+// row tile the scores, the walk over them (650 clocks to the maximum, 2000 of exponentials) and the products follow each other, and only
+// the two row tiles overlap.  2 x 8191 tokens, 32 heads of 128 on 16, window 4096: 1100 us, 750 TFLOP/s of what is visible; 2048 tokens, 10 heads:
+// 46 us, of which the plan, the first and last tiles and the joining are half.  Measured and not kept: scores in two halves of 64 positions a step ahead (a
+// product of 64 columns takes as long as one of 128, whose rows of Q are what is read: 1463 us), both softmax warpgroups on one row tile (the
+// exchange of maxima costs more than it hides: 1405 us), an MMA thread for each row tile (1235 us), codes instead of formed keys and values as operands (five
+// terms a position to load per row: 2750 us at the time, against 2285 with formed values), 128 scores in registers (89 KB of code: a
+// quarter of the warps' time went into fetching instructions).
 // Every wait is bounded: on expiry the block records TPQ_ERR_TIMEOUT, frees its tensor memory and returns.
 #include "kv_internal.h"
 
@@ -35,8 +44,10 @@ constexpr int RAW = 4;                          // copy stages
 constexpr int THREADS = 18 * 32;
 constexpr int UNPACK = 2, SOFTMAX = 10;         // first warps of those roles (eight each: two on every scheduler)
 constexpr int PLAN_THREADS = 1024;
-// Runs are dealt out in units: a (256 rows, key head) pair is its tiles and EXTRA more, which stand for its beginning and end.
-constexpr int EXTRA = 4;
+// Runs are dealt out in units: a (256 rows, key head) pair is its tiles and EXTRA more, which stand for its beginning and end (13 700
+// clocks against 4800 of a tile: fitted to the blocks' times.  2 x 8191 tokens, 32 heads on 16, window 4096: 1098 us; with 2 extra ones
+// 1266, 4: 1103, 6: 1122).
+constexpr int EXTRA = 3;
 
 // A sequence's rows row0 .. row0 + rows - 1 (row: new position x query head of a key head).
 struct alignas(16) plan_item {
@@ -929,17 +940,20 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
     }
 }
 
-// Puts the partial results together that run blockIdx.x ends with the first part of: a warp per row.
+// Puts the partial results together that run blockIdx.x ends with the first part of: a warp per row, JOIN_BLOCKS blocks.
+constexpr int JOIN_BLOCKS = 8;
 template <int D>
 __global__ void __launch_bounds__(256) attention_prompt_join(const prompt_params p)
 {
     constexpr int V = D / 32;  // values of a lane
     tpq_grid_dep_wait();
     const int4 head = p.headers[blockIdx.x];  // parts, item, key head
-    const int lane = threadIdx.x & 31, r = blockIdx.y * 8 + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31;
     if (head.x == 0) return;
     const plan_item &it = p.items[head.y];
-    if (r >= it.rows) return;
+    const int rows = it.rows;
+#pragma unroll 1
+    for (int r = blockIdx.y * (BM / JOIN_BLOCKS) + (threadIdx.x >> 5); r < min(rows, (int)(blockIdx.y + 1) * (BM / JOIN_BLOCKS)); r += 8) {
     float m = -INFINITY, l = 0.0f, o[V] = {};
     for (int i = 0; i < head.x; ++i) {
         const float *part = p.parts + ((((int64_t)blockIdx.x + i) * 2 + (i == 0 ? 1 : 0)) * BM + r) * (D + 4);
@@ -966,29 +980,29 @@ __global__ void __launch_bounds__(256) attention_prompt_join(const prompt_params
         const __nv_bfloat162 v = __floats2bfloat162_rn(o[2 * k] * inv, o[2 * k + 1] * inv);
         dst[k] = *reinterpret_cast<const uint32_t *>(&v);
     }
+    }
 }
 
-int64_t most_items(int64_t n_seqs, int64_t n_tokens, int64_t group, int few)
+int64_t most_items(int64_t n_seqs, int64_t n_tokens, int64_t group)  // full items and one more of every sequence with rows
 {
-    const int64_t rows = n_tokens * group, seqs = rows / (few + 1);  // sequences with more than `few` rows, full items
-    return rows / BM + (seqs < n_seqs ? seqs : n_seqs) + 1;
+    const int64_t rows = n_tokens * group;
+    return rows / BM + (rows < n_seqs ? rows : n_seqs) + 1;
 }
 
 size_t up16(size_t n) { return (n + 15) / 16 * 16; }
 
 }  // namespace
 
-size_t kv_prompt_workspace(int D, int group, int sm_count, int64_t n_seqs, int64_t n_tokens, int few)
+size_t kv_prompt_workspace(int D, int group, int sm_count, int64_t n_seqs, int64_t n_tokens)
 {
-    return up16(sizeof(plan_head)) + up16(sizeof(plan_item) * most_items(n_seqs, n_tokens, group, few)) + up16(4 * (size_t)n_seqs) + 16 * (size_t)sm_count +
+    return up16(sizeof(plan_head)) + up16(sizeof(plan_item) * most_items(n_seqs, n_tokens, group)) + up16(4 * (size_t)n_seqs) + 16 * (size_t)sm_count +
            (size_t)sm_count * 2 * BM * (D + 4) * 4;
 }
 
 cudaError_t kv_launch_prompt(const kv_batch &b, int D, const kv_attention_call &c, int few, void *workspace, int sm_count, cudaStream_t st, int64_t *launches)
 {
     const int group = b.n_heads / b.n_kv_heads;
-    const int64_t items = most_items(b.n_seqs, b.n_tokens, group, few);
-    if (b.n_tokens * group > INT32_MAX / 2 || items > INT32_MAX / 2) return cudaErrorInvalidConfiguration;
+    const int64_t items = most_items(b.n_seqs, b.n_tokens, group);
     uint8_t *w = static_cast<uint8_t *>(workspace);
     prompt_params p{b, c};
     p.head = reinterpret_cast<plan_head *>(w);
@@ -1015,8 +1029,8 @@ cudaError_t kv_launch_prompt(const kv_batch &b, int D, const kv_attention_call &
     e = D == 128 ? main(attention_prompt<128>, Smem<128>::BYTES) : main(attention_prompt<64>, Smem<64>::BYTES);
     if (e != cudaSuccess) return e;
     ++*launches;
-    e = D == 128 ? tpq_launch_pdl(attention_prompt_join<128>, dim3(sm_count, BM / 8), dim3(256), 0, st, p)
-                 : tpq_launch_pdl(attention_prompt_join<64>, dim3(sm_count, BM / 8), dim3(256), 0, st, p);
+    e = D == 128 ? tpq_launch_pdl(attention_prompt_join<128>, dim3(sm_count, JOIN_BLOCKS), dim3(256), 0, st, p)
+                 : tpq_launch_pdl(attention_prompt_join<64>, dim3(sm_count, JOIN_BLOCKS), dim3(256), 0, st, p);
     if (e == cudaSuccess) ++*launches;
     return e;
 }
