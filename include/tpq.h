@@ -370,8 +370,9 @@ size_t tpq_kv_page_bytes(const tpq_kv *kv); /* 0 for NULL */
  * tensors (none is allowed); they are its LAST positions: with n rows and length lengths[s] >= n, row i of the
  * sequence is position lengths[s] - n + i.  Position t lies in page page_table[s][t / page_size], entry t % page_size.
  * Only entries of the page table that a call needs are read (attention: pages with a visible position), so entries
- * of pages that a window has left behind may hold anything.  Rows from token_start[n_seqs] on belong to nobody: no
- * call reads or writes them, and a captured call can be replayed with fewer rows, sequences (n = 0) or other lengths. */
+ * of pages that a window has left behind may hold anything.  Rows from token_start[n_seqs] on belong to nobody: what
+ * they hold does not matter, nothing of theirs is written, and a captured call can be replayed with fewer rows, sequences (n = 0) or
+ * other lengths. */
 typedef struct tpq_kv_batch {
     void *cache_dev;               /* n_pages * tpq_kv_page_bytes bytes, 16-byte aligned */
     int64_t n_pages;

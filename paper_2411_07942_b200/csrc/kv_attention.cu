@@ -22,7 +22,7 @@
 // or column of a fragment is free as long as both sides agree: lanes read 16 (keys) and 8 (values) contiguous bytes of a
 // position, conflict-free and two-way.  mma.sync and not tcgen05: 16 positions x 8 rows are an eighth of the smallest
 // tcgen05 tile, and what bounds this kernel is the memory that the codes come from and the instructions that unpack them
-// (about 300 per warp and 16 positions of 2176 bytes).
+// (275 per warp and 16 positions of 2176 bytes).
 //
 // Work.  The positions of all sequences and key heads are cut into tiles of 256 (128 for more than 8 rows) and dealt out evenly, in order, to as many
 // blocks as the GPU holds at a time, whatever the lengths are (a graph with this call replays for others).  A block whose
@@ -30,7 +30,7 @@
 // together.  A warp takes a quarter of a tile, by itself: its copies (16 positions = one
 // contiguous block of the cache), its barriers, its running maximum; the warps meet at the end of a (sequence, key head).
 //
-// What bounds it: instructions, 57 % of the issue slots (three warps a scheduler; the rest is their latency).  32 sequences of 16 to 32
+// What bounds it: instructions, 53 % of the issue slots (three warps a scheduler; the rest is their latency).  32 sequences of 16 to 32
 // thousand positions, 64 heads of 128 on 8: 209 us, 4.2 TB/s (two blocks of positions at a time 245 us: copies' bookkeeping and maxima cost as much
 // again); 64 of up to 8000, 4 heads on 2: 34 us, half of it beginnings and ends of runs; one sequence of 777: 11 us, the host's two launches.
 #include "kv_internal.h"
