@@ -32,7 +32,7 @@
 //
 // What bounds it: instructions, 53 % of the issue slots (three warps a scheduler; the rest is their latency).  32 sequences of 16 to 32
 // thousand positions, 64 heads of 128 on 8: 209 us, 4.2 TB/s (two blocks of positions at a time 245 us: copies' bookkeeping and maxima cost as much
-// again); 64 of up to 8000, 4 heads on 2: 34 us, half of it beginnings and ends of runs; one sequence of 777: 11 us, the host's two launches.
+// again); 64 of up to 8000, 4 heads on 2: 33 us, half of it beginnings and ends of runs; one sequence of 777: 11 us, the host's two launches.
 #include "kv_internal.h"
 
 #include <cuda_bf16.h>
@@ -42,6 +42,10 @@ namespace {
 
 constexpr int WARPS = 4;
 constexpr int MAX_ROWS = 32;  // rows (new positions x query heads of a key head) of a sequence here: in groups of 8 NT, one after the other
+
+// Runs are dealt out in units: a (sequence, key head, group of rows) is its tiles and EXTRA more, which stand for its beginning and end
+// (24 sequences of 16 to 32 rows, ragged: 54.8 us with none, 50.2 with one, 44.4 with two or three; 64 of one row: 33.5, 32.7, 32.5, 32.3).
+constexpr int EXTRA = 2;
 
 // NT: groups of 8 rows.  Blocks of 16 positions that a warp takes at a time: what is done once for them (the copies' bookkeeping, the
 // maxima, adding the sums up) costs less the more they are; four where registers allow.  Stages of a warp's ring and blocks of an SM: what
@@ -114,6 +118,7 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x)
 // Tiles of a sequence that any of its rows sees: [0, first) and [from, end); its groups of rows.
 struct tiles_of {
     int first, from, count, groups;
+    __device__ int units() const { return count ? count + EXTRA : 0; }  // of a (sequence, key head, group of rows)
 };
 __device__ __forceinline__ tiles_of visible_tiles(const kv_seq &s, const kv_attention_call &c, int group, int tile, int rows)
 {
@@ -154,7 +159,7 @@ attention_split(const split_params p)
     int64_t want = 0;
     for (int s = s0; s < s1; ++s) {
         const tiles_of t = visible_tiles(kv_load_seq(b, s), p.c, p.group, tile(NT), 8 * NT);
-        want += (int64_t)t.count * t.groups * b.n_kv_heads;
+        want += (int64_t)t.units() * t.groups * b.n_kv_heads;
     }
     if (want >= 1 << 23) {  // (2^30 positions of key heads in a 128th of the sequences: the sums below are in 32 bits)
         kv_report(b);
@@ -185,7 +190,7 @@ attention_split(const split_params p)
         int off = unit - before, s = s0;
         for (;; ++s) {
             const tiles_of t = visible_tiles(kv_load_seq(b, s), p.c, p.group, tile(NT), 8 * NT);
-            const int n = t.count * t.groups * b.n_kv_heads;
+            const int n = t.units() * t.groups * b.n_kv_heads;
             if (off < n) break;
             off -= n;
         }
@@ -202,14 +207,18 @@ attention_split(const split_params p)
     while (unit < unit_end) {
         const kv_seq seq = kv_load_seq(b, s);
         const tiles_of tl = visible_tiles(seq, p.c, p.group, tile(NT), 8 * NT);
-        const int all_tiles = tl.count * tl.groups * b.n_kv_heads;
-        if (off >= all_tiles) {
-            off -= all_tiles;
+        const int units = tl.units(), all_units = units * tl.groups * b.n_kv_heads;
+        if (off >= all_units) {
+            off -= all_units;
             ++s;
             continue;
         }
-        const int pair = off / tl.count, kh = NT == 1 ? pair : pair / tl.groups, row0 = NT == 1 ? 0 : (pair - kh * tl.groups) * R, t0 = off - pair * tl.count;
-        const int nt = tl.count - t0 < unit_end - unit ? tl.count - t0 : unit_end - unit;
+        const int pair = off / units, kh = NT == 1 ? pair : pair / tl.groups, row0 = NT == 1 ? 0 : (pair - kh * tl.groups) * R, u0 = off - pair * units;
+        const int nu = units - u0 < unit_end - unit ? units - u0 : unit_end - unit;
+        const int t0 = u0 > EXTRA ? u0 - EXTRA : 0, nt = u0 + nu - EXTRA - t0;
+        unit += nu;
+        off += nu;
+        if (nt <= 0) continue;  // (the run begins or ends inside the extra units)
         const int rows = seq.n * p.group - row0 < R ? seq.n * p.group - row0 : R, p0 = seq.len - seq.n;
 
         // ---- copies: chunk j of the segment, block `lane` (below C) of it; the first ones are under way while the rows are fetched
@@ -567,8 +576,6 @@ attention_split(const split_params p)
             header = make_int4(1 + (tl.count - nt + share - 1) / share, seq.start, row0 << 16 | rows, kh);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the sums were written where copies go next
         __syncthreads();
-        unit += nt;
-        off += nt;
     }
     if (!ok && lane == 0) {  // giving up: let the copies in flight land before the shared memory is released
         atomicExch(b.status, (int)TPQ_ERR_TIMEOUT);
@@ -637,8 +644,8 @@ attention_join(const split_params p, int runs)
     }
 }
 
-// Groups of 8 rows that a warp takes at a time: one where no sequence has more rows, else two (24 sequences of 16 to 32 rows, heads of 64:
-// 55 us; four groups at once, with spilled registers and two blocks an SM, 81; one after the other 63).
+// Groups of 8 rows that a warp takes at a time: one where no sequence has more rows, else two (24 sequences of 16 to 32 rows, heads of 64,
+// before the runs were weighed: 55 us; four groups at once, with spilled registers and two blocks an SM, 81; one at a time 63).
 int row_groups(int64_t max_rows) { return max_rows <= 8 ? 1 : 2; }
 
 template <int D, int NT>
