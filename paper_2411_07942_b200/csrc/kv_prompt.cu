@@ -28,7 +28,8 @@
 // the two row tiles overlap.  2 x 8191 tokens, 32 heads of 128 on 16, window 4096: 1100 us, 750 TFLOP/s of what is visible; 2048 tokens, 10 heads:
 // 46 us, of which the plan, the first and last tiles and the joining are half.  Measured and not kept: scores in two halves of 64 positions a step ahead (a
 // product of 64 columns takes as long as one of 128, whose rows of Q are what is read: 1463 us), both softmax warpgroups on one row tile (the
-// exchange of maxima costs more than it hides: 1405 us), an MMA thread for each row tile (1235 us), codes instead of formed keys and values as operands (five
+// exchange of maxima costs more than it hides: 1405 us), an MMA thread for each row tile (1235 us), blocks of 16 scores
+// loaded while the one before is worked on (1209 us against 1104: more and smaller loads and stores of tensor memory), codes instead of formed keys and values as operands (five
 // terms a position to load per row: 2750 us at the time, against 2285 with formed values), 128 scores in registers (89 KB of code: a
 // quarter of the warps' time went into fetching instructions).
 // Every wait is bounded: on expiry the block records TPQ_ERR_TIMEOUT, frees its tensor memory and returns.
@@ -272,7 +273,10 @@ __device__ __forceinline__ void ld32(uint32_t addr, uint32_t *r)
         : "r"(addr)
         : "memory");
 }
-__device__ __forceinline__ void ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+#define T8(r, i) "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]), "+r"(r[i + 6]), "+r"(r[i + 7])
+// (the loaded registers pass through: nothing that uses them comes ahead of the wait; `loaded`: of another 32, behind the same wait)
+__device__ __forceinline__ void ld_wait(uint32_t *r) { asm volatile("tcgen05.wait::ld.sync.aligned;" : T8(r, 0), T8(r, 8), T8(r, 16), T8(r, 24)::"memory"); }
+__device__ __forceinline__ void loaded(uint32_t *r) { asm volatile("" : T8(r, 0), T8(r, 8), T8(r, 16), T8(r, 24)::"memory"); }
 __device__ __forceinline__ void st32(uint32_t addr, const uint32_t *r)
 {
     asm volatile(
@@ -777,7 +781,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                     for (int c = 0; c < TILE; c += 32) {
                         uint32_t x[32];
                         ld32(s_addr + c, x);
-                        ld_wait();
+                        ld_wait(x);
                         const int at = base + c;
                         const uint32_t see = low_bits(pos - at + 1) & (p.c.window ? ~low_bits(pos - p.c.window + 1 - at) | low_bits(p.c.n_first - at) : 0xffffffffu);
 #pragma unroll
@@ -794,7 +798,8 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                     uint32_t x[64];
                     ld32(s_addr + c, x);
                     ld32(s_addr + c + 32, x + 32);
-                    ld_wait();
+                    ld_wait(x);
+                    loaded(x + 32);
 #pragma unroll
                     for (int k = 0; k < 64; k += KV_BLOCK) {
                         const float4 tm = lds4(term + (c + k) / KV_BLOCK * 16);
@@ -818,7 +823,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                     for (int k = 0; k < D; k += 32) {
                         uint32_t o[32];
                         ld32(o_addr + k, o);
-                        ld_wait();
+                        ld_wait(o);
 #pragma unroll
                         for (int z = 0; z < 32; ++z) o[z] = __float_as_uint(__uint_as_float(o[z]) * a);
                         st32(o_addr + k, o);
@@ -831,7 +836,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                 for (int c = 0; c < TILE; c += 32) {
                     uint32_t x[32], h[16];
                     ld32(s_addr + c, x);
-                    ld_wait();
+                    ld_wait(x);
 #pragma unroll
                     for (int b0 = 0; b0 < 32; b0 += KV_BLOCK) {
                         const float4 tm = lds4(term + (c + b0) / KV_BLOCK * 16);
@@ -882,7 +887,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                 uint32_t o[32];
                 if (works) {
                     ld32(o_addr + k, o);
-                    ld_wait();
+                    ld_wait(o);
                 } else {
 #pragma unroll
                     for (int z = 0; z < 32; ++z) o[z] = 0;
