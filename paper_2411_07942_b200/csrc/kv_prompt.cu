@@ -578,55 +578,52 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
     } else if (warp == 1) {
         // ---------------- MMA: one thread, known to the compiler as such
         if (elect()) {
-        constexpr uint32_t qk_instr = instr(TILE, false), pv_instr = instr(D, true);
-        int it = 0;                             // tiles so far: operand buffer it % 2
-        // a bit for each row tile: phase of its scores' barrier, of its rows' and sums' barriers, whether it has had sums before
-        uint32_t p_phase = 0, q_phase = 0, begun = 0;
-        segment g;
-        while (ok && next_segment(p, r, g)) {
-            const reach re_a = reach_of(g, 0), re_b = reach_of(g, 1);
-            int last_a = -1, last_b = -1;
+            constexpr uint32_t qk_instr = instr(TILE, false), pv_instr = instr(D, true);
+            int it = 0;                             // tiles so far: operand buffer it % 2
+            // a bit for each row tile: phase of its scores' barrier, of its rows' and sums' barriers, whether it has had sums before
+            uint32_t p_phase = 0, q_phase = 0, begun = 0;
+            segment g;
+            while (ok && next_segment(p, r, g)) {
+                const reach re_a = reach_of(g, 0), re_b = reach_of(g, 1);
+                int last_a = -1, last_b = -1;
 #pragma unroll 1
-            for (int j = g.nt - 1; j >= 0 && last_a < 0; --j)
-                if (sees(p, re_a, g.base(j))) last_a = j;
+                for (int j = g.nt - 1; j >= 0 && last_a < 0; --j)
+                    if (sees(p, re_a, g.base(j))) last_a = j;
 #pragma unroll 1
-            for (int j = g.nt - 1; j >= 0 && last_b < 0; --j)
-                if (sees(p, re_b, g.base(j))) last_b = j;
-            uint32_t any = 0;  // row tiles with sums of this segment
-            // step j: P_t V(j) for both row tiles, each followed by Q_t K(j + 1); step -1 has the first scores only
+                for (int j = g.nt - 1; j >= 0 && last_b < 0; --j)
+                    if (sees(p, re_b, g.base(j))) last_b = j;
+                uint32_t any = 0;  // row tiles with sums of this segment
+                // step j: P_t V(j) for both row tiles, each followed by Q_t K(j + 1); step -1 has the first scores only
 #pragma unroll 1
-            for (int j = -1; j < g.nt && ok; ++j) {
-                const int i = it + j;
-                const bool more = j + 1 < g.nt;
-                if (j >= 0) ok = wait(bar(B_V_FULL + (i & 1)), (i >> 1) & 1);
+                for (int j = -1; j < g.nt && ok; ++j) {
+                    const int i = it + j;
+                    const bool more = j + 1 < g.nt;
+                    if (j >= 0) ok = wait(bar(B_V_FULL + (i & 1)), (i >> 1) & 1);
 #pragma unroll 1
-                for (int t = 0; t < 2 && ok; ++t) {
-                    if (j >= 0 && sees(p, t ? re_b : re_a, g.base(j))) {
-                        if (!(any >> t & 1) && (begun >> t & 1)) ok = wait(bar(B_O_EMPTY + t), (q_phase >> t & 1) ^ 1);
+                    for (int t = 0; t < 2 && ok; ++t) {
+                        if (j >= 0 && sees(p, t ? re_b : re_a, g.base(j))) {
+                            if (!(any >> t & 1) && (begun >> t & 1)) ok = wait(bar(B_O_EMPTY + t), (q_phase >> t & 1) ^ 1);
 #pragma unroll 1
-                        for (int half = 0; half < 2 && ok; ++half) {
-                            ok = wait(bar(B_P_FULL + 2 * half + t), p_phase >> t & 1);
-                            if (!ok) break;
-                            fence_after();
-                            {
+                            for (int half = 0; half < 2 && ok; ++half) {
+                                ok = wait(bar(B_P_FULL + 2 * half + t), p_phase >> t & 1);
+                                if (!ok) break;
+                                fence_after();
                                 const uint32_t v = operand(smem + L::V + (i & 1) * L::TILE_BYTES + half * (HALF * 128), TILE * 128);
 #pragma unroll
                                 for (int x = 0; x < HALF / 16; ++x)
                                     mma_ts(tmem + 256 + t * 128, tmem + t * TILE + half * (HALF / 2) + 8 * x, v + x * (2048 >> 4), OPERAND_HIGH, pv_instr, (any >> t & 1) | half | (x != 0));
                                 if (half == 1 && j == (t ? last_b : last_a)) commit(bar(B_O_FULL + t));
                             }
+                            if (!ok) break;
+                            any |= 1u << t;
+                            p_phase ^= 1u << t;
                         }
-                        if (!ok) break;
-                        any |= 1u << t;
-                        p_phase ^= 1u << t;
-                    }
-                    if (more) {
-                        if (j < 0 && (t ? last_b : last_a) >= 0) ok = wait(bar(B_Q_FULL + t), q_phase >> t & 1);
-                        if (t == 0 && ok) ok = wait(bar(B_K_FULL + ((i + 1) & 1)), ((i + 1) >> 1) & 1);
-                        if (!ok) break;
-                        fence_after();
-                        if (sees(p, t ? re_b : re_a, g.base(j + 1))) {
-                            {
+                        if (more) {
+                            if (j < 0 && (t ? last_b : last_a) >= 0) ok = wait(bar(B_Q_FULL + t), q_phase >> t & 1);
+                            if (t == 0 && ok) ok = wait(bar(B_K_FULL + ((i + 1) & 1)), ((i + 1) >> 1) & 1);
+                            if (!ok) break;
+                            fence_after();
+                            if (sees(p, t ? re_b : re_a, g.base(j + 1))) {
                                 const uint32_t a = operand(smem + L::Q + t * L::TILE_BYTES, 16), k = operand(smem + L::K + ((i + 1) & 1) * L::TILE_BYTES, 16);
 #pragma unroll
                                 for (int x = 0; x < D / 16; ++x) {
@@ -637,17 +634,14 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                             }
                         }
                     }
-                }
-                if (!ok) break;
-                {
+                    if (!ok) break;
                     if (j >= 0) commit(bar(B_V_EMPTY + (i & 1)));
                     if (more) commit(bar(B_K_EMPTY + ((i + 1) & 1)));
                 }
+                it += g.nt;
+                begun |= any;
+                q_phase ^= any;
             }
-            it += g.nt;
-            begun |= any;
-            q_phase ^= any;
-        }
         }
         __syncwarp();
     } else if (warp < SOFTMAX) {
@@ -959,32 +953,32 @@ __global__ void __launch_bounds__(256) attention_prompt_join(const prompt_params
     const int rows = it.rows;
 #pragma unroll 1
     for (int r = blockIdx.y * (BM / JOIN_BLOCKS) + (threadIdx.x >> 5); r < min(rows, (int)(blockIdx.y + 1) * (BM / JOIN_BLOCKS)); r += 8) {
-    float m = -INFINITY, l = 0.0f, o[V] = {};
-    for (int i = 0; i < head.x; ++i) {
-        const float *part = p.parts + ((((int64_t)blockIdx.x + i) * 2 + (i == 0 ? 1 : 0)) * BM + r) * (D + 4);
-        const float2 v = __ldcg(reinterpret_cast<const float2 *>(part + D));
-        float z[V];
-        if (V == 4) {
-            const float4 q = __ldcg(reinterpret_cast<const float4 *>(part) + lane);
-            z[0] = q.x, z[1] = q.y, z[V - 2] = q.z, z[V - 1] = q.w;
-        } else {
-            const float2 q = __ldcg(reinterpret_cast<const float2 *>(part) + lane);
-            z[0] = q.x, z[1] = q.y;
+        float m = -INFINITY, l = 0.0f, o[V] = {};
+        for (int i = 0; i < head.x; ++i) {
+            const float *part = p.parts + ((((int64_t)blockIdx.x + i) * 2 + (i == 0 ? 1 : 0)) * BM + r) * (D + 4);
+            const float2 v = __ldcg(reinterpret_cast<const float2 *>(part + D));
+            float z[V];
+            if (V == 4) {
+                const float4 q = __ldcg(reinterpret_cast<const float4 *>(part) + lane);
+                z[0] = q.x, z[1] = q.y, z[V - 2] = q.z, z[V - 1] = q.w;
+            } else {
+                const float2 q = __ldcg(reinterpret_cast<const float2 *>(part) + lane);
+                z[0] = q.x, z[1] = q.y;
+            }
+            const float top = fmaxf(m, v.x), from = top == -INFINITY ? 0.0f : top, a = ex2(m - from), f = ex2(v.x - from);
+            m = top;
+            l = fmaf(v.y, f, l * a);
+#pragma unroll
+            for (int k = 0; k < V; ++k) o[k] = fmaf(z[k], f, o[k] * a);
         }
-        const float top = fmaxf(m, v.x), from = top == -INFINITY ? 0.0f : top, a = ex2(m - from), f = ex2(v.x - from);
-        m = top;
-        l = fmaf(v.y, f, l * a);
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        const int local = it.head + r, dt = local / p.group, h = head.z * p.group + (local - dt * p.group);
+        uint32_t *dst = reinterpret_cast<uint32_t *>(p.c.out + (int64_t)(it.tok + dt) * p.c.out_stride + (int64_t)h * D + V * lane);
 #pragma unroll
-        for (int k = 0; k < V; ++k) o[k] = fmaf(z[k], f, o[k] * a);
-    }
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    const int local = it.head + r, dt = local / p.group, h = head.z * p.group + (local - dt * p.group);
-    uint32_t *dst = reinterpret_cast<uint32_t *>(p.c.out + (int64_t)(it.tok + dt) * p.c.out_stride + (int64_t)h * D + V * lane);
-#pragma unroll
-    for (int k = 0; k < V / 2; ++k) {
-        const __nv_bfloat162 v = __floats2bfloat162_rn(o[2 * k] * inv, o[2 * k + 1] * inv);
-        dst[k] = *reinterpret_cast<const uint32_t *>(&v);
-    }
+        for (int k = 0; k < V / 2; ++k) {
+            const __nv_bfloat162 v = __floats2bfloat162_rn(o[2 * k] * inv, o[2 * k + 1] * inv);
+            dst[k] = *reinterpret_cast<const uint32_t *>(&v);
+        }
     }
 }
 
