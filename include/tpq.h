@@ -350,6 +350,8 @@ tpq_status tpq_dequant_reduce_arrivals(tpq_ctx *ctx, const void *const *payloads
  * one range per vector as it arrives: unlike the partial sums' ranges (Section 3) the keys' and values' are not
  * static.  A vector that holds a NaN or an infinity, or whose max - min exceeds binary32, becomes low = NaN,
  * step = 1, codes 0: every value of it reads as NaN.  4 + 32/head_dim bits per value (4.25 at head_dim = 128).
+ * Pages that append has not written may hold anything, and are values by the same rule if a row sees them; attention
+ * takes a vector whose low or step is infinite, or whose step is negative and a value's, for one that is NaN.
  *
  * Conventions beside those above: a handle holds no data of a caller's and serves any number of layers and caches
  * of its geometry; its device must be the current one in every call (BAD_STATE).  What a batch says on the DEVICE
@@ -424,7 +426,7 @@ tpq_status tpq_kv_read(tpq_kv *kv, const tpq_kv_batch *batch, void *k_out_dev, i
  * the values' steps, or a power of two that 16 positions share); where a sequence brings more than 32 rows (new positions times query heads
  * per key head; any number in a batch of one sequence whose max_new allows more), the keys' and values' values too (bits below
  * 2^-28 of the largest value of 16 positions are lost).  One rounding to BF16 at the end.  A position whose key or value is NaN makes the rows that
- * see it NaN, and no others.
+ * see it NaN, and no others.  A value's step below 2^-60 or below 2^-24 |low| (append writes none) counts as that.
  *   q, out    : [n_tokens][n_heads * head_dim] BF16, rows 16-byte aligned; out must not overlap q; at most 2^30 rows times query
  *               heads per key head
  *   scale     : finite (1/sqrt(head_dim) as a rule);  window : 0 for none;  n_first : >= 0, without effect if there is no window

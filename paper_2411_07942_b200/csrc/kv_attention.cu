@@ -346,12 +346,15 @@ attention_split(const split_params p)
                 const float ks = __uint_as_float(kw << 16), kl = __uint_as_float(kw & 0xffff0000u);
                 const float vs = __uint_as_float(vw << 16), vl = __uint_as_float(vw & 0xffff0000u);
                 const bool on = pos < seq.len && ((there >> (at / KV_BLOCK)) & 1u);
+                // (the terms divide by the step.  Append writes none below 2^-60 or 2^-16 of `low`; in others' words a step below 2^-60 or
+                // 2^-24 of `low` counts as that, which is 15 codes of 2^-24, or of next to nothing, off: 1/0 would make a weight of 0 NaN)
+                const float r = fmaxf(vs, fmaxf(0x1p-60f, fabsf(vl) * 0x1p-24f));
                 float inv;
-                asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(vs));
-                // (positions of nobody: whatever their bytes are, NaN among them, weight 0 and finite terms.  A value vector that is
-                // no number makes the rows that see it NaN by way of their scores: a weight of 0 times NaN would reach the others)
-                const bool bad = !(fabsf(vl) < INFINITY) || !(vs < INFINITY);
-                sh.words[warp][at] = on ? make_float4(ks, bad ? NAN : kl, lg2(vs), inv) : make_float4(0.0f, 0.0f, -INFINITY, 0.0f);
+                asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(r));
+                // (positions of nobody: whatever their bytes are, NaN among them, weight 0 and finite terms.  A key or value vector that
+                // is no number makes the rows that see it NaN by way of their scores: a weight of 0 times NaN would reach the others)
+                const bool bad = !(fabsf(vl) < INFINITY) || !(vs >= 0.0f && vs < INFINITY) || !(fabsf(kl) < INFINITY) || !(fabsf(ks) < INFINITY);
+                sh.words[warp][at] = on ? make_float4(ks, bad ? NAN : kl, lg2(r), inv) : make_float4(0.0f, 0.0f, -INFINITY, 0.0f);
                 sh.lows[warp][at] = on && !bad ? fmaf(vl, inv, 8.0f) : 0.0f;
             }
             __syncwarp();

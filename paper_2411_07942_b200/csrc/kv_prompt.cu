@@ -663,7 +663,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
                 const float vs = __uint_as_float(vw << 16), vl = __uint_as_float(vw & 0xffff0000u);
                 // (a key or value vector that is no number makes the rows that see it NaN by way of their scores: a weight of
                 // 0 times NaN would reach the others)
-                const bool bad = !(fabsf(vl) < INFINITY) || !(vs < INFINITY) || !(fabsf(kl) < INFINITY) || !(ks < INFINITY);
+                const bool bad = !(fabsf(vl) < INFINITY) || !(vs >= 0.0f && vs < INFINITY) || !(fabsf(kl) < INFINITY) || !(fabsf(ks) < INFINITY);
                 int ek, ev;
                 uint32_t k_scaled = to_scale(ks, kl, on && !bad, ek);
                 const uint32_t v_scaled = to_scale(vs, vl, on && !bad, ev);

@@ -569,3 +569,73 @@ def test_an_attention_block_up_to_the_synchronised_sum():
     allowed = allowed + step.astype(np.float64).sum(0)[None] + 1e-5
     err = np.abs(out.cpu().numpy() - total)
     assert (err <= allowed).all(), float((err / allowed).max())
+
+
+def shared_scale(setup, window, first):
+    """What a sequence of more than 32 rows (new positions x query heads per key head) may be off beside the tolerance, [rows, heads, 1]: 16
+    positions share a power of two 2^F, the largest magnitude M of theirs is 2^14 .. 2^15 of it, and a weight is P = 2^(y + F - m) in FP16.  The
+    row's largest P is 2^7 at least, and P is off by 2^-25 where it is subnormal: a value (below 2^15 2^F) by 2^-25 2^15 2^F0 / 2^7 =
+    2^-17 2^F0 <= 2^-31 M0 of the block that the largest P is from, seen by this row or not except for one position.  Values themselves are
+    off by half of FP16's smallest step, 2^-25 2^F <= 2^-39 M."""
+    s, group = setup, setup.heads // setup.kv_heads
+    extra = np.zeros((s.T, s.heads, 1))
+    for i, ln in enumerate(s.lengths):
+        n, t = s.start[i + 1] - s.start[i], np.arange(ln)
+        for kh in range(s.kv_heads):
+            if n * group <= 32:
+                continue
+            step, low, _, _ = s.cache.sequence(s.table[i], int(ln), kh, 1)
+            big = np.zeros(-(-ln // 16) * 16)
+            big[:ln] = np.nan_to_num(np.maximum(np.abs(low), np.abs(low + 15 * step)))
+            big = np.repeat(big.reshape(-1, 16).max(1), 16)[:ln]
+            for r in range(n):
+                p = ln - n + r
+                see = (t <= p) & ((window == 0) | (t > p - window) | (t < first))
+                extra[s.start[i] + r, kh * group:(kh + 1) * group] = (see.sum() * 2.0 ** -31 + 2.0 ** -39) * big[see].max()
+    return extra
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("new", [1, 3, 40])
+def test_attention_over_steps_that_append_does_not_write(new, dim):
+    """Pages are the caller's: words with a step of 0 (a pool of zeros), of -0, subnormal or far below `low` stand for low + step * code
+    like any other.  Beyond the tolerance, 15 codes of the smallest step there is (2^-60, 2^-24 of `low`), and, as some values are 2^30,
+    what sharing a power of two with one may cost."""
+    s = Setup(4, 2, dim, 16, [new, new, 1], [200, 150, 40], seed=23, fill=0).fill_with_data()
+    patterns = [0x0000, 0x8000, 0x0001, 0x0780, 0x2180]                     # 0, -0, the smallest subnormal, 2^-112, 2^-60
+    lows = [0x0000, 0x3FA0, 0xBF80, 0x3100, 0x4E80]                         # 0, 1.25, -1, 2^-29, 2^30
+    for i, (at, h) in enumerate([(t, h) for t in list(range(5, 140, 7)) + list(range(200 - new, 200)) for h in (0, 1)]):
+        codes = s.rng.integers(0, 16, dim).astype(np.uint8)
+        for which in (0, 1):
+            low = lows[i % (5 if which else 4)]                             # (keys: none that outweighs all others)
+            for q in (0, 1):
+                if at < s.lengths[q] and (which or i % 3):
+                    s.cache.put(s.table[q, at // 16], h, at % 16, which, codes, patterns[(i + which) % 5] | low << 16)
+    for t in range(40):                                                     # a sequence whose pages hold nothing but zeros
+        for h in (0, 1):
+            for which in (0, 1):
+                s.cache.put(s.table[2, t // 16], h, t % 16, which, np.zeros(dim, np.uint8), 0)
+    s.d_cache.copy_(torch.from_numpy(s.cache.bytes))
+    q, q32 = rows_of(s.rng, s.T, 4 * dim)
+    for window, first in ((0, 0), (100, 5), (3, 0)):
+        got = s.attention(q, 0.1, window, first)
+        assert s.kv.device_status() == binding.TPQ_OK
+        want, bound = kv_ref.attention(s.cache, s.table, s.start, s.lengths, q32.reshape(s.T, 4, dim), 0.1, window, first)
+        err = np.abs(kv_ref.wide(got).reshape(s.T, 4, dim) - want)
+        allowed = tolerance(want, bound) + 15 * (2.0 ** -60 + 2.0 ** -24 * bound) + shared_scale(s, window, first)
+        assert (err <= allowed).all(), (window, float(np.nanmax(err)), int(np.isnan(err).sum()))
+        assert (want[2 * new] == 0).all()
+
+
+@pytest.mark.parametrize("new", [1, 3, 40])
+@pytest.mark.parametrize("which,word", [(0, 0x3F807F80), (0, 0x7F803F80), (0, 0xFF803F80), (1, 0x3F807F80), (1, 0x7F803F80), (1, 0x3F80BF80)])
+def test_a_word_without_a_range_counts_as_no_number(new, which, word):
+    """Steps and lows that are infinite, and negative steps of values: what a NaN is, in the kernels for few rows and in those for many."""
+    s = Setup(4, 2, 128, 16, [new, new], [200, 150], seed=25, fill=0xFF).fill_with_data()
+    at = 200 - new + (2 if new > 1 else 0)
+    s.cache.put(s.table[0, at // 16], 1, at % 16, which, s.rng.integers(0, 16, 128).astype(np.uint8), word)
+    s.d_cache.copy_(torch.from_numpy(s.cache.bytes))
+    q, _ = rows_of(s.rng, s.T, 512)
+    nan = np.isnan(kv_ref.wide(s.attention(q, 0.08, window=100, first=5)).reshape(s.T, 4, 128))
+    seen = 2 if new > 1 else 0
+    assert nan[seen:new, 2:].all() and not nan[:seen].any() and not nan[:, :2].any() and not nan[new:].any()
