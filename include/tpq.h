@@ -429,6 +429,9 @@ tpq_status tpq_kv_read(tpq_kv *kv, const tpq_kv_batch *batch, void *k_out_dev, i
  * see it NaN, and no others.  A value's step below 2^-60 or below 2^-24 |low| (append writes none) counts as that.
  *   q, out    : [n_tokens][n_heads * head_dim] BF16, rows 16-byte aligned; out must not overlap q; at most 2^30 rows times query
  *               heads per key head
+ *   work      : the sum over each 256 rows of a sequence of more than 32, and that over each 16 rows of the others, of (positions that
+ *               they see / 128 + 6) n_kv_heads must be below 2^31 - 1024 (as rows of a call: 1.4 million new tokens of 64 heads on 8);
+ *               beyond it those sequences are left out as above
  *   scale     : finite (1/sqrt(head_dim) as a rule);  window : 0 for none;  n_first : >= 0, without effect if there is no window
  *   workspace : >= tpq_kv_attention_workspace(kv, n_seqs, max_new, n_tokens) bytes of device memory, 16-byte aligned, whose
  *               contents need no preparation and mean nothing afterwards.  Calls that may overlap on the GPU (other

@@ -68,7 +68,7 @@ struct Shared {
     float m[WARPS][8 * NT], l[WARPS][8 * NT];
     uint64_t full[WARPS][stages(D, NT)];
     uint32_t there[WARPS][stages(D, NT)];                    // bit b: block b of the chunk was copied
-    int scan[WARPS];
+    int64_t scan[WARPS];
     int begin[2];                                            // where the block's run begins: sequence, tile of that sequence
 };
 
@@ -161,27 +161,27 @@ attention_split(const split_params p)
         const tiles_of t = visible_tiles(kv_load_seq(b, s), p.c, p.group, tile(NT), 8 * NT);
         want += (int64_t)t.units() * t.groups * b.n_kv_heads;
     }
-    if (want >= 1 << 23) {  // (2^30 positions of key heads in a 128th of the sequences: the sums below are in 32 bits)
-        kv_report(b);
-        want = 0;
-    }
-    const int mine = (int)want;
-    int sum = mine;
+    int64_t sum = want;
 #pragma unroll
     for (int m = 1; m < 32; m <<= 1) {
-        const int o = __shfl_up_sync(0xffffffffu, sum, m);
+        const int64_t o = __shfl_up_sync(0xffffffffu, sum, m);
         if (lane >= m) sum += o;
     }
     if (lane == 31) sh.scan[warp] = sum;
     __syncthreads();
-    int total = 0, before = sum - mine;
+    int64_t all = 0, ahead = sum - want;
     for (int w = 0; w < WARPS; ++w) {
-        if (w < warp) before += sh.scan[w];
-        total += sh.scan[w];
+        if (w < warp) ahead += sh.scan[w];
+        all += sh.scan[w];
     }
-    const int share = (total + gridDim.x - 1) / gridDim.x;
-    int unit = blockIdx.x * share;
-    const int unit_end = unit + share < total ? unit + share : total;
+    if (all > KV_MOST_UNITS) {  // the same in every block: nothing is done, and nothing joined
+        if (tid == 0) kv_report(b);
+        all = 0;
+    }
+    const int total = (int)all, mine = (int)want, before = (int)ahead;  // (numbers of units from here on: none is larger than the total)
+    const int share = (total + (int)gridDim.x - 1) / (int)gridDim.x;
+    int unit = (int)blockIdx.x * share;
+    const int unit_end = total - unit > share ? unit + share : total;
     if (unit >= unit_end) {
         if (tid == 0) p.headers[blockIdx.x] = make_int4(0, 0, 0, 0);
         return;

@@ -5,6 +5,7 @@
 
 #define KV_BLOCK 16  // positions of a block of the cache
 #define KV_MOST (1 << 30)  // positions of a sequence
+#define KV_MOST_UNITS (INT32_MAX - 1024)  // tiles that an attention call deals out (numbers of them are held in 32 bits; the sum is not)
 
 struct tpq_kv {
     int n_heads, n_kv_heads, head_dim, page_size;

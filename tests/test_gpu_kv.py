@@ -683,3 +683,54 @@ def test_append_divides_the_range_by_15(sign):
         step, low, codes, _ = s.cache.sequence(s.table[0], n, 0, which)
         assert np.array_equal(step, kv_ref.wide(want)) and np.array_equal(low, lo[pick])
         assert (np.delete(codes, 7, 1) == 0).all() and (codes[:, 7] == 15).all()
+
+
+class Alike:
+    """One or two sequences over a pool of two pages, `alike` positions of which are one page again and again: attention over them is attention
+    over that page (every weight as often).  The second sequence has 16 positions in the other page."""
+
+    def __init__(self, heads, kv_heads, lengths, new, seed=1):
+        self.page, self.dim, self.heads, self.kv_heads = 256, 64, heads, kv_heads
+        self.kv = binding.TpqKv(heads, kv_heads, 64, 256)
+        rng = self.rng = np.random.default_rng(seed)
+        self.cache = kv_ref.Cache(2, kv_heads, 64, 256, rng=rng)
+        word = rng.uniform(0.05, 0.3, (2, kv_heads, 16, 32)).astype(np.float32), rng.uniform(-2, -1, (2, kv_heads, 16, 32)).astype(np.float32)
+        self.cache.bytes[..., 16 * 64:] = (kv_ref.bf16(word[0]).astype(np.uint32) | kv_ref.bf16(word[1]).astype(np.uint32) << 16).view(np.uint8)
+        self.T = sum(new)
+        self.table = torch.zeros(len(lengths), -(-max(lengths) // 256), dtype=torch.int32, device="cuda")
+        self.table[1:] = 1
+        self.d = [dev(self.cache.bytes), dev(np.concatenate([[0], np.cumsum(new)]).astype(np.int32)), dev(np.array(lengths, np.int32))]
+        self.batch = binding.KvBatch(self.d[0].data_ptr(), 2, self.table.data_ptr(), self.table.shape[1], self.d[1].data_ptr(), self.d[2].data_ptr(), len(lengths), max(new), self.T)
+        self.q, self.q32 = rows_of(rng, self.T, heads * 64)
+
+    def run(self):
+        whole, view = guarded(self.T * self.heads * 128)
+        ws = torch.full((self.kv.attention_workspace_bytes(self.batch),), 0xFF, dtype=torch.uint8, device="cuda")
+        self.kv.attention(self.batch, self.q.data_ptr(), view.data_ptr(), ws.data_ptr(), ws.numel(), 0.1)
+        torch.cuda.synchronize()
+        assert guards_intact(whole, self.T * self.heads * 128)
+        return view.view(torch.int16).view(self.T, self.heads, 64).cpu().numpy().view(np.uint16)
+
+
+def test_a_sequence_of_millions_of_tiles():
+    """9.4 million tiles of 256 positions in one sequence (4096 key heads), beside a short one: both are answered.  A lane adds up 18
+    thousand weights one after the other (590 000 positions over 4 warps and 8 lanes), each time within 2^-24 of the sum: 2^-10 of
+    normaliser and offsets each (1.1 times that by the count, of which the tolerance's 2^-8 of the value has room for a tenth)."""
+    s = Alike(4096, 4096, [2304 * 256, 16], [1, 1])
+    got = kv_ref.wide(s.run()).astype(np.float64)
+    assert s.kv.device_status() == binding.TPQ_OK
+    want, bound = kv_ref.attention(s.cache, [[0], [1]], [0, 1, 2], [256, 16], s.q32.reshape(2, 4096, 64), 0.1)
+    assert (np.abs(got - want) <= tolerance(want, bound) + np.array([2.0 ** -9, 0])[:, None, None] * bound).all()
+
+
+@pytest.mark.parametrize("heads,kv_heads,new,length", [(4096, 4096, 1, 2 ** 27),      # few rows: 2^31 tiles and more
+                                                       (8192, 4096, 4, 2 ** 27)])     # the same in tiles of 128
+def test_more_work_than_can_be_numbered_is_left_out(heads, kv_heads, new, length):
+    s = Alike(heads, kv_heads, [length, 16], [new, 1])
+    assert (s.run() == 0xA5A5).all()
+    assert s.kv.device_status() == binding.TPQ_ERR_INVALID_ARG and s.kv.device_status() == binding.TPQ_OK
+    s.d[2].copy_(torch.tensor([16, 16], dtype=torch.int32))                           # and the same call with less to do is answered
+    got = kv_ref.wide(s.run()).astype(np.float64)
+    assert s.kv.device_status() == binding.TPQ_OK
+    want, bound = kv_ref.attention(s.cache, [[0], [1]], [0, new, new + 1], [16, 16], s.q32.reshape(new + 1, heads, 64), 0.1)
+    assert (np.abs(got - want) <= tolerance(want, bound)).all()
