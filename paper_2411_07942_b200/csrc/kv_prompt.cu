@@ -102,22 +102,22 @@ __device__ __forceinline__ plan_item item_of(const kv_seq &s, const kv_attention
     return t;
 }
 
-__device__ __forceinline__ int block_scan(int x, int *warps, int &total)  // inclusive; PLAN_THREADS threads
+__device__ __forceinline__ int64_t block_scan(int64_t x, int64_t *warps, int64_t &total)  // inclusive; PLAN_THREADS threads
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
     for (int m = 1; m < 32; m <<= 1) {
-        const int o = __shfl_up_sync(0xffffffffu, x, m);
+        const int64_t o = __shfl_up_sync(0xffffffffu, x, m);
         if (lane >= m) x += o;
     }
     __syncthreads();
     if (lane == 31) warps[warp] = x;
     __syncthreads();
     if (warp == 0) {
-        int y = warps[lane];
+        int64_t y = warps[lane];
 #pragma unroll
         for (int m = 1; m < 32; m <<= 1) {
-            const int o = __shfl_up_sync(0xffffffffu, y, m);
+            const int64_t o = __shfl_up_sync(0xffffffffu, y, m);
             if (lane >= m) y += o;
         }
         warps[lane] = y;
@@ -127,14 +127,14 @@ __device__ __forceinline__ int block_scan(int x, int *warps, int &total)  // inc
     return x + (warp ? warps[warp - 1] : 0);
 }
 
-// One block: the list of items, and the tiles ahead of each.
+// One block: the list of items, and the tiles ahead of each.  Sums in 64 bits: 1024 items may have 2^33 tiles.
 __global__ void __launch_bounds__(PLAN_THREADS) attention_plan(const prompt_params p)
 {
-    __shared__ int warps[32];
+    __shared__ int64_t warps[32];
     tpq_grid_dep_wait();
     tpq_grid_dep_launch();
     const kv_batch &b = p.b;
-    int items = 0;
+    int64_t items = 0;
     for (int s0 = 0; s0 < b.n_seqs; s0 += PLAN_THREADS) {
         const int s = s0 + threadIdx.x;
         int n = 0;
@@ -142,10 +142,10 @@ __global__ void __launch_bounds__(PLAN_THREADS) attention_plan(const prompt_para
             const kv_seq q = kv_load_seq(b, s);
             if (q.n * p.group > p.few) n = (q.n * p.group + BM - 1) / BM;
         }
-        int total;
-        const int at = items + block_scan(n, warps, total) - n;
-        if (s < b.n_seqs) p.seq_items[s] = at;
+        int64_t total;
+        const int64_t at = items + block_scan(n, warps, total) - n;
         items += total;
+        if (s < b.n_seqs && items <= p.most_items) p.seq_items[s] = (int)at;
         if (items > p.most_items) break;  // (uniform)
     }
     if (items > p.most_items) {  // starts that overlap: more rows than there are
@@ -172,20 +172,20 @@ __global__ void __launch_bounds__(PLAN_THREADS) attention_plan(const prompt_para
             it.seq = lo;
             n = it.tiles + EXTRA;
         }
-        int total;
-        const int64_t at = before + (int64_t)(block_scan(n, warps, total) - n) * b.n_kv_heads;
-        before += (int64_t)total * b.n_kv_heads;
+        int64_t total;
+        const int64_t at = before + (block_scan(n, warps, total) - n) * b.n_kv_heads;
+        before += total * b.n_kv_heads;
         if (i < items) {
-            it.before = (int)at;
+            it.before = (int)at;  // (used only if all of them fit)
             p.items[i] = it;
         }
     }
     if (threadIdx.x == 0) {
-        if (before > INT32_MAX - 1024) {
+        if (before > KV_MOST_UNITS) {
             kv_report(b);
             before = 0;
         }
-        *p.head = plan_head{items, (int)before, {0, 0}};
+        *p.head = plan_head{(int)items, (int)before, {0, 0}};
     }
 }
 
@@ -522,7 +522,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
         const plan_head h = *p.head;
         const int share = (int)(((int64_t)h.total + gridDim.x - 1) / gridDim.x);
         r0.unit = (int)min((int64_t)blockIdx.x * share, (int64_t)h.total);
-        r0.end = min(r0.unit + share, h.total);
+        r0.end = h.total - r0.unit > share ? r0.unit + share : h.total;
         int lo = 0, n = h.items;  // the last item that begins at or before the unit (every warp for itself): as in kv_find_seq
         while (n > 0) {
             const int step = (n + 31) / 32, at = (lane + 1) * step - 1 < n ? (lane + 1) * step - 1 : n - 1;

@@ -734,3 +734,16 @@ def test_more_work_than_can_be_numbered_is_left_out(heads, kv_heads, new, length
     assert s.kv.device_status() == binding.TPQ_OK
     want, bound = kv_ref.attention(s.cache, [[0], [1]], [0, new, new + 1], [16, 16], s.q32.reshape(new + 1, heads, 64), 0.1)
     assert (np.abs(got - want) <= tolerance(want, bound)).all()
+
+
+@pytest.mark.parametrize("new", [256, 300, 1024])   # 2^31 tiles and more, the same with a block of rows that is not full, 2^33 (0 in 32 bits)
+def test_more_tiles_of_many_rows_than_can_be_numbered_are_left_out(new):
+    s = Alike(256, 1, [2 ** 30, 16], [new, 1])
+    assert (s.run() == 0xA5A5).all()
+    assert s.kv.device_status() == binding.TPQ_ERR_INVALID_ARG and s.kv.device_status() == binding.TPQ_OK
+    s.d[1].copy_(torch.tensor([0, 40, 41], dtype=torch.int32))
+    s.d[2].copy_(torch.tensor([300, 16], dtype=torch.int32))
+    got = s.run()
+    assert s.kv.device_status() == binding.TPQ_OK and (got[41:] == 0xA5A5).all()
+    want, bound = kv_ref.attention(s.cache, [[0, 0], [1, 1]], [0, 40, 41], [300, 16], s.q32[:41].reshape(41, 256, 64), 0.1)
+    assert (np.abs(kv_ref.wide(got[:41]) - want) <= tolerance(want, bound)).all()
