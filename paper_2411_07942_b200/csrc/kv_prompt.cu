@@ -473,7 +473,11 @@ __global__ void __launch_bounds__(THREADS, 1) attention_prompt(const prompt_para
     const uint32_t smem = smem_u32(raw_smem);
     uint8_t *const gen = raw_smem;
     if (smem & 1023u) {  // (dynamic shared memory begins on such a boundary where there is no other; the swizzle needs it)
-        if (threadIdx.x == 0) atomicExch(p.b.status, (int)TPQ_ERR_ALIGN);
+        tpq_grid_dep_wait();
+        if (threadIdx.x == 0) {
+            p.headers[blockIdx.x] = make_int4(0, 0, 0, 0);  // nothing to join
+            atomicExch(p.b.status, (int)TPQ_ERR_ALIGN);
+        }
         return;
     }
     const uint32_t bars = smem + L::BARS;
