@@ -422,11 +422,15 @@ tpq_status tpq_kv_read(tpq_kv *kv, const tpq_kv_batch *batch, void *k_out_dev, i
  *   t <= p, and, if window > 0, t > p - window or t < n_first
  * (the sliding window of the last `window` positions, p's own among them, and the first n_first positions, which stay
  * visible).  k_t, v_t: the values low + step * code of key head h / (n_heads / n_kv_heads).  Zeros where nothing is
- * visible (all pages of a row were bad).  Sums and softmax statistics are binary32.  Roundings on the way, each to 11 bits: the weights (times
- * the values' steps, or a power of two that 16 positions share); where a sequence brings more than 32 rows (new positions times query heads
- * per key head; any number in a batch of one sequence whose max_new allows more), the keys' and values' values too (bits below
- * 2^-28 of the largest value of 16 positions are lost).  One rounding to BF16 at the end.  A position whose key or value is NaN makes the rows that
- * see it NaN, and no others.  A value's step below 2^-60 or below 2^-24 |low| (append writes none) counts as that.
+ * visible (all pages of a row were bad).  A position whose key or value is NaN makes the rows that see it NaN, and no
+ * others.  A value's step below 2^-60 or below 2^-24 |low| (append writes none) counts as that.
+ * Sums and softmax statistics are binary32.  Roundings on the way, for sequences of at most 32 rows (new positions times
+ * query heads per key head): the weights times the values' steps, to 11 bits (those below 2^-21 of a row's largest: to
+ * 2^-32 of it).  For sequences of more, and for any number in a batch of one sequence whose max_new allows more: the
+ * weights times a power of two that 16 positions share, likewise; the keys' and values' values, to 11 bits (those below
+ * 2^-28 of the 16 positions' largest magnitude M: to 2^-39 M).  That power of two is M's whether a row sees M's position
+ * or not, so that each of the positions may cost a row 2^-31 M.  Where the steps, or M, of a sequence's values differ by more
+ * than 2^100, weights of the smaller ones may be lost.  One rounding to BF16 at the end.
  *   q, out    : [n_tokens][n_heads * head_dim] BF16, rows 16-byte aligned; out must not overlap q; at most 2^30 rows times query
  *               heads per key head
  *   work      : the sum over each 256 rows of a sequence of more than 32, and that over each 16 rows of the others, of (positions that

@@ -2,8 +2,10 @@
 //
 // Scores S = Q K^T of 128 rows x 128 positions and sums O += P V run on tcgen05, P from tensor memory.  What a row's thread does per
 // element decides the speed, so that here, unlike in kv_attention.cu, keys and values are formed, in FP16: with 2^F the scale of a
-// block of 16 positions' values (their largest magnitude is 2^14 .. 2^15 of it), v_t 2^-F is rounded once, to 11 bits where it is at
-// least 2^-28 of that magnitude; keys likewise with 2^Fk, and a row of Q with its own power of two, which is exact.  A row (query head
+// block of 16 positions' values (their largest magnitude M is 2^14 .. 2^15 of it), v_t 2^-F is rounded once, to 11 bits where it is at
+// least 2^-28 of that magnitude; keys likewise with 2^Fk, and a row of Q with its own power of two, which is exact.  (F is also the
+// block's for rows that see only some of it: P of theirs is that much larger, and where M is 2^21 times what they see, other positions'
+// P fall below FP16's normal numbers; 2^-31 M a position in all.)  A row (query head
 // x new position) of S is one thread's, which finds
 //   y_t = S_t (2^Fk 2^Fq scale log2 e) + F,   P_t = 2^(y_t - m + 7) in FP16,
 //   l = sum over blocks of 2^-F sum P_t,   out = O / l.

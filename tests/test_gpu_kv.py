@@ -747,3 +747,22 @@ def test_more_tiles_of_many_rows_than_can_be_numbered_are_left_out(new):
     assert s.kv.device_status() == binding.TPQ_OK and (got[41:] == 0xA5A5).all()
     want, bound = kv_ref.attention(s.cache, [[0, 0], [1, 1]], [0, 40, 41], [300, 16], s.q32[:41].reshape(41, 256, 64), 0.1)
     assert (np.abs(kv_ref.wide(got[:41]) - want) <= tolerance(want, bound)).all()
+
+
+@pytest.mark.parametrize("new", [1, 5, 40])
+def test_values_of_sizes_far_apart(new):
+    """Zero vectors and blocks of them (steps of 2^-60) beside values of 2^37: their weights count all the same.  Beside the tolerance, what a
+    power of two for 16 positions may cost (the definition's 2^-31 of the largest a position)."""
+    s = Setup(4, 2, 128, 16, [new, new], [230, 90], seed=37, fill=0xFF).fill_with_data()
+    for i, ln in enumerate(s.lengths):
+        for t in range(ln):
+            for h in range(2):
+                x = np.zeros(128) if t // 16 % 3 == 1 or t % 5 == h else s.rng.standard_normal(128) * 2.0 ** 37
+                codes, words = kv_ref.quantise(x.astype(np.float32)[None])
+                s.cache.put(s.table[i, t // 16], h, t % 16, 1, codes[0], words[0])
+    s.d_cache.copy_(torch.from_numpy(s.cache.bytes))
+    q, q32 = rows_of(s.rng, s.T, 512)
+    for window in (0, 40):
+        got = kv_ref.wide(s.attention(q, 0.1, window)).reshape(s.T, 4, 128)
+        want, bound = kv_ref.attention(s.cache, s.table, s.start, s.lengths, q32.reshape(s.T, 4, 128), 0.1, window)
+        assert (np.abs(got - want) <= tolerance(want, bound) + shared_scale(s, window, 0)).all()
