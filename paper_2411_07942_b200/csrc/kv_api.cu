@@ -27,6 +27,13 @@ tpq_status cuda_fail(tpq_kv *kv, cudaError_t e, const char *what)
     return fail(kv, e == cudaErrorMemoryAllocation ? TPQ_ERR_NOMEM : TPQ_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
 }
 
+// (a memset may still be under way when it returns, and a kernel on a stream that does not wait for it may have reported by then)
+cudaError_t clear(int *word)
+{
+    const cudaError_t e = cudaMemset(word, 0, sizeof *word);
+    return e == cudaSuccess ? cudaStreamSynchronize(nullptr) : e;
+}
+
 inline bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
 tpq_status check_device(tpq_kv *kv)
@@ -98,7 +105,7 @@ tpq_status tpq_kv_create(tpq_kv **out, int n_heads, int n_kv_heads, int head_dim
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&kv->sm_count, cudaDevAttrMultiProcessorCount, kv->device);
     if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void **>(&kv->status), sizeof(int));
     if (e == cudaSuccess) {
-        e = cudaMemset(kv->status, 0, sizeof(int));
+        e = clear(kv->status);
         if (e != cudaSuccess) cudaFree(kv->status);
     }
     if (e != cudaSuccess) {
@@ -216,7 +223,7 @@ tpq_status tpq_kv_device_status(tpq_kv *kv)
     int word = 0;
     cudaError_t e = cudaDeviceSynchronize();
     if (e == cudaSuccess) e = cudaMemcpy(&word, kv->status, sizeof word, cudaMemcpyDeviceToHost);
-    if (e == cudaSuccess && word != 0) e = cudaMemset(kv->status, 0, sizeof word);
+    if (e == cudaSuccess && word != 0) e = clear(kv->status);
     if (e != cudaSuccess) return cuda_fail(kv, e, "device status");
     if (word != 0) return fail(kv, (tpq_status)word, "a kernel reported status %d", word);
     return TPQ_OK;

@@ -766,3 +766,15 @@ def test_values_of_sizes_far_apart(new):
         got = kv_ref.wide(s.attention(q, 0.1, window)).reshape(s.T, 4, 128)
         want, bound = kv_ref.attention(s.cache, s.table, s.start, s.lengths, q32.reshape(s.T, 4, 128), 0.1, window)
         assert (np.abs(got - want) <= tolerance(want, bound) + shared_scale(s, window, 0)).all()
+
+
+def test_reports_right_after_the_status_was_read_are_kept():
+    """The status word is cleared before the call that reads it returns: what a kernel on a stream of its own reports next is still there."""
+    s = Setup(4, 2, 128, 16, [1], [20], seed=39).fill_with_data()
+    q, _ = rows_of(s.rng, s.T, 512)
+    s.d_table.fill_(-1)
+    side = torch.cuda.Stream()
+    for _ in range(50):
+        s.attention(q, 0.1, stream=side.cuda_stream)
+        assert s.kv.device_status() == binding.TPQ_ERR_INVALID_ARG
+    assert s.kv.device_status() == binding.TPQ_OK
