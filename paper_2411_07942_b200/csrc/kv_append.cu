@@ -138,7 +138,7 @@ append_kernel(const kv_batch b, const rotation rot, const kv_rows k, const kv_ro
     const int s = kv_find_seq(b, row, lane);
     if (s < 0) return;
     const kv_seq seq = kv_load_seq(b, s);
-    if (seq.n < 0 || row >= seq.start + seq.n) return;
+    if (seq.n < 0 || !kv_owns(b, seq, row)) return;
     const int pos = seq.len - seq.n + (int)(row - seq.start);
 
     float cs[8], sn[8];  // of this lane's values; (half pairs) the partner's value times the signed sine is added
@@ -237,7 +237,7 @@ read_kernel(const kv_batch b, uint16_t *k_out, int64_t k_stride, uint16_t *v_out
     const int s = kv_find_seq(b, row, lane);
     if (s < 0) return;
     const kv_seq seq = kv_load_seq(b, s);
-    if (seq.n < 0 || row >= seq.start + seq.n) return;
+    if (seq.n < 0 || !kv_owns(b, seq, row)) return;
     const int pos = seq.len - seq.n + (int)(row - seq.start), r = pos % KV_BLOCK, h0 = job * ITER * PER + sub;
     const uint8_t *block = entry_block(b, s, pos, kv_block_bytes(D));
     if (!block) return;

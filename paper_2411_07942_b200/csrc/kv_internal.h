@@ -95,4 +95,10 @@ __device__ __forceinline__ int kv_find_seq(const kv_batch &b, int64_t row, int l
     }
     return lo - 1;
 }
+// Whether the sequence that kv_find_seq gave for a row has it.  Where starts do not ascend, that may be one that begins behind it.
+__device__ __forceinline__ bool kv_owns(const kv_batch &b, const kv_seq &q, int64_t row)
+{
+    if (row < q.start) kv_report(b);
+    return row >= q.start && row < q.start + q.n;
+}
 #endif

@@ -778,3 +778,34 @@ def test_reports_right_after_the_status_was_read_are_kept():
         s.attention(q, 0.1, stream=side.cuda_stream)
         assert s.kv.device_status() == binding.TPQ_ERR_INVALID_ARG
     assert s.kv.device_status() == binding.TPQ_OK
+
+
+@pytest.mark.parametrize("start", [[9, 10, 0, 20, 50], [12, 40, 41, 3, 45, 50], [30, 31, 30, 31, 30, 31, 0, 31, 31, 31, 50]], ids=lambda s: f"{len(s) - 1}")
+def test_rows_before_the_start_that_a_search_ends_at_are_nobodys(start):
+    """Starts that go down lead the search for a row's sequence to one that begins behind the row, whose positions would lie ahead of the
+    page table's row: nothing is read or written there.  Entries may be written for (row, sequence) pairs where the row is the sequence's."""
+    n, page = len(start) - 1, 16
+    s = Setup(4, 2, 128, page, [1] * n, [1] * n, pad=50 - n, seed=43, fill=0, max_new=50)
+    table = torch.full((n + 2, 1), 2 ** 30, dtype=torch.int32, device="cuda")          # ahead of the table and behind it: no page
+    table[1:-1] = dev(s.table)
+    s.batch.page_table_ptr = table[1].data_ptr()
+    d_start = dev(np.array(start, np.int32))
+    s.batch.token_start_ptr = d_start.data_ptr()
+    k, _ = rows_of(s.rng, 50, 256)
+    s.kv.append(s.batch, k.data_ptr(), k.data_ptr())
+    assert s.kv.device_status() == binding.TPQ_ERR_INVALID_ARG
+    want = kv_ref.Cache(s.n_pages, 2, 128, page, fill=0)
+    for i in range(n):
+        if start[i + 1] - start[i] == 1:                                               # (one row, one position: consistent by itself)
+            x = k[start[i]].float().cpu().numpy().reshape(1, 2, 128)
+            codes, words = kv_ref.quantise(x)
+            for h in range(2):
+                for which in (0, 1):
+                    want.put(s.table[i, 0], h, 0, which, codes[0, h], words[0, h])
+    got = s.d_cache.cpu().numpy()
+    assert ((got == want.bytes) | (got == 0)).all()                                    # (or left out, where the search does not find it)
+    out = torch.full((50, 256), 7, dtype=torch.int16, device="cuda")
+    s.kv.read(s.batch, out.data_ptr(), None)
+    assert s.kv.device_status() == binding.TPQ_ERR_INVALID_ARG
+    mine = {start[i] for i in range(n) if start[i + 1] - start[i] == 1}
+    assert all((out[r] == 7).all() for r in range(50) if r not in mine)
