@@ -809,3 +809,74 @@ def test_rows_before_the_start_that_a_search_ends_at_are_nobodys(start):
     assert s.kv.device_status() == binding.TPQ_ERR_INVALID_ARG
     mine = {start[i] for i in range(n) if start[i + 1] - start[i] == 1}
     assert all((out[r] == 7).all() for r in range(50) if r not in mine)
+
+
+FULL = [  # calls of so many vectors that a lane takes four at a time (12 warps for every SM), their last job filled in part
+    (10, 10, 128, 64, [720], [720], 128, False, 0, 0),
+    (10, 10, 128, 16, [1, 719], [40, 900], 48, False, 3, 8),
+    (18, 18, 64, 32, [800], [830], 64, False, 3, 8),
+    (17, 17, 64, 16, [400, 0, 500], [400, 3, 512], 16, True, 0, 0),
+    (20, 5, 128, 16, [300, 0, 1150], [320, 0, 1150], 64, True, 2, 8),
+]
+
+
+@pytest.mark.parametrize("case", FULL, ids=lambda c: f"{c[0]}x{c[1]}x{c[2]}p{c[3]}r{c[6]}{'i' if c[7] else ''}")
+def test_append_and_read_of_many_vectors(case):
+    heads, kvh, dim = case[:3]
+    warps = lambda vectors: (sum(case[4]) + case[8]) * vectors // (256 // dim) // 4  # noqa: E731
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    assert warps(2 * kvh) >= 12 * sms and warps(2 * kvh + heads) >= 12 * sms and (kvh % (4 * 256 // dim) or heads % (4 * 256 // dim))
+    test_append_writes_the_bytes_of_the_definition(case, True)
+
+
+def tolerance_many(setup, q32, out, bound, scale, window, first):
+    """Of sequences of more than 32 rows: keys are FP16 (2^-11 of a value, or 2^-25 2^Fk <= 2^-39 of its block's largest magnitude, the larger of
+    which counts), which moves an exponent by scale sum |q_d| dk_d, E at most over what a row sees; a weight by exp(E) - 1 of itself, and
+    numerator and normaliser by that of B.  The same for the weights' rounding (2^-11) and 2^-12 for the binary32 of the exponents: a sum of
+    dim products whose magnitudes add up to at most 30 128 / dim (held to) is off by dim 2^-24 of that, 0.94 2^-12.
+    Values 2^-11 of B, and what their shared power of two costs.  Half a step of BF16 of the answer."""
+    s, group, allowed = setup, setup.heads // setup.kv_heads, np.zeros_like(out)
+    q = np.abs(q32.reshape(s.T, s.heads, s.dim).astype(np.float64))
+    for i, ln in enumerate(s.lengths):
+        n, t = int(s.start[i + 1] - s.start[i]), np.arange(ln)
+        for kh in range(s.kv_heads):
+            step, low, codes, _ = s.cache.sequence(s.table[i], int(ln), kh, 0)
+            k = np.abs(low[:, None] + step[:, None] * codes)
+            big = np.zeros(-(-int(ln) // 16) * 16)
+            big[:ln] = np.maximum(np.abs(low), np.abs(low + 15 * step))
+            big = np.repeat(big.reshape(-1, 16).max(1), 16)[:ln, None]
+            dk = np.maximum(2.0 ** -11 * k, 2.0 ** -39 * big)
+            for r in range(n):
+                p = int(ln) - n + r
+                see = (t <= p) & ((window == 0) | (t > p - window) | (t < first))
+                rows = np.s_[s.start[i] + r, kh * group:(kh + 1) * group]
+                assert (abs(scale) * (q[rows] @ k[see].T)).max() < 30 * (128 / s.dim)
+                E = abs(scale) * (q[rows] @ dk[see].T).max(1)[:, None]
+                allowed[rows] = 2.0 ** -8 * np.abs(out[rows]) + (2 * np.expm1(E) + 2 * 2.0 ** -11 + 2 * 2.0 ** -12 + 2.0 ** -11) * bound[rows]
+    return allowed + shared_scale(s, window, first)
+
+
+@pytest.mark.parametrize("case", [(4, 2, 128, 32, [130], [130], 0, 0, 0.1), (6, 2, 64, 256, [40, 61], [40, 600], 0, 0, 0.15), (16, 2, 128, 32, [33, 64], [640, 64], 128, 128, 0.02),
+                                  (2, 2, 64, 16, [260], [300], 17, 20, -0.2), (40, 1, 128, 16, [1, 2], [500, 33], 0, 0, 0.1)],
+                         ids=lambda c: f"{c[0]}x{c[1]}x{c[2]}n{max(c[4])}l{max(c[5])}w{c[6]}")
+def test_attention_of_many_rows_within_what_its_roundings_allow(case):
+    heads, kvh, dim, page, new, lengths, window, first, scale = case
+    s = Setup(heads, kvh, dim, page, new, lengths, seed=45, fill=0xFF).fill_with_data()
+    q, q32 = rows_of(s.rng, s.T, heads * dim)
+    got = kv_ref.wide(s.attention(q, scale, window, first)).reshape(s.T, heads, dim)
+    assert s.kv.device_status() == binding.TPQ_OK
+    want, bound = kv_ref.attention(s.cache, s.table, s.start, s.lengths, q32.reshape(s.T, heads, dim), scale, window, first)
+    assert (np.abs(got - want) <= tolerance_many(s, q32, want, bound, scale, window, first)).all()
+
+
+@pytest.mark.parametrize("case", [(8, 1, 128, 64, [1, 4, 1, 0], [30000, 200, 9001, 50], 0, 0), (8, 1, 128, 256, [1, 40, 1], [30000, 300, 513], 0, 0), (4, 2, 64, 64, [1, 5, 2], [20000, 900, 7777], 0, 0),
+                                  (2, 1, 64, 256, [1, 9, 3], [40000, 9, 12000], 0, 0), (8, 1, 128, 64, [1, 2], [30000, 16000], 5000, 70)],
+                         ids=lambda c: f"{c[0]}x{c[1]}x{c[2]}n{max(c[4])}l{max(c[5])}w{c[6]}")
+def test_few_rows_beside_more_over_long_contexts(case):
+    """Sequences of at most 8 rows at long contexts, in batches whose other sequences have them taken 16 rows at a time."""
+    heads, kvh, dim, page, new, lengths, window, first = case
+    s = Setup(heads, kvh, dim, page, new, lengths, seed=47, fill=0xFF).fill_with_data()
+    q, q32 = rows_of(s.rng, s.T, heads * dim)
+    got = s.attention(q, 0.1, window, first)
+    assert s.kv.device_status() == binding.TPQ_OK
+    check(s, q32, got, 0.1, window, first)
