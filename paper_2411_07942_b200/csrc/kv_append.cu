@@ -74,10 +74,7 @@ __device__ __forceinline__ uint32_t quantise(const float (&x)[8], uint32_t &word
     const float top = fmaxf(fabsf(lo), fabsf(hi));
     // (2^-16 of the largest magnitude: a finer step than that says nothing beside `low`, whose rounding may be 2^-9 of it;
     // 2^-60: the attention kernels divide by the steps)
-    // d / 15, correctly rounded, as the quotients below (a product with the number next to 1/15 makes ties of the step's rounding go
-    // up); where d is not finite, what comes out does not matter.
-    const float f = __fmul_rn(d, 1.0f / 15.0f), range15 = __fmaf_rn(__fmaf_rn(-f, 15.0f, d), 1.0f / 15.0f, f);
-    const float want = fmaxf(fmaxf(range15, __fmul_rn(top, 0x1p-16f)), 0x1p-60f);
+    const float want = fmaxf(fmaxf(__fmul_rn(d, 1.0f / 15.0f), __fmul_rn(top, 0x1p-16f)), 0x1p-60f);
     const float step = __bfloat162float(__float2bfloat16_rn(want));
     if (!(d < INFINITY) || !isfinite(low)) {
         word = 0x7fc03f80u;  // low NaN, step 1
@@ -85,8 +82,8 @@ __device__ __forceinline__ uint32_t quantise(const float (&x)[8], uint32_t &word
     }
     word = (__float_as_uint(low) & 0xffff0000u) | (__float_as_uint(step) >> 16);
     // The quotients, correctly rounded, from one reciprocal (Markstein's theorem: q + r y is, where y is the correctly rounded
-    // reciprocal of the divisor, q = a y and r = a - q step exactly; the divisor's 8 bits leave r room to be exact where q is more than
-    // one unit off, and a quotient that far from every tie): a division per value took most of this kernel's time.  Adding 1.5 x 2^23 rounds half to even.
+    // reciprocal of the divisor, q = a y and r = a - q step exactly): a division per value took most of this kernel's time.  Adding
+    // 1.5 x 2^23 rounds half to even.
     const float y = __frcp_rn(step);
     uint32_t codes = 0;
 #pragma unroll
