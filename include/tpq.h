@@ -345,7 +345,8 @@ tpq_status tpq_dequant_reduce_arrivals(tpq_ctx *ctx, const void *const *payloads
  *      `low` in the high half.
  * Code c of a vector stands for  low + step * c.  A vector x (one position, one head, head_dim values in binary32)
  * becomes
- *   low  = bf16(min x),  step = bf16(max((max x - low) / 15, 2^-16 max |x|, 2^-60)),
+ *   low  = bf16(min x),  step = bf16(max((max x - low) c15, 2^-16 max |x|, 2^-60)),  c15 = binary32(1/15) (0x3D888889; a
+ *          product, rounded to binary32, and not a quotient: where a 15th of the range is a tie of BF16, the step goes up),
  *   code = clamp(round-half-to-even((x - low) / step), 0, 15),
  * one range per vector as it arrives: unlike the partial sums' ranges (Section 3) the keys' and values' are not
  * static.  A vector that holds a NaN or an infinity, or whose max - min exceeds binary32, becomes low = NaN,

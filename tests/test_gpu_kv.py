@@ -641,6 +641,50 @@ def test_a_word_without_a_range_counts_as_no_number(new, which, word):
     assert nan[seen:new, 2:].all() and not nan[:seen].any() and not nan[:, :2].any() and not nan[new:].any()
 
 
+def test_append_multiplies_the_range_by_the_number_next_to_a_15th():
+    """(22.5 - low) with low = -0.05859375 is 15 x 1.50390625, halfway between the BF16 numbers 1.5 and 1.5078125.  Times 0x3D888889, which is
+    5.2e-8 of itself more than 1/15, it is above: 1.5078125 (0x3FC1).  And the word of a vector whose 15 steps are exact."""
+    s = Setup(1, 1, 64, 16, [2], [2], seed=27, fill=0)
+    x = torch.zeros(2, 64, dtype=torch.bfloat16, device="cuda")
+    x[0, 0], x[0, 1], x[1, 5] = -0.05859375, 22.5, 15.0
+    s.kv.append(s.batch, x.data_ptr(), x.data_ptr())
+    torch.cuda.synchronize()
+    words = s.d_cache[int(s.table[0, 0]), 0, 0, 16 * 64:].cpu().numpy().view(np.uint32)
+    for which in (0, 1):
+        assert [hex(w) for w in words[16 * which: 16 * which + 2]] == ["0xbd703fc1", "0x3f80"]
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+def test_append_at_ties_of_the_step(sign):
+    """Pairs of BF16 ends whose difference (exact) times 0x3D888889 rounds to another step than its 15th, which is a tie of BF16, and as
+    many others: words of the product, the low end's codes 0, the high end's 15."""
+    f = np.float32
+    c15 = np.array([0x3D888889], np.uint32).view(f)[0]
+    hi = np.concatenate([np.arange(128, 256) * 2.0 ** (e - 7) for e in range(0, 6)])
+    lo = np.concatenate([np.arange(128, 256) * 2.0 ** (e - 7) for e in range(-8, 6)])
+    hi, lo = (x.ravel() for x in np.meshgrid(hi, -sign * lo, indexing="ij"))
+    d = (hi - lo).astype(f)
+    fits = (d == hi - lo) & (d > 0)
+    differ = fits & (kv_ref.bf16(d * c15) != kv_ref.bf16(d / f(15)))
+    assert differ.sum() > 2000
+    rng = np.random.default_rng(5)
+    pick = np.concatenate([np.flatnonzero(differ), rng.choice(np.flatnonzero(fits & ~differ), 2000, replace=False)])
+    n = len(pick)
+    s = Setup(1, 1, 64, 256, [n], [n], seed=29, fill=0)
+    x = np.repeat(lo[pick, None], 64, 1)
+    x[:, 7] = hi[pick]
+    t = torch.from_numpy(x.astype(f)).to(torch.bfloat16).cuda()
+    assert np.array_equal(t.double().cpu().numpy(), x)
+    s.kv.append(s.batch, t.data_ptr(), t.data_ptr())
+    torch.cuda.synchronize()
+    s.cache.bytes[:] = s.d_cache.cpu().numpy()
+    want = kv_ref.bf16(np.maximum(d[pick] * c15, np.maximum(np.abs(hi[pick]), np.abs(lo[pick])).astype(f) * f(2.0 ** -16)))
+    for which in (0, 1):
+        step, low, codes, _ = s.cache.sequence(s.table[0], n, 0, which)
+        assert np.array_equal(step, kv_ref.wide(want)) and np.array_equal(low, lo[pick])
+        assert (np.delete(codes, 7, 1) == 0).all() and (codes[:, 7] == 15).all()
+
+
 class Alike:
     """One or two sequences over a pool of two pages, `alike` positions of which are one page again and again: attention over them is attention
     over that page (every weight as often).  The second sequence has 16 positions in the other page."""
