@@ -2,7 +2,7 @@
 // (tpq_kv_read).
 //
 // A vector is one head of one row.  D/8 lanes hold it, 8 adjacent values each: one 16-byte load, and the lane's 8 codes
-// are one 32-bit word of the cache.  A warp takes one row and up to KV_ITER * 256/D heads of one kind (queries, keys or values:
+// are one 32-bit word of the cache.  A warp takes one row and up to ITER * 256/D heads of one kind (queries, keys or values:
 // no lane of a warp does another's work), all loads ahead of the arithmetic.  Nothing is read twice; what bounds a long prompt is
 // memory (7652 rows of 64 query and 2 x 8 key and value heads of 128, and reading them back: 70 us, 4.7 TB/s; the division per value
 // that was there first 80 us), what bounds one token is the chain token start -> length -> page number -> store (12 us with the read, all
@@ -82,8 +82,9 @@ __device__ __forceinline__ uint32_t quantise(const float (&x)[8], uint32_t &word
     }
     word = (__float_as_uint(low) & 0xffff0000u) | (__float_as_uint(step) >> 16);
     // The quotients, correctly rounded, from one reciprocal (Markstein's theorem: q + r y is, where y is the correctly rounded
-    // reciprocal of the divisor, q = a y and r = a - q step exactly): a division per value took most of this kernel's time.  Adding
-    // 1.5 x 2^23 rounds half to even.
+    // reciprocal of the divisor, q = a y and r = a - q step exactly; with a divisor of 8 bits r is exact also where q is more than
+    // a unit off, and no quotient comes within 2^-9 units of halfway between two numbers): a division per value took most of this kernel's
+    // time.  Adding 1.5 x 2^23 rounds half to even.
     const float y = __frcp_rn(step);
     uint32_t codes = 0;
 #pragma unroll

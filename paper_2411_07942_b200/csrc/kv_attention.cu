@@ -4,9 +4,10 @@
 //   x_t = scale log2(e) (s_t q.c_t + a_t sum(q)),  out = sum_t 2^x_t (b_t + r_t e_t) / sum_t 2^x_t.
 // The products with codes run on the tensor cores with the codes themselves as operands: no key or value is ever formed.
 // The values' steps go into the exponent, P_t = 2^(x_t + log2 r_t - m), so that a product P_t e_t needs no scale of its own
-// and P_t <= 1 whatever the steps are; then
+// and P_t is at most 2^15 whatever the steps are; then
 //   out = sum_t P_t (e_t - 8) + sum_t P_t (b_t / r_t + 8)   over   sum_t P_t / r_t,
-// m the running maximum of x_t + log2 r_t.
+// m 7 below the maximum of x_t + log2 r_t when it last moved, which it does where that has grown by more than 8: P_t of the largest is
+// 2^7 .. 2^15, within FP16.
 //
 // Codes become operands with little more than one logic instruction for two: a code in the low mantissa bits of FP16 1024
 // (0x6400 | c) is 1024 + c, in bits 4 .. 7 (0x6400 | 16 c) it is 16 (64 + c), both exact; the sums of offsets are what the
@@ -22,7 +23,7 @@
 // or column of a fragment is free as long as both sides agree: lanes read 16 (keys) and 8 (values) contiguous bytes of a
 // position, conflict-free and two-way.  mma.sync and not tcgen05: 16 positions x 8 rows are an eighth of the smallest
 // tcgen05 tile, and what bounds this kernel is the memory that the codes come from and the instructions that unpack them
-// (275 per warp and 16 positions of 2176 bytes).
+// (282 per warp and 16 positions of 2176 bytes).
 //
 // Work.  The positions of all sequences and key heads are cut into tiles of 256 (128 for more than 8 rows) and dealt out evenly, in order, to as many
 // blocks as the GPU holds at a time, whatever the lengths are (a graph with this call replays for others).  A block whose
@@ -30,9 +31,10 @@
 // together.  A warp takes a quarter of a tile, by itself: its copies (16 positions = one
 // contiguous block of the cache), its barriers, its running maximum; the warps meet at the end of a (sequence, key head).
 //
-// What bounds it: instructions, 53 % of the issue slots (three warps a scheduler; the rest is their latency).  32 sequences of 16 to 32
-// thousand positions, 64 heads of 128 on 8: 209 us, 4.2 TB/s (two blocks of positions at a time 245 us: copies' bookkeeping and maxima cost as much
-// again); 64 of up to 8000, 4 heads on 2: 33 us, half of it beginnings and ends of runs; one sequence of 777: 11 us, the host's two launches.
+// What bounds it: instructions, 53 % of the issue slots (three warps a scheduler, whose 168 registers a thread fill the register file; the rest
+// is their latency).  32 sequences of 16 to 32 thousand positions, 64 heads of 128 on 8: 210 to 222 us, 4.0 to 4.2 TB/s (two blocks of positions at a
+// time 245 us against 205 then: copies' bookkeeping and maxima cost as much again); 64 of up to 8000, 4 heads on 2: 35 us, half of it beginnings
+// and ends of runs; one sequence of 777: 11 us, the host's two launches.  Of the four kernels one spills: heads of 128, 16 rows at a time, 22 words.
 #include "kv_internal.h"
 
 #include <cuda_bf16.h>
@@ -41,7 +43,18 @@
 namespace {
 
 constexpr int WARPS = 4;
-constexpr int MAX_ROWS = 32;  // rows (new positions x query heads of a key head) of a sequence here: in groups of 8 NT, one after the other
+// Rows (new positions x query heads of a key head) of a sequence here: in groups of 8 NT, one after the other.  A sequence of more goes to the
+// kernels of kv_prompt.cu, whose 256 rows take about as long for 40 as for 128.  Both, us (theirs with these launched for nothing, as in a
+// batch of several), for rows of                          32   40   48   64   96  128  256
+//   24 sequences of 2000 to 4000, 4 key heads of 128      51   67   68   82  116  145  271   here, whatever the rows
+//                                                               69   69   69   69   70   84   there
+//   the same with heads of 64                             40   52   53   63   88  109  203   here
+//                                                               60   61   61   61   61   72   there
+//   8 of 10 000 to 20 000, 8 key heads of 128            117  166  168  215  309  407  790   here
+//                                                              155  155  156  157  158  180   there
+//   2 of 1000 to 2000, 10 key heads of 128                19   20   20   23   27   33   49   here
+//                                                               32   32   33   34   35   39   there
+constexpr int MAX_ROWS = 32;
 
 // Runs are dealt out in units: a (sequence, key head, group of rows) is its tiles and EXTRA more, which stand for its beginning and end
 // (24 sequences of 16 to 32 rows, ragged: 54.8 us with none, 50.2 with one, 44.4 with two or three; 64 of one row: 33.5, 32.7, 32.5, 32.3).
@@ -648,7 +661,9 @@ attention_join(const split_params p, int runs)
 }
 
 // Groups of 8 rows that a warp takes at a time: one where no sequence has more rows, else two (24 sequences of 16 to 32 rows, heads of 64,
-// before the runs were weighed: 55 us; four groups at once, with spilled registers and two blocks an SM, 81; one at a time 63).
+// before the runs were weighed: 55 us; four groups at once, with spilled registers and two blocks an SM, 81; one at a time 63).  A batch whose
+// max_new allows more than 8 rows pays for it where its sequences bring 8 or fewer: 32 of 16 to 32 thousand positions 328 us instead of 210, 64 of up
+// to 8000 44 instead of 33.
 int row_groups(int64_t max_rows) { return max_rows <= 8 ? 1 : 2; }
 
 template <int D, int NT>
@@ -687,7 +702,8 @@ cudaError_t kv_launch_attention(const kv_batch &b, int D, const kv_attention_cal
     const size_t blocks = (size_t)sm_count * BLOCKS_PER_SM;
     p.parts = reinterpret_cast<float *>(p.headers + blocks);
     if (max_rows > MAX_ROWS) {
-        // (of one sequence the kernels for many rows take whatever it brings: two launches less)
+        // (Of one sequence the kernels for many rows take whatever it brings: two launches less.  10 heads of 128, us, with and without these two:
+        // 2048 new 50.0 and 44.8, 100 of 777 30.7 and 25.3, one of 777 where max_new is 128 25.0 and 17.8, but one of 32 000 there 35 and 58.)
         const cudaError_t e = kv_launch_prompt(b, D, c, b.n_seqs == 1 ? 0 : MAX_ROWS, p.parts + blocks * 2 * 8 * nt * part_row(D), sm_count, st, launches);
         if (e != cudaSuccess || b.n_seqs == 1) return e;
     }

@@ -27,8 +27,10 @@
 //
 // What bounds it.  4800 clocks for 256 rows x 128 positions, 2080 of them on the tensor pipe (without contention for shared memory): of each
 // row tile the scores, the walk over them (650 clocks to the maximum, 2000 of exponentials) and the products follow each other, and only
-// the two row tiles overlap.  2 x 8191 tokens, 32 heads of 128 on 16, window 4096: 1100 us, 750 TFLOP/s of what is visible; 2048 tokens, 10 heads:
-// 46 us, of which the plan, the first and last tiles and the joining are half.  Measured and not kept: scores in two halves of 64 positions a step ahead (a
+// the two row tiles overlap.  Two limits lie close behind: a product of scores reads 64 KB of operands in its 520 clocks, all that shared memory
+// gives (128 bytes a clock), while the unpacking writes 64 KB a tile into it; and the tile's 32 768 exponentials are 2048 clocks at 16 a clock.
+// 2 x 8191 tokens, 32 heads of 128 on 16, window 4096: 1112 to 1135 us, 727 to 742 TFLOP/s of what is visible; 2048 tokens, 10 heads: 46 us, of which
+// the plan, the first and last tiles and the joining are half.  Heads of 64 leave half of the sums' columns unused.  Measured (against 1100 us then) and not kept: scores in two halves of 64 positions a step ahead (a
 // product of 64 columns takes as long as one of 128, whose rows of Q are what is read: 1463 us), both softmax warpgroups on one row tile (the
 // exchange of maxima costs more than it hides: 1405 us), an MMA thread for each row tile (1235 us), blocks of 16 scores
 // loaded while the one before is worked on (1209 us against 1104: more and smaller loads and stores of tensor memory), codes instead of formed keys and values as operands (five
