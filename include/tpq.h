@@ -423,7 +423,7 @@ tpq_status tpq_kv_read(tpq_kv *kv, const tpq_kv_batch *batch, void *k_out_dev, i
  *   t <= p, and, if window > 0, t > p - window or t < n_first
  * (the sliding window of the last `window` positions, p's own among them, and the first n_first positions, which stay
  * visible).  k_t, v_t: the values low + step * code of key head h / (n_heads / n_kv_heads).  Zeros where nothing is
- * visible (all pages of a row were bad).  A position whose key or value is NaN makes the rows that see it NaN, and no
+ * visible to a row of finite queries (all its pages were bad).  A position whose key or value is NaN makes the rows that see it NaN, and no
  * others.  A value's step below 2^-60 or below 2^-24 |low| (append writes none) counts as that.
  * Sums and softmax statistics are binary32.  Roundings on the way, for sequences of at most 32 rows (new positions times
  * query heads per key head): the weights times the values' steps, to 11 bits (those below 2^-21 of a row's largest: to
