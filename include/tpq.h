@@ -453,6 +453,100 @@ tpq_status tpq_kv_device_status(tpq_kv *kv);
 int64_t tpq_kv_launch_count(const tpq_kv *kv);
 const char *tpq_kv_last_error(const tpq_kv *kv);
 
+/* ------------------------------------------------- a device's own blocks: feed-forward, weights in 4 bits, answers
+ *
+ * What a device of a tensor-parallel group computes between the synchronisations: its columns of a gated feed-forward
+ * block's first two projections (tpq_gated), whose result is the x of the row-parallel down projection
+ * (tpq_linear_quantize_pack, or tpq_linear4 and tpq_quantize_pack where the weights are in 4 bits); and, behind the last
+ * synchronisation, its slice of the vocabulary's logits (tpq_linear4), from which log probabilities come
+ * (tpq_token_stats, tpq_token_logprobs).
+ *
+ * One handle serves any number of layers and keeps no data of a caller's; its device must be the current one in every call (BAD_STATE).
+ * Unlike a context's, its calls may overlap on the GPU (other streams, captured graphs): they share nothing but the status
+ * word.  From the host it is used by one thread at a time. */
+
+typedef struct tpq_block tpq_block; /* opaque */
+
+tpq_status tpq_block_create(tpq_block **block);   /* on the current CUDA device; errors: INVALID_ARG, NOMEM, CUDA */
+tpq_status tpq_block_destroy(tpq_block *block);   /* NULL is accepted */
+
+/* Weights in 4 bits.  W is [n_out][n_in], a row per output.  Every `group` (32, 64 or 128) adjacent values of a row share a step:
+ *   w = step * code,  code in -8 .. 7,  step = F 2^(e - 8) (1 + m/16)  with e, m in 0 .. 15 (one byte, e the high half) and
+ * one binary32 factor F per row.  step / F has 5 significant bits, so that code * step / F is a BF16 number exactly:
+ * products with the weights round nothing before they are summed.  4 + 8/group bits per value, and 32 per row.
+ *
+ * Quantised from BF16, the symmetric grid of Section 3 with one range per group: a the group's largest magnitude,
+ *   step = binary32(2a / 15) rounded up to 5 significant bits, but at least 2^(E - 15),
+ *   code = clamp(round-half-to-even(w / step), -8, 7),
+ * E the exponent of the row's largest step, or -87 if that is less; F = 2^(E - 7).  |w - step code| <= step / 2.  A row that holds a
+ * NaN, an infinity or a magnitude of 2^120 and more gets F = NaN: its output is NaN, and no other.
+ *
+ * Layout: [ceil(n_out / 128)][ceil(n_in / 128)] blocks of 128 outputs x 128 inputs, then ceil(n_out / 128) * 128 factors F
+ * (binary32).  A block is 8192 bytes of codes, then [128 / group][128] bytes of steps (the group's, of every output).  16 bytes at
+ * p * 2048 + 16 r hold inputs 32p .. 32p + 31 of output r as four words of eight; with u = code + 8, a word is
+ *   sum over i = 0 .. 3 of (u_2i 2^(4i) + u_2i+1 2^(16 + 4i)),  rotated left by 3 bits.
+ * Inputs and outputs beyond n_in and n_out have code 0. */
+typedef enum { TPQ_WEIGHT_BF16 = 0, TPQ_WEIGHT_INT4 = 1 } tpq_weight_kind;
+typedef struct tpq_weight {
+    const void *data_dev;   /* 16-byte aligned: BF16 [n_out][row_stride], or tpq_weight4_bytes bytes */
+    int64_t n_out, n_in;    /* 1 .. 2^30, 1 .. 2^17 */
+    int64_t row_stride;     /* BF16: elements, a multiple of 8, >= n_in; 4 bits: not read */
+    int32_t kind;           /* tpq_weight_kind */
+    int32_t group;          /* 4 bits: 32, 64 or 128; BF16: not read */
+} tpq_weight;
+
+size_t tpq_weight4_bytes(int64_t n_out, int64_t n_in, int group); /* 0 for what is not possible */
+
+/* BF16 rows (2-byte aligned, any stride >= n_in) to 4 bits; every byte of w4 (16-byte aligned, capacity >= tpq_weight4_bytes) is written.
+ * Enqueues on cuda_stream.  Errors: INVALID_ARG, ALIGN, SIZE, BAD_STATE, CUDA. */
+tpq_status tpq_quantize_weight(tpq_block *block, const void *w_bf16_dev, int64_t row_stride, int64_t n_out, int64_t n_in, int group,
+                               void *w4_dev, size_t capacity, void *cuda_stream);
+/* And back: bf16(step * code) (exact for what tpq_quantize_weight writes, where it is no subnormal of BF16); out: [n_out][n_in] BF16, 2-byte aligned. */
+tpq_status tpq_read_weight(tpq_block *block, const void *w4_dev, int64_t n_out, int64_t n_in, int group, void *out_bf16_dev,
+                           int64_t out_row_stride, void *cuda_stream);
+
+/* out = x W^T, W in 4 bits; binary32 sums on the tensor cores, one rounding for BF16 output.
+ *   x   : [T][n_in] BF16, 16-byte aligned, row stride a multiple of 8 elements (what lies between the rows is not read)
+ *   out : [T][n_out] of dt, aligned to its type, any stride >= n_out; it must not overlap x
+ * A row of x that holds infinities or NaN makes its own row of out such (an infinite input times a code of 0 is NaN), and no other.
+ * Enqueues on cuda_stream; T == 0 is a no-op.  Errors: INVALID_ARG, ALIGN, BAD_STATE, CUDA; TIMEOUT through the status. */
+tpq_status tpq_linear4(tpq_block *block, const tpq_weight *w, const void *x_bf16_dev, int64_t x_row_stride, int64_t T, void *out_dev,
+                       tpq_out_dtype dt, int64_t out_row_stride, void *cuda_stream);
+
+/* The gated feed-forward block ahead of the down projection: out = bf16(act(x Wg^T) * (x Wu^T)), in one kernel; sums, activation and
+ * product in binary32.  gate and up: both BF16 or both in 4 bits (the same group), the same sizes.
+ *   SILU g / (1 + e^-g);  GELU_ERF g (1 + erf(g / sqrt 2)) / 2;  GELU_TANH g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) / 2
+ * (an activation below 2^-100 may come out as 0).  x, out (BF16), T and errors as tpq_linear4. */
+typedef enum { TPQ_ACT_SILU = 0, TPQ_ACT_GELU_TANH = 1, TPQ_ACT_GELU_ERF = 2 } tpq_activation;
+tpq_status tpq_gated(tpq_block *block, const tpq_weight *gate, const tpq_weight *up, tpq_activation act, const void *x_bf16_dev,
+                     int64_t x_row_stride, int64_t T, void *out_dev, int64_t out_row_stride, void *cuda_stream);
+
+/* Answers.  The logits' columns are split over devices; a device reduces its own to a record of 5 + 2 n_top words per row, the records are
+ * exchanged as payloads are (20 + 8 n_top bytes a row instead of the logits), and every device joins them.
+ *
+ * tpq_token_stats: the records of columns first .. first + n_vocab - 1.
+ *   logits  : [T][n_vocab] of dt, aligned to its type, any stride
+ *   tokens  : NULL, or [T] the token of each row whose log probability is wanted (a column's number over all devices; negative: none)
+ *   n_top   : most likely tokens wanted, 0 .. 32
+ *   records : capacity >= tpq_token_record_bytes(T, n_top), 4-byte aligned
+ * tpq_token_logprobs: of n records (1 .. 64, HOST array of DEVICE pointers) of the same T and n_top, whose columns differ:
+ *   logprob[t]     = x_token - ln sum e^x; 0 where no token is wanted; NaN, and INVALID_ARG through the status, where no record has it
+ *   entropy[t]     = - sum p ln p
+ *   top[t][i], top_logprob[t][i] : the n_top largest logits' columns, largest first, equal ones by column; -1 and -inf where there are no more
+ * Any of the outputs may be NULL.  A logit of -inf is a token that cannot be; in a row of nothing else every log probability is -inf and the
+ * entropy 0.  A NaN or +inf makes its row's log probabilities and entropy NaN; a NaN is not among the most likely.  Sums are binary32.
+ * Both enqueue on cuda_stream; T == 0 is a no-op.  Errors: INVALID_ARG, ALIGN, SIZE, BAD_STATE, CUDA. */
+size_t tpq_token_record_bytes(int64_t T, int n_top);
+tpq_status tpq_token_stats(tpq_block *block, const void *logits_dev, tpq_out_dtype dt, int64_t row_stride, int64_t T, int64_t n_vocab,
+                           int64_t first, const int32_t *tokens_dev, int n_top, void *records_dev, size_t capacity, void *cuda_stream);
+tpq_status tpq_token_logprobs(tpq_block *block, const void *const *records_dev_host, int n, int64_t T, float *logprob_dev,
+                              float *entropy_dev, int n_top, int32_t *top_dev, float *top_logprob_dev, void *cuda_stream);
+
+/* As tpq_device_status, tpq_launch_count and tpq_last_error, for this handle. */
+tpq_status tpq_block_device_status(tpq_block *block);
+int64_t tpq_block_launch_count(const tpq_block *block);
+const char *tpq_block_last_error(const tpq_block *block);
+
 /* ------------------------------------------------- checkpoint and status */
 
 /* Serialise / restore the whole static state (N, E, bits, gamma, counts, m, M,

@@ -25,6 +25,8 @@ TPQ_OUT_BF16, TPQ_OUT_FP32 = 0, 1
 TPQ_OPT_KERNEL_PATH = 0
 TPQ_OPT_DEQUANT_KERNEL = 1
 DQ_AUTO, DQ_ROWS, DQ_TENSOR_PANELS, DQ_COPY_PANELS = 0, 1, 2, 3
+TPQ_WEIGHT_BF16, TPQ_WEIGHT_INT4 = 0, 1
+TPQ_ACT_SILU, TPQ_ACT_GELU_TANH, TPQ_ACT_GELU_ERF = 0, 1, 2
 PATH_AUTO, PATH_GENERIC, PATH_TILED = 0, 1, 2
 
 _LIB_PATH = Path(__file__).resolve().parent / "libtpq.so"
@@ -45,6 +47,11 @@ class KvBatch(ctypes.Structure):
 class KvRotation(ctypes.Structure):
     """Rotation by position (tpq_kv_rotation; device pointers as integers, positions_ptr may be None)."""
     _fields_ = [("table_ptr", c_void_p), ("n_positions", c_int64), ("rot_dim", c_int32), ("interleaved", c_int32), ("positions_ptr", c_void_p)]
+
+
+class Weight(ctypes.Structure):
+    """A weight matrix [n_out][n_in] (tpq_weight; the device pointer as an integer)."""
+    _fields_ = [("data_ptr", c_void_p), ("n_out", c_int64), ("n_in", c_int64), ("row_stride", c_int64), ("kind", c_int32), ("group", c_int32)]
 
 
 # name -> (restype, argtypes); one entry per declaration in include/tpq.h
@@ -96,6 +103,19 @@ SIGNATURES = {
     "tpq_kv_device_status": (c_int, [c_void_p]),
     "tpq_kv_launch_count": (c_int64, [c_void_p]),
     "tpq_kv_last_error": (c_char_p, [c_void_p]),
+    "tpq_block_create": (c_int, [POINTER(c_void_p)]),
+    "tpq_block_destroy": (c_int, [c_void_p]),
+    "tpq_weight4_bytes": (c_size_t, [c_int64, c_int64, c_int]),
+    "tpq_quantize_weight": (c_int, [c_void_p, c_void_p, c_int64, c_int64, c_int64, c_int, c_void_p, c_size_t, c_void_p]),
+    "tpq_read_weight": (c_int, [c_void_p, c_void_p, c_int64, c_int64, c_int, c_void_p, c_int64, c_void_p]),
+    "tpq_linear4": (c_int, [c_void_p, POINTER(Weight), c_void_p, c_int64, c_int64, c_void_p, c_int, c_int64, c_void_p]),
+    "tpq_gated": (c_int, [c_void_p, POINTER(Weight), POINTER(Weight), c_int, c_void_p, c_int64, c_int64, c_void_p, c_int64, c_void_p]),
+    "tpq_token_record_bytes": (c_size_t, [c_int64, c_int]),
+    "tpq_token_stats": (c_int, [c_void_p, c_void_p, c_int, c_int64, c_int64, c_int64, c_int64, c_void_p, c_int, c_void_p, c_size_t, c_void_p]),
+    "tpq_token_logprobs": (c_int, [c_void_p, POINTER(c_void_p), c_int, c_int64, c_void_p, c_void_p, c_int, c_void_p, c_void_p, c_void_p]),
+    "tpq_block_device_status": (c_int, [c_void_p]),
+    "tpq_block_launch_count": (c_int64, [c_void_p]),
+    "tpq_block_last_error": (c_char_p, [c_void_p]),
     "tpq_status_string": (c_char_p, [c_int]),
     "tpq_last_error": (c_char_p, [c_void_p]),
     "tpq_version": (c_char_p, []),
@@ -112,7 +132,7 @@ _ctypes_only = types.SimpleNamespace(**{f: lambda *args: None for f in (
     "linear_quantize_pack", "kv_append", "kv_attention")})
 _fast = types.SimpleNamespace()   # the calls below that take pointer arrays, as functions that take what _ptrs returns
 _FAST = ("tpq_quantize_pack_batch", "tpq_dequant_reduce", "tpq_dequant_reduce_bias", "tpq_quantize_pack_push",
-         "tpq_dequant_reduce_arrivals")
+         "tpq_dequant_reduce_arrivals", "tpq_token_logprobs")
 
 
 def lib() -> ctypes.CDLL:
@@ -450,6 +470,86 @@ class TpqKv:
 
     def launch_count(self) -> int:
         return int(lib().tpq_kv_launch_count(self._h))
+
+
+class TpqBlock:
+    """A device's own blocks between the synchronisations: feed-forward, products with weights in 4 bits, answers (tpq_block_*)."""
+
+    def __init__(self):
+        self._h = c_void_p()
+        st = lib().tpq_block_create(byref(self._h))
+        if st != TPQ_OK:
+            self._h = c_void_p()
+            raise TpqError(st, "tpq_block_create failed")
+        self._p = self._h.value   # (as a plain integer, for _calls)
+
+    def close(self):
+        if getattr(self, "_h", None) and self._h.value:
+            lib().tpq_block_destroy(self._h)
+            self._h = c_void_p()
+            self._p = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _check(self, st: int):
+        if st != TPQ_OK:
+            raise TpqError(st, lib().tpq_block_last_error(self._h).decode())
+
+    # raw status-returning calls (for error-path tests)
+    def raw(self, name: str, *args) -> int:
+        return getattr(lib(), name)(self._h, *args)
+
+    def quantize_weight(self, w_ptr: int, n_out: int, n_in: int, group: int, w4_ptr: int, capacity: int, row_stride: int | None = None,
+                        stream: int = 0):
+        self._check(lib().tpq_quantize_weight(self._h, w_ptr, n_in if row_stride is None else row_stride, n_out, n_in, group, w4_ptr, capacity, stream))
+
+    def read_weight(self, w4_ptr: int, n_out: int, n_in: int, group: int, out_ptr: int, out_stride: int | None = None, stream: int = 0):
+        self._check(lib().tpq_read_weight(self._h, w4_ptr, n_out, n_in, group, out_ptr, n_in if out_stride is None else out_stride, stream))
+
+    def linear4(self, weight: Weight, x_ptr: int, T: int, out_ptr: int, out_dtype: int = TPQ_OUT_BF16, x_stride: int | None = None,
+                out_stride: int | None = None, stream: int = 0):
+        xs, os = weight.n_in if x_stride is None else x_stride, weight.n_out if out_stride is None else out_stride
+        st = _lib.tpq_linear4(self._h, weight, x_ptr, xs, T, out_ptr, out_dtype, os, stream)
+        if st:
+            self._check(st)
+
+    def gated(self, gate: Weight, up: Weight, act: int, x_ptr: int, T: int, out_ptr: int, x_stride: int | None = None,
+              out_stride: int | None = None, stream: int = 0):
+        xs, os = gate.n_in if x_stride is None else x_stride, gate.n_out if out_stride is None else out_stride
+        st = _lib.tpq_gated(self._h, gate, up, act, x_ptr, xs, T, out_ptr, os, stream)
+        if st:
+            self._check(st)
+
+    def token_stats(self, logits_ptr: int, T: int, n_vocab: int, records_ptr: int, capacity: int, dtype: int = TPQ_OUT_BF16,
+                    stride: int | None = None, first: int = 0, tokens_ptr: int | None = None, n_top: int = 0, stream: int = 0):
+        st = _lib.tpq_token_stats(self._h, logits_ptr, dtype, n_vocab if stride is None else stride, T, n_vocab, first, tokens_ptr, n_top,
+                                  records_ptr, capacity, stream)
+        if st:
+            self._check(st)
+
+    def token_logprobs(self, record_ptrs, T: int, logprob_ptr: int | None, entropy_ptr: int | None = None, n_top: int = 0,
+                       top_ptr: int | None = None, top_logprob_ptr: int | None = None, stream: int = 0):
+        st = _fast.tpq_token_logprobs(self._h, _ptrs(record_ptrs), len(record_ptrs), T, logprob_ptr, entropy_ptr, n_top, top_ptr, top_logprob_ptr, stream)
+        if st:
+            self._check(st)
+
+    def device_status(self) -> int:
+        return int(lib().tpq_block_device_status(self._h))
+
+    def launch_count(self) -> int:
+        return int(lib().tpq_block_launch_count(self._h))
+
+
+def weight4_bytes(n_out: int, n_in: int, group: int) -> int:
+    return int(lib().tpq_weight4_bytes(n_out, n_in, group))
+
+
+def token_record_bytes(T: int, n_top: int) -> int:
+    return int(lib().tpq_token_record_bytes(T, n_top))
 
 
 def payload_bytes_for(T: int, E: int, k: int, bits: int = 4) -> int:
