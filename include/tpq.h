@@ -484,7 +484,7 @@ tpq_status tpq_block_destroy(tpq_block *block);   /* NULL is accepted */
  * Layout: [ceil(n_out / 128)][ceil(n_in / 128)] blocks of 128 outputs x 128 inputs, then ceil(n_out / 128) * 128 factors F
  * (binary32).  A block is 8192 bytes of codes, then [128 / group][128] bytes of steps (the group's, of every output).  16 bytes at
  * p * 2048 + 16 r hold inputs 32p .. 32p + 31 of output r as four words of eight; with u = code + 8, a word is
- *   sum over i = 0 .. 3 of (u_2i 2^(4i) + u_2i+1 2^(16 + 4i)),  rotated left by 3 bits.
+ *   sum over i = 0 .. 3 of (u_2i 2^(4i) + u_2i+1 2^(16 + 4i)).
  * Inputs and outputs beyond n_in and n_out have code 0. */
 typedef enum { TPQ_WEIGHT_BF16 = 0, TPQ_WEIGHT_INT4 = 1 } tpq_weight_kind;
 typedef struct tpq_weight {

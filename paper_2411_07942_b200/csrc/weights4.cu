@@ -13,13 +13,13 @@ namespace {
 constexpr int ROWS = 8, THREADS = 256, PIECE = 32;
 constexpr int LANES = THREADS / ROWS;  // pieces of a row at a time
 
-// codes 8q .. 8q + 7 as a word: pair i (codes 2i, 2i + 1) in bits 4i and 16 + 4i, the word rotated left by 3
+// codes 8q .. 8q + 7 as a word: pair i (codes 2i, 2i + 1) in bits 4i and 16 + 4i
 __device__ __forceinline__ uint32_t pack8(const uint32_t (&c)[8])
 {
     uint32_t w = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) w |= c[2 * i] << (4 * i) | c[2 * i + 1] << (16 + 4 * i);
-    return __funnelshift_l(w, w, 3);
+    return w;
 }
 
 // 32 values of a row from k0 on (zeros behind its end) as 16 words of BF16 pairs
@@ -137,7 +137,7 @@ __global__ void __launch_bounds__(THREADS) read_weight(const uint8_t *w4, const 
         uint32_t v[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            const uint32_t w = __funnelshift_r(words[i / 4], words[i / 4], 3) >> (4 * (i % 4));
+            const uint32_t w = words[i / 4] >> (4 * (i % 4));
             const __nv_bfloat162 b = __floats2bfloat162_rn(step * (float)((int)(w & 15u) - 8), step * (float)((int)(w >> 16 & 15u) - 8));
             v[i] = *reinterpret_cast<const uint32_t *>(&b);
         }

@@ -51,7 +51,6 @@ def pack(codes, byte, factor, group) -> np.ndarray:
     u = u.reshape(tiles, TILE, blocks, 4, 4, 4, 2)             # tile, output, block, 16-byte piece, word, pair, one of the pair
     i = np.arange(4, dtype=np.uint32)
     word = ((u[..., 0] << (4 * i)) | (u[..., 1] << (16 + 4 * i))).sum(-1).astype(np.uint32)
-    word = (word << np.uint32(3)) | (word >> np.uint32(29))
     codes_at = np.ascontiguousarray(word.transpose(0, 2, 3, 1, 4)).view(np.uint8).reshape(tiles, blocks, -1)     # tile, block, piece, output, word
     steps_at = step.reshape(tiles, TILE, blocks, groups).transpose(0, 2, 3, 1).reshape(tiles, blocks, -1)
     f = np.full(tiles * TILE, 2.0 ** -94, np.float32)          # (rows of nobody: the factor of a row of zeros)

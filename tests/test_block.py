@@ -47,8 +47,8 @@ def test_the_layout_of_a_block():
     block = 8192 + 256
     assert raw.size == 2 * 2 * block + 256 * 4
     word = raw[2048 + 2 * 16: 2048 + 2 * 16 + 4].view(np.uint32)[0]
-    assert word == ((0x88888888 - (8 << (16 + 8))) << 3 | 0x88888888 >> 29) & 0xFFFFFFFF
-    assert raw[2048 + 2 * 16 + 4: 2048 + 2 * 16 + 8].view(np.uint32)[0] == 0x44444444      # eights, rotated
+    assert word == 0x88888888 - (8 << (16 + 8))
+    assert raw[2048 + 2 * 16 + 4: 2048 + 2 * 16 + 8].view(np.uint32)[0] == 0x88888888
     assert raw[block + 8192 + 128 + 2] == 0xAB                                              # inputs 192 .. are group 1 of block 1
     assert raw[4 * block:].view(np.float32)[:130].tolist() == [1.0] * 130
 
