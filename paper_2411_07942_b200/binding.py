@@ -125,11 +125,11 @@ _lib = None
 _calls = None   # the extension module (csrc/calls.c): the calls of a step with plain arguments; it returns None for others
 _CALLS = ("tpq_calibrate_ranges", "tpq_quantize_pack", "tpq_quantize_pack_batch", "tpq_dequant_reduce", "tpq_dequant_reduce_bias",
           "tpq_dequant_reduce_arrivals", "tpq_quantize_pack_push", "tpq_linear_quantize_pack", "tpq_kv_append",
-          "tpq_kv_attention")   # in the order of its table
+          "tpq_kv_attention", "tpq_linear4", "tpq_gated", "tpq_token_stats", "tpq_token_logprobs")   # in the order of its table
 # where that module cannot be loaded: every call of its functions is left to ctypes
 _ctypes_only = types.SimpleNamespace(**{f: lambda *args: None for f in (
     "calibrate_ranges", "quantize_pack", "quantize_pack_batch", "dequant_reduce", "dequant_reduce_arrivals", "quantize_pack_push",
-    "linear_quantize_pack", "kv_append", "kv_attention")})
+    "linear_quantize_pack", "kv_append", "kv_attention", "linear4", "gated", "token_stats", "token_logprobs")})
 _fast = types.SimpleNamespace()   # the calls below that take pointer arrays, as functions that take what _ptrs returns
 _FAST = ("tpq_quantize_pack_batch", "tpq_dequant_reduce", "tpq_dequant_reduce_bias", "tpq_quantize_pack_push",
          "tpq_dequant_reduce_arrivals", "tpq_token_logprobs")
@@ -155,7 +155,7 @@ def lib() -> ctypes.CDLL:
         try:
             from . import _calls as calls
             calls.bind([ctypes.cast(getattr(L, name), c_void_p).value for name in _CALLS])
-            calls.bind_types(KvBatch, KvRotation)
+            calls.bind_types(KvBatch, KvRotation, Weight)
         except (ImportError, ValueError, AttributeError) as e:   # not built, or built for another interpreter or table
             warnings.warn(f"the extension module _calls cannot be used ({e}): every call goes through ctypes, 1 to 2 us slower "
                           "each; `python -m paper_2411_07942_b200.build` builds it", RuntimeWarning)
@@ -513,27 +513,35 @@ class TpqBlock:
     def linear4(self, weight: Weight, x_ptr: int, T: int, out_ptr: int, out_dtype: int = TPQ_OUT_BF16, x_stride: int | None = None,
                 out_stride: int | None = None, stream: int = 0):
         xs, os = weight.n_in if x_stride is None else x_stride, weight.n_out if out_stride is None else out_stride
-        st = _lib.tpq_linear4(self._h, weight, x_ptr, xs, T, out_ptr, out_dtype, os, stream)
+        st = _calls.linear4(self._p, weight, x_ptr, xs, T, out_ptr, out_dtype, os, stream)
+        if st is None:
+            st = _lib.tpq_linear4(self._h, weight, x_ptr, xs, T, out_ptr, out_dtype, os, stream)
         if st:
             self._check(st)
 
     def gated(self, gate: Weight, up: Weight, act: int, x_ptr: int, T: int, out_ptr: int, x_stride: int | None = None,
               out_stride: int | None = None, stream: int = 0):
         xs, os = gate.n_in if x_stride is None else x_stride, gate.n_out if out_stride is None else out_stride
-        st = _lib.tpq_gated(self._h, gate, up, act, x_ptr, xs, T, out_ptr, os, stream)
+        st = _calls.gated(self._p, gate, up, act, x_ptr, xs, T, out_ptr, os, stream)
+        if st is None:
+            st = _lib.tpq_gated(self._h, gate, up, act, x_ptr, xs, T, out_ptr, os, stream)
         if st:
             self._check(st)
 
     def token_stats(self, logits_ptr: int, T: int, n_vocab: int, records_ptr: int, capacity: int, dtype: int = TPQ_OUT_BF16,
                     stride: int | None = None, first: int = 0, tokens_ptr: int | None = None, n_top: int = 0, stream: int = 0):
-        st = _lib.tpq_token_stats(self._h, logits_ptr, dtype, n_vocab if stride is None else stride, T, n_vocab, first, tokens_ptr, n_top,
-                                  records_ptr, capacity, stream)
+        stride = n_vocab if stride is None else stride
+        st = _calls.token_stats(self._p, logits_ptr, dtype, stride, T, n_vocab, first, tokens_ptr, n_top, records_ptr, capacity, stream)
+        if st is None:
+            st = _lib.tpq_token_stats(self._h, logits_ptr, dtype, stride, T, n_vocab, first, tokens_ptr, n_top, records_ptr, capacity, stream)
         if st:
             self._check(st)
 
     def token_logprobs(self, record_ptrs, T: int, logprob_ptr: int | None, entropy_ptr: int | None = None, n_top: int = 0,
                        top_ptr: int | None = None, top_logprob_ptr: int | None = None, stream: int = 0):
-        st = _fast.tpq_token_logprobs(self._h, _ptrs(record_ptrs), len(record_ptrs), T, logprob_ptr, entropy_ptr, n_top, top_ptr, top_logprob_ptr, stream)
+        st = _calls.token_logprobs(self._p, record_ptrs, T, logprob_ptr, entropy_ptr, n_top, top_ptr, top_logprob_ptr, stream)
+        if st is None:
+            st = _fast.tpq_token_logprobs(self._h, _ptrs(record_ptrs), len(record_ptrs), T, logprob_ptr, entropy_ptr, n_top, top_ptr, top_logprob_ptr, stream)
         if st:
             self._check(st)
 

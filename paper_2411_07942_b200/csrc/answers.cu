@@ -4,8 +4,11 @@
 // One walk over the logits.  A thread keeps the running maximum m of its values, S = sum e^(x - m) and A = sum e^(x - m) (x - m); two such
 // triples combine as S = S1 e^(m1 - m) + S2 e^(m2 - m), A likewise with e^(m1 - m) (A1 + (m1 - m) S1).  Then with all of a row's
 //   log p(t) = x_t - m - ln S,      entropy = -sum p ln p = ln S - A / S.
+// What bounds the walk is memory, close behind it the exponentials (16 a clock: 14.6 us of 2048 rows of 32000 where memory takes 20) and the
+// instructions: 5 to 6 a value, with differences, sums and products of two values at a time.
 // The most likely tokens: a thread's maximum is a by-product; the n-th largest of the maxima of 64 groups of threads is a bound that at least n
-// values reach, and only threads whose maximum does read their values again (from L2): about n of 256.
+// values reach.  Of the values, whose maxima per 32 to 64 of a thread's are kept, only those chunks are read again (from L2) whose maximum
+// reaches the bound: about n of them.
 #include <cuda_bf16.h>
 
 #include <cmath>
@@ -14,7 +17,7 @@
 
 namespace {
 
-constexpr int THREADS = 256, GROUPS = 64, MOST_TOP = 32, LIST = 1024, AHEAD = 4;
+constexpr int GROUPS = 64, MOST_TOP = 32, LIST = 512, MOST_SPLIT = 8, CHUNKS = 4096;
 constexpr float LOG2E = 1.4426950408889634f;
 
 struct triple {
@@ -55,15 +58,17 @@ template <bool FP32>
 struct row_reader {  // the row as 16-byte pieces that start at 16-byte boundaries; piece v holds values v * VE - off ...
     static constexpr int VE = FP32 ? 4 : 8;
     const uint8_t *at;  // piece 0 (its first `off` values lie ahead of the row)
-    int off, n;
+    int off, n, whole0, whole1;  // pieces whole0 .. whole1 - 1 lie inside the row
     __device__ __forceinline__ row_reader(const void *row, int n_) : n(n_)
     {
         const uintptr_t a = reinterpret_cast<uintptr_t>(row);
         off = (int)(a & 15) / (FP32 ? 4 : 2);
         at = reinterpret_cast<const uint8_t *>(a & ~(uintptr_t)15);
+        whole0 = off != 0;
+        whole1 = (off + n) / VE;
     }
     __device__ __forceinline__ int pieces() const { return (off + n + VE - 1) / VE; }
-    __device__ __forceinline__ bool whole(int v) const { return v * VE >= off && (v + 1) * VE <= off + n; }
+    __device__ __forceinline__ bool whole(int v) const { return v >= whole0 && v < whole1; }
     __device__ __forceinline__ uint4 raw(int v) const  // a piece; values outside the row are -inf
     {
         if (whole(v)) return __ldcs(reinterpret_cast<const uint4 *>(at) + v);
@@ -96,50 +101,66 @@ struct row_reader {  // the row as 16-byte pieces that start at 16-byte boundari
     __device__ __forceinline__ int index(int v, int i) const { return v * VE + i - off; }
 };
 
+template <int THREADS>
 struct shared {
     uint32_t group[GROUPS];
     uint32_t bound;
     int n_active, n_above, n_equal;
-    uint16_t active[THREADS];
+    uint16_t chunk[CHUNKS / THREADS][THREADS];  // high halves of the keys of chunks' maxima
+    uint16_t active[LIST];                       // chunks to read again, numbered through that array
     uint32_t above_key[LIST];
     int32_t above_at[LIST], equal_at[LIST];
     triple warps[THREADS / 32];
-    triple all;
-    uint32_t top_key[MOST_TOP];
-    int32_t top_at[MOST_TOP];
+    unsigned long long top[MOST_TOP];  // order_of, largest first, 0 where there are no more
     unsigned long long best;
     int counts[THREADS / 32];
+    // of the cluster's first block: what the others found
+    triple parts[MOST_SPLIT];
+    unsigned long long lists[MOST_SPLIT][MOST_TOP], merged[MOST_TOP];
 };
 
 __device__ __forceinline__ unsigned long long order_of(uint32_t key, int at) { return (unsigned long long)key << 32 | (uint32_t)~at; }
 
-// The n largest of a block's part of a row, largest first, equal ones by index: s.top_key (0 where there are no more) and s.top_at.
-// mine: the largest key of this thread's pieces v0 + threadIdx.x, + THREADS, ... < v1.
-template <bool FP32>
-__device__ void most_likely(shared &s, const row_reader<FP32> &r, int v0, int v1, uint32_t mine, int n)
+// The n largest of a block's part of a row, largest first, equal ones by index: s.top.
+// mine: the largest key of this thread's pieces v0 + threadIdx.x, + THREADS, ... < v1; a chunk has `span` of them, the thread `chunks` chunks.
+template <bool FP32, int THREADS>
+__device__ void most_likely(shared<THREADS> &s, const row_reader<FP32> &r, int v0, int v1, uint32_t mine, int n, int span, int chunks)
 {
-    constexpr int VE = row_reader<FP32>::VE;
+    constexpr int VE = row_reader<FP32>::VE, EACH = THREADS / GROUPS;
     const int tid = threadIdx.x;
-    uint32_t g = max(mine, __shfl_xor_sync(0xffffffffu, mine, 1));
-    g = max(g, __shfl_xor_sync(0xffffffffu, g, 2));
-    if (tid % 4 == 0) s.group[tid / 4] = g;
+    uint32_t g = mine;
+#pragma unroll
+    for (int m = 1; m < EACH; m <<= 1) g = max(g, __shfl_xor_sync(0xffffffffu, g, m));
+    if (tid % EACH == 0) s.group[tid / EACH] = g;
     if (tid == 0) s.n_active = s.n_above = s.n_equal = 0;
-    if (tid < MOST_TOP) s.top_key[tid] = 0, s.top_at[tid] = -1;
+    if (tid < MOST_TOP) s.top[tid] = 0;
     __syncthreads();
-    {   // the place of each group's maximum among the 64: four threads a group
+    {   // the place of each group's maximum among the 64, by the group's threads
         int above = 0;
-        for (int i = tid % 4; i < GROUPS; i += 4) above += s.group[i] > g || (s.group[i] == g && i < tid / 4);
-        above += __shfl_xor_sync(0xffffffffu, above, 1);
-        above += __shfl_xor_sync(0xffffffffu, above, 2);
-        if (tid % 4 == 0 && above == n - 1) s.bound = g;
+#pragma unroll 8
+        for (int i = tid % EACH; i < GROUPS; i += EACH) above += s.group[i] > g || (s.group[i] == g && i < tid / EACH);
+#pragma unroll
+        for (int m = 1; m < EACH; m <<= 1) above += __shfl_xor_sync(0xffffffffu, above, m);
+        if (tid % EACH == 0 && above == n - 1) s.bound = g;
     }
     __syncthreads();
     const uint32_t bound = s.bound;
-    if (mine >= bound && mine) s.active[atomicAdd(&s.n_active, 1)] = (uint16_t)tid;
+    if (mine >= bound && mine)
+        for (int i = 0; i < chunks; ++i)
+            if (s.chunk[i][tid] >= bound >> 16) {
+                const int to = atomicAdd(&s.n_active, 1);
+                if (to < LIST) s.active[to] = (uint16_t)(i * THREADS + tid);
+            }
     __syncthreads();
-    const int each = (v1 - v0 + THREADS - 1) / THREADS, items = s.n_active * each;
+    // (very many chunks: equal values all over the row; then all of it)
+    const bool listed = s.n_active <= LIST;
+    const int items = listed ? s.n_active * span : v1 - v0;
     for (int i = tid; i < items; i += THREADS) {
-        const int v = v0 + s.active[i / each] + i % each * THREADS;
+        int v = v0 + i;
+        if (listed) {
+            const int k = s.active[i / span], chunk = k / THREADS;
+            v = v0 + k % THREADS + (chunk * span + i % span) * THREADS;
+        }
         if (v >= v1) continue;
         float x[VE];
         r.values(r.raw(v), x);
@@ -178,7 +199,7 @@ __device__ void most_likely(shared &s, const row_reader<FP32> &r, int v0, int v1
             atomicMax(&s.best, b);
             __syncthreads();
             last = s.best;
-            if (tid == 0 && last) s.top_key[i] = (uint32_t)(last >> 32), s.top_at[i] = (int)~(uint32_t)last;
+            if (tid == 0) s.top[i] = last;
             __syncthreads();
         }
         return;
@@ -187,14 +208,14 @@ __device__ void most_likely(shared &s, const row_reader<FP32> &r, int v0, int v1
         const unsigned long long mine_ = order_of(s.above_key[i], s.above_at[i]);
         int place = 0;
         for (int j = 0; j < above; ++j) place += order_of(s.above_key[j], s.above_at[j]) > mine_;
-        if (place < n) s.top_key[place] = s.above_key[i], s.top_at[place] = s.above_at[i];
+        if (place < n) s.top[place] = mine_;
     }
     const int left = n - above;  // the rest: those equal to the bound, the lowest indexes
     if (left > 0 && equal <= LIST) {
         for (int i = tid; i < equal; i += THREADS) {
             int place = 0;
             for (int j = 0; j < equal; ++j) place += s.equal_at[j] < s.equal_at[i];
-            if (place < left) s.top_key[above + place] = bound, s.top_at[above + place] = s.equal_at[i];
+            if (place < left) s.top[above + place] = order_of(bound, s.equal_at[i]);
         }
     } else if (left > 0) {  // very many of them (masked columns): in order from the front until there are enough
         int found = 0;
@@ -221,7 +242,7 @@ __device__ void most_likely(shared &s, const row_reader<FP32> &r, int v0, int v1
             if (mine_)
                 for (int j = 0; j < VE; ++j)
                     if (key_of(x[j]) == bound && r.index(v + tid, j) >= 0 && r.index(v + tid, j) < r.n) {
-                        if (to < left) s.top_key[above + to] = bound, s.top_at[above + to] = r.index(v + tid, j);
+                        if (to < left) s.top[above + to] = order_of(bound, r.index(v + tid, j));
                         ++to;
                     }
             found += all;
@@ -231,183 +252,302 @@ __device__ void most_likely(shared &s, const row_reader<FP32> &r, int v0, int v1
     __syncthreads();
 }
 
-__device__ __forceinline__ uint32_t peer(const void *p, uint32_t rank)
+// Puts `lists` sorted lists of n (order_of, 0: no more; list l at from + l * pitch) together: the n first to `out`.  By all threads of a block.
+template <int THREADS>
+__device__ void merge(const unsigned long long *from, int pitch, int lists, int n, unsigned long long *out)
 {
-    uint32_t a;
-    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
-    return a;
-}
-__device__ __forceinline__ uint32_t ld_cluster(uint32_t a)
-{
-    uint32_t v;
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a));
-    return v;
-}
-__device__ __forceinline__ void cluster_sync()
-{
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    for (int i = threadIdx.x; i < n; i += THREADS) out[i] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < lists * n; i += THREADS) {
+        const int l = i / n, p = i - l * n;
+        const unsigned long long o = from[l * pitch + p];
+        if (!o) continue;
+        int place = p;  // and those of the other lists that come first
+#pragma unroll 4
+        for (int k = 0; k < lists; ++k) {
+            if (k == l) continue;
+            int before = 0;
+#pragma unroll
+            for (int step = MOST_TOP; step; step >>= 1)
+                if (before + step <= n && from[k * pitch + before + step - 1] > o) before += step;
+            place += before;
+        }
+        if (place < n) out[place] = o;
+    }
+    __syncthreads();
 }
 
-// The first n of `lists` sorted lists, by a warp: lane <-> lists lane and lane + 32, whose heads (order_of) `head` gives.
-template <typename Head, typename Take>
-__device__ __forceinline__ void merge(int lists, int n, Head head, Take take)
+// Of a warp's triples: one (in a fixed order), for lane 0.
+__device__ __forceinline__ triple join_warp(triple a)
 {
-    const int lane = threadIdx.x & 31;
-    int p0 = 0, p1 = 0;
-    unsigned long long h0 = lane < lists ? head(lane, 0) : 0, h1 = lane + 32 < lists ? head(lane + 32, 0) : 0;
-    for (int i = 0; i < n; ++i) {
-        const unsigned long long mine = h0 > h1 ? h0 : h1;
-        const uint32_t key = __reduce_max_sync(0xffffffffu, (uint32_t)(mine >> 32));
-        const uint32_t at = __reduce_max_sync(0xffffffffu, (uint32_t)(mine >> 32) == key ? (uint32_t)mine : 0u);
-        const unsigned long long best = (unsigned long long)key << 32 | at;
-        take(i, key, (int)~at);
-        if (!key) continue;
-        if (h0 == best) h0 = ++p0 < n ? head(lane, p0) : 0;
-        else if (h1 == best) h1 = ++p1 < n ? head(lane + 32, p1) : 0;
+#pragma unroll
+    for (int m = 16; m; m >>= 1) {
+        const triple o = {__shfl_down_sync(0xffffffffu, a.m, m), __shfl_down_sync(0xffffffffu, a.S, m), __shfl_down_sync(0xffffffffu, a.A, m)};
+        a = join(a, o);
     }
+    return a;
+}
+
+__device__ __forceinline__ uint32_t first_block(const void *p)  // the same place in the cluster's first block
+{
+    uint32_t a;
+    asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(a) : "r"(smem_u32(p)));
+    return a;
+}
+__device__ __forceinline__ void st_cluster(uint32_t a, uint32_t v) { asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(a), "r"(v) : "memory"); }
+__device__ __forceinline__ void st_cluster(uint32_t a, unsigned long long v) { asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(a), "l"(v) : "memory"); }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+// two values at a time
+__device__ __forceinline__ uint64_t pack2(float a, float b)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ float ex2(float x)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+// A piece with what is below -3e38 at -3e38 (of BF16: the number next to it), and its values' largest
+template <bool FP32>
+__device__ __forceinline__ uint4 clamped(uint4 q)
+{
+    uint32_t *const w = reinterpret_cast<uint32_t *>(&q);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (FP32) asm("max.NaN.f32 %0, %0, %1;" : "+f"(reinterpret_cast<float *>(w)[i]) : "f"(-3e38f));
+        else asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(w[i]) : "r"(0xFF62FF62u));
+    }
+    return q;
+}
+template <bool FP32>
+__device__ __forceinline__ float largest(const uint4 &q, float m)
+{
+    if (FP32) return fmaxf(fmaxf(m, fmaxf(__uint_as_float(q.x), __uint_as_float(q.y))), fmaxf(__uint_as_float(q.z), __uint_as_float(q.w)));
+    uint32_t a, b;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(a) : "r"(q.x), "r"(q.y));
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(b) : "r"(q.z), "r"(q.w));
+    asm("max.bf16x2 %0, %0, %1;" : "+r"(a) : "r"(b));
+    return fmaxf(m, fmaxf(__uint_as_float(a << 16), __uint_as_float(a & 0xFFFF0000u)));
 }
 
 constexpr int HEAD_WORDS = 5;  // of a record: m, S, A, the token's logit, 0: not here, 1: here, 2: none asked for; then n keys, n indexes
 
 // A cluster of `split` blocks a row (gridDim.x = rows * split).
-template <bool FP32>
-__global__ void __launch_bounds__(THREADS) token_stats(const stats_call c, int split)
+template <bool FP32, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS == 128 ? 8 : 2) token_stats(const stats_call c, int split)
 {
-    __shared__ shared s;
-    constexpr int VE = row_reader<FP32>::VE;
+    __shared__ shared<THREADS> s;
+    constexpr int VE = row_reader<FP32>::VE, AHEAD = THREADS == 128 ? 8 : 4;  // pieces on the way to a thread
     const int tid = threadIdx.x, rank = split > 1 ? blockIdx.x % split : 0;
     const int64_t t = blockIdx.x / split;
+    if (split > 1) cluster_arrive();  // (the first block's memory is there: waited for ahead of the first store to it)
     tpq_grid_dep_wait();
     tpq_grid_dep_launch();
     const uint8_t *const row = static_cast<const uint8_t *>(c.logits) + t * c.stride * (FP32 ? 4 : 2);
     const row_reader<FP32> r(row, c.n_vocab);
     const int v0 = (int)((int64_t)r.pieces() * rank / split), v1 = (int)((int64_t)r.pieces() * (rank + 1) / split);
+    // chunks of whole rounds of the walk, as few rounds each as there is room for
+    const int rounds = (v1 - v0 + AHEAD * THREADS - 1) / (AHEAD * THREADS), each = (rounds + CHUNKS / THREADS - 1) / (CHUNKS / THREADS);
     triple a = {-INFINITY, 0.0f, 0.0f};
-    float most = -INFINITY;
-    uint32_t any = 0;
+    bool any = false;
+    float of_chunk = -INFINITY;
+    int chunk = 0, in_chunk = 0;
     for (int v = v0 + tid; v < v1; v += AHEAD * THREADS) {
         uint4 q[AHEAD];
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) q[i] = v + i * THREADS < v1 ? r.raw(v + i * THREADS) : (FP32 ? make_uint4(0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u) : make_uint4(0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u));
-        any = 1;
-        float m = a.m;
-#pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
-            float x[VE];
-            r.values(q[i], x);
-#pragma unroll
-            for (int j = 0; j < VE; ++j) m = fmaxf(m, x[j]);
+        for (int i = 0; i < AHEAD; ++i) {  // (pieces beyond the block's are -inf)
+            const uint32_t out = FP32 ? 0xFF800000u : 0xFF80FF80u;
+            q[i] = v + i * THREADS < v1 ? r.raw(v + i * THREADS) : make_uint4(out, out, out, out);
         }
-        most = m;
+        any = true;
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) of_chunk = largest<FP32>(q[i], of_chunk);
+        const float m = fmaxf(a.m, of_chunk);
+        if (c.n_top) {
+            s.chunk[chunk][tid] = (uint16_t)(key_of(of_chunk) >> 16);
+            if (++in_chunk == each) ++chunk, in_chunk = 0, of_chunk = -INFINITY;
+        }
         const float ref = or_zero(m);
         move_to(a, ref);
+        if (fabsf(ref) < 1e30f) {
+            // What is below -3e38 counts as that, which is e^-inf = 0 for a maximum above -1e30, and stays finite.
+            const uint64_t ref2 = pack2(-ref, -ref), log2 = pack2(LOG2E, LOG2E);
+            uint64_t S = pack2(0.0f, 0.0f), A = S;
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
-            float x[VE];
-            r.values(q[i], x);
+            for (int i = 0; i < AHEAD; ++i) {
+                if (v + i * THREADS >= v1) break;
+                float x[VE];
+                r.values(clamped<FP32>(q[i]), x);
 #pragma unroll
-            for (int j = 0; j < VE; ++j) {
-                const float d = x[j] - ref, e = exp_of(d);
-                a.S += e;
-                a.A = fmaf(e, fmaxf(d, -1e4f), a.A);
+                for (int j = 0; j < VE; j += 2) {
+                    const uint64_t d = add2(pack2(x[j], x[j + 1]), ref2);
+                    float y0, y1;
+                    unpack2(mul2(d, log2), y0, y1);
+                    const uint64_t e = pack2(ex2(y0), ex2(y1));
+                    S = add2(S, e);
+                    A = fma2(e, d, A);
+                }
+            }
+            float s0, s1, a0, a1;
+            unpack2(S, s0, s1);
+            unpack2(A, a0, a1);
+            a.S += s0 + s1;
+            a.A += a0 + a1;
+        } else {
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                float x[VE];
+                r.values(q[i], x);
+#pragma unroll
+                for (int j = 0; j < VE; ++j) {
+                    const float d = x[j] - ref, e = exp_of(d);
+                    a.S += e;
+                    a.A = fmaf(e, fmaxf(d, -1e4f), a.A);
+                }
             }
         }
         a.m = m;
     }
+    const float most = a.m;
+    // of a warp: one reference for all, then sums
+    {
+        float m = a.m;
 #pragma unroll
-    for (int m = 16; m; m >>= 1) {
-        const triple o = {__shfl_xor_sync(0xffffffffu, a.m, m), __shfl_xor_sync(0xffffffffu, a.S, m), __shfl_xor_sync(0xffffffffu, a.A, m)};
-        a = (tid & m) ? join(o, a) : join(a, o);
+        for (int k = 16; k; k >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
+        move_to(a, or_zero(m));
+#pragma unroll
+        for (int k = 16; k; k >>= 1) {
+            a.S += __shfl_xor_sync(0xffffffffu, a.S, k);
+            a.A += __shfl_xor_sync(0xffffffffu, a.A, k);
+        }
+        a.m = m;
     }
     if (tid % 32 == 0) s.warps[tid / 32] = a;
-    if (c.n_top) most_likely<FP32>(s, r, v0, v1, any ? key_of(most) : 0u, c.n_top);
+    if (c.n_top) most_likely<FP32, THREADS>(s, r, v0, v1, any ? key_of(most) : 0u, c.n_top, AHEAD * each, chunk + (in_chunk != 0));
     else __syncthreads();
     uint32_t *const out = c.records + t * (HEAD_WORDS + 2 * c.n_top);
-    if (split > 1) cluster_sync();
-    if (rank == 0 && tid < 32) {
-        triple all = s.warps[0];
-        for (int k = 0; k < split; ++k)
-            for (int w = k ? 0 : 1; w < THREADS / 32; ++w) {
-                triple o;
-                if (split > 1) {
-                    const uint32_t at = peer(&s.warps[w], k);
-                    o = {__uint_as_float(ld_cluster(at)), __uint_as_float(ld_cluster(at + 4)), __uint_as_float(ld_cluster(at + 8))};
-                } else {
-                    o = s.warps[w];
-                }
-                all = join(all, o);
-            }
-        if (tid == 0) {
-            out[0] = __float_as_uint(all.m);
-            out[1] = __float_as_uint(all.S);
-            out[2] = __float_as_uint(all.A);
-            const int64_t token = c.tokens ? c.tokens[t] : -1, at = token - c.first;
-            const bool here = token >= 0 && at >= 0 && at < c.n_vocab;
-            float x = 0.0f;
-            if (here) x = FP32 ? reinterpret_cast<const float *>(row)[at] : __uint_as_float((uint32_t) reinterpret_cast<const uint16_t *>(row)[at] << 16);
-            out[3] = __float_as_uint(x);
-            out[4] = here ? 1u : token < 0 ? 2u : 0u;
-        }
-        if (c.n_top)
-            merge(split, c.n_top,
-                  [&](int k, int p) { return split > 1 ? order_of(ld_cluster(peer(&s.top_key[p], k)), (int)ld_cluster(peer(&s.top_at[p], k))) : order_of(s.top_key[p], s.top_at[p]); },
-                  [&](int i, uint32_t key, int at) {
-                      if (tid == 0) {
-                          out[HEAD_WORDS + i] = key;
-                          out[HEAD_WORDS + c.n_top + i] = key ? (uint32_t)(at + c.first) : 0xFFFFFFFFu;
-                      }
-                  });
+    triple all = {-INFINITY, 0.0f, 0.0f};
+    if (tid < 32) {
+        if (tid < THREADS / 32) all = s.warps[tid];
+        all = join_warp(all);
     }
-    if (split > 1) cluster_sync();
+    const unsigned long long *top = s.top;
+    if (split > 1) {
+        cluster_wait();
+        if (tid == 0) {
+            const uint32_t to = first_block(&s.parts[rank]);
+            st_cluster(to, __float_as_uint(all.m));
+            st_cluster(to + 4, __float_as_uint(all.S));
+            st_cluster(to + 8, __float_as_uint(all.A));
+        }
+        if (tid < c.n_top) st_cluster(first_block(&s.lists[rank][tid]), s.top[tid]);
+        cluster_arrive();
+        if (rank != 0) return;  // (nobody reads this block's memory)
+        cluster_wait();
+        if (tid < 32) {
+            all = triple{-INFINITY, 0.0f, 0.0f};
+            if (tid < split) all = s.parts[tid];
+            all = join_warp(all);
+        }
+        if (c.n_top) merge<THREADS>(&s.lists[0][0], MOST_TOP, split, c.n_top, s.merged);
+        top = s.merged;
+    }
+    if (tid == 0) {
+        out[0] = __float_as_uint(all.m);
+        out[1] = __float_as_uint(all.S);
+        out[2] = __float_as_uint(all.A);
+        const int64_t token = c.tokens ? c.tokens[t] : -1, at = token - c.first;
+        const bool here = token >= 0 && at >= 0 && at < c.n_vocab;
+        float x = 0.0f;
+        if (here) x = FP32 ? reinterpret_cast<const float *>(row)[at] : __uint_as_float((uint32_t) reinterpret_cast<const uint16_t *>(row)[at] << 16);
+        out[3] = __float_as_uint(x);
+        out[4] = here ? 1u : token < 0 ? 2u : 0u;
+    }
+    if (tid < c.n_top) {
+        const unsigned long long o = top[tid];
+        out[HEAD_WORDS + tid] = (uint32_t)(o >> 32);
+        out[HEAD_WORDS + c.n_top + tid] = o ? (uint32_t)(~(uint32_t)o + (uint32_t)c.first) : 0xFFFFFFFFu;
+    }
 }
 
-// A warp a row.
+// A warp a row, or with alternatives a block of 4 warps.  Record i is lane i's, and i + 32.
 __global__ void __launch_bounds__(128) token_logprobs(const join_call c, int *status)
 {
+    extern __shared__ unsigned long long lists[];  // [n + 1][n_top]
     const int lane = threadIdx.x & 31;
-    const int64_t t = (int64_t)blockIdx.x * 4 + threadIdx.x / 32;
+    const int64_t t = c.n_top ? blockIdx.x : (int64_t)blockIdx.x * 4 + threadIdx.x / 32;
     tpq_grid_dep_wait();
     tpq_grid_dep_launch();
-    if (t >= c.T) return;
+    if (t >= c.T) return;  // (whole warps; with alternatives no thread)
     const int64_t at = t * (HEAD_WORDS + 2 * c.n_top);
     triple a = {-INFINITY, 0.0f, 0.0f};
     float x = 0.0f;
-    uint32_t state = 0;
-    for (int i = 0; i < c.n; ++i) {
+    uint32_t here = 0, none_asked = 0;
+    for (int i = lane; i < c.n; i += 32) {
         const uint32_t *const r = c.records[i] + at;
-        a = join(a, {__uint_as_float(r[0]), __uint_as_float(r[1]), __uint_as_float(r[2])});
-        if (r[4] == 1u && state != 1u) x = __uint_as_float(r[3]);
-        if (state != 1u && r[4] != 0u) state = r[4];
+        const uint32_t m = r[0], S = r[1], A = r[2], v = r[3], state = r[4];
+        a = join(a, {__uint_as_float(m), __uint_as_float(S), __uint_as_float(A)});
+        if (state == 1u && !here) x = __uint_as_float(v);
+        here |= state == 1u;
+        none_asked |= state == 2u;
     }
+    a = join_warp(a);
+    a.m = __shfl_sync(0xffffffffu, a.m, 0), a.S = __shfl_sync(0xffffffffu, a.S, 0), a.A = __shfl_sync(0xffffffffu, a.A, 0);
+    const uint32_t has = __ballot_sync(0xffffffffu, here), without = __ballot_sync(0xffffffffu, none_asked);
+    x = __shfl_sync(0xffffffffu, x, has ? __ffs(has) - 1 : 0);
     // (S is 0 where every logit is -inf: nothing is likely, and nothing is unsure)
     const bool none = a.S == 0.0f;
     const float ln = logf(a.S);
     auto logp = [&](float v) { return none ? -INFINITY : (v - a.m) - ln; };
-    if (lane == 0) {
-        if (c.logprob) c.logprob[t] = state == 1u ? logp(x) : state == 2u ? 0.0f : NAN;
+    if (lane == 0 && (c.n_top == 0 || threadIdx.x == 0)) {
+        if (c.logprob) c.logprob[t] = has ? logp(x) : without ? 0.0f : NAN;
         if (c.entropy) c.entropy[t] = none ? 0.0f : ln - a.A / a.S;
-        if (state == 0u) atomicExch(status, (int)TPQ_ERR_INVALID_ARG);
+        if (!has && !without) atomicExch(status, (int)TPQ_ERR_INVALID_ARG);
     }
-    if (c.n_top)
-        merge(c.n, c.n_top,
-              [&](int k, int p) {
-                  const uint32_t *const r = c.records[k] + at + HEAD_WORDS;
-                  return r[p] ? order_of(r[p], (int)r[c.n_top + p]) : 0ull;
-              },
-              [&](int i, uint32_t key, int index) {
-                  if (lane != 0) return;
-                  if (c.top) c.top[t * c.n_top + i] = key ? index : -1;
-                  if (c.top_logprob) c.top_logprob[t * c.n_top + i] = key ? logp(value_of(key)) : -INFINITY;
-              });
+    if (c.n_top == 0) return;
+    for (int i = threadIdx.x; i < c.n * c.n_top; i += 128) {
+        const int k = i / c.n_top, p = i - k * c.n_top;
+        const uint32_t *const r = c.records[k] + at + HEAD_WORDS;
+        const uint32_t key = r[p], index = r[c.n_top + p];
+        lists[i] = key ? order_of(key, (int)index) : 0ull;
+    }
+    __syncthreads();
+    unsigned long long *const merged = lists + c.n * c.n_top;
+    merge<128>(lists, c.n_top, c.n, c.n_top, merged);
+    if (threadIdx.x < c.n_top) {
+        const unsigned long long o = merged[threadIdx.x];
+        if (c.top) c.top[t * c.n_top + threadIdx.x] = o ? (int)~(uint32_t)o : -1;
+        if (c.top_logprob) c.top_logprob[t * c.n_top + threadIdx.x] = o ? logp(value_of((uint32_t)(o >> 32))) : -INFINITY;
+    }
 }
 
-template <bool FP32>
-cudaError_t launch_stats(const stats_call &c, const tpq_block *b, cudaStream_t st)
+template <bool FP32, int THREADS>
+cudaError_t launch_stats(const stats_call &c, int split, cudaStream_t st)
 {
-    // Few rows: a cluster for each, as long as all blocks run at once and a block has 4096 values.
-    int split = 1;
-    while (split < 8 && c.T * split * 2 <= 2 * b->sm_count && c.n_vocab / (split * 2) >= 4096) split *= 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(c.T * split));
     cfg.blockDim = dim3(THREADS);
@@ -421,21 +561,29 @@ cudaError_t launch_stats(const stats_call &c, const tpq_block *b, cudaStream_t s
     at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = split > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, token_stats<FP32>, c, split);
+    return cudaLaunchKernelEx(&cfg, token_stats<FP32, THREADS>, c, split);
 }
 
 }  // namespace
 
 cudaError_t answers_launch_stats(const stats_call &c, const tpq_block *b, cudaStream_t st, int64_t *launches)
 {
-    const cudaError_t e = c.fp32 ? launch_stats<true>(c, b, st) : launch_stats<false>(c, b, st);
+    // Few rows: blocks of 512 threads, and a cluster of them for each row as long as all run at once and a block has 4096 values.  Many, or short
+    // ones: blocks of 128.
+    int split = 1;
+    while (split < MOST_SPLIT && c.T * split * 2 <= 2 * b->sm_count && c.n_vocab / (split * 2) >= 4096) split *= 2;
+    const bool few = c.T <= 2 * b->sm_count && c.n_vocab / split >= 4096;
+    cudaError_t e;
+    if (c.fp32) e = few ? launch_stats<true, 512>(c, split, st) : launch_stats<true, 128>(c, split, st);
+    else e = few ? launch_stats<false, 512>(c, split, st) : launch_stats<false, 128>(c, split, st);
     if (e == cudaSuccess) ++*launches;
     return e;
 }
 
 cudaError_t answers_launch_join(const join_call &c, const tpq_block *b, cudaStream_t st, int64_t *launches)
 {
-    const cudaError_t e = tpq_launch_pdl(token_logprobs, dim3((unsigned)((c.T + 3) / 4)), dim3(128), 0, st, c, b->status);
+    const int64_t blocks = c.n_top ? c.T : (c.T + 3) / 4;
+    const cudaError_t e = tpq_launch_pdl(token_logprobs, dim3((unsigned)blocks), dim3(128), (size_t)(c.n + 1) * c.n_top * 8, st, c, b->status);
     if (e == cudaSuccess) ++*launches;
     return e;
 }

@@ -5,7 +5,7 @@
 
 struct tpq_block {
     int device, sm_count;
-    int clusters[9];  // clusters of 2 .. 8 blocks of the product kernels that run side by side
+    int clusters[9], clusters_half[9];  // clusters of 2 .. 8 blocks of the product kernels that run side by side: one block an SM, two
     int *status;  // device status word (0 = ok)
     int64_t launches;
     char err[512];

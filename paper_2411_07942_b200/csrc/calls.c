@@ -30,10 +30,14 @@ static struct {
                             int64_t, void *, int64_t, void *);
     tpq_status (*kv_attention)(tpq_kv *, const tpq_kv_batch *, const void *, int64_t, float, int64_t, int64_t, void *, int64_t, void *, size_t,
                                void *);
+    tpq_status (*linear4)(tpq_block *, const tpq_weight *, const void *, int64_t, int64_t, void *, tpq_out_dtype, int64_t, void *);
+    tpq_status (*gated)(tpq_block *, const tpq_weight *, const tpq_weight *, tpq_activation, const void *, int64_t, int64_t, void *, int64_t, void *);
+    tpq_status (*token_stats)(tpq_block *, const void *, tpq_out_dtype, int64_t, int64_t, int64_t, int64_t, const int32_t *, int, void *, size_t, void *);
+    tpq_status (*token_logprobs)(tpq_block *, const void *const *, int, int64_t, float *, float *, int, int32_t *, float *, void *);
 } lib;
 
-/* the types of binding.py that hold a tpq_kv_batch and a tpq_kv_rotation */
-static PyTypeObject *batch_type, *rotation_type;
+/* the types of binding.py that hold a tpq_kv_batch, a tpq_kv_rotation and a tpq_weight */
+static PyTypeObject *batch_type, *rotation_type, *weight_type;
 
 /* conversions: 1, or 0 where the argument is not of the plain form (no exception is left set) */
 static int as_i64(PyObject *o, int64_t *v)
@@ -212,17 +216,62 @@ static PyObject *kv_attention(PyObject *self, PyObject *const *a, Py_ssize_t n_a
          lib.kv_attention(ctx, &batch, q, qs, scale, window, first, out, os, ws, bytes, stream));
 }
 
-/* bind_types(batch, rotation): the types that kv_append and kv_attention take */
+static PyObject *linear4(PyObject *self, PyObject *const *a, Py_ssize_t n_args)
+{
+    tpq_weight w;
+    int dtype;
+    int64_t xs, T, os;
+    void *x, *out, *stream;
+    CALL(9, as_struct(a[1], weight_type, sizeof w, &w) && as_ptr(a[2], &x) && as_i64(a[3], &xs) && as_i64(a[4], &T) && as_ptr(a[5], &out) &&
+            as_int(a[6], &dtype) && as_i64(a[7], &os) && as_ptr(a[8], &stream),
+         lib.linear4(ctx, &w, x, xs, T, out, (tpq_out_dtype)dtype, os, stream));
+}
+
+static PyObject *gated(PyObject *self, PyObject *const *a, Py_ssize_t n_args)
+{
+    tpq_weight gate, up;
+    int act;
+    int64_t xs, T, os;
+    void *x, *out, *stream;
+    CALL(10, as_struct(a[1], weight_type, sizeof gate, &gate) && as_struct(a[2], weight_type, sizeof up, &up) && as_int(a[3], &act) && as_ptr(a[4], &x) &&
+             as_i64(a[5], &xs) && as_i64(a[6], &T) && as_ptr(a[7], &out) && as_i64(a[8], &os) && as_ptr(a[9], &stream),
+         lib.gated(ctx, &gate, &up, (tpq_activation)act, x, xs, T, out, os, stream));
+}
+
+static PyObject *token_stats(PyObject *self, PyObject *const *a, Py_ssize_t n_args)
+{
+    int dtype, n_top;
+    int64_t stride, T, n_vocab, first;
+    uint64_t capacity;
+    void *logits, *tokens, *records, *stream;
+    CALL(12, as_ptr(a[1], &logits) && as_int(a[2], &dtype) && as_i64(a[3], &stride) && as_i64(a[4], &T) && as_i64(a[5], &n_vocab) && as_i64(a[6], &first) &&
+             as_ptr_or_none(a[7], &tokens) && as_int(a[8], &n_top) && as_ptr(a[9], &records) && as_u64(a[10], &capacity) && as_ptr(a[11], &stream),
+         lib.token_stats(ctx, logits, (tpq_out_dtype)dtype, stride, T, n_vocab, first, tokens, n_top, records, capacity, stream));
+}
+
+static PyObject *token_logprobs(PyObject *self, PyObject *const *a, Py_ssize_t n_args)
+{
+    int n, n_top;
+    int64_t T;
+    void *records[MOST], *logprob, *entropy, *top, *top_logprob, *stream;
+    CALL(9, as_ptrs(a[1], records, &n) && as_i64(a[2], &T) && as_ptr_or_none(a[3], &logprob) && as_ptr_or_none(a[4], &entropy) && as_int(a[5], &n_top) &&
+            as_ptr_or_none(a[6], &top) && as_ptr_or_none(a[7], &top_logprob) && as_ptr(a[8], &stream),
+         lib.token_logprobs(ctx, (const void *const *)records, n, T, logprob, entropy, n_top, top, top_logprob, stream));
+}
+
+/* bind_types(batch, rotation, weight): the types that kv_append, kv_attention, linear4 and gated take */
 static PyObject *bind_types(PyObject *self, PyObject *const *a, Py_ssize_t n_args)
 {
-    if (n_args != 2 || !PyType_Check(a[0]) || !PyType_Check(a[1])) {
-        PyErr_SetString(PyExc_ValueError, "bind_types() takes two types");
+    if (n_args != 3 || !PyType_Check(a[0]) || !PyType_Check(a[1]) || !PyType_Check(a[2])) {
+        PyErr_SetString(PyExc_ValueError, "bind_types() takes three types");
         return NULL;
     }
     Py_INCREF(a[0]);
     Py_INCREF(a[1]);
+    Py_INCREF(a[2]);
     Py_XSETREF(batch_type, (PyTypeObject *)a[0]);
     Py_XSETREF(rotation_type, (PyTypeObject *)a[1]);
+    Py_XSETREF(weight_type, (PyTypeObject *)a[2]);
     Py_RETURN_NONE;
 }
 
@@ -243,7 +292,8 @@ static PyMethodDef methods[] = {
     {"bind", bind, METH_O, NULL},
 #define METHOD(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, NULL}
     METHOD(calibrate_ranges), METHOD(quantize_pack), METHOD(quantize_pack_batch), METHOD(dequant_reduce),
-    METHOD(dequant_reduce_arrivals), METHOD(quantize_pack_push), METHOD(linear_quantize_pack), METHOD(kv_append), METHOD(kv_attention), METHOD(bind_types),
+    METHOD(dequant_reduce_arrivals), METHOD(quantize_pack_push), METHOD(linear_quantize_pack), METHOD(kv_append), METHOD(kv_attention), METHOD(linear4),
+    METHOD(gated), METHOD(token_stats), METHOD(token_logprobs), METHOD(bind_types),
     {NULL, NULL, 0, NULL}};
 
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", NULL, -1, methods, NULL, NULL, NULL, NULL};

@@ -28,10 +28,10 @@
 
 namespace {
 
-constexpr int BM = 128, MOST_STAGES = 16, MOST_DEPTH = 4, WORKERS = 16, THREADS = (2 + WORKERS) * 32;
+constexpr int BM = 128, MOST_STAGES = 16, MOST_DEPTH = 4;
 constexpr int WAIT_LIMIT = 1 << 24;                     // try_wait attempts (each suspends for a hardware time slice) ...
 constexpr unsigned long long WAIT_NS = 1000000000ull;   // ... and one second, whichever ends first
-constexpr uint32_t SMEM_MAX = 227u * 1024u;
+constexpr uint32_t SMEM_MAX = 227u * 1024u, SMEM_HALF = 112u * 1024u;  // of a block that has an SM for itself, of two beside one another
 constexpr uint32_t BAR_BYTES = 512;                     // barriers and the tensor-memory address
 constexpr uint32_t W_BF16_BYTES = BM * 64 * 2;
 
@@ -41,6 +41,7 @@ struct params {
     int kstages, blocks;                // stages of a tile, blocks (4 bits) of a row of tiles
     int split, stages, depth;           // blocks of a tile; ring; stages whose operands fit tensor memory
     uint32_t w_block, x_at, stage, tmem_cols;
+    uint32_t sums_at;                   // of a split tile: where the cluster's partial sums go, from the first stage on (0: over the stages)
     int group_shift;
     const uint8_t *w4[2];
     const float *factor[2];
@@ -190,9 +191,10 @@ struct ring {  // a stage and its parity
     }
 };
 
-// NW weights.  KB: inputs of a stage, 128 KB; 0: BF16 weights, 64 inputs.
-template <int NW, int KB>
-__global__ void __launch_bounds__(THREADS, 1)
+// NW weights.  KB: inputs of a stage, 128 KB; 0: BF16 weights, 64 inputs.  WORKERS: 8 or 16.  HALF: of an SM, for two blocks.
+// (An SM's registers are given to warps by fours: 10 warps cost as much as 12.)
+template <int NW, int KB, int WORKERS, bool HALF>
+__global__ void __launch_bounds__(HALF ? 384 : (2 + WORKERS) * 32, HALF ? 2 : 1)
 product(const params p, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ CUtensorMap map_w1)
 {
     extern __shared__ uint8_t raw[];
@@ -222,12 +224,14 @@ product(const params p, const __grid_constant__ CUtensorMap map_x, const __grid_
     // pieces of stage kb (with two blocks a stage, the last one of a row may have one)
     auto pieces = [&](int kb) { return KB == 2 && 2 * kb + 1 == p.blocks ? 2 : KX; };
 
+    if (p.split > 1 && p.sums_at) cluster_arrive();  // (the blocks' memory is there: waited for ahead of the first store to it)
     if (tid == 0) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_x) : "memory");
         for (int s = 0; s < p.stages; ++s) {
             mbar_init(full(s), 1);
             mbar_init(empty(s), 1);
         }
-        for (int s = 0; s < MOST_DEPTH; ++s) mbar_init(a_full(s), WORKERS / 2);  // one arrival per warp of a group
+        for (int s = 0; s < MOST_DEPTH; ++s) mbar_init(a_full(s), 8);  // one arrival per warp of a group
         mbar_init(acc_full, 1);
         mbar_init(acc_empty, WORKERS);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -344,7 +348,7 @@ product(const params p, const __grid_constant__ CUtensorMap map_x, const __grid_
     } else {
         const int q = warp & 3, part = (warp - 2) >> 2;  // rows q * 32 .. of a tile (the quarter of tensor memory that this warp reaches)
         uint32_t filled = 0;
-        // The tile's sums: scaled, through the activation, to memory; or, of a split tile, to this block's shared memory.
+        // The tile's sums: scaled, through the activation, to memory.
         auto epilogue = [&](int tile) {
             int tn, tt;
             origin(tile, tn, tt);
@@ -367,14 +371,7 @@ product(const params p, const __grid_constant__ CUtensorMap map_x, const __grid_
                 if (NW == 2) ld16(from + p.pitch + c, y1);
                 ld_wait(y0);
                 if (NW == 2) ld_wait(y1);
-                if (p.split > 1) {
-                    float *const sums = reinterpret_cast<float *>(gen) + q * 32 + lane;
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        sums[(c + j) * BM] = __uint_as_float(y0[j]);
-                        if (NW == 2) sums[(p.N + c + j) * BM] = __uint_as_float(y1[j]);
-                    }
-                } else if (col < p.n) {
+                if (col < p.n) {
 #pragma unroll
                     for (int j = 0; j < 16; ++j) {
                         if (t0 + c + j >= p.T) break;
@@ -389,11 +386,12 @@ product(const params p, const __grid_constant__ CUtensorMap map_x, const __grid_
             if (lane == 0) mbar_arrive(acc_empty);
         };
         if (!W4) {
-            for (int tile = first_tile; tile < tiles && ok; tile += places) epilogue(tile);
+            if (p.split == 1)
+                for (int tile = first_tile; tile < tiles && ok; tile += places) epilogue(tile);
         } else {
             // A warp of the stage's group has half of its 64-wide pieces: of one weight consecutive ones, of two weights one of each.
             constexpr int MINE = KX * NW / 2;
-            const int half = part & 1, turn = part >> 1;
+            const int half = part & 1, turn = part >> 1;  // (8 warps: one group)
             const uint32_t row = (uint32_t)(q * 32 + lane);
             uint32_t codes[MINE], steps[MINE];
 #pragma unroll
@@ -407,19 +405,24 @@ product(const params p, const __grid_constant__ CUtensorMap map_x, const __grid_
             const uint32_t to = a_at + ((uint32_t)(q * 32) << 16) + (uint32_t)(half * MINE * 32);
             ring r, t, done;  // done: the stage whose operands lay in the same place, `depth` stages ago
             const int nk = kb1 - kb0;
-            int undrained = first_tile;                       // the oldest tile that is not drained yet ...
-            int64_t it = 0, drain = (int64_t)nk + p.depth;    // ... and the stage ahead of which it is
+            int undrained = first_tile, left = nk + p.depth;  // the oldest tile that is not drained yet; stages until it is
+            int fresh = p.depth, skip = turn;                 // places that held no operands yet; whether the next stage is the other group's
             for (int tile = first_tile; tile < tiles && ok; tile += places) {
-                for (int kb = kb0; kb < kb1; ++kb, ++it, r.next(p.stages), t.next(p.depth)) {
-                    if (it == drain) {
+                for (int kb = kb0; kb < kb1; ++kb, r.next(p.stages), t.next(p.depth)) {
+                    if (left-- == 0) {
                         epilogue(undrained);
                         if (!ok) break;
                         undrained += places;
-                        drain += nk;
+                        left = nk - 1;
                     }
                     const ring free = done;
-                    if (it >= p.depth) done.next(p.stages);
-                    if ((int)(it & 1) != turn) continue;
+                    const bool used = fresh == 0;
+                    if (used) done.next(p.stages);
+                    else --fresh;
+                    if (WORKERS == 16) {
+                        skip ^= 1;
+                        if (!skip) continue;
+                    }
                     ok = wait_warp(full(r.s), r.phase);
                     if (!ok) break;
                     const uint32_t at = base + r.s * p.stage;
@@ -428,13 +431,13 @@ product(const params p, const __grid_constant__ CUtensorMap map_x, const __grid_
                     for (int m = 0; m < MINE; ++m) {
                         uint32_t v[32];
                         if (there) {
-                            const uint4 c0 = lds128(at + codes[m]), c1 = lds128(at + codes[m] + BM * 16);
                             const uint32_t s0 = lds8(at + steps[m]), s1 = lds8(at + steps[m] + second);
+                            const uint4 c0 = lds128(at + codes[m]), c1 = lds128(at + codes[m] + BM * 16);
                             unpack32(c0, s0, v);
                             unpack32(c1, s1, v + 16);
                         }
                         if (m == 0) {
-                            if (it >= p.depth) ok = wait_warp(empty(free.s), free.phase);
+                            if (used) ok = wait_warp(empty(free.s), free.phase);
                             if (!ok) break;
                             fence_after();
                         }
@@ -447,34 +450,70 @@ product(const params p, const __grid_constant__ CUtensorMap map_x, const __grid_
                     if (lane == 0) mbar_arrive(a_full(t.s));
                 }
             }
-            for (; undrained < tiles && ok; undrained += places) epilogue(undrained);
+            if (p.split == 1)
+                for (; undrained < tiles && ok; undrained += places) epilogue(undrained);
         }
+        if (p.split > 1) ok = ok && wait_warp(acc_full, 0);
     }
     if (!ok) atomicExch(p.status, (int)TPQ_ERR_TIMEOUT);
     if (p.split > 1) {
-        // the cluster's partial sums, in the order of its blocks; each block ends with its share of the tile's tokens
-        cluster_sync();
+        // Every block ends with a share of the tile's cells (token, output): the others store theirs of it to its memory, [block][weight][cell],
+        // and it adds them in the order of the blocks.
         int tn, tt;
         origin(first_tile, tn, tt);
         const int64_t t0 = (int64_t)tt * p.N;
-        const int cells = (int)(p.T - t0 < p.N ? p.T - t0 : p.N) * BM;
-        const int from = (int)((int64_t)cells * rank / p.split), to = (int)((int64_t)cells * (rank + 1) / p.split);
-        for (int i = from + tid; i < to; i += blockDim.x) {
-            const int col = tn * BM + (i & (BM - 1));
+        const int tokens = (int)(p.T - t0 < p.N ? p.T - t0 : p.N);
+        const int share = ((tokens + p.split - 1) / p.split) * BM, from = rank * share;
+        const int mine = tokens * BM - from < share ? tokens * BM - from : share;
+        const float *const sums = reinterpret_cast<const float *>(gen + p.sums_at);
+        const int first_col = tn * BM + (tid & (BM - 1));
+        float f0 = 1.0f, f1 = 1.0f;
+        if (W4 && tid < mine) {
+            f0 = W4_SCALE * p.factor[0][first_col];
+            if (NW == 2) f1 = W4_SCALE * p.factor[1][first_col];
+        }
+        if (!p.sums_at) cluster_arrive();  // (this block's stages are free)
+        cluster_wait();
+        if (warp >= 2 && ok) {
+            fence_after();
+            const int q = warp & 3, part = (warp - 2) >> 2, per = (tokens + p.split - 1) / p.split;
+            const uint32_t at = tmem + ((uint32_t)(q * 32) << 16), cell0 = base + p.sums_at + 4u * (uint32_t)(rank * NW * share + q * 32 + lane);
+            for (int c = 16 * part; c < tokens; c += 4 * WORKERS) {
+                uint32_t y0[16], y1[16];
+                ld16(at + c, y0);
+                if (NW == 2) ld16(at + p.pitch + c, y1);
+                ld_wait(y0);
+                if (NW == 2) ld_wait(y1);
+                int owner = c / per, in = c - owner * per;
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    if (c + j >= tokens) break;
+                    const uint32_t to = map_cluster(cell0 + 4u * (uint32_t)(in * BM), owner);
+                    st_cluster(to, y0[j]);
+                    if (NW == 2) st_cluster(to + 4u * (uint32_t)share, y1[j]);
+                    if (++in == per) in = 0, ++owner;
+                }
+            }
+        }
+        cluster_arrive();
+        cluster_wait();
+        for (int i = tid; i < mine; i += blockDim.x) {
+            const int cell = from + i, col = tn * BM + (cell & (BM - 1));
             float v = 0.0f, u = 0.0f;
+#pragma unroll 8
             for (int k = 0; k < p.split; ++k) {
-                v += lds_cluster(base + 4u * i, k);
-                if (NW == 2) u += lds_cluster(base + 4u * (p.N * BM + i), k);
+                v += sums[k * NW * share + i];
+                if (NW == 2) u += sums[(k * NW + 1) * share + i];
             }
             if (col >= p.n || !ok) continue;
-            if (KB > 0) v *= W4_SCALE * p.factor[0][col];
-            if (NW == 2) {
-                if (KB > 0) u *= W4_SCALE * p.factor[1][col];
-                v = activation(v, p.act) * u;
+            if (W4 && i != tid) {
+                f0 = W4_SCALE * p.factor[0][col];
+                if (NW == 2) f1 = W4_SCALE * p.factor[1][col];
             }
-            store(p, t0 + i / BM, col, v);
+            v *= f0;
+            if (NW == 2) v = activation(v, p.act) * (u * f1);
+            store(p, t0 + cell / BM, col, v);
         }
-        cluster_sync();  // nobody reads this block's shared memory any more
     }
     fence_before();
     __syncthreads();
@@ -496,25 +535,36 @@ bool make_map(const void *ptr, int64_t rows, int64_t K, int64_t stride, int box_
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int NW, int KB>
+template <int NW, int KB, int WORKERS, bool HALF>
 cudaError_t launch(params p, const product_call &c, const tpq_block *b, cudaStream_t st)
 {
     constexpr bool W4 = KB > 0;
-    constexpr int KX = W4 ? 2 * KB : 1;
+    constexpr int KX = W4 ? 2 * KB : 1, TMEM = HALF ? 256 : 512;
+    const int places = b->sm_count * (HALF ? 2 : 1);
     p.kstages = (int)((c.K + KX * 64 - 1) / (KX * 64));
     p.blocks = (int)((c.K + 127) / 128);
     p.w_block = W4 ? w4_block_bytes(c.group) : W_BF16_BYTES;
     p.x_at = ((W4 ? NW * KB : NW) * p.w_block + 1023) / 1024 * 1024;
     p.stage = p.x_at + KX * p.N * 128;
-    p.stages = (int)((SMEM_MAX - 1024 - BAR_BYTES) / p.stage);
+    p.stages = (int)(((HALF ? SMEM_HALF : SMEM_MAX) - 1024 - BAR_BYTES) / p.stage);
     if (p.stages > MOST_STAGES) p.stages = MOST_STAGES;
     const int64_t tiles = (int64_t)p.tiles_n * p.tiles_t;
-    // few tiles: the inputs of each split over a cluster
-    p.split = 1;
-    for (int s = 2; s <= 8 && s <= p.kstages; ++s)
-        if (tiles <= b->clusters[s] && (uint64_t)NW * p.N * BM * 4 <= (uint64_t)p.stages * p.stage) p.split = s;
+    // The partial sums' place is beside the ring, or, where the ring would lose half of itself, in it.
+    const uint32_t sums = p.split > 1 ? (uint32_t)(p.split * NW * ((p.N + p.split - 1) / p.split) * BM * 4) : 0;
+    const int most = p.stages, walk = (p.kstages + p.split - 1) / p.split;
+    // (no more of the ring than a single tile fills: the next kernel's blocks then start beside this one's)
+    if (tiles * p.split <= places && p.stages > walk) p.stages = walk;
+    bool beside = false;
+    if (sums) {
+        const uint32_t room = (HALF ? SMEM_HALF : SMEM_MAX) - 1024 - BAR_BYTES;
+        const int with = (int)((room - sums) / p.stage);
+        beside = with >= p.stages || 2 * with > most;
+        if (beside && with < p.stages) p.stages = with;
+        if (!beside && p.stages * p.stage < sums) p.stages = (int)((sums + p.stage - 1) / p.stage);
+    }
+    p.sums_at = beside ? p.stages * p.stage + BAR_BYTES : 0;
     const int a_cols = KX * NW * 32;
-    p.depth = W4 ? (512 - NW * p.pitch) / a_cols : 1;
+    p.depth = W4 ? (TMEM - NW * p.pitch) / a_cols : 1;
     if (p.depth > MOST_DEPTH) p.depth = MOST_DEPTH;
     if (p.depth > p.stages) p.depth = p.stages;
     const int cols = NW * p.pitch + (W4 ? p.depth * a_cols : 0);
@@ -526,9 +576,9 @@ cudaError_t launch(params p, const product_call &c, const tpq_block *b, cudaStre
         if (!W4 && a < NW && !make_map(c.w[a], c.n, c.K, c.w_stride[a], BM, &mw[a])) return cudaErrorNotSupported;
     }
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(p.split > 1 ? tiles * p.split : tiles < b->sm_count ? tiles : b->sm_count));
-    cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = 1024 + (size_t)p.stages * p.stage + BAR_BYTES;
+    cfg.gridDim = dim3((unsigned)(p.split > 1 ? tiles * p.split : tiles < places ? tiles : places));
+    cfg.blockDim = dim3((2 + WORKERS) * 32);
+    cfg.dynamicSmemBytes = 1024 + (size_t)p.stages * p.stage + BAR_BYTES + (beside ? sums : 0);
     cfg.stream = st;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -539,40 +589,113 @@ cudaError_t launch(params p, const product_call &c, const tpq_block *b, cudaStre
     at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = p.split > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, product<NW, KB>, p, mx, mw[0], mw[1]);
+    return cudaLaunchKernelEx(&cfg, product<NW, KB, WORKERS, HALF>, p, mx, mw[0], mw[1]);
 }
 
-template <int NW, int KB>
+template <int NW, int KB, int WORKERS, bool HALF>
 cudaError_t prepare()
 {
-    return cudaFuncSetAttribute(product<NW, KB>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SMEM_MAX);
+    return cudaFuncSetAttribute(product<NW, KB, WORKERS, HALF>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(HALF ? SMEM_HALF : SMEM_MAX));
+}
+
+// (What a block of half an SM takes, for the question of how many clusters run side by side.  Of the product kernels it is answered as if
+// one block filled an SM, which two do: 27 % more warps were active than with one.)
+__global__ void __launch_bounds__(384, 2) half_block() {}
+
+// clusters of `split` blocks that run side by side
+template <bool HALF>
+cudaError_t count_clusters(int split, int *n)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(split * 148));
+    cfg.blockDim = dim3((2 + (HALF ? 8 : 16)) * 32);
+    cfg.dynamicSmemBytes = HALF ? SMEM_HALF : SMEM_MAX;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = split;
+    at[0].val.clusterDim.y = 1;
+    at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    if (HALF) return cudaOccupancyMaxActiveClusters(n, half_block, &cfg);
+    return cudaOccupancyMaxActiveClusters(n, product<2, 1, 16, false>, &cfg);
 }
 
 }  // namespace
 
-// Once per handle: the kernels' shared memory, and how many clusters of each size run side by side (one block an SM).
+// Once per handle: the kernels' shared memory, and how many clusters of each size run side by side.
 cudaError_t product_prepare(tpq_block *b)
 {
-    cudaError_t e = prepare<1, 1>();
-    if (e == cudaSuccess) e = prepare<1, 2>();
-    if (e == cudaSuccess) e = prepare<2, 1>();
-    if (e == cudaSuccess) e = prepare<2, 0>();
+    cudaError_t e = prepare<1, 1, 16, false>();
+    if (e == cudaSuccess) e = prepare<2, 1, 16, false>();
+    if (e == cudaSuccess) e = prepare<2, 0, 16, false>();
+    if (e == cudaSuccess) e = prepare<1, 1, 8, true>();
+    if (e == cudaSuccess) e = prepare<1, 2, 8, true>();
+    if (e == cudaSuccess) e = prepare<2, 1, 8, true>();
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(half_block, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SMEM_HALF);
     for (int s = 2; s <= 8 && e == cudaSuccess; ++s) {
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3((unsigned)s);
-        cfg.blockDim = dim3(THREADS);
-        cfg.dynamicSmemBytes = SMEM_MAX;
-        cudaLaunchAttribute at[1];
-        at[0].id = cudaLaunchAttributeClusterDimension;
-        at[0].val.clusterDim.x = s;
-        at[0].val.clusterDim.y = 1;
-        at[0].val.clusterDim.z = 1;
-        cfg.attrs = at;
-        cfg.numAttrs = 1;
-        e = cudaOccupancyMaxActiveClusters(&b->clusters[s], product<2, 1>, &cfg);
+        e = count_clusters<false>(s, &b->clusters[s]);
+        if (e == cudaSuccess) e = count_clusters<true>(s, &b->clusters_half[s]);
     }
     return e;
 }
+
+namespace {
+
+enum kernel_kind { BF16_GATED, GATED, GATED_HALF, LINEAR, LINEAR_HALF, LINEAR_HALF_DEEP };
+struct plan {
+    kernel_kind kind;
+    int N, split;
+};
+
+// The kernel, the tokens of a tile and the blocks that share one: the least estimated time, in clocks.  A stage's (`one` or, per token of the tile,
+// `token`, whichever is more) are measured: 4 bits and many tokens are what the tensor cores take under the power limit (256 tokens 1500, with
+// two weights 128 tokens 1640); few are what unpacking takes, more where a second block is on the SM (`beside`); BF16 weights are bound by shared
+// memory, 128 bytes a clock for the copies in and the operands out (512 + 3 a token), or by memory.
+// 2048 x 3456 x 5120 in 4 bits: tiles of 192 tokens 58 us (three rounds), of 256 63.5 (three, the third a sixth full); gated 2048 x 5120 x 3456 in
+// BF16: of 208 106 us, of 256 111.  32000 outputs of 5120, one token: 22.7 us with two blocks on an SM, 27.3 with one; 64 tokens 27.2 and 30.8; but
+// two weights of 4608 x 4608 and 61 tokens 21.0 and 15.1.  One token of 4608 x 4608, gated: 11.1 us with 7 blocks to a tile, 13.0 with 4.
+plan choose(const product_call &c, const tpq_block *b, int tiles_n)
+{
+    const bool two = c.n_weights == 2;
+    const int most = c.group && two ? 128 : 256;
+    const int64_t t0 = (c.T + most - 1) / most;
+    plan best = {};
+    int64_t best_cost = 0;
+    for (int64_t t = t0; t < t0 + (c.T > 64 ? 8 : 1); ++t) {
+        const int N = (int)(((c.T + t - 1) / t + 15) / 16 * 16);
+        const int64_t tiles = tiles_n * ((c.T + N - 1) / N);
+        const kernel_kind kind = !c.group ? BF16_GATED : two ? N <= 32 ? GATED_HALF : GATED : N <= 32 ? LINEAR_HALF_DEEP : N <= 64 ? LINEAR_HALF : LINEAR;
+        const bool half = kind == GATED_HALF || kind == LINEAR_HALF || kind == LINEAR_HALF_DEEP;
+        const int deep = kind == BF16_GATED ? 64 : kind == LINEAR_HALF_DEEP ? 256 : 128;
+        const int kstages = (int)((c.K + deep - 1) / deep);
+        int64_t one, token = 0, beside = 0;  // beside: with a second block on the SM
+        switch (kind) {
+        case BF16_GATED: one = 512 + 3 * N > 1100 ? 512 + 3 * N : 1100; break;
+        case GATED: one = 1450, token = 13; break;
+        case LINEAR: one = 900, token = 6; break;
+        case GATED_HALF: one = 1700, beside = 1900; break;
+        case LINEAR_HALF: one = 750, beside = 1100; break;
+        default: one = 1170, beside = 1800; break;
+        }
+        if (token * N > one) one = token * N;
+        const int64_t end = 800 + (two ? 7 : 4) * N;
+        const int *const clusters = half ? b->clusters_half : b->clusters;
+        for (int s = 1; s <= 8 && s <= kstages; ++s) {
+            if (s > 1 && tiles > clusters[s]) continue;
+            if (s > 1 && (int64_t)s * c.n_weights * ((N + s - 1) / s) * BM * 4 > 128 * 1024) continue;  // (partial sums that no ring has room for)
+            const int64_t blocks = tiles * s, places = (int64_t)b->sm_count * (half ? 2 : 1), rounds = (blocks + places - 1) / places;
+            const int64_t stage = half && blocks > b->sm_count ? beside : one;
+            const int64_t cost = rounds * ((kstages + s - 1) / s * stage + end) + (s > 1 ? 2000 + 150 * s : 0);
+            if (best_cost && cost >= best_cost) continue;
+            best_cost = cost;
+            best = {kind, N, s};
+        }
+    }
+    return best;
+}
+
+}  // namespace
 
 cudaError_t product_launch(const product_call &c, const tpq_block *b, cudaStream_t st, int64_t *launches)
 {
@@ -590,18 +713,21 @@ cudaError_t product_launch(const product_call &c, const tpq_block *b, cudaStream
             p.w4[a] = static_cast<const uint8_t *>(c.w[a]);
             p.factor[a] = reinterpret_cast<const float *>(p.w4[a] + w4_factors_at(c.n, c.K, c.group));
         }
-    // the tile's tokens
-    const int most = c.group && c.n_weights == 2 ? 128 : 256;
-    p.tiles_t = (int)((c.T + most - 1) / most);
-    p.N = (int)(((c.T + p.tiles_t - 1) / p.tiles_t + 15) / 16 * 16);
+    p.tiles_n = (int)((c.n + BM - 1) / BM);
+    const plan best = choose(c, b, p.tiles_n);
+    p.N = best.N;
     p.tiles_t = (int)((c.T + p.N - 1) / p.N);
     p.pitch = (p.N + 31) / 32 * 32;
-    p.tiles_n = (int)((c.n + BM - 1) / BM);
+    p.split = best.split;
     cudaError_t e;
-    if (!c.group) e = launch<2, 0>(p, c, b, st);
-    else if (c.n_weights == 2) e = launch<2, 1>(p, c, b, st);
-    else if (p.N <= 64) e = launch<1, 2>(p, c, b, st);
-    else e = launch<1, 1>(p, c, b, st);
+    switch (best.kind) {
+    case BF16_GATED: e = launch<2, 0, 16, false>(p, c, b, st); break;
+    case GATED: e = launch<2, 1, 16, false>(p, c, b, st); break;
+    case GATED_HALF: e = launch<2, 1, 8, true>(p, c, b, st); break;
+    case LINEAR: e = launch<1, 1, 16, false>(p, c, b, st); break;
+    case LINEAR_HALF: e = launch<1, 1, 8, true>(p, c, b, st); break;
+    default: e = launch<1, 2, 8, true>(p, c, b, st); break;
+    }
     if (e == cudaSuccess) ++*launches;
     return e;
 }

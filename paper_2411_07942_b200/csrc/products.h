@@ -37,16 +37,13 @@ __device__ __forceinline__ float activation(float g, int act)
     return 0.5f * g * erfcf(-0.70710678118654752f * g);  // (1 + erf z) = erfc(-z), without the cancellation
 }
 
-__device__ __forceinline__ float lds_cluster(uint32_t addr, uint32_t rank)
+// the same place in the shared memory of block `rank` of the cluster
+__device__ __forceinline__ uint32_t map_cluster(uint32_t addr, uint32_t rank)
 {
     uint32_t a;
-    float v;
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a));
-    return v;
+    return a;
 }
-__device__ __forceinline__ void cluster_sync()
-{
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
+__device__ __forceinline__ void st_cluster(uint32_t a, uint32_t v) { asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(a), "r"(v) : "memory"); }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
