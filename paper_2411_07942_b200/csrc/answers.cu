@@ -117,6 +117,7 @@ struct shared {
     // of the cluster's first block: what the others found
     triple parts[MOST_SPLIT];
     unsigned long long lists[MOST_SPLIT][MOST_TOP], merged[MOST_TOP];
+    int place[MOST_SPLIT * MOST_TOP];
 };
 
 __device__ __forceinline__ unsigned long long order_of(uint32_t key, int at) { return (unsigned long long)key << 32 | (uint32_t)~at; }
@@ -252,27 +253,29 @@ __device__ void most_likely(shared<THREADS> &s, const row_reader<FP32> &r, int v
     __syncthreads();
 }
 
-// Puts `lists` sorted lists of n (order_of, 0: no more; list l at from + l * pitch) together: the n first to `out`.  By all threads of a block.
+// Puts `lists` sorted lists of n (order_of, 0: no more; list l at from + l * pitch) together: the n first to `out`.  By all threads of a block, one
+// for each pair of an entry and another list; place: room for lists * n numbers.
 template <int THREADS>
-__device__ void merge(const unsigned long long *from, int pitch, int lists, int n, unsigned long long *out)
+__device__ void merge(const unsigned long long *from, int pitch, int lists, int n, int *place, unsigned long long *out)
 {
+    const int entries = lists * n;
     for (int i = threadIdx.x; i < n; i += THREADS) out[i] = 0;
+    for (int i = threadIdx.x; i < entries; i += THREADS) place[i] = i % n;  // and those of the other lists that come first:
     __syncthreads();
-    for (int i = threadIdx.x; i < lists * n; i += THREADS) {
-        const int l = i / n, p = i - l * n;
-        const unsigned long long o = from[l * pitch + p];
-        if (!o) continue;
-        int place = p;  // and those of the other lists that come first
-#pragma unroll 4
-        for (int k = 0; k < lists; ++k) {
-            if (k == l) continue;
-            int before = 0;
+    for (int i = threadIdx.x; i < entries * lists; i += THREADS) {
+        const int k = i / entries, e = i - k * entries, l = e / n;
+        const unsigned long long o = from[l * pitch + e - l * n];
+        if (!o || k == l) continue;
+        int before = 0;
 #pragma unroll
-            for (int step = MOST_TOP; step; step >>= 1)
-                if (before + step <= n && from[k * pitch + before + step - 1] > o) before += step;
-            place += before;
-        }
-        if (place < n) out[place] = o;
+        for (int step = MOST_TOP; step; step >>= 1)
+            if (before + step <= n && from[k * pitch + before + step - 1] > o) before += step;
+        if (before) atomicAdd(&place[e], before);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < entries; i += THREADS) {
+        const unsigned long long o = from[i / n * pitch + i % n];
+        if (o && place[i] < n) out[place[i]] = o;
     }
     __syncthreads();
 }
@@ -473,7 +476,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 8 : 2) token_stats(c
             if (tid < split) all = s.parts[tid];
             all = join_warp(all);
         }
-        if (c.n_top) merge<THREADS>(&s.lists[0][0], MOST_TOP, split, c.n_top, s.merged);
+        if (c.n_top) merge<THREADS>(&s.lists[0][0], MOST_TOP, split, c.n_top, s.place, s.merged);
         top = s.merged;
     }
     if (tid == 0) {
@@ -497,7 +500,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 8 : 2) token_stats(c
 // A warp a row, or with alternatives a block of 4 warps.  Record i is lane i's, and i + 32.
 __global__ void __launch_bounds__(128) token_logprobs(const join_call c, int *status)
 {
-    extern __shared__ unsigned long long lists[];  // [n + 1][n_top]
+    extern __shared__ unsigned long long lists[];  // [n + 1][n_top], and as many places
     const int lane = threadIdx.x & 31;
     const int64_t t = c.n_top ? blockIdx.x : (int64_t)blockIdx.x * 4 + threadIdx.x / 32;
     tpq_grid_dep_wait();
@@ -537,7 +540,7 @@ __global__ void __launch_bounds__(128) token_logprobs(const join_call c, int *st
     }
     __syncthreads();
     unsigned long long *const merged = lists + c.n * c.n_top;
-    merge<128>(lists, c.n_top, c.n, c.n_top, merged);
+    merge<128>(lists, c.n_top, c.n, c.n_top, reinterpret_cast<int *>(merged + c.n_top), merged);
     if (threadIdx.x < c.n_top) {
         const unsigned long long o = merged[threadIdx.x];
         if (c.top) c.top[t * c.n_top + threadIdx.x] = o ? (int)~(uint32_t)o : -1;
@@ -583,7 +586,7 @@ cudaError_t answers_launch_stats(const stats_call &c, const tpq_block *b, cudaSt
 cudaError_t answers_launch_join(const join_call &c, const tpq_block *b, cudaStream_t st, int64_t *launches)
 {
     const int64_t blocks = c.n_top ? c.T : (c.T + 3) / 4;
-    const cudaError_t e = tpq_launch_pdl(token_logprobs, dim3((unsigned)blocks), dim3(128), (size_t)(c.n + 1) * c.n_top * 8, st, c, b->status);
+    const cudaError_t e = tpq_launch_pdl(token_logprobs, dim3((unsigned)blocks), dim3(128), (size_t)(c.n + 1) * c.n_top * 12, st, c, b->status);
     if (e == cudaSuccess) ++*launches;
     return e;
 }

@@ -3,9 +3,10 @@
 // Both stream: 2 bytes in and half a byte out a value, or the other way round; memory is the bound.  A warp takes 8 rows x 128 inputs, a block
 // of the layout's: lane (r, q) has of each 16-byte piece of codes word q, 8 values.  So a warp reads or writes 64 adjacent bytes of each row and
 // 128 adjacent bytes of the pieces at a time.  A row's steps share a factor that depends on all of the row (its largest step's exponent): a first
-// walk over the rows finds the groups' largest magnitudes, the second one reads them again, from L2.
-// 32000 x 5120 (412 MB): TIME_Q to 4 bits, TIME_R back.  With a thread to 32 values of a row (16-byte loads and stores 64 bytes apart) and
-// quotients by __fdiv_rn they took 153 and 101 us.
+// walk over the rows finds the groups' largest magnitudes; for the second one rows of up to 5120 stay in registers, longer ones are read again,
+// from L2.
+// 32000 x 5120 (412 MB): TIME_Q us to 4 bits, 67 back (6.1 TB/s).  With a thread to 32 values of a row (16-byte loads and stores 64 bytes apart) and
+// quotients by __fdiv_rn they took 153 and 101, and with the second walk from L2 the first took 119.
 #include <cuda_bf16.h>
 
 #include "block_internal.h"
@@ -39,7 +40,8 @@ __device__ __forceinline__ uint32_t code_bits(float x, float inv)
     return __float_as_uint(__fadd_rn(__fadd_rn(u, 768.0f + 8.0f), 12582912.0f - 768.0f));
 }
 
-template <int GROUP>
+// KEEP: blocks of a warp that stay in registers between the walks (0: as many as there are, read again)
+template <int GROUP, int KEEP>
 __global__ void __launch_bounds__(THREADS) quantize_weight(const uint16_t *w, int64_t stride, int64_t n, int64_t K, int wide, uint8_t *w4, float *factors)
 {
     extern __shared__ uint16_t largest[];  // [ROWS][groups], bits of BF16 magnitudes (ordered like the numbers, NaN above infinity above those)
@@ -52,11 +54,16 @@ __global__ void __launch_bounds__(THREADS) quantize_weight(const uint16_t *w, in
     const uint16_t *in = w + row * stride;
     const bool there = row < n;
     uint32_t top = 0;
-    for (int b = warp; b < kb; b += WARPS) {
+    uint4 kept[KEEP ? KEEP : 1][4];
+    auto fetch = [&](int b, uint4 (&v)[4]) {
+#pragma unroll
+        for (int p = 0; p < 4; ++p) v[p] = there && b < kb ? load8(in, (int64_t)b * W4_TILE + p * 32 + q * 8, K, wide) : make_uint4(0, 0, 0, 0);
+    };
+    auto measure = [&](int b, const uint4 (&values)[4]) {
         uint32_t m[4];
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
-            const uint4 v = there ? load8(in, (int64_t)b * W4_TILE + p * 32 + q * 8, K, wide) : make_uint4(0, 0, 0, 0);
+            const uint4 &v = values[p];
             uint32_t a = __vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
             a = __vmaxu2(a, __shfl_xor_sync(0xffffffffu, a, 1));
             a = __vmaxu2(a, __shfl_xor_sync(0xffffffffu, a, 2));
@@ -70,6 +77,18 @@ __global__ void __launch_bounds__(THREADS) quantize_weight(const uint16_t *w, in
             if (q == 0) largest[(b * GROUPS + g) * ROWS + r] = (uint16_t)a;
             top = max(top, a);
         }
+    };
+    if (KEEP) {
+#pragma unroll
+        for (int i = 0; i < KEEP; ++i) fetch(warp + i * WARPS, kept[i]);
+#pragma unroll
+        for (int i = 0; i < KEEP; ++i)
+            if (warp + i * WARPS < kb) measure(warp + i * WARPS, kept[i]);
+    } else {
+        for (int b = warp; b < kb; b += WARPS) {
+            fetch(b, kept[0]);
+            measure(b, kept[0]);
+        }
     }
     if (q == 0) tops[warp][r] = top;
     __syncthreads();
@@ -81,7 +100,7 @@ __global__ void __launch_bounds__(THREADS) quantize_weight(const uint16_t *w, in
     if (warp == 0 && q == 0) factors[row] = bad ? __uint_as_float(0x7FC00000u) : __uint_as_float((uint32_t)(E - 7) << 23);
     uint8_t *const tile = w4 + (row / W4_TILE) * (int64_t)kb * BLOCK;
     const int in_tile = (int)(row % W4_TILE);
-    for (int b = warp; b < kb; b += WARPS) {
+    auto encode = [&](int b, const uint4 (&values)[4]) {
         uint8_t *const block = tile + (int64_t)b * BLOCK;
         float inv[GROUPS];
 #pragma unroll
@@ -93,7 +112,7 @@ __global__ void __launch_bounds__(THREADS) quantize_weight(const uint16_t *w, in
         }
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
-            const uint4 v = there && !bad ? load8(in, (int64_t)b * W4_TILE + p * 32 + q * 8, K, wide) : make_uint4(0, 0, 0, 0);
+            const uint4 &v = values[p];
             const uint32_t pairs[4] = {v.x, v.y, v.z, v.w};
             uint32_t word = 0;
 #pragma unroll
@@ -101,7 +120,17 @@ __global__ void __launch_bounds__(THREADS) quantize_weight(const uint16_t *w, in
                 const float f = inv[p / (4 / GROUPS)];
                 word = word * 16 + __byte_perm(code_bits(__uint_as_float(pairs[i] << 16), f), code_bits(__uint_as_float(pairs[i] & 0xFFFF0000u), f), 0x5410);
             }
-            *reinterpret_cast<uint32_t *>(block + p * (W4_TILE * 16) + in_tile * 16 + q * 4) = word;
+            *reinterpret_cast<uint32_t *>(block + p * (W4_TILE * 16) + in_tile * 16 + q * 4) = bad ? 0x88888888u : word;
+        }
+    };
+    if (KEEP) {
+#pragma unroll
+        for (int i = 0; i < KEEP; ++i)
+            if (warp + i * WARPS < kb) encode(warp + i * WARPS, kept[i]);
+    } else {
+        for (int b = warp; b < kb; b += WARPS) {
+            fetch(b, kept[0]);
+            encode(b, kept[0]);
         }
     }
 }
@@ -155,7 +184,10 @@ bool wide_rows(const void *p, int64_t stride) { return (reinterpret_cast<uintptr
 
 cudaError_t w4_launch_quantize(const uint16_t *w, int64_t stride, int64_t n, int64_t K, int group, uint8_t *w4, cudaStream_t st, int64_t *launches)
 {
-    auto kern = group == 32 ? quantize_weight<32> : group == 64 ? quantize_weight<64> : quantize_weight<128>;
+    const int64_t each = (w4_tiles(K) + WARPS - 1) / WARPS;  // blocks of a warp
+#define KERNEL(KEEP) (group == 32 ? quantize_weight<32, KEEP> : group == 64 ? quantize_weight<64, KEEP> : quantize_weight<128, KEEP>)
+    auto kern = each <= 2 ? KERNEL(2) : each <= 5 ? KERNEL(5) : KERNEL(0);
+#undef KERNEL
     const size_t smem = (size_t)ROWS * w4_tiles(K) * (W4_TILE / group) * 2;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
