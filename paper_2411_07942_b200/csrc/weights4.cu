@@ -31,13 +31,32 @@ __device__ __forceinline__ uint4 load8(const uint16_t *row, int64_t k0, int64_t 
 // 2a/15 rounded up to 5 significant bits, as the bits of a binary32; a: a BF16 magnitude's bits
 __device__ __forceinline__ uint32_t step_bits(uint32_t a) { return (__float_as_uint(__fdiv_rn(2.0f * __uint_as_float(a << 16), 15.0f)) + 0x7FFFFu) & ~0x7FFFFu; }
 
-// The code of x / step plus 8, in the low bits of a binary32 next to 1.5 * 2^23.  x has 8 significant bits and the step 5: where their quotient
-// is at least a half, it is a tie or further than 2^-10 from every tie, so rounding the product with the reciprocal (off by 2^-19 at most)
-// to multiples of 2^-14 first leaves exactly the ties.
-__device__ __forceinline__ uint32_t code_bits(float x, float inv)
+// Of two magnitudes each the larger (NaN above all), and of two numbers each the smaller
+__device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b)
 {
-    const float u = fminf(__fmul_rn(x, inv), 7.0f);  // (never below -8: the step is no smaller than 2/15 of the magnitude)
-    return __float_as_uint(__fadd_rn(__fadd_rn(u, 768.0f + 8.0f), 12582912.0f - 768.0f));
+    asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(a) : "r"(b));
+    return a;
+}
+__device__ __forceinline__ uint32_t min2(uint32_t a, uint32_t b)
+{
+    asm("min.bf16x2 %0, %0, %1;" : "+r"(a) : "r"(b));
+    return a;
+}
+// The codes of a pair x / step plus 8, in the low halves' low bits.  x has 8 significant bits and the step 5: where their quotient
+// is at least a half, it is a tie or further than 2^-10 from every tie, so rounding the product with the reciprocal (off by 2^-19 at most)
+// to multiples of 2^-14 first leaves exactly the ties; the second sum, with 1.5 * 2^23, rounds to integers.  (Above 7 steps, an exact BF16 number, is 7;
+// nothing is below -8: the step is no smaller than 2/15 of the magnitude.)
+__device__ __forceinline__ uint32_t code_pair(uint32_t x, uint32_t most, uint64_t inv)
+{
+    const uint32_t v = min2(x, most);
+    uint64_t u;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(u) : "r"(v << 16), "r"(v & 0xFFFF0000u));
+    asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(u) : "l"(inv));
+    asm("add.rn.f32x2 %0, %0, %1;" : "+l"(u) : "l"(0x4442000044420000ull));  // 768 + 8
+    asm("add.rn.f32x2 %0, %0, %1;" : "+l"(u) : "l"(0x4B3FFD004B3FFD00ull));  // 1.5 * 2^23 - 768
+    uint32_t lo, hi;
+    asm("mov.b64 {%0, %1}, %2;" : "=r"(lo), "=r"(hi) : "l"(u));
+    return __byte_perm(lo, hi, 0x5410);
 }
 
 // KEEP: blocks of a warp that stay in registers between the walks (0: as many as there are, read again)
@@ -64,9 +83,9 @@ __global__ void __launch_bounds__(THREADS) quantize_weight(const uint16_t *w, in
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
             const uint4 &v = values[p];
-            uint32_t a = __vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
-            a = __vmaxu2(a, __shfl_xor_sync(0xffffffffu, a, 1));
-            a = __vmaxu2(a, __shfl_xor_sync(0xffffffffu, a, 2));
+            uint32_t a = max2(max2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), max2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
+            a = max2(a, __shfl_xor_sync(0xffffffffu, a, 1));
+            a = max2(a, __shfl_xor_sync(0xffffffffu, a, 2));
             m[p] = max(a & 0xFFFFu, a >> 16);
         }
 #pragma unroll
@@ -102,12 +121,16 @@ __global__ void __launch_bounds__(THREADS) quantize_weight(const uint16_t *w, in
     const int in_tile = (int)(row % W4_TILE);
     auto encode = [&](int b, const uint4 (&values)[4]) {
         uint8_t *const block = tile + (int64_t)b * BLOCK;
-        float inv[GROUPS];
+        uint64_t inv[GROUPS];
+        uint32_t most[GROUPS];  // 7 steps
 #pragma unroll
         for (int g = 0; g < GROUPS; ++g) {
             const uint32_t bits = bad ? 0u : step_bits(largest[(b * GROUPS + g) * ROWS + r]);
             const int e = (int)(bits >> 23) - E + 15;
-            inv[g] = __frcp_rn(__uint_as_float(e < 0 ? (uint32_t)(bad ? 127 : E - 15) << 23 : bits));
+            const float step = __uint_as_float(e < 0 ? (uint32_t)(bad ? 127 : E - 15) << 23 : bits);
+            const uint32_t inverse = __float_as_uint(__frcp_rn(step));
+            inv[g] = (uint64_t)inverse << 32 | inverse;
+            most[g] = (__float_as_uint(7.0f * step) >> 16) * 0x00010001u;
             if (q == 0) block[W4_CODE_BYTES + g * W4_TILE + in_tile] = (uint8_t)(e < 0 ? 0u : (uint32_t)e << 4 | (bits >> 19 & 15u));
         }
 #pragma unroll
@@ -116,10 +139,7 @@ __global__ void __launch_bounds__(THREADS) quantize_weight(const uint16_t *w, in
             const uint32_t pairs[4] = {v.x, v.y, v.z, v.w};
             uint32_t word = 0;
 #pragma unroll
-            for (int i = 3; i >= 0; --i) {  // pair i in bits 4i and 16 + 4i
-                const float f = inv[p / (4 / GROUPS)];
-                word = word * 16 + __byte_perm(code_bits(__uint_as_float(pairs[i] << 16), f), code_bits(__uint_as_float(pairs[i] & 0xFFFF0000u), f), 0x5410);
-            }
+            for (int i = 3; i >= 0; --i) word = word * 16 + code_pair(pairs[i], most[p / (4 / GROUPS)], inv[p / (4 / GROUPS)]);  // pair i in bits 4i and 16 + 4i
             *reinterpret_cast<uint32_t *>(block + p * (W4_TILE * 16) + in_tile * 16 + q * 4) = bad ? 0x88888888u : word;
         }
     };
