@@ -66,6 +66,7 @@ tpq_status check_weight(tpq_block *b, const char *name, const tpq_weight *w)
         if (!group_ok(w->group)) return fail(b, TPQ_ERR_INVALID_ARG, "%s: group = %d is not 32, 64 or 128", name, w->group);
     } else {
         if (w->row_stride < w->n_in) return fail(b, TPQ_ERR_INVALID_ARG, "row stride %lld of %s < %lld", (long long)w->row_stride, name, (long long)w->n_in);
+        if (w->row_stride > (INT64_C(1) << 38)) return fail(b, TPQ_ERR_INVALID_ARG, "row stride %lld of %s is above 2^38", (long long)w->row_stride, name);
         if (w->row_stride % 8) return fail(b, TPQ_ERR_ALIGN, "row stride %lld of %s is not a multiple of 8 elements", (long long)w->row_stride, name);
     }
     return TPQ_OK;
