@@ -505,7 +505,8 @@ tpq_status tpq_quantize_weight(tpq_block *block, const void *w_bf16_dev, int64_t
 tpq_status tpq_read_weight(tpq_block *block, const void *w4_dev, int64_t n_out, int64_t n_in, int group, void *out_bf16_dev,
                            int64_t out_row_stride, void *cuda_stream);
 
-/* out = x W^T, W in 4 bits; binary32 sums on the tensor cores, one rounding for BF16 output.
+/* out = x W^T, W in 4 bits; binary32 sums on the tensor cores (which cut off what does not fit; for FP32 output of at most 32 rows those of 256
+ * inputs are added up in binary32, rounded), one rounding for BF16 output.
  *   x   : [T][n_in] BF16, 16-byte aligned, row stride a multiple of 8 elements (what lies between the rows is not read)
  *   out : [T][n_out] of dt, aligned to its type, any stride >= n_out; it must not overlap x
  * A row of x that holds infinities or NaN makes its own row of out such (an infinite input times a code of 0 is NaN), and no other.

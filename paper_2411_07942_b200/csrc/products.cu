@@ -18,8 +18,16 @@
 // set would.  The first stages of the next tile are unpacked ahead of it.  One commit a stage frees its shared memory and its operands: a
 // commit costs the tensor pipe about 300 clocks (with one for each 64-wide piece, one token's head of 32000 outputs x 5120 took 49 us).
 //
-// Few tokens: a tile's inputs are split over the blocks of a cluster, so that all SMs read weights; the partial sums meet in the
-// cluster's shared memory and are added in the order of the blocks (the same call gives the same bits).
+// Few tokens: a tile's inputs are split over the blocks of a cluster, so that all SMs read weights; each block stores its part of the sums to the
+// block of the cluster that ends with them, which adds them in the order of the blocks (the same call gives the same bits).
+//
+// What bounds it (B200; products of other work in turn, so that weights come from memory).  Many tokens: the tensor pipe (67 % of all cycles active at the clock
+// that the power limit leaves): gated 1999 x 5120 x 3456 in 4 bits 103 us (1370 TFLOP/s), 2048 in BF16 106 us, where shared memory is as close.  Few tokens,
+// 4 bits: unpacking (9 instructions for 8 codes of 32 outputs, 20 with all that goes round it) and what is left over when tiles of 128 outputs
+// are dealt out: 32000 x 5120, one token, BF16 out 22.7 us (3.8 TB/s); without unpacking, stores to tensor memory and MMAs it would be 18.6.  BF16: memory, 17.5 us of
+// 2 x 4608 x 4608 (4.9 TB/s).  One token of 5120 x 1728: 5.5 us, latency (2.7 us from the first copy to the sums, 1.7 us cluster and stores).
+// Tried for few tokens and not kept: mma.sync (16 outputs x 16 inputs x 8 tokens) with weights unpacked in registers, no barriers and no tensor memory:
+// 32 to 38 us of the 32000 x 5120 whatever was done to it, 66 with 16 tokens, 138 with 32: one takes 33 clocks of a scheduler.
 // Every wait is bounded: on expiry the block records TPQ_ERR_TIMEOUT, skips its stores, frees its tensor memory and returns.
 #include <cuda_bf16.h>
 
