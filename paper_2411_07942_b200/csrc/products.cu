@@ -657,7 +657,7 @@ cudaError_t prepare()
 }
 
 // (What a block of half an SM takes, for the question of how many clusters run side by side.  Of the product kernels it is answered as if
-// one block filled an SM, which two do: 27 % more warps were active than with one.)
+// one block filled an SM; two do: 15.8 warps were active on average, where one block has 10.)
 __global__ void __launch_bounds__(384, 2) half_block() {}
 
 // clusters of `split` blocks that run side by side
