@@ -351,7 +351,7 @@ product(const params p, const __grid_constant__ CUtensorMap map_x, const __grid_
                                 mma_ss(a ? tmem1 : tmem, w + a * (W_BF16_BYTES >> 4) + 2 * k, x + 2 * k, idesc, k ? 1u : (uint32_t)(kb != kb0));
                     }
                     commit(empty(r.s));
-                    if (kb == kb1 - 1) commit(acc_full);
+                    if (!ADD && kb == kb1 - 1) commit(acc_full);  // (a barrier that somebody waits on: an arrival must not outlive the block)
                 }
                 __syncwarp();
                 if (W4) t.next(p.depth);
