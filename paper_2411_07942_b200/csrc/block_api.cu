@@ -41,7 +41,7 @@ tpq_status check_device(tpq_block *b)
     return TPQ_OK;
 }
 
-constexpr int64_t MOST_OUTPUTS = INT64_C(1) << 30, MOST_INPUTS = INT64_C(1) << 17, MOST_ROWS = INT64_C(1) << 30;
+constexpr int64_t MOST_OUTPUTS = INT64_C(1) << 30, MOST_INPUTS = W4_MOST_INPUTS, MOST_ROWS = INT64_C(1) << 30;
 
 bool group_ok(int group) { return group == 32 || group == 64 || group == 128; }
 bool shape_ok(int64_t n, int64_t K) { return n >= 1 && n <= MOST_OUTPUTS && K >= 1 && K <= MOST_INPUTS; }
@@ -117,6 +117,7 @@ tpq_status tpq_block_create(tpq_block **out)
     cudaError_t e = cudaGetDevice(&b->device);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&b->sm_count, cudaDevAttrMultiProcessorCount, b->device);
     if (e == cudaSuccess) e = product_prepare(b);
+    if (e == cudaSuccess) e = w4_prepare();
     if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void **>(&b->status), sizeof(int));
     if (e == cudaSuccess) {
         e = clear(b->status);

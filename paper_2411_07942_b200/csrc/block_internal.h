@@ -14,6 +14,7 @@ struct tpq_block {
 // Weights in 4 bits (layout in tpq.h): blocks of 128 outputs x 128 inputs, the outputs' factors behind them.
 #define W4_TILE 128
 #define W4_CODE_BYTES 8192
+#define W4_MOST_INPUTS (INT64_C(1) << 17)
 static inline int64_t w4_tiles(int64_t n) { return (n + W4_TILE - 1) / W4_TILE; }
 #ifdef __CUDACC__
 __host__ __device__
@@ -22,6 +23,7 @@ static inline int w4_block_bytes(int group) { return W4_CODE_BYTES + W4_TILE * (
 static inline int64_t w4_factors_at(int64_t n, int64_t K, int group) { return w4_tiles(n) * w4_tiles(K) * w4_block_bytes(group); }
 static inline int64_t w4_bytes(int64_t n, int64_t K, int group) { return w4_factors_at(n, K, group) + w4_tiles(n) * W4_TILE * 4; }
 
+cudaError_t w4_prepare();
 cudaError_t w4_launch_quantize(const uint16_t *w, int64_t stride, int64_t n, int64_t K, int group, uint8_t *w4, cudaStream_t st, int64_t *launches);
 cudaError_t w4_launch_read(const uint8_t *w4, int64_t n, int64_t K, int group, uint16_t *out, int64_t stride, cudaStream_t st, int64_t *launches);
 

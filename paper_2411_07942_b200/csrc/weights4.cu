@@ -201,7 +201,16 @@ __global__ void __launch_bounds__(THREADS) read_weight(const uint8_t *w4, const 
 
 bool wide_rows(const void *p, int64_t stride) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && stride % 8 == 0; }
 
+size_t shared_bytes(int64_t K, int group) { return (size_t)ROWS * w4_tiles(K) * (W4_TILE / group) * 2; }
+
 }  // namespace
+
+// Once per handle.  The limit of shared memory belongs to the kernel on this device and not to a handle, so it is the same whoever sets it: what the
+// longest rows take (64 KB; the other kernels stay below the 48 KB that need no leave).
+cudaError_t w4_prepare()
+{
+    return cudaFuncSetAttribute(quantize_weight<32, 0>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared_bytes(W4_MOST_INPUTS, 32));
+}
 
 cudaError_t w4_launch_quantize(const uint16_t *w, int64_t stride, int64_t n, int64_t K, int group, uint8_t *w4, cudaStream_t st, int64_t *launches)
 {
@@ -209,11 +218,8 @@ cudaError_t w4_launch_quantize(const uint16_t *w, int64_t stride, int64_t n, int
 #define KERNEL(KEEP) (group == 32 ? quantize_weight<32, KEEP> : group == 64 ? quantize_weight<64, KEEP> : quantize_weight<128, KEEP>)
     auto kern = each <= 2 ? KERNEL(2) : each <= 5 ? KERNEL(5) : KERNEL(0);
 #undef KERNEL
-    const size_t smem = (size_t)ROWS * w4_tiles(K) * (W4_TILE / group) * 2;
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return e;
-    e = tpq_launch_pdl(kern, dim3((unsigned)(w4_tiles(n) * (W4_TILE / ROWS))), dim3(THREADS), smem, st, w, stride, n, K, (int)wide_rows(w, stride), w4,
-                       reinterpret_cast<float *>(w4 + w4_factors_at(n, K, group)));
+    const cudaError_t e = tpq_launch_pdl(kern, dim3((unsigned)(w4_tiles(n) * (W4_TILE / ROWS))), dim3(THREADS), shared_bytes(K, group), st, w, stride, n, K,
+                                         (int)wide_rows(w, stride), w4, reinterpret_cast<float *>(w4 + w4_factors_at(n, K, group)));
     if (e == cudaSuccess) ++*launches;
     return e;
 }
