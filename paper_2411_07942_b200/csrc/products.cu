@@ -28,7 +28,8 @@
 // 2 x 4608 x 4608 (4.9 TB/s).  One token of 5120 x 1728: 5.5 us, latency (2.7 us from the first copy to the sums, 1.7 us cluster and stores).
 // Tried for few tokens and not kept: mma.sync (16 outputs x 16 inputs x 8 tokens) with weights unpacked in registers, no barriers and no tensor memory:
 // 32 to 38 us of the 32000 x 5120 whatever was done to it, 66 with 16 tokens, 138 with 32: one takes 33 clocks of a scheduler.
-// Every wait is bounded: on expiry the block records TPQ_ERR_TIMEOUT, skips its stores, frees its tensor memory and returns.
+// Every wait is bounded.  A warp whose wait expires records TPQ_ERR_TIMEOUT and tells its block and its cluster: a split tile is then not stored at all,
+// of others what has its sums is; the copies and MMAs that are under way end before the block's memory is given back.
 #include <cuda_bf16.h>
 
 #include "block_internal.h"
@@ -39,8 +40,15 @@ namespace {
 constexpr int BM = 128, MOST_STAGES = 16, MOST_DEPTH = 4;
 constexpr int WAIT_LIMIT = 1 << 24;                     // try_wait attempts (each suspends for a hardware time slice) ...
 constexpr unsigned long long WAIT_NS = 1000000000ull;   // ... and one second, whichever ends first
+#ifdef TPQ_GIVE_UP  // (a test's build: bit p of it has waits for parity p expire that are not over at the first look, the others after 10 ms)
+constexpr unsigned GIVE_UP = TPQ_GIVE_UP;
+constexpr unsigned long long PATIENCE_NS = 10000000ull;
+#else
+constexpr unsigned GIVE_UP = 0;
+constexpr unsigned long long PATIENCE_NS = WAIT_NS;
+#endif
 constexpr uint32_t SMEM_MAX = 227u * 1024u, SMEM_HALF = 112u * 1024u;  // of a block that has an SM for itself, of two beside one another
-constexpr uint32_t BAR_BYTES = 512;                     // barriers and the tensor-memory address
+constexpr uint32_t BAR_BYTES = 512;                     // barriers, the tensor-memory address, whether a wait expired
 constexpr uint32_t W_BF16_BYTES = BM * 64 * 2;
 
 struct params {
@@ -72,6 +80,7 @@ __device__ __forceinline__ uint32_t try_wait(uint32_t bar, uint32_t parity)
     return ok;
 }
 // (out of line: most waits end at the first attempt, and the loop's code would cost them 30 of their 90 clocks)
+template <unsigned long long NS>
 __device__ __noinline__ bool wait_long(uint32_t bar, uint32_t parity)
 {
     unsigned long long t0 = 0;
@@ -83,14 +92,30 @@ __device__ __noinline__ bool wait_long(uint32_t bar, uint32_t parity)
             unsigned long long t;
             asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
             if (t0 == 0) t0 = t;
-            else if (t - t0 > WAIT_NS) break;
+            else if (t - t0 > NS) break;
         }
     }
     return __all_sync(0xffffffffu, ok);
 }
+template <unsigned long long NS = WAIT_NS>
+__device__ __forceinline__ bool wait_end(uint32_t bar, uint32_t parity)
+{
+    return __all_sync(0xffffffffu, try_wait(bar, parity)) || wait_long<NS>(bar, parity);
+}
 __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity)  // by a whole warp
 {
-    return __all_sync(0xffffffffu, try_wait(bar, parity)) || wait_long(bar, parity);
+    if (GIVE_UP >> (parity & 1) & 1) {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok)
+            : "r"(bar), "r"(parity)
+            : "memory");
+        return __all_sync(0xffffffffu, ok);
+    }
+    return wait_end<PATIENCE_NS>(bar, parity);
 }
 
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -216,6 +241,7 @@ product(const params p, const __grid_constant__ CUtensorMap map_x, const __grid_
     const uint32_t bars = base + p.stages * p.stage;
     uint8_t *const gen = raw + (base - smem_u32(raw));
     uint32_t *const tmem_slot = reinterpret_cast<uint32_t *>(gen + p.stages * p.stage + BAR_BYTES - 16);
+    volatile uint32_t *const expired = tmem_slot + 1;  // a wait of this block or of its cluster
     auto full = [&](int s) { return bars + 8u * s; };
     auto empty = [&](int s) { return bars + 8u * (MOST_STAGES + s); };
     auto a_full = [&](int s) { return bars + 8u * (2 * MOST_STAGES + s); };
@@ -235,6 +261,8 @@ product(const params p, const __grid_constant__ CUtensorMap map_x, const __grid_
     // pieces of stage kb (with two blocks a stage, the last one of a row may have one)
     auto pieces = [&](int kb) { return KB == 2 && 2 * kb + 1 == p.blocks ? 2 : KX; };
 
+    if (tid == 0) *expired = 0;
+    __syncwarp();
     if (p.split > 1 && p.sums_at) cluster_arrive();  // (the blocks' memory is there: waited for ahead of the first store to it)
     if (tid == 0) {
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_x) : "memory");
@@ -276,19 +304,21 @@ product(const params p, const __grid_constant__ CUtensorMap map_x, const __grid_
     const uint32_t tmem = *tmem_slot;
     const uint32_t a_at = tmem + (uint32_t)(NW * p.pitch);  // operands behind the accumulators
     bool ok = true;
+    ring last;      // warp 0: behind the last stage copied; warp 1: the last stage multiplied
+    int issued = 0;  // stages, warp 0 up to the ring's length
+    uint32_t done_tiles = 0;  // warp 1: tiles whose last MMA is issued
     float sum[ADD ? 16 : 1];  // of columns 16 * part .. of the warp's rows
 
     if (warp == 0) {
         // the copies of a stage leave from as many lanes
         ring r;
-        int used = 0;  // stages issued so far, up to the ring's length
         for (int tile = first_tile; tile < tiles && ok; tile += places) {
             int tn, tt;
             origin(tile, tn, tt);
             const uint8_t *w = W4 && lane < NW ? p.w4[lane] + ((int64_t)tn * p.blocks + KB * kb0) * p.w_block : nullptr;
             for (int kb = kb0; kb < kb1; ++kb, r.next(p.stages)) {
-                if (used == p.stages) ok = wait_warp(empty(r.s), r.phase ^ 1);
-                else ++used;
+                if (issued == p.stages) ok = wait_warp(empty(r.s), r.phase ^ 1);
+                else ++issued;
                 if (!ok) break;
                 const uint32_t at = base + r.s * p.stage, bar = full(r.s);
                 const int kx = pieces(kb);
@@ -304,13 +334,7 @@ product(const params p, const __grid_constant__ CUtensorMap map_x, const __grid_
                 if (lane < kx) tma_load_2d(at + p.x_at + lane * (p.N * 128), &map_x, (kb * KX + lane) * 64, tt * p.N, bar);
             }
         }
-        if (!ok) {  // giving up: let the copies already issued land before the shared memory is released
-            ring l = r;
-            for (int j = 0; j < p.stages; ++j) {
-                (void)wait_warp(full(l.s), l.phase ^ 1);
-                l.next(p.stages);
-            }
-        }
+        last = r;
     } else if (warp == 1) {
         const uint32_t idesc = instr(p.N), tmem1 = tmem + (uint32_t)p.pitch, x_piece = (uint32_t)p.N * 128 >> 4;
         ring r, t;  // of shared memory and of the operands in tensor memory
@@ -354,6 +378,9 @@ product(const params p, const __grid_constant__ CUtensorMap map_x, const __grid_
                     if (!ADD && kb == kb1 - 1) commit(acc_full);  // (a barrier that somebody waits on: an arrival must not outlive the block)
                 }
                 __syncwarp();
+                last = r;
+                issued = 1;
+                if (!ADD && kb == kb1 - 1) ++done_tiles;
                 if (W4) t.next(p.depth);
             }
         }
@@ -507,7 +534,10 @@ product(const params p, const __grid_constant__ CUtensorMap map_x, const __grid_
         }
         if (p.split > 1 && !ADD) ok = ok && wait_warp(acc_full, 0);
     }
-    if (!ok) atomicExch(p.status, (int)TPQ_ERR_TIMEOUT);
+    if (!ok) {
+        atomicExch(p.status, (int)TPQ_ERR_TIMEOUT);
+        *expired = 1;
+    }
     if (p.split > 1) {
         // Every block ends with a share of the tile's cells (token, output): the others store theirs of it to its memory, [block][weight][cell],
         // and it adds them in the order of the blocks.
@@ -526,6 +556,8 @@ product(const params p, const __grid_constant__ CUtensorMap map_x, const __grid_
         }
         if (!p.sums_at) cluster_arrive();  // (this block's stages are free)
         cluster_wait();
+        if (!ok && lane < p.split) st_cluster(map_cluster(smem_u32(tmem_slot + 1), lane), 1u);
+        __syncwarp();
         if (warp >= 2 && ok) {
             fence_after();
             const int q = warp & 3, part = (warp - 2) >> 2, per = (tokens + p.split - 1) / p.split;
@@ -554,6 +586,7 @@ product(const params p, const __grid_constant__ CUtensorMap map_x, const __grid_
         }
         cluster_arrive();
         cluster_wait();
+        const bool all_there = *expired == 0;
         for (int i = tid; i < mine; i += blockDim.x) {
             const int cell = from + i, col = tn * BM + (cell & (BM - 1));
             float v = 0.0f, u = 0.0f;
@@ -562,7 +595,7 @@ product(const params p, const __grid_constant__ CUtensorMap map_x, const __grid_
                 v += sums[k * NW * share + i];
                 if (NW == 2) u += sums[(k * NW + 1) * share + i];
             }
-            if (col >= p.n || !ok) continue;
+            if (col >= p.n || !all_there) continue;
             if (W4 && i != tid) {
                 f0 = W4_SCALE * p.factor[0][col];
                 if (NW == 2) f1 = W4_SCALE * p.factor[1][col];
@@ -574,6 +607,16 @@ product(const params p, const __grid_constant__ CUtensorMap map_x, const __grid_
     }
     fence_before();
     __syncthreads();
+    if (*expired) {
+        // giving up: what was issued ends before shared and tensor memory are given back (the rest of a whole walk has been waited for)
+        if (warp == 0) {
+            if (issued < p.stages) last = ring{0, 1};
+            for (int j = 0; j < issued; ++j, last.next(p.stages)) (void)wait_end(full(last.s), last.phase ^ 1);
+        } else if (warp == 1 && issued) {
+            (void)wait_end(empty(last.s), last.phase);
+            if (done_tiles) (void)wait_end(acc_full, (done_tiles - 1) & 1);
+        }
+    }
     if (warp == 1) {
         __syncwarp();
         fence_after();

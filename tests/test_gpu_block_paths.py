@@ -3,6 +3,7 @@
 Helpers and worst-case bounds per element are those of test_gpu_block.py."""
 import ctypes
 import math
+import os
 import subprocess
 import threading
 
@@ -30,6 +31,20 @@ def block():
     yield b
     assert b.device_status() == 0
     b.close()
+
+
+def some_weights(n, K, seed):
+    g = torch.Generator("cuda").manual_seed(seed)
+    return (torch.randn(n, K, generator=g, device="cuda") / math.sqrt(K)).to(torch.bfloat16)
+
+
+def in_4_bits(block, n, K, group, seed=0):
+    """(binding.Weight, its buffer) of some_weights."""
+    w = some_weights(n, K, seed)
+    w4 = torch.empty(binding.weight4_bytes(n, K, group), dtype=torch.uint8, device="cuda")
+    block.quantize_weight(w.data_ptr(), n, K, group, w4.data_ptr(), w4.numel())
+    torch.cuda.synchronize()
+    return binding.Weight(w4.data_ptr(), n, K, 0, binding.TPQ_WEIGHT_INT4, group), w4
 
 
 # ------------------------------------------------------------------------------------------------ products
@@ -104,3 +119,74 @@ def test_threads_with_a_handle_each_quantise_side_by_side(tmp_path):
         codes, byte, factor = block_ref.quantise(np.ones((n, K)), 32)
         assert np.array_equal(w4[i].cpu().numpy(), block_ref.pack(codes, byte, factor, 32))
         b[i].close()
+
+
+# ------------------------------------------------------------------------------------------------ waits that expire
+NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
+@pytest.fixture(scope="module")
+def expiring(tmp_path_factory):
+    """The library, built so that waits for a parity expire that are not over at the first look (parities -> library)."""
+    out = tmp_path_factory.mktemp("expiring")
+    flags = [f for f in build.NVCC_FLAGS] + [f"-I{build.INCLUDE}", f"-I{build.CSRC}"]
+    jobs = {f"products{m}": ["products.cu", f"-DTPQ_GIVE_UP={m}"] for m in (1, 2, 3)}
+    jobs |= {f"{s.stem}": [s.name] for s in build.sources() if s.stem != "products" and not (build.OBJ / f"{s.stem}.o").exists()}
+    running = [subprocess.Popen([NVCC, *flags, "-c", str(build.CSRC / f[0]), *f[1:], "-o", str(out / f"{name}.o")])
+               for name, f in jobs.items()]
+    assert [p.wait() for p in running] == [0] * len(running)
+    rest = [str(o if (o := build.OBJ / f"{s.stem}.o").exists() else out / f"{s.stem}.o") for s in build.sources() if s.stem != "products"]
+    libs = {}
+    for m in (1, 2, 3):
+        so = out / f"expiring{m}.so"
+        subprocess.run([NVCC, *build.LINK_FLAGS, "-o", str(so), str(out / f"products{m}.o"), *rest], check=True)
+        libs[m] = ctypes.CDLL(str(so))
+        for name, (res, args) in binding.SIGNATURES.items():
+            f = getattr(libs[m], name)
+            f.restype, f.argtypes = res, args
+    return libs
+
+
+EXPIRING = [
+    (1, 5120, 1728, 64, 0),          # a tile over a cluster, two blocks an SM
+    (1, 45000, 700, 32, 0), (1, 45000, 700, 32, 1), (20, 40000, 1300, 128, 1),     # several tiles a block, two blocks an SM
+    (60, 40000, 640, 64, 0), (60, 2000, 4096, 64, 1),
+    (300, 2304, 3456, 128, 0), (300, 2304, 3456, 128, 1), (2048, 1280, 3456, 64, 0), (2048, 1280, 3456, 64, 1)]
+
+
+@pytest.mark.parametrize("gated,T,n,K,group,out_fp32", [(None, *c) for c in EXPIRING] + [(g, *c) for g in (0, 64) for c in EXPIRING if not c[4]])
+@pytest.mark.parametrize("parities", [1, 2, 3])
+def test_waits_that_expire_leave_everything_in_order(block, expiring, parities, gated, T, n, K, group, out_fp32):
+    """Every role of the kernels gives up where it does not find at once what it waits for, at the beginning (parity 0) or in the midst of its walk: the
+    status says so, nothing wrong is stored, nothing is written beside the output, and calls that follow are as ever.  The limits by which copies and
+    MMAs under way are waited for at the end are the shipped ones."""
+    L, rng = expiring[parities], np.random.default_rng(T + n + K)
+    handle = ctypes.c_void_p()
+    assert L.tpq_block_create(ctypes.byref(handle)) == 0
+    x = bf16(rng.standard_normal((T, K)))
+    xbuf, xptr = rows(x, up8(K))
+    n_weights = 1 if gated is None else 2
+    if gated == 0:
+        keep = [torch.nn.functional.pad(some_weights(n, K, seed), (0, up8(K) - K)) for seed in range(2)]
+        made = [binding.Weight(w.data_ptr(), n, K, up8(K), binding.TPQ_WEIGHT_BF16, 0) for w in keep]
+    else:
+        made, keep = zip(*[in_4_bits(block, n, K, gated or group, seed) for seed in range(n_weights)])
+    kind = torch.float32 if out_fp32 else torch.bfloat16
+
+    def call(lib, h, out):
+        if gated is None:
+            return lib.tpq_linear4(h, made[0], xptr, up8(K), T, out.data_ptr(), out_fp32, n, None)
+        return lib.tpq_gated(h, made[0], made[1], 0, xptr, up8(K), T, out.data_ptr(), n, None)
+
+    want = torch.zeros(T, n, dtype=kind, device="cuda")
+    assert call(binding.lib(), block._h, want) == 0 and block.device_status() == 0
+    for _ in range(5):
+        whole = torch.full((2 * 4096 + T * n,), 7.0, dtype=kind, device="cuda")
+        got = whole[4096: 4096 + T * n].view(T, n)
+        assert call(L, handle, got) == 0
+        status = L.tpq_block_device_status(handle)
+        assert status in ((binding.TPQ_ERR_TIMEOUT,) if parities & 1 else (0, binding.TPQ_ERR_TIMEOUT))
+        assert ((got == want) | (got == 7.0)).all() and (status or torch.equal(got, want))
+        assert (whole[:4096] == 7.0).all() and (whole[4096 + T * n:] == 7.0).all()
+        again = torch.zeros(T, n, dtype=kind, device="cuda")
+        assert call(binding.lib(), block._h, again) == 0 and block.device_status() == 0
+        assert torch.equal(again, want)
+    assert L.tpq_block_destroy(handle) == 0
