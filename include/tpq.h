@@ -505,8 +505,9 @@ tpq_status tpq_quantize_weight(tpq_block *block, const void *w_bf16_dev, int64_t
 tpq_status tpq_read_weight(tpq_block *block, const void *w4_dev, int64_t n_out, int64_t n_in, int group, void *out_bf16_dev,
                            int64_t out_row_stride, void *cuda_stream);
 
-/* out = x W^T, W in 4 bits; binary32 sums on the tensor cores (which cut off what does not fit; for FP32 output of at most 32 rows those of 256
- * inputs are added up in binary32, rounded), one rounding for BF16 output.
+/* out = x W^T, W in 4 bits; binary32 sums, one rounding for BF16 output.  The tensor cores cut off what does not fit their sums (3 to 4e-9 of the
+ * output's norm for every 16 inputs, which the rounding to BF16 hides); for FP32 output, whatever T is, they add up at most 512 inputs, and these sums are added
+ * up in binary32, rounded: about 1e-7 of the norm, as a sum of binary32 products has.
  *   x   : [T][n_in] BF16, 16-byte aligned, row stride a multiple of 8 elements (what lies between the rows is not read)
  *   out : [T][n_out] of dt, aligned to its type, any stride >= n_out; it must not overlap x
  * A row of x that holds infinities or NaN makes its own row of out such (an infinite input times a code of 0 is NaN), and no other.
@@ -514,7 +515,7 @@ tpq_status tpq_read_weight(tpq_block *block, const void *w4_dev, int64_t n_out, 
 tpq_status tpq_linear4(tpq_block *block, const tpq_weight *w, const void *x_bf16_dev, int64_t x_row_stride, int64_t T, void *out_dev,
                        tpq_out_dtype dt, int64_t out_row_stride, void *cuda_stream);
 
-/* The gated feed-forward block ahead of the down projection: out = bf16(act(x Wg^T) * (x Wu^T)), in one kernel; sums, activation and
+/* The gated feed-forward block ahead of the down projection: out = bf16(act(x Wg^T) * (x Wu^T)), in one kernel; sums (the tensor cores' own), activation and
  * product in binary32.  gate and up: both BF16 or both in 4 bits (the same group), the same sizes.
  *   SILU g / (1 + e^-g);  GELU_ERF g (1 + erf(g / sqrt 2)) / 2;  GELU_TANH g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) / 2
  * (an activation below 2^-100 may come out as 0).  x, out (BF16), T and errors as tpq_linear4. */

@@ -37,7 +37,7 @@
 
 namespace {
 
-constexpr int BM = 128, MOST_STAGES = 16, MOST_DEPTH = 4;
+constexpr int BM = 128, MOST_STAGES = 16, MOST_DEPTH = 4, ADD_STAGES = 4;
 constexpr int WAIT_LIMIT = 1 << 24;                     // try_wait attempts (each suspends for a hardware time slice) ...
 constexpr unsigned long long WAIT_NS = 1000000000ull;   // ... and one second, whichever ends first
 #ifdef TPQ_GIVE_UP  // (a test's build: bit p of it has waits for parity p expire that are not over at the first look, the others after 10 ms)
@@ -57,6 +57,7 @@ struct params {
     int kstages, blocks;                // stages of a tile, blocks (4 bits) of a row of tiles
     int split, stages, depth;           // blocks of a tile; ring; stages whose operands fit tensor memory
     uint32_t w_block, x_at, stage, tmem_cols;
+    int turns;                          // ADD with sums in tensor memory: 1 where two accumulators take turns, 0 where there is one
     uint32_t sums_at;                   // of a split tile: where the cluster's partial sums go, from the first stage on (0: over the stages)
     int group_shift;
     const uint8_t *w4[2];
@@ -184,6 +185,13 @@ __device__ __forceinline__ void st(uint32_t addr, const uint32_t (&r)[32])
         ::S4(r, 0), S4(r, 4), S4(r, 8), S4(r, 12), S4(r, 16), S4(r, 20), S4(r, 24), S4(r, 28), "r"(addr)
         : "memory");
 }
+__device__ __forceinline__ void st(uint32_t addr, const uint32_t (&r)[16])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::S4(r, 0), S4(r, 4), S4(r, 8),
+        S4(r, 12), "r"(addr)
+        : "memory");
+}
 __device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ uint4 lds128(uint32_t addr)
 {
@@ -226,9 +234,13 @@ struct ring {  // a stage and its parity
 
 // NW weights.  KB: inputs of a stage, 128 KB; 0: BF16 weights, 64 inputs.  WORKERS: 8 or 16.  HALF: of an SM, for two blocks.
 // (An SM's registers are given to warps by fours: 10 warps cost as much as 12.)
-// ADD: the tensor cores cut off what does not fit their binary32 sums, up to 2^-23 of a sum for every 16 inputs.  For FP32 outputs of at most 32 tokens,
-// where a warp's share of the sums fits its registers, a stage's sums are added up there, rounded to nearest: logits of 5120 inputs are then off by
-// 1.1e-7 of their norm instead of 1.9e-6 (and a head of 32000 takes 25.8 us instead of 22.8).
+// ADD (FP32 outputs): the tensor cores cut off what does not fit their binary32 sums, 4e-9 of the norm for every 16 inputs.  So they add up at most 512 inputs, and
+// the warps that unpack add these sums up, rounded to nearest:
+//   few tokens (KB = 2)   a stage's, in registers, ahead of handing over the next one's operands: it is complete when these have room.
+//   more (KB = 1)         those of 4 stages (a chunk), in tensor memory: 32 sums of a thread in registers made unpacking 15 % slower.  Up to 128 tokens two accumulators
+//                         take turns; beyond, and with two blocks on an SM, there is room for one, and the tensor cores wait while a chunk is drained.
+// Logits of 5120 inputs are off by 0.8 to 1.1e-7 of their norm (sums of binary32 products: 0.9e-7), cut off over all inputs by 1.3e-6; 32000 outputs of 5120 in FP32 take 27.0 us
+// for one token (BF16 24.2), 34.5 for 64 (28.0), 45 for 128 (42), 151 for 512 (125); 2048 x 3456 x 5120 63 us (56.5).
 template <int NW, int KB, int WORKERS, bool HALF, bool ADD>
 __global__ void __launch_bounds__(HALF ? 384 : (2 + WORKERS) * 32, HALF ? 2 : 1)
 product(const params p, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ CUtensorMap map_w1)
@@ -237,6 +249,9 @@ product(const params p, const __grid_constant__ CUtensorMap map_x, const __grid_
     constexpr bool W4 = KB > 0;
     constexpr int KX = W4 ? 2 * KB : 1;          // 64-wide pieces of the inputs in a stage
     constexpr uint32_t A_COLS = KX * NW * 32;    // of tensor memory for a stage's operands
+    constexpr bool IN_REGS = ADD && KB == 2, IN_TMEM = ADD && KB == 1;
+    constexpr int CHUNK = IN_TMEM ? ADD_STAGES : 1 << 30;  // stages that the tensor cores add up
+    const int turns = HALF ? 0 : p.turns, accs = IN_TMEM ? 2 + turns : NW;  // accumulators (IN_TMEM: and the sums)
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
     const uint32_t bars = base + p.stages * p.stage;
     uint8_t *const gen = raw + (base - smem_u32(raw));
@@ -245,7 +260,11 @@ product(const params p, const __grid_constant__ CUtensorMap map_x, const __grid_
     auto full = [&](int s) { return bars + 8u * s; };
     auto empty = [&](int s) { return bars + 8u * (MOST_STAGES + s); };
     auto a_full = [&](int s) { return bars + 8u * (2 * MOST_STAGES + s); };
-    const uint32_t acc_full = bars + 8u * (2 * MOST_STAGES + MOST_DEPTH), acc_empty = acc_full + 8u;
+    auto acc_full = [&](int b) { return bars + 8u * (2 * MOST_STAGES + MOST_DEPTH + b); };  // (IN_TMEM: of the two accumulators; else 0)
+    auto acc_empty = [&](int b) { return bars + 8u * (2 * MOST_STAGES + MOST_DEPTH + 2 + b); };
+    // the accumulator of the n-th set of sums, and its barriers' parity
+    auto which = [&](uint32_t n) { return IN_TMEM ? n & turns : 0u; };
+    auto parity = [&](uint32_t n) { return IN_TMEM ? n >> turns & 1 : n & 1; };
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int tiles = p.tiles_n * p.tiles_t, places = gridDim.x / p.split;
@@ -271,8 +290,10 @@ product(const params p, const __grid_constant__ CUtensorMap map_x, const __grid_
             mbar_init(empty(s), 1);
         }
         for (int s = 0; s < MOST_DEPTH; ++s) mbar_init(a_full(s), 8);  // one arrival per warp of a group
-        mbar_init(acc_full, 1);
-        mbar_init(acc_empty, WORKERS);
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(acc_full(b), 1);
+            mbar_init(acc_empty(b), WORKERS);
+        }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -302,12 +323,12 @@ product(const params p, const __grid_constant__ CUtensorMap map_x, const __grid_
     tpq_grid_dep_launch();
     fence_after();
     const uint32_t tmem = *tmem_slot;
-    const uint32_t a_at = tmem + (uint32_t)(NW * p.pitch);  // operands behind the accumulators
+    const uint32_t a_at = tmem + (uint32_t)(accs * p.pitch);  // operands behind the accumulators
     bool ok = true;
     ring last;      // warp 0: behind the last stage copied; warp 1: the last stage multiplied
     int issued = 0;  // stages, warp 0 up to the ring's length
-    uint32_t done_tiles = 0;  // warp 1: tiles whose last MMA is issued
-    float sum[ADD ? 16 : 1];  // of columns 16 * part .. of the warp's rows
+    uint32_t complete = 0;  // warp 1: commits of the accumulators
+    float sum[IN_REGS ? 16 : 1];  // of columns 16 * part .. of the warp's rows
 
     if (warp == 0) {
         // the copies of a stage leave from as many lanes
@@ -338,16 +359,14 @@ product(const params p, const __grid_constant__ CUtensorMap map_x, const __grid_
     } else if (warp == 1) {
         const uint32_t idesc = instr(p.N), tmem1 = tmem + (uint32_t)p.pitch, x_piece = (uint32_t)p.N * 128 >> 4;
         ring r, t;  // of shared memory and of the operands in tensor memory
-        bool more = false;
-        uint32_t drained = 0;
         for (int tile = first_tile; tile < tiles && ok; tile += places) {
-            if (more && !ADD) {
-                ok = wait_warp(acc_empty, drained);
-                drained ^= 1;
-            }
-            more = true;
-            if (!ok) break;
             for (int kb = kb0; kb < kb1; ++kb, r.next(p.stages)) {
+                const int in_chunk = IN_TMEM ? (kb - kb0) % CHUNK : kb - kb0;
+                const bool first = IN_REGS || in_chunk == 0, end = !IN_REGS && (kb == kb1 - 1 || in_chunk == CHUNK - 1);
+                if (!IN_REGS && first) {  // (ahead of an accumulator's first set there is nothing to wait for)
+                    ok = wait_warp(acc_empty(which(complete)), parity(complete) ^ 1);
+                    if (!ok) break;
+                }
                 // (operands in tensor memory are there: so is the rest of their stage, which their warps waited for)
                 ok = W4 ? wait_warp(a_full(t.s), t.phase) : wait_warp(full(r.s), r.phase);
                 if (!ok) break;
@@ -356,7 +375,7 @@ product(const params p, const __grid_constant__ CUtensorMap map_x, const __grid_
                     const uint32_t at = base + r.s * p.stage, x = operand_low(at + p.x_at);
                     if (W4) {
                         const int kx = pieces(kb);
-                        const uint32_t a0 = a_at + t.s * A_COLS;
+                        const uint32_t a0 = a_at + t.s * A_COLS, d = which(complete) ? tmem1 : tmem;
 #pragma unroll
                         for (int j = 0; j < KX; ++j) {
                             if (j >= kx) break;
@@ -364,7 +383,7 @@ product(const params p, const __grid_constant__ CUtensorMap map_x, const __grid_
                             for (int k = 0; k < 4; ++k)
 #pragma unroll
                                 for (int a = 0; a < NW; ++a)
-                                    mma_ts(a ? tmem1 : tmem, a0 + (uint32_t)((j * NW + a) * 32 + k * 8), x + j * x_piece + 2 * k, idesc, j + k ? 1u : (uint32_t)(!ADD && kb != kb0));
+                                    mma_ts(a ? tmem1 : d, a0 + (uint32_t)((j * NW + a) * 32 + k * 8), x + j * x_piece + 2 * k, idesc, j + k ? 1u : (uint32_t)!first);
                         }
                     } else {
                         const uint32_t w = operand_low(at);
@@ -372,49 +391,81 @@ product(const params p, const __grid_constant__ CUtensorMap map_x, const __grid_
                         for (int k = 0; k < 4; ++k)
 #pragma unroll
                             for (int a = 0; a < NW; ++a)
-                                mma_ss(a ? tmem1 : tmem, w + a * (W_BF16_BYTES >> 4) + 2 * k, x + 2 * k, idesc, k ? 1u : (uint32_t)(kb != kb0));
+                                mma_ss(a ? tmem1 : tmem, w + a * (W_BF16_BYTES >> 4) + 2 * k, x + 2 * k, idesc, k ? 1u : (uint32_t)!first);
                     }
                     commit(empty(r.s));
-                    if (!ADD && kb == kb1 - 1) commit(acc_full);  // (a barrier that somebody waits on: an arrival must not outlive the block)
+                    if (end) commit(acc_full(which(complete)));
                 }
                 __syncwarp();
                 last = r;
                 issued = 1;
-                if (!ADD && kb == kb1 - 1) ++done_tiles;
+                complete += end;
                 if (W4) t.next(p.depth);
             }
         }
     } else {
         const int q = warp & 3, part = (warp - 2) >> 2;  // rows q * 32 .. of a tile (the quarter of tensor memory that this warp reaches)
-        uint32_t filled = 0;
-        // The tile's sums: scaled, through the activation, to memory.
-        auto epilogue = [&](int tile) {
+        const uint32_t from = tmem + ((uint32_t)(q * 32) << 16);
+        const uint32_t sums_or_up = (uint32_t)((IN_TMEM ? 1 + turns : 1) * p.pitch);
+        uint32_t filled = 0;  // sets of sums drained
+        // What the tensor cores have added up: the oldest chunk that is not drained, of tile `undrained`.
+        const int nk = kb1 - kb0, chunks = IN_TMEM ? (nk + CHUNK - 1) / CHUNK : 1;
+        int undrained = first_tile, chunk = 0;
+        // one that is not its tile's last: to the tile's sums
+        auto gather = [&]() {
+            ok = wait_warp(acc_full(which(filled)), parity(filled));
+            if (!ok) return;
+            fence_after();
+            const uint32_t acc = from + which(filled) * p.pitch + 16 * part, sums = from + sums_or_up + 16 * part;
+#pragma unroll
+            for (int c = 0; c < (HALF ? 64 : 192); c += 4 * WORKERS) {
+                if (16 * part + c >= p.N) break;
+                uint32_t y[16], z[16];
+                ld16(acc + c, y);
+                if (chunk) {
+                    ld16(sums + c, z);
+                    ld_wait(y);
+                    ld_wait(z);
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) y[j] = __float_as_uint(__uint_as_float(z[j]) + __uint_as_float(y[j]));
+                } else ld_wait(y);
+                st(sums + c, y);
+            }
+            st_wait();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(acc_empty(which(filled)));
+            ++filled;
+            ++chunk;
+        };
+        // The last one, and with it its tile's sums: scaled, through the activation, to memory.  (A split tile's is left for the cluster.)
+        auto epilogue = [&]() {
             int tn, tt;
-            origin(tile, tn, tt);
+            origin(undrained, tn, tt);
             const int col = tn * BM + q * 32 + lane;
             float f0 = 1.0f, f1 = 1.0f;
             if (W4) {
                 f0 = W4_SCALE * p.factor[0][col];
                 if (NW == 2) f1 = W4_SCALE * p.factor[1][col];
             }
-            ok = wait_warp(acc_full, filled);
-            filled ^= 1;
+            ok = wait_warp(acc_full(which(filled)), parity(filled));
             if (!ok) return;
             fence_after();
-            const uint32_t from = tmem + ((uint32_t)(q * 32) << 16);
             const int64_t t0 = (int64_t)tt * p.N;
             for (int c = 16 * part; c < p.N; c += 4 * WORKERS) {
                 if (t0 + c >= p.T) break;
                 uint32_t y0[16], y1[16];
-                ld16(from + c, y0);
-                if (NW == 2) ld16(from + p.pitch + c, y1);
+                ld16(from + which(filled) * p.pitch + c, y0);
+                if (NW == 2 || (IN_TMEM && chunk)) ld16(from + sums_or_up + c, y1);
                 ld_wait(y0);
-                if (NW == 2) ld_wait(y1);
+                if (NW == 2 || (IN_TMEM && chunk)) ld_wait(y1);
                 if (col < p.n) {
 #pragma unroll
                     for (int j = 0; j < 16; ++j) {
                         if (t0 + c + j >= p.T) break;
-                        float v = __uint_as_float(y0[j]) * f0;
+                        float v = __uint_as_float(y0[j]);
+                        if (IN_TMEM && chunk) v += __uint_as_float(y1[j]);
+                        v *= f0;
                         if (NW == 2) v = activation(v, p.act) * (__uint_as_float(y1[j]) * f1);
                         store(p, t0 + c + j, col, v);
                     }
@@ -422,12 +473,25 @@ product(const params p, const __grid_constant__ CUtensorMap map_x, const __grid_
             }
             fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(acc_empty);
+            if (lane == 0) mbar_arrive(acc_empty(which(filled)));
+            ++filled;
+            undrained += places;
+            chunk = 0;
         };
-        // a stage's sums to the tile's
-        const uint32_t my_sums = tmem + ((uint32_t)(q * 32) << 16) + 16 * part;
-        const bool summing = ADD && 16 * part < p.N;
-        // of a tile whose sums are in registers: what epilogue does
+        auto drain = [&]() {
+            if (IN_TMEM && chunk < chunks - 1) gather();
+            else epilogue();
+        };
+        // IN_REGS: a stage's sums to its tile's, and those to memory
+        const uint32_t my_sums = from + 16 * part;
+        const bool summing = IN_REGS && 16 * part < p.N;
+        auto add = [&]() {
+            uint32_t y[16];
+            ld16(my_sums, y);
+            ld_wait(y);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) sum[IN_REGS ? j : 0] += __uint_as_float(y[j]);
+        };
         auto finish = [&](int tile) {
             int tn, tt;
             origin(tile, tn, tt);
@@ -436,13 +500,13 @@ product(const params p, const __grid_constant__ CUtensorMap map_x, const __grid_
             const float f = W4_SCALE * p.factor[0][col];
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
-                if (ADD && summing && col < p.n && t0 + j < p.T) store(p, t0 + j, col, sum[ADD ? j : 0] * f);
-                sum[ADD ? j : 0] = 0.0f;
+                if (IN_REGS && summing && col < p.n && t0 + j < p.T) store(p, t0 + j, col, sum[IN_REGS ? j : 0] * f);
+                sum[IN_REGS ? j : 0] = 0.0f;
             }
         };
         if (!W4) {
             if (p.split == 1)
-                for (int tile = first_tile; tile < tiles && ok; tile += places) epilogue(tile);
+                while (undrained < tiles && ok) drain();
         } else {
             // A warp of the stage's group has half of its 64-wide pieces: of one weight consecutive ones, of two weights one of each.
             constexpr int MINE = KX * NW / 2;
@@ -459,24 +523,19 @@ product(const params p, const __grid_constant__ CUtensorMap map_x, const __grid_
             const uint32_t second = (uint32_t)((32 >> p.group_shift) * BM);  // from the step of a piece's first 32 inputs to that of the others
             const uint32_t to = a_at + ((uint32_t)(q * 32) << 16) + (uint32_t)(half * MINE * 32);
             ring r, t, done;  // done: the stage whose operands lay in the same place, `depth` stages ago
-            const int nk = kb1 - kb0;
-            int undrained = first_tile, left = nk + p.depth;  // the oldest tile that is not drained yet; stages until it is
+            // Stages until the next chunk is drained.  That is ahead of the one whose operands take the place of those that wait for it, `depth` stages behind
+            // the chunk; sums of parts of a tile are drained a stage behind it, with two accumulators two (they are complete by then).
+            int left = (IN_TMEM && chunks > 1 ? CHUNK : nk) + (IN_TMEM ? 1 + turns : p.depth);
             int fresh = p.depth, skip = turn;                 // places that held no operands yet; whether the next stage is the other group's
-            if (ADD)
+            if (IN_REGS)
 #pragma unroll
-                for (int j = 0; j < 16; ++j) sum[ADD ? j : 0] = 0.0f;
-            auto add = [&](uint32_t (&y)[16]) {
-                ld_wait(y);
-#pragma unroll
-                for (int j = 0; j < 16; ++j) sum[ADD ? j : 0] += __uint_as_float(y[j]);
-            };
+                for (int j = 0; j < 16; ++j) sum[IN_REGS ? j : 0] = 0.0f;
             for (int tile = first_tile; tile < tiles && ok; tile += places) {
                 for (int kb = kb0; kb < kb1; ++kb, r.next(p.stages), t.next(p.depth)) {
-                    if (!ADD && left-- == 0) {
-                        epilogue(undrained);
+                    if (!IN_REGS && left-- == 0) {
+                        drain();
                         if (!ok) break;
-                        undrained += places;
-                        left = nk - 1;
+                        left = (chunk == chunks - 1 ? nk - chunk * (IN_TMEM ? CHUNK : 0) : CHUNK) - 1;
                     }
                     const ring free = done;
                     const bool used = fresh == 0;
@@ -505,34 +564,30 @@ product(const params p, const __grid_constant__ CUtensorMap map_x, const __grid_
                             fence_after();
                         }
                         if (there) st(to + t.s * A_COLS + m * 32, v);
-                        if (m == MINE - 1 && used && summing) {  // the stage before this one's sums, complete as its operands are free (depth is 1)
-                            uint32_t y[16];
-                            ld16(my_sums, y);
-                            add(y);
-                        }
+                        if (IN_REGS && m == MINE - 1 && used && summing) add();  // (the stage before this one's, complete as its operands are free: depth is 1)
                     }
                     if (!ok) break;
-                    if (ADD && used && kb == kb0 && p.split == 1) finish(tile - places);
+                    if (IN_REGS && used && kb == kb0 && p.split == 1) finish(tile - places);
                     st_wait();
                     fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(a_full(t.s));
                 }
             }
-            if (ADD) {
+            if (IN_REGS) {
                 ok = ok && wait_warp(empty(done.s), done.phase);
-                if (ok && summing) {
-                    uint32_t y[16];
+                if (ok) {
                     fence_after();
-                    ld16(my_sums, y);
-                    add(y);
+                    if (summing) add();
+                    if (p.split == 1) finish(first_tile + (tiles - 1 - first_tile) / places * places);
                 }
-                if (ok && p.split == 1) finish(first_tile + (tiles - 1 - first_tile) / places * places);
             } else if (p.split == 1) {
-                for (; undrained < tiles && ok; undrained += places) epilogue(undrained);
+                while (undrained < tiles && ok) drain();
+            } else {
+                while (chunk < chunks - 1 && ok) gather();
             }
         }
-        if (p.split > 1 && !ADD) ok = ok && wait_warp(acc_full, 0);
+        if (p.split > 1 && !IN_REGS) ok = ok && wait_warp(acc_full(which(filled)), parity(filled));
     }
     if (!ok) {
         atomicExch(p.status, (int)TPQ_ERR_TIMEOUT);
@@ -564,14 +619,19 @@ product(const params p, const __grid_constant__ CUtensorMap map_x, const __grid_
             const uint32_t at = tmem + ((uint32_t)(q * 32) << 16), cell0 = base + p.sums_at + 4u * (uint32_t)(rank * NW * share + q * 32 + lane);
             for (int c = 16 * part; c < tokens; c += 4 * WORKERS) {
                 uint32_t y0[16], y1[16];
-                if (ADD) {
+                if (IN_REGS) {
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) y0[j] = __float_as_uint(sum[ADD ? j : 0]);
+                    for (int j = 0; j < 16; ++j) y0[j] = __float_as_uint(sum[IN_REGS ? j : 0]);
                 } else {
-                    ld16(at + c, y0);
-                    if (NW == 2) ld16(at + p.pitch + c, y1);
+                    const int chunk = IN_TMEM ? (kb1 - kb0 - 1) / CHUNK : 0;  // the last one
+                    const bool added = chunk > 0;
+                    ld16(at + which(chunk) * p.pitch + c, y0);
+                    if (NW == 2 || added) ld16(at + (IN_TMEM ? 1 + turns : 1) * p.pitch + c, y1);
                     ld_wait(y0);
-                    if (NW == 2) ld_wait(y1);
+                    if (NW == 2 || added) ld_wait(y1);
+                    if (added)
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) y0[j] = __float_as_uint(__uint_as_float(y1[j]) + __uint_as_float(y0[j]));
                 }
                 int owner = c / per, in = c - owner * per;
 #pragma unroll
@@ -614,7 +674,7 @@ product(const params p, const __grid_constant__ CUtensorMap map_x, const __grid_
             for (int j = 0; j < issued; ++j, last.next(p.stages)) (void)wait_end(full(last.s), last.phase ^ 1);
         } else if (warp == 1 && issued) {
             (void)wait_end(empty(last.s), last.phase);
-            if (done_tiles) (void)wait_end(acc_full, (done_tiles - 1) & 1);
+            if (complete) (void)wait_end(acc_full(which(complete - 1)), parity(complete - 1));
         }
     }
     if (warp == 1) {
@@ -664,11 +724,13 @@ cudaError_t launch(params p, const product_call &c, const tpq_block *b, cudaStre
     }
     p.sums_at = beside ? p.stages * p.stage + BAR_BYTES : 0;
     const int a_cols = KX * NW * 32;
-    p.depth = W4 ? (TMEM - NW * p.pitch) / a_cols : 1;
-    if (ADD) p.depth = 1;  // (the sums of a stage are read ahead of the next one's)
+    p.turns = ADD && KB == 1 && !HALF && p.N <= 128;
+    const int accs = ADD && KB == 1 ? 2 + p.turns : NW;
+    p.depth = W4 ? (TMEM - accs * p.pitch) / a_cols : 1;
+    if (ADD && KB == 2) p.depth = 1;  // (the sums of a stage are read ahead of the next one's)
     if (p.depth > MOST_DEPTH) p.depth = MOST_DEPTH;
     if (p.depth > p.stages) p.depth = p.stages;
-    const int cols = NW * p.pitch + (W4 ? p.depth * a_cols : 0);
+    const int cols = accs * p.pitch + (W4 ? p.depth * a_cols : 0);
     p.tmem_cols = cols <= 32 ? 32 : cols <= 64 ? 64 : cols <= 128 ? 128 : cols <= 256 ? 256 : 512;
     CUtensorMap mx, mw[2];
     if (!make_map(c.x, c.T, c.K, c.x_stride, p.N, &mx)) return cudaErrorNotSupported;
@@ -728,9 +790,11 @@ cudaError_t count_clusters(int split, int *n)
 cudaError_t product_prepare(tpq_block *b)
 {
     cudaError_t e = prepare<1, 1, 16, false>();
+    if (e == cudaSuccess) e = prepare<1, 1, 16, false, true>();
     if (e == cudaSuccess) e = prepare<2, 1, 16, false>();
     if (e == cudaSuccess) e = prepare<2, 0, 16, false>();
     if (e == cudaSuccess) e = prepare<1, 1, 8, true>();
+    if (e == cudaSuccess) e = prepare<1, 1, 8, true, true>();
     if (e == cudaSuccess) e = prepare<1, 2, 8, true>();
     if (e == cudaSuccess) e = prepare<1, 2, 8, true, true>();
     if (e == cudaSuccess) e = prepare<2, 1, 8, true>();
@@ -750,8 +814,8 @@ struct plan {
     int N, split;
 };
 
-// The kernel, the tokens of a tile and the blocks that share one: the least estimated time, in clocks.  A stage's (`one` or, per token of the tile,
-// `token`, whichever is more) are measured: 4 bits and many tokens are what the tensor cores take under the power limit (256 tokens 1500, with
+// The kernel, the tokens of a tile and the blocks that share one: the least estimated time, in clocks.  A stage's (`one` or, for two tokens of the tile,
+// `token`, whichever is more; sums of FP32 outputs cost 7 % more, and 25 % of 64 tokens) are measured: 4 bits and many tokens are what the tensor cores take under the power limit (256 tokens 1500, with
 // two weights 128 tokens 1640); few are what unpacking takes, more where a second block is on the SM (`beside`); BF16 weights are bound by shared
 // memory, 128 bytes a clock for the copies in and the operands out (512 + 3 a token), or by memory.
 // 2048 x 3456 x 5120 in 4 bits: tiles of 192 tokens 58 us (three rounds), of 256 63.5 (three, the third a sixth full); gated 2048 x 5120 x 3456 in
@@ -760,7 +824,7 @@ struct plan {
 plan choose(const product_call &c, const tpq_block *b, int tiles_n)
 {
     const bool two = c.n_weights == 2;
-    const int most = c.group && two ? 128 : 256;
+    const int most = c.group && two ? 128 : c.out_fp32 ? 192 : 256;
     const int64_t t0 = (c.T + most - 1) / most;
     plan best = {};
     int64_t best_cost = 0;
@@ -771,16 +835,16 @@ plan choose(const product_call &c, const tpq_block *b, int tiles_n)
         const bool half = kind == GATED_HALF || kind == LINEAR_HALF || kind == LINEAR_HALF_DEEP;
         const int deep = kind == BF16_GATED ? 64 : kind == LINEAR_HALF_DEEP ? 256 : 128;
         const int kstages = (int)((c.K + deep - 1) / deep);
-        int64_t one, token = 0, beside = 0;  // beside: with a second block on the SM
+        int64_t one, token = 0, beside = 0;  // token: of two tokens; beside: with a second block on the SM
         switch (kind) {
         case BF16_GATED: one = 512 + 3 * N > 1100 ? 512 + 3 * N : 1100; break;
-        case GATED: one = 1450, token = 13; break;
-        case LINEAR: one = 900, token = 6; break;
+        case GATED: one = 1450, token = 26; break;
+        case LINEAR: one = c.out_fp32 ? 960 : 900, token = c.out_fp32 ? 15 : 12; break;
         case GATED_HALF: one = 1700, beside = 1900; break;
-        case LINEAR_HALF: one = 750, beside = 1100; break;
+        case LINEAR_HALF: one = c.out_fp32 ? 950 : 750, beside = c.out_fp32 ? 1350 : 1100; break;
         default: one = 1170, beside = 1800; break;
         }
-        if (token * N > one) one = token * N;
+        if (token * N / 2 > one) one = token * N / 2;
         const int64_t end = 800 + (two ? 7 : 4) * N;
         const int *const clusters = half ? b->clusters_half : b->clusters;
         for (int s = 1; s <= 8 && s <= kstages; ++s) {
@@ -826,8 +890,8 @@ cudaError_t product_launch(const product_call &c, const tpq_block *b, cudaStream
     case BF16_GATED: e = launch<2, 0, 16, false>(p, c, b, st); break;
     case GATED: e = launch<2, 1, 16, false>(p, c, b, st); break;
     case GATED_HALF: e = launch<2, 1, 8, true>(p, c, b, st); break;
-    case LINEAR: e = launch<1, 1, 16, false>(p, c, b, st); break;
-    case LINEAR_HALF: e = launch<1, 1, 8, true>(p, c, b, st); break;
+    case LINEAR: e = c.out_fp32 ? launch<1, 1, 16, false, true>(p, c, b, st) : launch<1, 1, 16, false>(p, c, b, st); break;
+    case LINEAR_HALF: e = c.out_fp32 ? launch<1, 1, 8, true, true>(p, c, b, st) : launch<1, 1, 8, true>(p, c, b, st); break;
     default: e = c.out_fp32 ? launch<1, 2, 8, true, true>(p, c, b, st) : launch<1, 2, 8, true>(p, c, b, st); break;
     }
     if (e == cudaSuccess) ++*launches;

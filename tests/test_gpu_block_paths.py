@@ -71,6 +71,36 @@ def test_fp32_products_back_to_back_leave_each_other_alone(block, T):
     assert block.device_status() == 0
 
 
+def values_of(block, weight):
+    """step * code in 64 bits on the device, read back (exactly)."""
+    out = torch.empty(weight.n_out, weight.n_in, dtype=torch.bfloat16, device="cuda")
+    block.read_weight(weight.data_ptr, weight.n_out, weight.n_in, weight.group, out.data_ptr())
+    return out.double()
+
+
+@pytest.mark.parametrize("T", [1, 31, 33, 64, 65, 100, 128, 300, 2048])
+@pytest.mark.parametrize("n,K", [(1000, 5120), (700, 13825), (40000, 2000)])
+def test_sums_are_near_in_norm_whatever_the_number_of_tokens(block, T, n, K):
+    """FP32 outputs.  The tensor cores' own sums cut off what does not fit: 4e-9 of the norm for every 16 inputs, measured over 2000 (5e-7).  They add up at most 512 inputs:
+    1.28e-7, 2.15 * 2^-24.  The sums of 256 or 512 are added with roundings of at most 2^-24, which have signs of their own, over partial sums that grow like sqrt(j):
+    sqrt(K / 512) 2^-24.  One rounding of the product with the row's factor.  In all (3.2 + sqrt(K / 512)) 2^-24 of the norm, 3.8e-7 at 5120 inputs, for one
+    token as for thousands (sums cut off over all of these: 1.3e-6).  BF16 outputs: 2^-9 of the norm for the rounding (log-uniform values:
+    2^-7 / sqrt(12) / 1.47 = 1.5e-3), and sums that may be cut off over all inputs, twice 4e-9 for every 16."""
+    if T * n > 40000 * 300:
+        n = 5000
+    weight, keep = in_4_bits(block, n, K, 64)
+    value = values_of(block, weight)
+    x = torch.randn(T, up8(K), generator=torch.Generator("cuda").manual_seed(T), device="cuda").to(torch.bfloat16)
+    want = x[:, :K].double() @ value.T
+    for kind, dtype, bound in ((torch.float32, binding.TPQ_OUT_FP32, (3.2 + math.sqrt(K / 512)) * 2.0 ** -24),
+                               (torch.bfloat16, binding.TPQ_OUT_BF16, 2.0 ** -9 + K / 16 * 8e-9)):
+        out = torch.zeros(T, n, dtype=kind, device="cuda")
+        block.linear4(weight, x.data_ptr(), T, out.data_ptr(), dtype, x_stride=up8(K))
+        err = (out.double() - want).norm() / want.norm()
+        print(f"T {T} n {n} K {K} {dtype}: {err:.3g} of the norm, bound {bound:.3g}")
+        assert err <= bound
+
+
 # ------------------------------------------------------------------------------------------------ weights
 LOOP = """
 #include <stdint.h>
