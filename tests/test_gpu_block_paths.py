@@ -101,6 +101,66 @@ def test_sums_are_near_in_norm_whatever_the_number_of_tokens(block, T, n, K):
         assert err <= bound
 
 
+# Sizes at which blocks walk more stages than their ring holds (up to 16), and more than one tile; what runs together on the GPU is at most 296 blocks.
+LONG_WALKS = [
+    (300, 2304, 3456, 128), (2048, 1280, 3456, 64), (700, 1500, 2000, 32),
+    (1, 45000, 1500, 64), (20, 45000, 2500, 32), (40, 40000, 1300, 128), (60, 40000, 2300, 64), (100, 20000, 3000, 64), (200, 25000, 1100, 128),
+    (128, 3840, 5120, 64),         # (partial sums of two weights in the place of the stages)
+    (3, 700, 36864, 128), (40, 300, 36864, 32)]
+
+
+def with_lone_terms(T, K, seed):
+    """x [T][K]: in each row one input that outweighs all others, at the ends of pieces of 64, 128 and 256 and of shares of the inputs in turn, so that no tolerance hides its absence."""
+    x = torch.randn(T, K, generator=torch.Generator("cuda").manual_seed(seed), device="cuda")
+    at = sorted({min(K - 1, max(0, p + d)) for p in [0, K, *(64 * round(K * i / 64 / s) for s in (1, 2, 3, 4, 5, 6, 7, 8) for i in range(s)), 64, 128, 256, 512, 1024] for d in (-1, 0)})
+    x[torch.arange(T), torch.tensor(at, device="cuda")[torch.arange(T, device="cuda") % len(at)]] = 512.0
+    return x.to(torch.bfloat16)
+
+
+@pytest.mark.parametrize("T,n,K,group", LONG_WALKS)
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("lone", [False, True])
+def test_products_of_long_walks(block, T, n, K, group, dtype, lone):
+    weight, keep = in_4_bits(block, n, K, group)
+    value = values_of(block, weight)
+    x = with_lone_terms(T, K, T) if lone else torch.randn(T, K, generator=torch.Generator("cuda").manual_seed(T), device="cuda").to(torch.bfloat16)
+    xd = torch.full((T, up8(K)), NAN, dtype=torch.bfloat16, device="cuda")
+    xd[:, :K] = x
+    out = torch.full((T, n), 7.0, dtype=torch.bfloat16 if dtype == "bf16" else torch.float32, device="cuda")
+    again = out.clone()
+    for o in (out, again):
+        block.linear4(weight, xd.data_ptr(), T, o.data_ptr(), binding.TPQ_OUT_BF16 if dtype == "bf16" else binding.TPQ_OUT_FP32, x_stride=up8(K))
+    xl = x.double()
+    check_product(out, xl @ value.T, K * 2.0 ** -24 * (xl.abs() @ value.abs().T))
+    assert torch.equal(out, again)
+
+
+@pytest.mark.parametrize("T,n,K,group", LONG_WALKS)
+@pytest.mark.parametrize("bf16_weights", [False, True])
+@pytest.mark.parametrize("lone", [False, True])
+def test_gated_blocks_of_long_walks(block, T, n, K, group, bf16_weights, lone):
+    if bf16_weights:
+        keep = [torch.nn.functional.pad(some_weights(n, K, seed), (0, up8(K) - K)) for seed in range(2)]
+        made = [binding.Weight(w.data_ptr(), n, K, up8(K), binding.TPQ_WEIGHT_BF16, 0) for w in keep]
+        value = [w[:, :K].double() for w in keep]
+    else:
+        made, keep = zip(*[in_4_bits(block, n, K, group, seed) for seed in range(2)])
+        value = [values_of(block, w) for w in made]
+    x = with_lone_terms(T, K, T) if lone else torch.randn(T, K, generator=torch.Generator("cuda").manual_seed(T), device="cuda").to(torch.bfloat16)
+    xd = torch.full((T, up8(K)), NAN, dtype=torch.bfloat16, device="cuda")
+    xd[:, :K] = x
+    out = torch.full((T, n), 7.0, dtype=torch.bfloat16, device="cuda")
+    again = out.clone()
+    for o in (out, again):
+        block.gated(*made, binding.TPQ_ACT_SILU, xd.data_ptr(), T, o.data_ptr(), x_stride=up8(K))
+    want, bound = block_ref.gated(x.double(), *value, 0)
+    check_product(out, want, bound)
+    assert torch.equal(out, again)
+    if not lone:
+        # (of the norm: the rounding to BF16; the sums, cut off over all inputs, of gate and up)
+        assert (out.double() - want).norm() <= (2.0 ** -9 + 3 * K / 16 * 8e-9) * want.norm()
+
+
 # ------------------------------------------------------------------------------------------------ weights
 LOOP = """
 #include <stdint.h>
@@ -149,6 +209,136 @@ def test_threads_with_a_handle_each_quantise_side_by_side(tmp_path):
         codes, byte, factor = block_ref.quantise(np.ones((n, K)), 32)
         assert np.array_equal(w4[i].cpu().numpy(), block_ref.pack(codes, byte, factor, 32))
         b[i].close()
+
+
+@pytest.mark.parametrize("n,K,group,pad,offset", [(5, 5121, 32, 0, 0), (3, 9216, 128, 0, 8), (130, 9216, 64, 8, 8), (7, 13824, 32, 0, 8), (4, 14337, 64, 3, 1), (2, 36864, 128, 0, 3), (3, 2 ** 17, 32, 0, 8),
+                                                  (2, 2 ** 17 - 1, 64, 2, 2), (1, 98305, 32, 7, 0)])
+def test_long_rows_in_4_bits_are_the_bytes_of_the_definition(block, n, K, group, pad, offset):
+    """Rows that are read twice, aligned or not, above 48 KB of shared memory too (groups of 32 of more than 98304 inputs)."""
+    rng = np.random.default_rng(K)
+    w = weights(rng, n, K)
+    if n > 2:
+        w[1] = bf16(rng.standard_normal(K) * np.exp(8 * rng.standard_normal(K)))
+        w[2, K - 1] = math.inf
+    if n > 3:
+        w[3, : K - 1] = 0
+    buf, ptr = rows(w, K + pad, offset)
+    size = binding.weight4_bytes(n, K, group)
+    whole, w4 = gu.guarded(size)
+    block.quantize_weight(ptr, n, K, group, w4.data_ptr(), size, row_stride=K + pad)
+    out = torch.full((n * (K + pad) + 1,), 7.0, dtype=torch.bfloat16, device="cuda")
+    block.read_weight(w4.data_ptr(), n, K, group, out.data_ptr() + 2 * (offset % 2), out_stride=K + pad)
+    torch.cuda.synchronize()
+    codes, byte, factor = block_ref.quantise(w.double().numpy(), group)
+    assert np.array_equal(w4.cpu().numpy(), block_ref.pack(codes, byte, factor, group)) and gu.guards_intact(whole, size)
+    got = out[offset % 2: offset % 2 + n * (K + pad)].view(n, K + pad)
+    value = block_ref.values(codes, byte, factor, group)
+    assert np.array_equal(got[:, :K].double().cpu().numpy(), value, equal_nan=True)
+    assert (got[:, K:] == 7).all()
+
+
+# ------------------------------------------------------------------------------------------------ answers
+def exact_answers(x, n_top):
+    """x [T][V] on the device -> log probabilities (64 bits), entropy, the n_top largest (lowest index first), and per row sum p |x - m| and sum p (x - m)^2."""
+    got = [[], [], [], [], []]
+    for part in x.split(max(1, (1 << 26) // x.shape[1])):
+        p = part.double()
+        d = p - p.amax(1, keepdim=True)
+        logp = torch.log_softmax(p, 1)
+        prob = logp.exp()
+        d = torch.where(torch.isneginf(d), torch.zeros_like(d), d)
+        got[0].append(logp), got[1].append(torch.special.entr(prob).sum(1)), got[3].append((prob * d.abs()).sum(1)), got[4].append((prob * d * d).sum(1))
+        got[2].append(torch.argsort(p, dim=1, descending=True, stable=True)[:, :n_top])
+    return [torch.cat(g) for g in got]
+
+
+class Answers:
+    """A row's logits on one device: the calls and where their results go."""
+
+    def __init__(self, T, V, n_top):
+        self.T, self.V, self.n_top = T, V, n_top
+        self.record = torch.full((binding.token_record_bytes(T, n_top),), 0xA5, dtype=torch.uint8, device="cuda")
+        self.logprob, self.entropy = torch.full((T,), 7.0, device="cuda"), torch.full((T,), 7.0, device="cuda")
+        self.top, self.top_logprob = torch.full((T, n_top), 7, dtype=torch.int32, device="cuda"), torch.full((T, n_top), 7.0, device="cuda")
+
+    def run(self, block, x, tokens, stream=0):
+        dtype = binding.TPQ_OUT_BF16 if x.dtype == torch.bfloat16 else binding.TPQ_OUT_FP32
+        block.token_stats(x.data_ptr(), self.T, self.V, self.record.data_ptr(), self.record.numel(), dtype=dtype, stride=x.stride(0), tokens_ptr=tokens.data_ptr(), n_top=self.n_top, stream=stream)
+        block.token_logprobs([self.record.data_ptr()], self.T, self.logprob.data_ptr(), self.entropy.data_ptr(), self.n_top, self.top.data_ptr() if self.n_top else None,
+                             self.top_logprob.data_ptr() if self.n_top else None, stream=stream)
+
+    def results(self):
+        return [t.clone() for t in (self.logprob, self.entropy, self.top, self.top_logprob)]
+
+
+def check_in_norm(got, x, tokens, n_top):
+    """With u = 2^-24: x - m is off by u of itself, the exponential's argument by as much again, the exponential by 4u; a thread's sums (of V / 256 terms at least two
+    at a time) by roundings that have signs of their own, below 2u of the whole; a logarithm, a difference and their sum by 2u of their sizes.  So ln S is off by
+    (2 sum p |x - m| + 6) u, log p by 2 |log p| u more, and the entropy, whose A / S = sum p (x - m) has terms |x - m| times as far off, by
+    (2 sum p (x - m)^2 + 8 sum p |x - m| + 8) u beside ln S's.  Of the norm over the rows."""
+    logp, entropy, top, first, second = exact_answers(x, n_top)
+    u = 2.0 ** -24
+    want = logp.gather(1, tokens.long()[:, None])[:, 0]
+    lns = (2 * first + 6) * u
+
+    def near(a, b, bound):
+        assert (a.double() - b).norm() <= bound.norm(), ((a.double() - b).norm() / bound.norm()).item()
+
+    near(got[0], want, lns + 2 * want.abs() * u)
+    near(got[1], entropy, lns + (2 * second + 8 * first + 8) * u)
+    assert torch.equal(got[2].long(), top)
+    if n_top:
+        best = logp.gather(1, top)
+        near(got[3], best, lns[:, None] + 2 * best.abs() * u)
+
+
+@pytest.mark.parametrize("T,V,n_top", [(2048, 32000, 0), (300, 32000, 20), (61, 64000, 20), (7, 128256, 32), (1000, 1003, 5), (100, 256000, 32), (299, 256000, 20), (400, 262144, 32), (2, 5000000, 32), (1, 2500001, 1)])
+@pytest.mark.parametrize("kind", [torch.bfloat16, torch.float32])
+def test_answers_are_near_in_norm(block, T, V, n_top, kind):
+    """From rows that a thread walks once to such as have more rounds of it than there is room for their maxima (100 and more of 256000 in FP32, millions of columns)."""
+    g = torch.Generator("cuda").manual_seed(T + V)
+    x = torch.empty(T, V, dtype=kind, device="cuda")
+    for a in range(0, T, 64):
+        part = torch.randn(min(64, T - a), V, generator=g, device="cuda")
+        x[a: a + 64] = part * (1 + 2 * torch.rand(part.shape[0], 1, generator=g, device="cuda"))
+    tokens = torch.randint(0, V, (T,), generator=g, device="cuda", dtype=torch.int32)
+    a = Answers(T, V, n_top)
+    a.run(block, x, tokens)
+    got = a.results()
+    some = torch.arange(T, device="cuda") if T * V < 1 << 25 else torch.unique(torch.cat([torch.tensor([0, T - 1], device="cuda"), torch.randint(0, T, (40,), generator=g, device="cuda")]))
+    check_in_norm([v[some] for v in got], x[some], tokens[some], n_top)
+
+
+@pytest.mark.parametrize("T,V,n_top", [(1, 32000, 20), (61, 64000, 20), (500, 8000, 5), (2048, 2000, 0)])
+def test_answers_on_two_streams_and_in_a_graph(block, T, V, n_top):
+    """Calls side by side with buffers of their own, then captured and replayed over new logits: the bits of calls one by one."""
+    g = torch.Generator("cuda").manual_seed(T)
+    xs = [(torch.randn(T, V, generator=g, device="cuda") * 3).to(torch.bfloat16) for _ in range(3)]
+    tokens = torch.randint(0, V, (T,), generator=g, device="cuda", dtype=torch.int32)
+    want = []
+    for x in xs:
+        a = Answers(T, V, n_top)
+        a.run(block, x, tokens)
+        want.append(a.results())
+        check_in_norm(want[-1], x, tokens, n_top)
+    streams, sets = [torch.cuda.Stream() for _ in range(2)], [Answers(T, V, n_top) for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(30):
+        for i in range(2):
+            sets[i].run(block, xs[i], tokens, streams[i].cuda_stream)
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(a, b) for a, b in zip(sets[i].results(), want[i]))
+    x, a, b = xs[2].clone(), Answers(T, V, n_top), Answers(T, V, n_top)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        a.run(block, x, tokens, torch.cuda.current_stream().cuda_stream)
+    for i in (0, 2, 1):
+        x.copy_(xs[i])
+        graph.replay()
+        b.run(block, xs[i - 1], tokens)           # (an eager call with buffers of its own behind it)
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(a.results(), want[i])) and all(torch.equal(p, q) for p, q in zip(b.results(), want[i - 1]))
 
 
 # ------------------------------------------------------------------------------------------------ waits that expire
