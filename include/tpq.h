@@ -535,7 +535,7 @@ tpq_status tpq_gated(tpq_block *block, const tpq_weight *gate, const tpq_weight 
  *   logprob[t]     = x_token - ln sum e^x; 0 where no token is wanted; NaN, and INVALID_ARG through the status, where no record has it
  *   entropy[t]     = - sum p ln p
  *   top[t][i], top_logprob[t][i] : the n_top largest logits' columns, largest first, equal ones by column; -1 and -inf where there are no more
- * Any of the outputs may be NULL.  A logit of -inf is a token that cannot be; in a row of nothing else every log probability is -inf and the
+ * Any of the outputs may be NULL.  Logits are taken as they are: a cap or a temperature comes ahead.  A logit of -inf is a token that cannot be; in a row of nothing else every log probability is -inf and the
  * entropy 0.  A NaN or +inf makes its row's log probabilities and entropy NaN; a NaN is not among the most likely.  Sums are binary32.
  * Both enqueue on cuda_stream; T == 0 is a no-op.  Errors: INVALID_ARG, ALIGN, SIZE, BAD_STATE, CUDA. */
 size_t tpq_token_record_bytes(int64_t T, int n_top);

@@ -2,7 +2,7 @@
 // act(x Wg^T) * (x Wu^T) with both matrices in BF16 or in 4 bits (tpq_gated), in one kernel for one token and for thousands.
 //
 // The OUTPUTS are the rows of the tensor cores' tile and the tokens its columns (tcgen05, M = 128, N = 16 .. 256 tokens, K = 16): few tokens
-// then cost few columns, and weights are read once whatever T is.  Gate and up are two accumulators over the same tokens, so the
+// then cost few columns, and a tile of tokens reads the weights once: up to 256 tokens (128 with two weights in 4 bits, 192 for FP32 outputs) all do.  Gate and up are two accumulators over the same tokens, so the
 // activation and the product are the epilogue's, in binary32, with one rounding.
 //
 // Weights in 4 bits become BF16 operands in TENSOR memory: a thread is a row of the tile (an output), takes 64 codes of it from shared
@@ -12,20 +12,21 @@
 //   warp 0      copies (one lane): blocks of weights (4 bits: as they lie, 128 outputs x 128 inputs) and the tokens' inputs
 //   warp 1      tensor memory, MMA issue (one elected lane)
 //   warps 2-17  4 bits: codes to operands, two groups of warps in turns, of which one waits and loads while the other computes; a warp has 32 rows x
-//               half of a stage's inputs; then, as with BF16, the epilogue
+//               half of a stage's inputs (few tokens: 8 warps, one group); then, as with BF16, the epilogue
 //
-// One accumulator set: the epilogue, which all 16 warps share, is 1 to 3 % of a large tile's time, and wider tiles save more than a second
-// set would.  The first stages of the next tile are unpacked ahead of it.  One commit a stage frees its shared memory and its operands: a
+// One accumulator set (for FP32 outputs see ADD): the epilogue, which all 16 warps share, is 1 to 3 % of a large tile's time, and wider tiles save more
+// than a second set would.  The first stages of the next tile are unpacked ahead of it.  One commit a stage frees its shared memory and its operands: a
 // commit costs the tensor pipe about 300 clocks (with one for each 64-wide piece, one token's head of 32000 outputs x 5120 took 49 us).
 //
 // Few tokens: a tile's inputs are split over the blocks of a cluster, so that all SMs read weights; each block stores its part of the sums to the
 // block of the cluster that ends with them, which adds them in the order of the blocks (the same call gives the same bits).
 //
 // What bounds it (B200; products of other work in turn, so that weights come from memory).  Many tokens: the tensor pipe (67 % of all cycles active at the clock
-// that the power limit leaves): gated 1999 x 5120 x 3456 in 4 bits 103 us (1370 TFLOP/s), 2048 in BF16 106 us, where shared memory is as close.  Few tokens,
+// that the power limit leaves): gated 1999 x 5120 x 3456 in 4 bits 103 us (1370 TFLOP/s) in passes one behind the other in a graph, 124 in a program under that limit; 2048 in
+// BF16 106 and 125 us, where shared memory is as close.  Few tokens,
 // 4 bits: unpacking (9 instructions for 8 codes of 32 outputs, 20 with all that goes round it) and what is left over when tiles of 128 outputs
-// are dealt out: 32000 x 5120, one token, BF16 out 22.7 us (3.8 TB/s); without unpacking, stores to tensor memory and MMAs it would be 18.6.  BF16: memory, 17.5 us of
-// 2 x 4608 x 4608 (4.9 TB/s).  One token of 5120 x 1728: 5.5 us, latency (2.7 us from the first copy to the sums, 1.7 us cluster and stores).
+// are dealt out: 32000 x 5120, one token, BF16 out 22.7 to 24 us (3.5 to 3.8 TB/s); without unpacking, stores to tensor memory and MMAs it would be 18.6.  BF16: memory, 18 us of
+// 2 x 4608 x 4608, one token (4.7 TB/s).  One token of 5120 x 1728: 5.5 us, latency (2.7 us from the first copy to the sums, 1.7 us cluster and stores).
 // Tried for few tokens and not kept: mma.sync (16 outputs x 16 inputs x 8 tokens) with weights unpacked in registers, no barriers and no tensor memory:
 // 32 to 38 us of the 32000 x 5120 whatever was done to it, 66 with 16 tokens, 138 with 32: one takes 33 clocks of a scheduler.
 // Every wait is bounded.  A warp whose wait expires records TPQ_ERR_TIMEOUT and tells its block and its cluster: a split tile is then not stored at all,

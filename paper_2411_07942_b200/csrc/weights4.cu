@@ -5,7 +5,7 @@
 // 128 adjacent bytes of the pieces at a time.  A row's steps share a factor that depends on all of the row (its largest step's exponent): a first
 // walk over the rows finds the groups' largest magnitudes; for the second one rows of up to 5120 stay in registers, longer ones are read again,
 // from L2.
-// 32000 x 5120 (412 MB): 97 us to 4 bits (4.3 TB/s; 10 instructions a value), 67 back (6.1 TB/s).  With a thread to 32 values of a row (16-byte loads and stores 64 bytes apart) and
+// 32000 x 5120 (412 MB): 97 us to 4 bits (4.3 TB/s; 10 instructions a value, 57 % of the issue slots and 54 % of the ALU's: latency as much), 67 to 71 back (6 TB/s).  With a thread to 32 values of a row (16-byte loads and stores 64 bytes apart) and
 // quotients by __fdiv_rn they took 153 and 101, with the second walk
 // from L2 the first took 119, with one value at a time 110.
 #include <cuda_bf16.h>
